@@ -76,7 +76,7 @@ def draw(rng):
     if op in ("loss", "loss_grad"):
         hidden = rng.choice([1024, 3584, 4096, _width(rng, 16)])
         vocab = rng.choice([32768, _log_int(rng, 1000, 131072)])
-        rows = min(_log_int(rng, 1, 32768), 32768 * 32768 * 3584 // (vocab * hidden), (1 << 30) // vocab)
+        rows = min(_log_int(rng, 1, 32768), 16384 * 32768 * 3584 // (vocab * hidden), (1 << 30) // vocab)
         return dict(op=op, rows=rows, hidden=hidden, vocab=vocab, valid=rng.choice([1.0, round(rng.uniform(0.2, 1.0), 3)]))
     total, sizes = _log_int(rng, 1000, 100_000_000), []
     for _ in range(rng.randint(1, 24)):
