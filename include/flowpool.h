@@ -451,6 +451,121 @@ int32_t pool_embed_grad(ft_pool* pool, const ft_plan* plan, uint32_t mb_begin, u
                         const void* grad_out, float* grad_table, uint32_t vocab, void* stream);
 
 /*
+ * The backbone's last layer and its optimizer: the operators between an assembled microbatch's last hidden states and
+ * the updated embedding table.  pool_gather_padded gives the labels they start from and pool_embed_grad the gradient the
+ * table receives through the model's input; the calls below give the rest of a training step on that side.  The paper
+ * has no passage on them: the formulas stand here.
+ *
+ * They touch only the caller's buffers, run on `stream` in stream order, need none of the pool's samples, and take the
+ * pool for its device, its status word and its launch count.  The device current at the call must be the pool's
+ * (INVALID_ARG).  Row strides (ldx, ...) are in elements.  Workspaces are the caller's (256-byte aligned device memory,
+ * contents of no meaning between calls): one workspace serves any number of calls on one stream.  All of them can be
+ * captured in a CUDA graph.  Results do not depend on the launch geometry or on other work: no floating-point atomics.
+ */
+
+/*
+ * pool_layer_norm -- y = (x - mean) * rstd * weight + bias for each row, mean = sum(x) / cols,
+ * rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps); statistics and products in fp32, y rounded once.
+ *   x, y          device [rows, cols] of `dtype` (FT_BF16 or FT_F32), strides ldx, ldy >= cols; y may be x
+ *   weight, bias  device [cols] of `param_dtype`; NULL = ones, zeros
+ *   mean, rstd    device fp32 [rows], what the backward pass reads; may be NULL
+ * A row's result depends on that row alone (a NaN stays in its row).  Rows whose operands all start on 16-byte boundaries
+ * take wide accesses; any other width and stride works element by element.
+ * Errors: cols 0, a type, eps negative or not finite, a NULL or misaligned operand, a stride below cols INVALID_ARG;
+ * cols > 2^30 CAPACITY.  rows = 0 does nothing.
+ */
+int32_t pool_layer_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void* x, uint64_t ldx, uint32_t dtype,
+                        const void* weight, const void* bias, uint32_t param_dtype, float eps, void* y, uint64_t ldy,
+                        float* mean, float* rstd, void* stream);
+
+/*
+ * pool_layer_norm_grad -- with xhat = (x - mean) * rstd and a = weight * dy:
+ *   dx = rstd * (a - sum(a) / cols - xhat * sum(a * xhat) / cols)     device [rows, cols] of `dtype`; dx may be dy or x
+ *   dweight = sum over rows of dy * xhat, dbias = sum over rows of dy  device fp32 [cols], either may be NULL;
+ *             accumulate != 0 adds to what they hold
+ * mean and rstd as pool_layer_norm gave them.  Sums over rows are fp32, in an order fixed by the shapes and the device.
+ * pool_layer_norm_grad_workspace gives the workspace's size.  rows = 0: dweight and dbias become zero unless accumulating.
+ * Errors as pool_layer_norm; workspace NULL or misaligned INVALID_ARG, too small CAPACITY.
+ */
+int32_t pool_layer_norm_grad_workspace(ft_pool* pool, uint64_t rows, uint32_t cols, uint64_t* bytes);
+int32_t pool_layer_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const void* dy, uint64_t lddy, const void* x,
+                             uint64_t ldx, uint32_t dtype, const void* weight, uint32_t param_dtype, const float* mean,
+                             const float* rstd, void* dx, uint64_t lddx, float* dweight, float* dbias,
+                             uint32_t accumulate, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * pool_token_loss -- softmax cross entropy of every row against a vocabulary, without the matrix of logits.  With
+ * z = x[i] . W^T (bf16 operands, fp32 sums):
+ *   lse[i] = log(sum over v of exp(z_v)), loss[i] = lse[i] - z_label[i]         device fp32 [rows]
+ *   x       device bf16 [rows, hidden], stride ldx           w  device bf16 [vocab, hidden], stride ldw (the embedding
+ *   labels  device int32 [rows], as pool_gather_padded writes them              table itself where it is tied)
+ * A row labelled -100 counts nothing: its loss and lse are 0, and whatever its x holds (NaN, infinities) reaches no
+ * result; such rows also cost nothing.  Asynchronous: any other label outside [0, vocab) BAD_TOKEN_ID (detail = row; the
+ * row is treated as labelled -100).
+ *
+ * pool_token_loss_grad -- the same in one call with the gradients, for an upstream gradient g_i = grad_loss[i * grad_stride]
+ * (grad_loss device fp32; grad_stride 0: one number for all rows, such as 1 / rows that count; NULL: 1):
+ *   d_iv = g_i * (exp(z_v - lse_i) - [v = label_i])
+ *   dx[i] = sum over v of d_iv * W[v]     device bf16 [rows, hidden], stride lddx; zero for rows that count nothing
+ *   dw[v] = sum over i of d_iv * x[i]     device [vocab, hidden] contiguous, FT_F32 or FT_BF16 (dw_dtype);
+ *                                         accumulate != 0 (FT_F32 only) adds to what it holds, as pool_embed_grad does
+ * The products run on the tensor cores: d is rounded to bf16 for them, sums are fp32.
+ *
+ * hidden, ldx, ldw, lddx are multiples of 8; x, w, dx and dw start on 16-byte boundaries.  pool_token_loss_workspace
+ * gives the smallest workspace (*least) and the one from which more brings nothing (*best; with gradients a piece of the
+ * rows at a time has its probabilities there in bf16, and *best stops at pieces of 4 GiB); any size between the two works.
+ * Errors: hidden or vocab 0 or a size that is no multiple of 8, a NULL or misaligned operand, a stride below hidden,
+ * grad_stride > 1, accumulate with FT_BF16 INVALID_ARG; rows or vocab >= 2^31 CAPACITY; workspace NULL or misaligned
+ * INVALID_ARG, below *least CAPACITY.  rows = 0: dw becomes zero unless accumulating.
+ */
+int32_t pool_token_loss_workspace(ft_pool* pool, uint64_t rows, uint32_t hidden, uint32_t vocab, uint32_t with_grad,
+                                  uint32_t dw_dtype, uint64_t* least, uint64_t* best);
+int32_t pool_token_loss(ft_pool* pool, uint64_t rows, uint32_t hidden, uint32_t vocab, const void* x, uint64_t ldx,
+                        const void* w, uint64_t ldw, const int32_t* labels, float* loss, float* lse, void* workspace,
+                        uint64_t workspace_bytes, void* stream);
+int32_t pool_token_loss_grad(ft_pool* pool, uint64_t rows, uint32_t hidden, uint32_t vocab, const void* x, uint64_t ldx,
+                             const void* w, uint64_t ldw, const int32_t* labels, const float* grad_loss,
+                             uint32_t grad_stride, float* loss, float* lse, void* dx, uint64_t lddx, void* dw,
+                             uint32_t dw_dtype, uint32_t accumulate, void* workspace, uint64_t workspace_bytes,
+                             void* stream);
+
+/*
+ * pool_adamw_step -- one AdamW step over a list of tensors (host array, read before the call returns).  With
+ * g = *grad_scale * grad (device fp32, e.g. a clipping factor; NULL = 1):
+ *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * g^2
+ *   param = param * (1 - lr * weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in fp32 (the factors that depend on the step in double, on the host); param is rounded once to its type, `copy` (bf16
+ * [n], may be NULL) receives the new parameters as well, as the 16-bit table that pool_gather_* reads beside 32-bit
+ * master weights.
+ *   state_bits 32   m, v fp32 [n]
+ *   state_bits 8    m, v are float8 e4m3 [n]: m's and sqrt(v)'s values over a scale per 256 elements (m_scale, v_scale fp32
+ *                   [ceil(n / 256)]), the smallest power of two that brings the block's largest value to 448 or less, from
+ *                   2^-100 to 2^100; a positive sqrt(v) is held as at least 2^-9 of its scale.  All zero = no history.
+ *                   A block with a value that is not finite reads back as NaN
+ * Any alignment of a tensor's elements works; 16-byte starts (8 for float8 states) take wide accesses.  No array of the
+ * list may overlap another.
+ * Errors: lr, eps or a weight_decay not finite, eps < 0, a beta outside [0, 1), step 0, a type, a NULL or misaligned array of
+ * a tensor with n > 0 INVALID_ARG; n > 2^40 CAPACITY.
+ */
+typedef struct {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale; /* 8-bit states only */
+  void* copy;
+  uint64_t n;
+  double weight_decay;
+  uint32_t param_dtype, grad_dtype, state_bits, reserved;
+} ft_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps;
+  const float* grad_scale;
+  uint64_t step; /* counted from 1 */
+} ft_adamw_config;
+int32_t pool_adamw_step(ft_pool* pool, const ft_adamw_tensor* tensors, uint32_t n_tensors, const ft_adamw_config* cfg,
+                        void* stream);
+
+/*
  * Kernel timing for benchmarks.  While enabled, the library brackets each of its copy kernels with CUDA
  * events on the stream that kernel is launched on (the host-tier kernels run on the pool's side stream).
  * pool_profile_read synchronises the device, adds up the elapsed time and launch count per kernel class

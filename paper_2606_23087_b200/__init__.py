@@ -7,7 +7,7 @@ from .build import build  # noqa: F401
 def __getattr__(name):
     # the binding (and with it the shared library) loads on first use, so importing the package
     # for a build check needs no CUDA device
-    if name in ("binding", "Pool", "Plan", "PoolConfig", "PlanConfig", "FlowpoolError", "lib"):
+    if name in ("binding", "Pool", "Plan", "PoolConfig", "PlanConfig", "AdamwTensor", "AdamwConfig", "FlowpoolError", "lib"):
         import importlib
         mod = importlib.import_module(".binding", __name__)
         return mod if name == "binding" else getattr(mod, name)

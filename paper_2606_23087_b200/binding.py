@@ -25,7 +25,8 @@ STATUS = {
 EXPORTS = (
     "pool_create", "pool_register_samples", "pool_write_embeddings", "pool_write_embeddings_noalloc",
     "pool_plan_microbatches", "plan_summary",
-    "plan_arrays", "plan_destroy", "pool_gather_packed", "pool_gather_list", "pool_set_span_grids", "pool_gather_padded", "pool_embed_grad", "pool_free", "pool_status", "pool_stats",
+    "plan_arrays", "plan_destroy", "pool_gather_packed", "pool_gather_list", "pool_set_span_grids", "pool_gather_padded", "pool_embed_grad", "pool_layer_norm", "pool_layer_norm_grad", "pool_layer_norm_grad_workspace", "pool_token_loss",
+    "pool_token_loss_grad", "pool_token_loss_workspace", "pool_adamw_step", "pool_free", "pool_status", "pool_stats",
     "pool_ready_count", "pool_take_ready", "pool_backing", "pool_ipc_export", "pool_ipc_open", "pool_ipc_close", "pool_export_mapping", "pool_import_mapping", "pool_export_samples", "pool_import_samples",
     "pool_get_tuning", "pool_set_tuning", "pool_profile_enable", "pool_profile_read", "pool_debug_span_pages", "pool_debug_ring", "pool_debug_translate", "pool_destroy", "flowpool_last_cuda_error",
 )
@@ -63,6 +64,19 @@ class PoolStats(C.Structure):
     _fields_ = [(k, C.c_uint64) for k in (
         "pages_total", "pages_free", "hbm_pages", "host_pages", "text_pages_total", "text_pages_free",
         "live_samples", "live_spans", "bytes_written", "bytes_gathered", "gpu_launches")]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [
+        ("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+        ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_uint64), ("weight_decay", C.c_double),
+        ("param_dtype", C.c_uint32), ("grad_dtype", C.c_uint32), ("state_bits", C.c_uint32), ("reserved", C.c_uint32),
+    ]
+
+
+class AdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_void_p), ("step", C.c_uint64)]
 
 
 TUNING_FIELDS = ("dev_ctas_per_sm", "scatter_ctas_per_sm", "scatter_group", "chunk_shift", "host_ctas", "host_store_ctas",
@@ -105,7 +119,7 @@ def lib():
         if not os.path.exists(SO):
             build()
         _lib = C.CDLL(SO)
-        P, u32, u64, i32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32
+        P, u32, u64, i32, f32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32, C.c_float
         sig = {
             "pool_create": [P, P, P, P],
             "pool_register_samples": [P, u32, P, P, P, P, P, P, P],
@@ -120,6 +134,13 @@ def lib():
             "pool_set_span_grids": [P, u32, P, P, P, P],
             "pool_gather_padded": [P, P, u32, u32, P, u32, i32, P, P, P, P, P, P, P],
             "pool_embed_grad": [P, P, u32, u32, u32, P, P, u32, P],
+            "pool_layer_norm": [P, u64, u32, P, u64, u32, P, P, u32, f32, P, u64, P, P, P],
+            "pool_layer_norm_grad_workspace": [P, u64, u32, P],
+            "pool_layer_norm_grad": [P, u64, u32, P, u64, P, u64, u32, P, u32, P, P, P, u64, P, P, u32, P, u64, P],
+            "pool_token_loss_workspace": [P, u64, u32, u32, u32, u32, P, P],
+            "pool_token_loss": [P, u64, u32, u32, P, u64, P, u64, P, P, P, P, u64, P],
+            "pool_token_loss_grad": [P, u64, u32, u32, P, u64, P, u64, P, P, u32, P, P, P, u64, P, u32, u32, P, u64, P],
+            "pool_adamw_step": [P, P, u32, P, P],
             "pool_free": [P, P, u32, P],
             "pool_status": [P, P, P],
             "pool_stats": [P, P],
@@ -260,6 +281,52 @@ class Pool:
                    stream: int = 0):
         return lib().pool_embed_grad(self.h, plan.h, mb_begin, mb_end, 1 if padded else 0, grad_out_ptr or None,
                                      grad_table_ptr or None, vocab, stream or None)
+
+    def layer_norm(self, rows, cols, x_ptr: int, ldx, dtype, weight_ptr: int, bias_ptr: int, param_dtype, eps, y_ptr: int, ldy,
+                   mean_ptr: int = 0, rstd_ptr: int = 0, stream: int = 0):
+        return lib().pool_layer_norm(self.h, rows, cols, x_ptr or None, ldx, dtype, weight_ptr or None, bias_ptr or None,
+                                     param_dtype, eps, y_ptr or None, ldy, mean_ptr or None, rstd_ptr or None, stream or None)
+
+    def layer_norm_grad_workspace(self, rows, cols):
+        n = C.c_uint64()
+        rc = lib().pool_layer_norm_grad_workspace(self.h, rows, cols, C.byref(n))
+        if rc:
+            raise FlowpoolError(rc, "pool_layer_norm_grad_workspace")
+        return n.value
+
+    def layer_norm_grad(self, rows, cols, dy_ptr: int, lddy, x_ptr: int, ldx, dtype, weight_ptr: int, param_dtype, mean_ptr: int,
+                        rstd_ptr: int, dx_ptr: int, lddx, dweight_ptr: int, dbias_ptr: int, accumulate, ws_ptr: int, ws_bytes,
+                        stream: int = 0):
+        return lib().pool_layer_norm_grad(self.h, rows, cols, dy_ptr or None, lddy, x_ptr or None, ldx, dtype, weight_ptr or None,
+                                          param_dtype, mean_ptr or None, rstd_ptr or None, dx_ptr or None, lddx,
+                                          dweight_ptr or None, dbias_ptr or None, 1 if accumulate else 0, ws_ptr or None, ws_bytes,
+                                          stream or None)
+
+    def token_loss_workspace(self, rows, hidden, vocab, with_grad, dw_dtype=FT_F32):
+        """(least, best) workspace bytes of token_loss (with_grad false) or token_loss_grad."""
+        a, b = C.c_uint64(), C.c_uint64()
+        rc = lib().pool_token_loss_workspace(self.h, rows, hidden, vocab, 1 if with_grad else 0, dw_dtype, C.byref(a), C.byref(b))
+        if rc:
+            raise FlowpoolError(rc, "pool_token_loss_workspace")
+        return a.value, b.value
+
+    def token_loss(self, rows, hidden, vocab, x_ptr: int, ldx, w_ptr: int, ldw, labels_ptr: int, loss_ptr: int, lse_ptr: int,
+                   ws_ptr: int, ws_bytes, stream: int = 0):
+        return lib().pool_token_loss(self.h, rows, hidden, vocab, x_ptr or None, ldx, w_ptr or None, ldw, labels_ptr or None,
+                                     loss_ptr or None, lse_ptr or None, ws_ptr or None, ws_bytes, stream or None)
+
+    def token_loss_grad(self, rows, hidden, vocab, x_ptr: int, ldx, w_ptr: int, ldw, labels_ptr: int, grad_loss_ptr: int, grad_stride,
+                        loss_ptr: int, lse_ptr: int, dx_ptr: int, lddx, dw_ptr: int, dw_dtype, accumulate, ws_ptr: int, ws_bytes,
+                        stream: int = 0):
+        return lib().pool_token_loss_grad(self.h, rows, hidden, vocab, x_ptr or None, ldx, w_ptr or None, ldw, labels_ptr or None,
+                                          grad_loss_ptr or None, grad_stride, loss_ptr or None, lse_ptr or None, dx_ptr or None, lddx,
+                                          dw_ptr or None, dw_dtype, 1 if accumulate else 0, ws_ptr or None, ws_bytes, stream or None)
+
+    def adamw_step(self, tensors, cfg: AdamwConfig, stream: int = 0):
+        """pool_adamw_step; `tensors` is a ctypes array of AdamwTensor (kept by the caller from step to step) or a list of them."""
+        if not isinstance(tensors, C.Array):
+            tensors = (AdamwTensor * len(tensors))(*tensors)
+        return lib().pool_adamw_step(self.h, tensors, len(tensors), C.byref(cfg), stream or None)
 
     def free(self, slots, stream: int = 0):
         slots = _u32(slots)

@@ -1,0 +1,76 @@
+// What the operators of the backbone's last layer and of its optimizer share: element types, reductions over a warp and
+// a block, per-thread asynchronous copies, and the checks of their arguments.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "flowpool_internal.cuh"
+
+namespace ft {
+
+// 16 bytes of a row in its stored type <-> fp32.  Widening bf16 is exact; narrowing rounds to nearest even.
+template <typename T>
+struct Pack;
+template <>
+struct Pack<float> {
+  static constexpr int kElems = 4;
+  static __device__ __forceinline__ void widen(const uint4 v, float* f) {
+    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 narrow(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+struct Pack<__nv_bfloat16> {
+  static constexpr int kElems = 8;
+  static __device__ __forceinline__ void widen(const uint4 v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  }
+  static __device__ __forceinline__ uint4 narrow(const float* f) {
+    return make_uint4(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]), bf16x2(f[4], f[5]), bf16x2(f[6], f[7]));
+  }
+};
+__device__ __forceinline__ float widen1(float x) { return x; }
+__device__ __forceinline__ float widen1(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T narrow1(float x);
+template <>
+__device__ __forceinline__ float narrow1<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 narrow1<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// element i of an array whose type is known at run time
+__device__ __forceinline__ float load_as(const void* p, uint32_t dtype, uint64_t i) {
+  return dtype == FT_F32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+  return x;
+}
+
+__device__ __forceinline__ void copy16_async(void* smem_dst, const void* gmem_src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem_dst)), "l"(gmem_src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+inline bool dtype_ok(uint32_t t) { return t == FT_BF16 || t == FT_F32; }
+inline uint32_t dtype_size(uint32_t t) { return t == FT_F32 ? 4u : 2u; }
+inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline bool on_pool_device(const ft_pool* p) {
+  int d = -1;
+  return cudaGetDevice(&d) == cudaSuccess && d == p->device;
+}
+
+}  // namespace ft
+
+#define FT_EXPORT extern "C" __attribute__((visibility("default")))
