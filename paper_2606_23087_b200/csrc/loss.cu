@@ -13,16 +13,20 @@
 //   k_dx, k_dw  the two products
 #include <algorithm>
 
-#include "operators.cuh"
+#include "mma_pair.cuh"
 
 namespace ft {
 
-constexpr uint32_t kTile = 64;  // rows and columns of a tile
+constexpr uint32_t kStatCols = 128;  // columns of the vocabulary that share a row's maximum
+constexpr uint32_t kTileCost = 8;    // a tile's epilogue and start, in blocks of K
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int32_t kNoLabel = -100;
 constexpr uint32_t kPieceRowsMost = 65536;
+constexpr uint32_t kMinSlots = 296;  // few rows: room for four tiles a pair
 
 struct LossPiece {
-  uint32_t rows, hidden, vocab, ld_p, tiles;  // tiles: tiles of the vocabulary
+  uint32_t rows, hidden, vocab, ld_p, tiles, slots;  // tiles: of kStatCols columns; slots: tiles that dx_slots holds
+  uint32_t padded;  // rows of xc and p: `rows` in whole tiles
   uint64_t row0, ldx, ldw, lddx;
   const __nv_bfloat16 *x, *w;
   const int32_t* labels;
@@ -39,6 +43,7 @@ struct LossPiece {
   float2* stat;            // [tiles][rows] maximum and sum of a row in a tile
   __nv_bfloat16* xc;       // [rows][hidden]
   __nv_bfloat16* p;        // [rows][ld_p]
+  float* dx_slots;         // [slots][256][256] dx by tiles and slices of the vocabulary
   float* dw_acc;           // [vocab][hidden]: bf16 dw of several pieces
 };
 
@@ -83,6 +88,11 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
   __syncthreads();
   const uint32_t vecs = a.hidden / 8, rows = min(kPickRows, a.rows - r0);
   const uint4 zero = make_uint4(0, 0, 0, 0);
+  if (blockIdx.x == gridDim.x - 1) {  // the product over rows runs to a whole block of K: those rows' x must be finite
+    const uint32_t end = (total + kMmaK - 1) / kMmaK * kMmaK;
+    uint4* tail = reinterpret_cast<uint4*>(a.xc + (uint64_t)total * a.hidden);
+    for (uint32_t c = threadIdx.x; c < (end - total) * vecs; c += blockDim.x) tail[c] = zero;
+  }
   for (uint32_t k = warp; k < rows; k += blockDim.x / 32) {
     if (dest[k] >= 0) {
       const uint4* src = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
@@ -95,58 +105,87 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
   }
 }
 
-// 64 x 64 tile of A B^T in fp32 by a 16 x 16 block, four rows and four columns a thread; fetch_a(m, k), fetch_b(n, k)
-template <class FA, class FB>
-__device__ __forceinline__ void tile_product(uint32_t m0, uint32_t n0, uint32_t K, FA fetch_a, FB fetch_b, float (&acc)[4][4]) {
-  __shared__ float sa[16][kTile + 1], sb[16][kTile + 1];
-  const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (uint32_t k0 = 0; k0 < K; k0 += 16) {
-    for (uint32_t i = threadIdx.x; i < 16 * kTile; i += 256) {
-      const uint32_t k = i % 16, m = i / 16;
-      sa[k][m] = k0 + k < K ? fetch_a(m0 + m, k0 + k) : 0.f;
-      sb[k][m] = k0 + k < K ? fetch_b(n0 + m, k0 + k) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t k = 0; k < 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += sa[k][ty * 4 + i] * sb[k][tx * 4 + j];
-    __syncthreads();
-  }
+// ---- the three products ---------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp; results below 2^-126 are zero
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 32 bytes in one access: a whole sector a lane, where 16 bytes would write it in halves
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ void load32(const float* p, float (&v)[8]) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p) : "memory");
 }
 
+__device__ __forceinline__ void give_up(const PoolView& v, uint64_t call_seq, bool lost) {
+  if (lost && threadIdx.x == 0) note_error(v, call_seq, FT_ERR_TIMEOUT, blockIdx.x);
+}
+
+// z by tiles.  A lane owns a row's 128 columns: their maximum from a first pass over tensor memory, the exponentials from
+// a second one.
 template <bool kKeep>
-__global__ void __launch_bounds__(256) k_logits(LossPiece a) {
-  const uint32_t n = *a.count, m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-  if (m0 >= n) return;
-  float z[4][4] = {};
-  tile_product(m0, n0, a.hidden, [&](uint32_t m, uint32_t k) { return m < n ? __bfloat162float(a.xc[(uint64_t)m * a.hidden + k]) : 0.f; },
-               [&](uint32_t v, uint32_t k) { return v < a.vocab ? __bfloat162float(a.w[(uint64_t)v * a.ldw + k]) : 0.f; }, z);
-  const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
+k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
+         const __grid_constant__ LossPiece a) {
+  const uint32_t n = *a.count, m_tiles = (n + kMmaTile - 1) / kMmaTile, n_tiles = (a.vocab + kMmaTile - 1) / kMmaTile;
+  const uint32_t k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
+  bool lost;
+  mma_pair_tiles<false, false>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+    [&](uint32_t i) {
+      // bands of eight row tiles, all columns of a band before the next: a band's rows (8 x 256 x hidden) stay in L2
+      const uint32_t band = i / (8 * n_tiles), in = i - band * 8 * n_tiles, high = min(8u, m_tiles - band * 8);
+      return MmaTile{(band * 8 + in % high) * kMmaTile, in / high * kMmaTile, 0, k_blocks};
+    },
+    [&](uint32_t, const MmaTile& t, uint32_t tmem, uint32_t row, uint32_t col0) {
+      const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
+      if (c0 >= a.vocab) return;
+      const uint32_t cols = min(kStatCols, a.vocab - c0);
+      const int32_t label = m < n ? a.label[m] : kNoLabel;
+      float top = -INFINITY, sum = 0.f, z[32];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t m = m0 + ty * 4 + i;
-    float top = -INFINITY, sum = 0.f;
+      for (uint32_t c = 0; c < kStatCols; c += 32) {
+        if (c >= cols) break;
+        tmem_load32(tmem + c, z);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n0 + tx * 4 + j < a.vocab) top = fmaxf(top, z[i][j]);
+        for (uint32_t j = 0; j < 32; ++j)
+          if (c + j < cols) top = fmaxf(top, z[j]);
+      }
 #pragma unroll
-    for (int d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      for (uint32_t c = 0; c < kStatCols; c += 32) {
+        if (c >= cols) break;
+        tmem_load32(tmem + c, z);
+        const uint32_t at = (uint32_t)label - (c0 + c);
+        if (at < 32) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t v = n0 + tx * 4 + j;
-      if (v >= a.vocab) continue;
-      const float e = expf(z[i][j] - top);
-      sum += e;
-      if (m < n && (int32_t)v == a.label[m]) a.target[m] = z[i][j];
-      if (kKeep && m < n) a.p[(uint64_t)m * a.ld_p + v] = __float2bfloat16_rn(e);
-    }
+          for (uint32_t j = 0; j < 32; ++j)
+            if (j == at) a.target[m] = z[j];
+        }
 #pragma unroll
-    for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    if (m < n && tx == 0) a.stat[(uint64_t)blockIdx.x * a.rows + m] = make_float2(top, sum);
-  }
+        for (uint32_t j = 0; j < 32; ++j) {
+          z[j] = c + j < cols ? exp2_fast((z[j] - top) * kLog2e) : 0.f;
+          sum += z[j];
+        }
+        if constexpr (kKeep) {
+          // rows beyond the last one that counts: zeros, which the product over rows adds
+          const uint32_t keep = m < n ? 0xFFFFFFFFu : 0u;
+          __nv_bfloat16* p = a.p + (uint64_t)m * a.ld_p + c0 + c;
+#pragma unroll
+          for (uint32_t q = 0; q < 2; ++q) {
+            uint32_t w[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(z[q * 16 + 2 * j], z[q * 16 + 2 * j + 1]) & keep;
+            store32(p + q * 16, w);
+          }
+        }
+      }
+      if (m < n) a.stat[(uint64_t)(c0 / kStatCols) * a.rows + m] = make_float2(top, sum);
+    });
+  give_up(v, a.call_seq, lost);
 }
 
 // 32 rows a CTA, its warps share the tiles
@@ -182,48 +221,129 @@ __global__ void __launch_bounds__(256) k_scale(LossPiece a) {
     const float lse = a.row_lse[m], g = a.grad_loss ? a.grad_loss[(a.row0 + a.row_of[m]) * a.grad_stride] : 1.f;
     for (uint32_t v = blockIdx.x * 256 + threadIdx.x; v < a.vocab; v += gridDim.x * 256) {
       __nv_bfloat16* e = a.p + (uint64_t)m * a.ld_p + v;
-      const float f = g * expf(a.stat[(uint64_t)(v / kTile) * a.rows + m].x - lse);
+      const float f = g * expf(a.stat[(uint64_t)(v / kStatCols) * a.rows + m].x - lse);
       *e = __float2bfloat16_rn((int32_t)v == a.label[m] ? g * expm1f(a.target[m] - lse) : f * __bfloat162float(*e));
     }
   }
 }
 
-__global__ void __launch_bounds__(256) k_dx(LossPiece a) {
-  const uint32_t n = *a.count, m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-  if (m0 >= n) return;
-  float c[4][4] = {};
-  tile_product(m0, n0, a.vocab, [&](uint32_t m, uint32_t k) { return m < n ? __bfloat162float(a.p[(uint64_t)m * a.ld_p + k]) : 0.f; },
-               [&](uint32_t h, uint32_t k) { return h < a.hidden ? __bfloat162float(a.w[(uint64_t)k * a.ldw + h]) : 0.f; }, c);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t m = m0 + threadIdx.x / 16 * 4 + i, h = n0 + threadIdx.x % 16 * 4 + j;
-      if (m < n && h < a.hidden) a.dx[(a.row0 + a.row_of[m]) * a.lddx + h] = __float2bfloat16_rn(c[i][j]);
-    }
+// Slices of K = vocab for dx's tiles: hidden / 256 columns of tiles rarely divide among the pairs, and few rows have few
+// tiles at all.  Taken is the number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile
+// costs beside its products; every CTA (and the kernel that joins the slices) computes the same number.
+__device__ __forceinline__ uint32_t dx_slices(uint32_t tiles, uint32_t k_blocks, uint32_t pairs, uint32_t slots) {
+  uint32_t best = 1, best_cost = 0xFFFFFFFFu;
+  for (uint32_t s = 1; s <= 32 && s <= k_blocks && (s == 1 || (uint64_t)tiles * s <= slots); ++s) {
+    const uint32_t cost = (tiles * s + pairs - 1) / pairs * ((k_blocks + s - 1) / s + kTileCost);
+    if (cost < best_cost) { best = s; best_cost = cost; }
+  }
+  return best;
 }
 
-__global__ void __launch_bounds__(256) k_dw(LossPiece a) {
-  const uint32_t n = *a.count, m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-  float c[4][4] = {};
-  tile_product(m0, n0, n, [&](uint32_t v, uint32_t k) { return v < a.vocab ? __bfloat162float(a.p[(uint64_t)k * a.ld_p + v]) : 0.f; },
-               [&](uint32_t h, uint32_t k) { return h < a.hidden ? __bfloat162float(a.xc[(uint64_t)k * a.hidden + h]) : 0.f; }, c);
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
+k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
+     const __grid_constant__ LossPiece a) {
+  const uint32_t n = *a.count, m_tiles = (n + kMmaTile - 1) / kMmaTile, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile;
+  const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK, tiles = m_tiles * n_tiles;
+  const uint32_t slices = dx_slices(tiles, k_blocks, gridDim.x >> 1, a.slots), each = (k_blocks + slices - 1) / slices;
+  bool lost;
+  mma_pair_tiles<false, true>(map_p, map_w, tiles * slices, v.bulk_wait_ns, &lost,
+    [&](uint32_t i) {
+      const uint32_t s = i / tiles, t = i - s * tiles;
+      return MmaTile{t / n_tiles * kMmaTile, t % n_tiles * kMmaTile, min(s * each, k_blocks), min((s + 1) * each, k_blocks)};
+    },
+    [&](uint32_t i, const MmaTile& t, uint32_t tmem, uint32_t row, uint32_t col0) {
+      const uint32_t r = row + (threadIdx.x & 31), m = t.m + r, c0 = t.n + col0;
+      if (c0 >= a.hidden) return;
+      const uint32_t cols = min(128u, a.hidden - c0);
+      float* slot = a.dx_slots + ((uint64_t)i * kMmaTile + r) * kMmaTile + col0;
+      float d[32];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+      for (uint32_t c = 0; c < 128; c += 32) {
+        if (c >= cols) break;
+        if (tmem == kNone) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t v = m0 + threadIdx.x / 16 * 4 + i, h = n0 + threadIdx.x % 16 * 4 + j;
-      if (v >= a.vocab || h >= a.hidden) continue;
-      const uint64_t at = (uint64_t)v * a.hidden + h;
-      if (a.dw_dtype == FT_F32) {
-        float* d = static_cast<float*>(a.dw) + at;
-        *d = a.add_dw ? *d + c[i][j] : c[i][j];
-      } else {
-        const float s = a.add_dw ? a.dw_acc[at] + c[i][j] : c[i][j];
-        if (a.last) static_cast<__nv_bfloat16*>(a.dw)[at] = __float2bfloat16_rn(s);
-        else a.dw_acc[at] = s;
+          for (uint32_t j = 0; j < 32; ++j) d[j] = 0.f;
+        } else {
+          tmem_load32(tmem + c, d);
+        }
+        if (m >= n) continue;
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+          if (c + q * 8 >= cols) break;
+          uint32_t w[8];
+#pragma unroll
+          for (uint32_t j = 0; j < 8; ++j) w[j] = __float_as_uint(d[q * 8 + j]);
+          store32(slot + c + q * 8, w);
+        }
       }
+    });
+  give_up(v, a.call_seq, lost);
+}
+
+// dx of a counted row from the slices, in slice order, rounded once
+__global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
+  const uint32_t n = *a.count, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile, tiles = (n + kMmaTile - 1) / kMmaTile * n_tiles;
+  const uint32_t slices = dx_slices(tiles, (a.vocab + kMmaK - 1) / kMmaK, pairs, a.slots), vecs = a.hidden / 8;
+  const uint64_t all = (uint64_t)n * vecs;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+    const uint32_t m = (uint32_t)(i / vecs), c = (uint32_t)(i % vecs) * 8;
+    const float* slot = a.dx_slots + (((uint64_t)(m / kMmaTile) * n_tiles + c / kMmaTile) * kMmaTile + m % kMmaTile) * kMmaTile + c % kMmaTile;
+    float s[8], t[8];
+    load32(slot, s);
+    for (uint32_t k = 1; k < slices; ++k) {
+      load32(slot + (uint64_t)k * tiles * kMmaTile * kMmaTile, t);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] += t[j];
     }
+    *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[m]) * a.lddx + c) = Pack<__nv_bfloat16>::narrow(s);
+  }
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
+k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PoolView v,
+     const __grid_constant__ LossPiece a) {
+  const uint32_t n = *a.count, m_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile;
+  const uint32_t k_blocks = (n + kMmaK - 1) / kMmaK;
+  bool lost;
+  mma_pair_tiles<true, true>(map_p, map_x, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+    [&](uint32_t i) { return MmaTile{i / n_tiles * kMmaTile, i % n_tiles * kMmaTile, 0, k_blocks}; },
+    [&](uint32_t, const MmaTile& t, uint32_t tmem, uint32_t row, uint32_t col0) {
+      const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
+      if (c0 >= a.hidden) return;
+      const uint32_t cols = min(128u, a.hidden - c0);
+      const uint64_t at = (uint64_t)m * a.hidden + c0;
+      const float* base = a.add_dw ? (a.dw_dtype == FT_F32 ? static_cast<const float*>(a.dw) : a.dw_acc) : nullptr;
+      const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;
+      float* out = a.dw_dtype == FT_F32 ? static_cast<float*>(a.dw) : a.dw_acc;
+      float d[32];
+#pragma unroll
+      for (uint32_t c = 0; c < 128; c += 32) {
+        if (c >= cols) break;
+        if (tmem == kNone) {
+#pragma unroll
+          for (uint32_t j = 0; j < 32; ++j) d[j] = 0.f;
+        } else {
+          tmem_load32(tmem + c, d);
+        }
+        if (m >= a.vocab) continue;
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+          if (c + q * 8 >= cols) break;
+          float (&f)[8] = *reinterpret_cast<float (*)[8]>(d + q * 8);
+          if (base) {
+            const float4 b0 = *reinterpret_cast<const float4*>(base + at + c + q * 8), b1 = *reinterpret_cast<const float4*>(base + at + c + q * 8 + 4);
+            f[0] += b0.x; f[1] += b0.y; f[2] += b0.z; f[3] += b0.w; f[4] += b1.x; f[5] += b1.y; f[6] += b1.z; f[7] += b1.w;
+          }
+          if (in_fp32) {
+            *reinterpret_cast<uint4*>(out + at + c + q * 8) = Pack<float>::narrow(f);
+            *reinterpret_cast<uint4*>(out + at + c + q * 8 + 4) = Pack<float>::narrow(f + 4);
+          } else {
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dw) + at + c + q * 8) = Pack<__nv_bfloat16>::narrow(f);
+          }
+        }
+      }
+    });
+  give_up(v, a.call_seq, lost);
 }
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
@@ -232,10 +352,13 @@ __global__ void __launch_bounds__(256) k_dw(LossPiece a) {
 static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, bool grad, bool acc) {
   uint64_t off = 0;
   auto take = [&](uint64_t bytes) { const uint64_t o = off; off += align_up_sz(bytes, 256); return base + o; };
-  const uint64_t padded = align_up_sz(rows, kTile);
+  const uint64_t padded = align_up_sz(rows, kMmaTile);
   a->rows = rows;
-  a->tiles = (vocab + kTile - 1) / kTile;
-  a->ld_p = (uint32_t)align_up_sz(vocab, 8);
+  a->padded = (uint32_t)padded;
+  a->tiles = (vocab + kStatCols - 1) / kStatCols;
+  a->ld_p = (uint32_t)align_up_sz(vocab, 128);  // an epilogue lane's 32-byte stores stay inside its row
+  const uint64_t dx_tiles = padded / kMmaTile * ((hidden + kMmaTile - 1) / kMmaTile);
+  a->slots = (uint32_t)std::max<uint64_t>(dx_tiles, kMinSlots);
   a->count = reinterpret_cast<uint32_t*>(take(4));
   a->row_of = reinterpret_cast<int32_t*>(take(4ull * rows));
   a->label = reinterpret_cast<int32_t*>(take(4ull * rows));
@@ -244,6 +367,7 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
   a->stat = reinterpret_cast<float2*>(take(8ull * rows * a->tiles));
   a->xc = reinterpret_cast<__nv_bfloat16*>(take(2ull * padded * hidden));
   a->p = reinterpret_cast<__nv_bfloat16*>(take(grad ? 2ull * padded * a->ld_p : 0));
+  a->dx_slots = reinterpret_cast<float*>(take(grad ? 4ull * a->slots * kMmaTile * kMmaTile : 0));
   a->dw_acc = reinterpret_cast<float*>(take(acc ? 4ull * vocab * hidden : 0));
   return off;
 }
@@ -284,23 +408,34 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
   const uint32_t piece = work.piece_for(workspace_bytes);
   loss_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, grad, grad && a.dw_dtype == FT_BF16 && piece < rows);
   a.call_seq = status_seq(p);
+  CUtensorMap map_x, map_w, map_p;
+  if (mma_map(&map_x, a.xc, a.hidden, a.padded, a.hidden) != CUDA_SUCCESS || mma_map(&map_w, a.w, a.hidden, a.vocab, a.ldw) != CUDA_SUCCESS ||
+      (grad && mma_map(&map_p, a.p, a.vocab, a.padded, a.ld_p) != CUDA_SUCCESS))
+    return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+  const unsigned pairs = (unsigned)p->sm_count / 2, grid = 2 * pairs;
+  if (!p->loss_attr_set) {  // once per pool, hence once per device the pool lives on
+    FT_CUDA(cudaFuncSetAttribute(k_logits<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
+    FT_CUDA(cudaFuncSetAttribute(k_logits<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
+    FT_CUDA(cudaFuncSetAttribute(k_dx, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
+    FT_CUDA(cudaFuncSetAttribute(k_dw, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
+    p->loss_attr_set = true;
+  }
   for (uint64_t r0 = 0; r0 < rows; r0 += piece) {
     a.row0 = r0;
     a.rows = (uint32_t)std::min<uint64_t>(piece, rows - r0);
     a.add_dw = r0 > 0 || accumulate;
     a.last = r0 + a.rows == rows;
-    const uint32_t row_tiles = (a.rows + kTile - 1) / kTile;
     k_pick<<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
-    if (grad) k_logits<true><<<dim3(a.tiles, row_tiles), 256, 0, st>>>(a);
-    else k_logits<false><<<dim3(a.tiles, row_tiles), 256, 0, st>>>(a);
+    if (grad) k_logits<true><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+    else k_logits<false><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
     k_join<<<(a.rows + 31) / 32, 32 * kJoinRowWarps, 0, st>>>(a);
     p->gpu_launches += 3;
     if (grad) {
-      const uint32_t h_tiles = (a.hidden + kTile - 1) / kTile;
       k_scale<<<dim3(std::min(8u, (a.vocab + 255) / 256), std::min(a.rows, 4096u)), 256, 0, st>>>(a);
-      k_dx<<<dim3(h_tiles, row_tiles), 256, 0, st>>>(a);
-      k_dw<<<dim3(h_tiles, a.tiles), 256, 0, st>>>(a);
-      p->gpu_launches += 3;
+      k_dx<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_w, p->view, a);
+      k_dx_join<<<(unsigned)p->sm_count * 4, 256, 0, st>>>(a, pairs);
+      k_dw<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_x, p->view, a);
+      p->gpu_launches += 4;
     }
     FT_CUDA(cudaGetLastError());
   }

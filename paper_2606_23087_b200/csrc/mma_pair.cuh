@@ -1,0 +1,253 @@
+// A persistent bf16 matrix product on CTA pairs: 256 x 256 tiles of D = A B^T, fp32 sums in tensor memory, the epilogue
+// supplied by the caller.
+//
+// Two CTAs of a cluster (two SMs) work on one tile.  Each holds half of A's rows and half of B's: 16 KiB + 16 KiB a stage of
+// 64 columns of K, brought by TMA (128-byte swizzle) into a ring of kStages stages.  One thread of the even CTA issues the
+// matrix instructions of both (M 256, N 256, K 16); each CTA's tensor memory receives its 128 rows, in one of two
+// accumulators of 256 columns, so the epilogue of one tile runs beside the products of the next.  With a pair a stage
+// carries 64 KiB for 2 x 64 KiB of operands used: shared-memory traffic per product is half of a single CTA's 128 x 256.
+//
+// Operands need not be stored with K innermost: `kMn` operands have the tile's own dimension innermost (a row of the matrix
+// in memory per K index), as P and x in dW = P^T x; TMA brings 64 x 64 boxes either way and the descriptor says which.
+//
+// Warps: 0 TMA, 1 matrix instructions (even CTA), 2 tensor memory, 4..11 epilogue: quarter w % 4 of the rows, columns
+// [0, 128) for 4..7 and [128, 256) for 8..11.
+//
+// Every wait is bounded (PoolView::bulk_wait_ns).  A role that gives up stops issuing; before the pair leaves, the loads
+// and products under way are waited for once more, bounded again, and the tensor memory is freed.
+#pragma once
+#include <cuda.h>
+
+#include "bulk_copy.cuh"
+#include "operators.cuh"
+
+namespace ft {
+
+constexpr uint32_t kMmaTile = 256;    // rows and columns of a pair's tile
+constexpr uint32_t kMmaK = 64;        // K a stage: 128 bytes of bf16
+constexpr int kMmaStages = 6;
+constexpr uint32_t kMmaBox = 64 * kMmaK * 2;         // one TMA box, 8 KiB
+constexpr uint32_t kMmaOperand = 2 * kMmaBox;        // a CTA's half of an operand, a stage
+constexpr uint32_t kMmaStage = 2 * kMmaOperand;
+constexpr int kMmaThreads = 384;
+constexpr int kMmaEpilogueWarps = 8;
+constexpr size_t kMmaSmem = (size_t)kMmaStages * kMmaStage + 1024 + 256;  // tiles on a 1 KiB boundary, then the barriers
+
+struct MmaBarriers {
+  uint64_t full[kMmaStages], empty[kMmaStages], acc_full[2], acc_empty[2], drain;
+  uint32_t tmem, lost;
+};
+static_assert(sizeof(MmaBarriers) <= 256, "kMmaSmem");
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of the same shared-memory object in the pair's even CTA
+__device__ __forceinline__ uint32_t in_even_cta(const void* p) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
+  return r;
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// false: the barrier's phase did not complete within the limit
+__device__ __forceinline__ bool mbar_wait_bounded(uint64_t* b, uint32_t parity, uint64_t limit_ns) {
+  if (mbar_try_wait_cluster(b, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  uint32_t spins = 0;
+  while (!mbar_try_wait_cluster(b, parity))
+    if ((++spins & 1023u) == 0 && global_timer_ns() - t0 > limit_ns) return false;
+  return true;
+}
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// one 64 x 64 box to this CTA, its bytes counted on the even CTA's barrier
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// arrives on the barrier of both CTAs once the products issued so far are done
+__device__ __forceinline__ void mma_commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(smem_u32(b)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mma_issue(uint32_t tmem, uint64_t da, uint64_t db, uint32_t idesc, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+               "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(tmem), "l"(da), "l"(db), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// 32 columns of the warp's 32 rows; the whole warp takes part
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&f)[32]) {
+  uint32_t r[32];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
+}
+
+// Shared-memory descriptor (PTX ISA, "matrix descriptor"): bits 0-13 address / 16, 16-29 leading offset / 16, 32-45 stride
+// offset / 16, 46-47 = 1, 61-63 = 2 for the 128-byte swizzle.
+//   K innermost: rows of 128 bytes, groups of eight rows 1 KiB apart (stride offset); the leading offset is not used
+//   tile dimension innermost: 64 elements of it a row of 128 bytes, eight K indices in 1 KiB (stride offset), the next 64
+//   elements one box further (leading offset)
+template <bool kMn>
+__device__ __forceinline__ uint64_t mma_desc(uint32_t addr) {
+  constexpr uint64_t kLead = kMn ? kMmaBox >> 4 : 1, kStride = 1024 >> 4;
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | kLead << 16 | kStride << 32 | 1ull << 46 | 2ull << 61;
+}
+// 16 further along K: 32 bytes of a row, or 16 rows
+template <bool kMn>
+constexpr uint32_t kMmaStep = kMn ? 2048 : 32;
+
+// fp32 sums of bf16 x bf16, M 256, N 256; bits 15 and 16: A, B with the tile dimension innermost
+template <bool kAMn, bool kBMn>
+constexpr uint32_t kMmaInstr = 1u << 4 | 1u << 7 | 1u << 10 | (kAMn ? 1u << 15 : 0) | (kBMn ? 1u << 16 : 0) | (256 >> 3) << 17 | (256 >> 4) << 24;
+
+// One tile of work: rows from m, columns from n, K blocks [k0, k1).
+struct MmaTile {
+  uint32_t m, n, k0, k1;
+};
+
+// Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; epilogue(i, tile, tmem, row, col0) is called by
+// every epilogue warp with the tensor-memory address of its quarter and half: lane l holds row `row` + l of the tile, columns
+// col0 .. col0 + 127 follow `tmem`.  A tile without K blocks calls epilogue with tmem = kNone (all sums zero).
+template <bool kAMn, bool kBMn, class TileAt, class Epilogue>
+__device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, uint64_t limit_ns, bool* lost_out,
+                                               TileAt tile_at, Epilogue epilogue) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  MmaBarriers* bar = reinterpret_cast<MmaBarriers*>(stages + (size_t)kMmaStages * kMmaStage);
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
+  const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMmaStages; ++s) { mbar_init(&bar->full[s], 1); mbar_init(&bar->empty[s], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar->acc_full[i], 1); mbar_init(&bar->acc_empty[i], 2 * kMmaEpilogueWarps); }
+    mbar_init(&bar->drain, 1);
+    bar->lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bar->tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = bar->tmem;
+  bool lost = false;
+
+  if (warp == 0 && lane == 0) {
+    uint32_t it = 0;  // stages filled so far
+    const uint32_t base = smem_u32(stages);
+    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
+      const MmaTile t = tile_at(i);
+      const int32_t a0 = (int32_t)(t.m + rank * 128), b0 = (int32_t)(t.n + rank * 128);
+      for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
+        const uint32_t s = it % kMmaStages, ph = (it / kMmaStages) & 1;
+        if (!mbar_wait_bounded(&bar->empty[s], ph ^ 1, limit_ns)) { lost = true; break; }
+        if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * kMmaStage);
+        const uint32_t full = in_even_cta(&bar->full[s]), sa = base + s * kMmaStage, sb = sa + kMmaOperand;
+        const int32_t kk = (int32_t)(k * kMmaK);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (kAMn) tma_box(sa + h * kMmaBox, &map_a, a0 + 64 * h, kk, full);
+          else tma_box(sa + h * kMmaBox, &map_a, kk, a0 + 64 * h, full);
+          if (kBMn) tma_box(sb + h * kMmaBox, &map_b, b0 + 64 * h, kk, full);
+          else tma_box(sb + h * kMmaBox, &map_b, kk, b0 + 64 * h, full);
+        }
+      }
+    }
+    // what still arrives in this CTA's shared memory: the loads of the last stages (both CTAs' bytes are counted in the
+    // even one), and the even CTA's signals that it is done with them
+    const uint32_t j0 = it > kMmaStages ? it - kMmaStages : 0;
+    if (lost && rank == 0)
+      for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
+    for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
+  } else if (warp == 1 && lane == 0 && rank == 0) {
+    uint32_t it = 0, local = 0;
+    const uint32_t base = smem_u32(stages);
+    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
+      const MmaTile t = tile_at(i);
+      if (t.k0 == t.k1) continue;
+      const uint32_t acc = local & 1, aph = (local >> 1) & 1;
+      ++local;
+      if (!mbar_wait_bounded(&bar->acc_empty[acc], aph ^ 1, limit_ns)) { lost = true; break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
+        const uint32_t s = it % kMmaStages;
+        if (!mbar_wait_bounded(&bar->full[s], (it / kMmaStages) & 1, limit_ns)) { lost = true; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t sa = base + s * kMmaStage, sb = sa + kMmaOperand;
+#pragma unroll
+        for (uint32_t j = 0; j < kMmaK / 16; ++j)
+          mma_issue(tmem + acc * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>), kMmaInstr<kAMn, kBMn>,
+                    k > t.k0 || j > 0);
+        mma_commit(&bar->empty[s]);
+      }
+      if (!lost) mma_commit(&bar->acc_full[acc]);
+    }
+    if (lost) {  // products under way still read shared memory and write tensor memory
+      mma_commit(&bar->drain);
+      mbar_wait_bounded(&bar->drain, 0, limit_ns);
+    }
+  } else if (warp >= 4) {
+    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;
+    uint32_t local = 0;
+    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
+      const MmaTile t = tile_at(i);
+      const uint32_t row = rank * 128 + quarter * 32, col0 = half * 128;
+      if (t.k0 == t.k1) { epilogue(i, t, kNone, row, col0); continue; }
+      const uint32_t acc = local & 1, aph = (local >> 1) & 1;
+      ++local;
+      lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], aph, limit_ns));
+      if (lost) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      epilogue(i, t, tmem + acc * 256 + col0 + (quarter << 21), row, col0);
+      __syncwarp();
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(in_even_cta(&bar->acc_empty[acc]));
+    }
+  }
+  if (lost) bar->lost = 1;
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  *lost_out = bar->lost != 0;
+}
+
+// A matrix of bf16 rows, brought in 64 x 64 boxes; reads beyond its extents give zeros.
+inline CUresult mma_map(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t ld) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode) return CUDA_ERROR_NOT_FOUND;
+  const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
+  const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+}  // namespace ft
