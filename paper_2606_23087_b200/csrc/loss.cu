@@ -4,22 +4,31 @@
 //   d = g (exp(z - lse) - [v = label]),  dx = d W,  dW = d^T x
 //
 //   k_pick    takes the rows that count out of a piece of the rows: a dense copy of their x, their labels and row
-//             numbers.  Rows labelled -100 cost no products, and what they hold cannot reach dW as 0 * NaN
-//   k_logits  z by tiles; of a tile, each row keeps its maximum and the sum of exp(z - maximum), and with gradients
-//             exp(z - maximum) itself in bf16 (relative to the tile's own maximum, so rounding it costs 2^-8 of a
-//             probability, where rounding z would cost 2^-8 of z)
-//   k_join    joins the tiles' maxima and sums: lse, loss
-//   k_scale   turns exp(z - tile maximum) into d: one factor a row and tile, and the label's element from its own logit
+//             numbers.  Rows labelled -100 cost no products, and what they hold cannot reach dW as 0 * NaN.  It also
+//             takes each row's reference: the label's logit, x . W[label]
+//   k_logits  z by tiles; a row of a tile gives the sum of e = exp(z - reference), and with gradients e itself in bf16
+//             (rounding e costs 2^-8 of a probability, where rounding z would cost 2^-8 of z)
+//   k_join    adds a row's sums: lse = reference + log(sum)
+//   k_finish  d = f e with one factor f = g exp(reference - lse) a row: f goes to the row's x for dW (rounded to bf16) and to
+//             the row's sums for dx, so e is not touched again but for the label's element, (exp(z - lse) - 1) exp(lse - reference)
 //   k_dx, k_dw  the two products
+//
+// Why a reference known before any logit: with each tile's own maximum, the usual choice, e has to be read, scaled and
+// written again once lse is known (1.1 ms of 10.7 for 16384 rows x 32768).  bf16 has fp32's range, so any reference within
+// 2^60 of exp(lse) serves as well as the maximum; the label's logit is that, unless a row's loss is above 41.  Such a row
+// (and one whose reference is far above everything or not finite) gets its maximum as reference, and its row tile's logits
+// are worked out once more (k_logits<., true>, which returns at once where there is none).
 #include <algorithm>
 
 #include "mma_pair.cuh"
 
 namespace ft {
 
-constexpr uint32_t kStatCols = 128;  // columns of the vocabulary that share a row's maximum
+constexpr uint32_t kStatCols = 128;  // columns of the vocabulary that share a row's sum
 constexpr uint32_t kTileCost = 8;    // a tile's epilogue and start, in blocks of K
+constexpr uint32_t kPartBlocks = 8;  // blocks of K whose logits are summed by the tensor cores alone
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSumLimit = 0x1p60f;  // a row's sum outside [1 / limit, limit] wants another reference
 constexpr int32_t kNoLabel = -100;
 constexpr uint32_t kPieceRowsMost = 65536;
 constexpr uint32_t kMinSlots = 296;  // few rows: room for four tiles a pair
@@ -39,41 +48,58 @@ struct LossPiece {
   // workspace
   uint32_t* count;         // rows of the piece that count
   int32_t *row_of, *label; // [count] row in the piece, label
-  float *target, *row_lse; // [count]
-  float2* stat;            // [tiles][rows] maximum and sum of a row in a tile
-  __nv_bfloat16* xc;       // [rows][hidden]
-  __nv_bfloat16* p;        // [rows][ld_p]
+  uint32_t* redo;          // [1 + row tiles] whether any, and which row tiles need another reference
+  float *ref, *target;     // [count] the reference, and the label's logit as the product gives it
+  float* factor;           // [count] f
+  float2* stat;            // [tiles][rows] maximum of z and sum of e of a row in a tile
+  __nv_bfloat16* xc;       // [padded][hidden]
+  __nv_bfloat16* p;        // [padded][ld_p] e
   float* dx_slots;         // [slots][256][256] dx by tiles and slices of the vocabulary
   float* dw_acc;           // [vocab][hidden]: bf16 dw of several pieces
 };
 
-constexpr uint32_t kPickRows = 64;
+constexpr uint32_t kPickRows = 32;
 
+__device__ __forceinline__ bool has_label(int32_t l, uint32_t vocab) { return (uint32_t)l < vocab; }
+
+// this thread's share of the rows among the first n that count
+__device__ __forceinline__ uint32_t count_labels(const int32_t* labels, uint32_t n, uint32_t vocab) {
+  const uint32_t head = min(n, (uint32_t)((16 - (reinterpret_cast<uintptr_t>(labels) & 15)) & 15) / 4), quads = (n - head) / 4;
+  uint32_t c = 0;
+  if (threadIdx.x < head) c += has_label(labels[threadIdx.x], vocab);
+  const int4* q = reinterpret_cast<const int4*>(labels + head);
+#pragma unroll 8
+  for (uint32_t i = threadIdx.x; i < quads; i += blockDim.x) {
+    const int4 l = q[i];
+    c += has_label(l.x, vocab) + has_label(l.y, vocab) + has_label(l.z, vocab) + has_label(l.w, vocab);
+  }
+  const uint32_t r = head + 4 * quads + threadIdx.x;
+  if (r < n) c += has_label(labels[r], vocab);
+  return c;
+}
+
+// A CTA takes 32 rows; where they go it learns by counting the labels before them itself (a piece's labels stay in L2),
+// so nothing has to wait for another CTA.
 __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
-  __shared__ uint32_t before, warp_count[2];
-  __shared__ int32_t dest[kPickRows];
+  __shared__ uint32_t warp_count[8];
+  __shared__ int32_t dest[kPickRows], s_label[kPickRows];
   const uint32_t r0 = blockIdx.x * kPickRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t* labels = a.labels + a.row0;
-  if (threadIdx.x == 0) before = 0;
+  if (blockIdx.x == 0)
+    for (uint32_t i = threadIdx.x; i <= a.padded / kMmaTile; i += blockDim.x) a.redo[i] = 0;
+  const uint32_t mine = __reduce_add_sync(0xFFFFFFFFu, count_labels(labels, r0, a.vocab));
+  if (lane == 0) warp_count[warp] = mine;
   __syncthreads();
-  uint32_t mine = 0;
-  for (uint32_t r = threadIdx.x; r < r0; r += blockDim.x) { const int32_t l = labels[r]; mine += l >= 0 && (uint32_t)l < a.vocab; }
-  mine = __reduce_add_sync(0xFFFFFFFFu, mine);
-  if (lane == 0 && mine) atomicAdd(&before, mine);
-  const uint32_t r = r0 + threadIdx.x;
-  bool counts = false;
-  int32_t l = kNoLabel;
-  uint32_t mask = 0;
-  if (threadIdx.x < kPickRows) {
-    if (r < a.rows) l = labels[r];
-    counts = l >= 0 && (uint32_t)l < a.vocab;
-    mask = __ballot_sync(0xFFFFFFFFu, counts);
-    if (lane == 0) warp_count[warp] = __popc(mask);
-  }
-  __syncthreads();
-  if (threadIdx.x < kPickRows) {
-    const uint32_t pos = before + (warp ? warp_count[0] : 0) + __popc(mask & ((1u << lane) - 1));
-    dest[threadIdx.x] = counts ? (int32_t)pos : -1;
+  uint32_t before = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) before += warp_count[w];
+  const uint32_t r = r0 + lane;
+  const int32_t l = r < a.rows ? labels[r] : kNoLabel;
+  const bool counts = has_label(l, a.vocab);
+  const uint32_t mask = __ballot_sync(0xFFFFFFFFu, counts), pos = before + __popc(mask & ((1u << lane) - 1)), total = before + __popc(mask);
+  if (warp == 0) {
+    dest[lane] = counts ? (int32_t)pos : -1;
+    s_label[lane] = l;
     if (counts) {
       a.row_of[pos] = (int32_t)r;
       a.label[pos] = l;
@@ -82,9 +108,8 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
       a.lse[a.row0 + r] = 0.f;
       if (l != kNoLabel) note_error(v, a.call_seq, FT_ERR_BAD_TOKEN_ID, (uint32_t)(a.row0 + r));
     }
+    if (blockIdx.x == gridDim.x - 1 && lane == 0) *a.count = total;
   }
-  const uint32_t total = before + warp_count[0] + warp_count[1];
-  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *a.count = total;
   __syncthreads();
   const uint32_t vecs = a.hidden / 8, rows = min(kPickRows, a.rows - r0);
   const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -93,11 +118,24 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
     uint4* tail = reinterpret_cast<uint4*>(a.xc + (uint64_t)total * a.hidden);
     for (uint32_t c = threadIdx.x; c < (end - total) * vecs; c += blockDim.x) tail[c] = zero;
   }
-  for (uint32_t k = warp; k < rows; k += blockDim.x / 32) {
+  for (uint32_t k = warp; k < rows; k += 8) {
     if (dest[k] >= 0) {
-      const uint4* src = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
-      uint4* dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)dest[k] * a.hidden);
-      for (uint32_t c = lane; c < vecs; c += 32) dst[c] = src[c];
+      const uint4* __restrict__ src = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
+      const uint4* __restrict__ wl = reinterpret_cast<const uint4*>(a.w + (uint64_t)s_label[k] * a.ldw);
+      uint4* __restrict__ dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)dest[k] * a.hidden);
+      float dot = 0.f;
+#pragma unroll 4
+      for (uint32_t c = lane; c < vecs; c += 32) {
+        const uint4 xv = src[c], wv = wl[c];
+        float f[8], g[8];
+        Pack<__nv_bfloat16>::widen(xv, f);
+        Pack<__nv_bfloat16>::widen(wv, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = fmaf(f[e], g[e], dot);
+        dst[c] = xv;
+      }
+      dot = warp_sum(dot);
+      if (lane == 0) a.ref[dest[k]] = dot;
     } else if (a.dx) {
       uint4* dst = reinterpret_cast<uint4*>(a.dx + (a.row0 + r0 + k) * a.lddx);
       for (uint32_t c = lane; c < vecs; c += 32) dst[c] = zero;
@@ -126,103 +164,171 @@ __device__ __forceinline__ void give_up(const PoolView& v, uint64_t call_seq, bo
   if (lost && threadIdx.x == 0) note_error(v, call_seq, FT_ERR_TIMEOUT, blockIdx.x);
 }
 
-// z by tiles.  A lane owns a row's 128 columns: their maximum from a first pass over tensor memory, the exponentials from
-// a second one.
-template <bool kKeep>
+// z by tiles.  A lane owns a row's 128 columns, whose sums it adds up in registers from parts of K.
+template <bool kKeep, bool kRedo>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
 k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
          const __grid_constant__ LossPiece a) {
-  const uint32_t n = *a.count, m_tiles = (n + kMmaTile - 1) / kMmaTile, n_tiles = (a.vocab + kMmaTile - 1) / kMmaTile;
-  const uint32_t k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
+  __shared__ uint8_t s_tile[kRedo ? kPieceRowsMost / kMmaTile : 1];
+  __shared__ uint32_t s_tiles;
+  const uint32_t n = *a.count, n_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
+  uint32_t m_tiles = (n + kMmaTile - 1) / kMmaTile;
+  if constexpr (kRedo) {
+    if (a.redo[0] == 0) return;
+    if (threadIdx.x == 0) {
+      uint32_t c = 0;
+      for (uint32_t t = 0; t < m_tiles; ++t)
+        if (a.redo[1 + t]) s_tile[c++] = (uint8_t)t;
+      s_tiles = c;
+    }
+    __syncthreads();
+    m_tiles = s_tiles;
+  }
   bool lost;
-  mma_pair_tiles<false, false>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+  float z[kStatCols];  // zero between tiles
+#pragma unroll
+  for (uint32_t j = 0; j < kStatCols; ++j) z[j] = 0.f;
+  mma_pair_tiles<false, false, kPartBlocks>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
     [&](uint32_t i) {
       // bands of eight row tiles, all columns of a band before the next: a band's rows (8 x 256 x hidden) stay in L2
-      const uint32_t band = i / (8 * n_tiles), in = i - band * 8 * n_tiles, high = min(8u, m_tiles - band * 8);
-      return MmaTile{(band * 8 + in % high) * kMmaTile, in / high * kMmaTile, 0, k_blocks};
+      const uint32_t band = i / (8 * n_tiles), in = i - band * 8 * n_tiles, high = min(8u, m_tiles - band * 8), m = band * 8 + in % high;
+      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m) * kMmaTile, in / high * kMmaTile, 0, k_blocks};
     },
-    [&](uint32_t, const MmaTile& t, uint32_t tmem, uint32_t row, uint32_t col0) {
-      const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
+    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, bool last, auto&& release) {
+      const uint32_t c0 = t.n + col0;
       if (c0 >= a.vocab) return;
-      const uint32_t cols = min(kStatCols, a.vocab - c0);
-      const int32_t label = m < n ? a.label[m] : kNoLabel;
-      float top = -INFINITY, sum = 0.f, z[32];
 #pragma unroll
-      for (uint32_t c = 0; c < kStatCols; c += 32) {
-        if (c >= cols) break;
-        tmem_load32(tmem + c, z);
+      for (uint32_t c = 0; c < kStatCols; c += 16) {
+        float s[16];
+        tmem_load16(tmem + c, s);
 #pragma unroll
-        for (uint32_t j = 0; j < 32; ++j)
-          if (c + j < cols) top = fmaxf(top, z[j]);
+        for (uint32_t j = 0; j < 16; ++j) z[c + j] += s[j];
+      }
+      if (!last) return;
+      release();
+      const uint32_t m = t.m + row + (threadIdx.x & 31), cols = min(kStatCols, a.vocab - c0);
+      const uint32_t label_at = m < n ? (uint32_t)a.label[m] - c0 : kNone;
+      const float ref = m < n ? a.ref[m] : 0.f;
+      if (label_at < kStatCols) {
+#pragma unroll
+        for (uint32_t j = 0; j < kStatCols; ++j)
+          if (j == label_at) a.target[m] = z[j];
+      }
+      float top = -INFINITY, sum = 0.f;
+      if (cols < kStatCols) {  // beyond the vocabulary: e = 0
+#pragma unroll
+        for (uint32_t j = 0; j < kStatCols; ++j)
+          if (j >= cols) z[j] = -INFINITY;
       }
 #pragma unroll
-      for (uint32_t c = 0; c < kStatCols; c += 32) {
-        if (c >= cols) break;
-        tmem_load32(tmem + c, z);
-        const uint32_t at = (uint32_t)label - (c0 + c);
-        if (at < 32) {
+      for (uint32_t c = 0; c < kStatCols; c += 16) {
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j)
-            if (j == at) a.target[m] = z[j];
-        }
-#pragma unroll
-        for (uint32_t j = 0; j < 32; ++j) {
-          z[j] = c + j < cols ? exp2_fast((z[j] - top) * kLog2e) : 0.f;
-          sum += z[j];
+        for (uint32_t j = 0; j < 16; ++j) {
+          top = fmaxf(top, z[c + j]);
+          z[c + j] = exp2_fast((z[c + j] - ref) * kLog2e);
+          sum += z[c + j];
         }
         if constexpr (kKeep) {
           // rows beyond the last one that counts: zeros, which the product over rows adds
           const uint32_t keep = m < n ? 0xFFFFFFFFu : 0u;
-          __nv_bfloat16* p = a.p + (uint64_t)m * a.ld_p + c0 + c;
+          uint32_t w[8];
 #pragma unroll
-          for (uint32_t q = 0; q < 2; ++q) {
-            uint32_t w[8];
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(z[q * 16 + 2 * j], z[q * 16 + 2 * j + 1]) & keep;
-            store32(p + q * 16, w);
-          }
+          for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(z[c + 2 * j], z[c + 2 * j + 1]) & keep;
+          store32(a.p + (uint64_t)m * a.ld_p + c0 + c, w);
         }
       }
       if (m < n) a.stat[(uint64_t)(c0 / kStatCols) * a.rows + m] = make_float2(top, sum);
+#pragma unroll
+      for (uint32_t j = 0; j < kStatCols; ++j) z[j] = 0.f;
     });
   give_up(v, a.call_seq, lost);
 }
 
-// 32 rows a CTA, its warps share the tiles
+// ---- joining the tiles of a row -------------------------------------------------------------------------------------
+
+// 32 rows a CTA, a lane a row, the CTA's warps share the tiles; warp 0 gets the result.
 constexpr int kJoinRowWarps = 8;
-__global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
+__device__ __forceinline__ float2 join_tiles(const LossPiece& a, uint32_t n, uint32_t m) {
   __shared__ float2 part[kJoinRowWarps][32];
-  const uint32_t n = *a.count, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = blockIdx.x * 32 + lane;
-  if (blockIdx.x * 32 >= n) return;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float top = -INFINITY, sum = 0.f;
-  auto add = [&](float2 s) {
-    const float t = fmaxf(top, s.x);
-    // an empty side contributes nothing (and -inf - -inf must not be formed for it)
-    sum = (sum == 0.f ? 0.f : sum * expf(top - t)) + (s.y == 0.f ? 0.f : s.y * expf(s.x - t));
-    top = t;
-  };
-  if (m < n)
-    for (uint32_t t = warp; t < a.tiles; t += kJoinRowWarps) add(a.stat[(uint64_t)t * a.rows + m]);
+  if (m < n) {
+#pragma unroll 8
+    for (uint32_t t = warp; t < a.tiles; t += kJoinRowWarps) {
+      const float2 s = a.stat[(uint64_t)t * a.rows + m];
+      top = fmaxf(top, s.x);
+      sum += s.y;
+    }
+  }
   part[warp][lane] = make_float2(top, sum);
   __syncthreads();
-  if (warp || m >= n) return;
+  if (warp == 0) {
 #pragma unroll
-  for (int w = 1; w < kJoinRowWarps; ++w) add(part[w][lane]);
-  const float lse = top + logf(sum);
-  a.row_lse[m] = lse;
+    for (int w = 1; w < kJoinRowWarps; ++w) { top = fmaxf(top, part[w][lane].x); sum += part[w][lane].y; }
+  }
+  return make_float2(top, sum);
+}
+__device__ __forceinline__ float store_loss(const LossPiece& a, uint32_t m, float sum) {
+  const float lse = a.ref[m] + logf(sum);
   const uint64_t row = a.row0 + a.row_of[m];
   a.lse[row] = lse;
   a.loss[row] = lse - a.target[m];
+  return lse;
 }
 
-__global__ void __launch_bounds__(256) k_scale(LossPiece a) {
-  const uint32_t n = *a.count;
-  for (uint32_t m = blockIdx.y; m < n; m += gridDim.y) {
-    const float lse = a.row_lse[m], g = a.grad_loss ? a.grad_loss[(a.row0 + a.row_of[m]) * a.grad_stride] : 1.f;
-    for (uint32_t v = blockIdx.x * 256 + threadIdx.x; v < a.vocab; v += gridDim.x * 256) {
-      __nv_bfloat16* e = a.p + (uint64_t)m * a.ld_p + v;
-      const float f = g * expf(a.stat[(uint64_t)(v / kStatCols) * a.rows + m].x - lse);
-      *e = __float2bfloat16_rn((int32_t)v == a.label[m] ? g * expm1f(a.target[m] - lse) : f * __bfloat162float(*e));
+__global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
+  const uint32_t n = *a.count, m = blockIdx.x * 32 + (threadIdx.x & 31);
+  if (blockIdx.x * 32 >= n) return;
+  const float2 s = join_tiles(a, n, m);
+  if (threadIdx.x >= 32 || m >= n) return;
+  const bool other = (s.y > kSumLimit || s.y < 1.f / kSumLimit || isinf(a.ref[m])) && s.x < INFINITY && s.x > -INFINITY;
+  if (other) {
+    a.ref[m] = s.x;
+    a.redo[1 + m / kMmaTile] = 1;
+    a.redo[0] = 1;
+  } else {
+    store_loss(a, m, s.y);
+  }
+}
+
+// Row tiles with new references: their rows' sums once more.  With gradients: f, the label's element of e, and f x.
+template <bool kGrad>
+__global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
+  __shared__ float s_f[32];
+  const uint32_t n = *a.count, r0 = blockIdx.x * 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = r0 + lane;
+  if (r0 >= n) return;
+  const bool again = a.redo[1 + r0 / kMmaTile] != 0;
+  if (!kGrad && !again) return;
+  float sum = 0.f;
+  if (again) sum = join_tiles(a, n, m).y;
+  if (warp == 0 && m < n) {
+    const float lse = again ? store_loss(a, m, sum) : a.lse[a.row0 + a.row_of[m]];
+    if constexpr (kGrad) {
+      const float g = a.grad_loss ? a.grad_loss[(a.row0 + a.row_of[m]) * a.grad_stride] : 1.f;
+      // The label's element outweighs the row's others together, so f takes up its rounding (at most 2^-8): f q is the label's d,
+      // and dw's error that of f x's rounding alone (2.4e-3 of its norm instead of 2.7e-3, the output's own 1.7e-3 included).
+      const float e = expm1f(a.target[m] - lse) * expf(lse - a.ref[m]);
+      const __nv_bfloat16 q = __float2bfloat16_rn(e);
+      const float r = e / __bfloat162float(q), f = g * expf(a.ref[m] - lse) * (r > 0.99f && r < 1.01f ? r : 1.f);
+      a.factor[m] = f;
+      s_f[lane] = f;
+      a.p[(uint64_t)m * a.ld_p + a.label[m]] = q;
+    }
+  }
+  if constexpr (kGrad) {
+    __syncthreads();
+    const uint32_t vecs = a.hidden / 8;
+    for (uint32_t k = warp; k < 32 && r0 + k < n; k += kJoinRowWarps) {
+      uint4* x = reinterpret_cast<uint4*>(a.xc + (uint64_t)(r0 + k) * a.hidden);
+      const float f = s_f[k];
+#pragma unroll 4
+      for (uint32_t c = lane; c < vecs; c += 32) {
+        float t[8];
+        Pack<__nv_bfloat16>::widen(x[c], t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] *= f;
+        x[c] = Pack<__nv_bfloat16>::narrow(t);
+      }
     }
   }
 }
@@ -246,12 +352,12 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK, tiles = m_tiles * n_tiles;
   const uint32_t slices = dx_slices(tiles, k_blocks, gridDim.x >> 1, a.slots), each = (k_blocks + slices - 1) / slices;
   bool lost;
-  mma_pair_tiles<false, true>(map_p, map_w, tiles * slices, v.bulk_wait_ns, &lost,
+  mma_pair_tiles<false, true, 0>(map_p, map_w, tiles * slices, v.bulk_wait_ns, &lost,
     [&](uint32_t i) {
       const uint32_t s = i / tiles, t = i - s * tiles;
       return MmaTile{t / n_tiles * kMmaTile, t % n_tiles * kMmaTile, min(s * each, k_blocks), min((s + 1) * each, k_blocks)};
     },
-    [&](uint32_t i, const MmaTile& t, uint32_t tmem, uint32_t row, uint32_t col0) {
+    [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, bool, auto&&) {
       const uint32_t r = row + (threadIdx.x & 31), m = t.m + r, c0 = t.n + col0;
       if (c0 >= a.hidden) return;
       const uint32_t cols = min(128u, a.hidden - c0);
@@ -280,7 +386,7 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   give_up(v, a.call_seq, lost);
 }
 
-// dx of a counted row from the slices, in slice order, rounded once
+// dx of a counted row: f times the sum of the slices, in slice order, rounded once
 __global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
   const uint32_t n = *a.count, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile, tiles = (n + kMmaTile - 1) / kMmaTile * n_tiles;
   const uint32_t slices = dx_slices(tiles, (a.vocab + kMmaK - 1) / kMmaK, pairs, a.slots), vecs = a.hidden / 8;
@@ -288,6 +394,7 @@ __global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
     const uint32_t m = (uint32_t)(i / vecs), c = (uint32_t)(i % vecs) * 8;
     const float* slot = a.dx_slots + (((uint64_t)(m / kMmaTile) * n_tiles + c / kMmaTile) * kMmaTile + m % kMmaTile) * kMmaTile + c % kMmaTile;
+    const float f = a.factor[m];
     float s[8], t[8];
     load32(slot, s);
     for (uint32_t k = 1; k < slices; ++k) {
@@ -295,6 +402,8 @@ __global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += t[j];
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] *= f;
     *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[m]) * a.lddx + c) = Pack<__nv_bfloat16>::narrow(s);
   }
 }
@@ -305,9 +414,9 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   const uint32_t n = *a.count, m_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile;
   const uint32_t k_blocks = (n + kMmaK - 1) / kMmaK;
   bool lost;
-  mma_pair_tiles<true, true>(map_p, map_x, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+  mma_pair_tiles<true, true, 0>(map_p, map_x, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
     [&](uint32_t i) { return MmaTile{i / n_tiles * kMmaTile, i % n_tiles * kMmaTile, 0, k_blocks}; },
-    [&](uint32_t, const MmaTile& t, uint32_t tmem, uint32_t row, uint32_t col0) {
+    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, bool, auto&&) {
       const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
       const uint32_t cols = min(128u, a.hidden - c0);
@@ -362,8 +471,10 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
   a->count = reinterpret_cast<uint32_t*>(take(4));
   a->row_of = reinterpret_cast<int32_t*>(take(4ull * rows));
   a->label = reinterpret_cast<int32_t*>(take(4ull * rows));
+  a->redo = reinterpret_cast<uint32_t*>(take(4ull * (1 + padded / kMmaTile)));
+  a->ref = reinterpret_cast<float*>(take(4ull * rows));
   a->target = reinterpret_cast<float*>(take(4ull * rows));
-  a->row_lse = reinterpret_cast<float*>(take(4ull * rows));
+  a->factor = reinterpret_cast<float*>(take(4ull * rows));
   a->stat = reinterpret_cast<float2*>(take(8ull * rows * a->tiles));
   a->xc = reinterpret_cast<__nv_bfloat16*>(take(2ull * padded * hidden));
   a->p = reinterpret_cast<__nv_bfloat16*>(take(grad ? 2ull * padded * a->ld_p : 0));
@@ -414,8 +525,8 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   const unsigned pairs = (unsigned)p->sm_count / 2, grid = 2 * pairs;
   if (!p->loss_attr_set) {  // once per pool, hence once per device the pool lives on
-    FT_CUDA(cudaFuncSetAttribute(k_logits<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
-    FT_CUDA(cudaFuncSetAttribute(k_logits<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
+    for (auto k : {k_logits<false, false>, k_logits<false, true>, k_logits<true, false>, k_logits<true, true>})
+      FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
     FT_CUDA(cudaFuncSetAttribute(k_dx, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
     FT_CUDA(cudaFuncSetAttribute(k_dw, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
     p->loss_attr_set = true;
@@ -426,17 +537,22 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     a.add_dw = r0 > 0 || accumulate;
     a.last = r0 + a.rows == rows;
     k_pick<<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
-    if (grad) k_logits<true><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
-    else k_logits<false><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
-    k_join<<<(a.rows + 31) / 32, 32 * kJoinRowWarps, 0, st>>>(a);
-    p->gpu_launches += 3;
+    const unsigned joins = (a.rows + 31) / 32;
     if (grad) {
-      k_scale<<<dim3(std::min(8u, (a.vocab + 255) / 256), std::min(a.rows, 4096u)), 256, 0, st>>>(a);
+      k_logits<true, false><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      k_join<<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
+      k_logits<true, true><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      k_finish<true><<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
       k_dx<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_w, p->view, a);
       k_dx_join<<<(unsigned)p->sm_count * 4, 256, 0, st>>>(a, pairs);
       k_dw<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_x, p->view, a);
-      p->gpu_launches += 4;
+    } else {
+      k_logits<false, false><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      k_join<<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
+      k_logits<false, true><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      k_finish<false><<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
     }
+    p->gpu_launches += grad ? 8 : 5;
     FT_CUDA(cudaGetLastError());
   }
   return FT_OK;

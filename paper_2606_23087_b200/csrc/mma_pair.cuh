@@ -82,17 +82,25 @@ __device__ __forceinline__ void mma_issue(uint32_t tmem, uint64_t da, uint64_t d
                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                ::"r"(tmem), "l"(da), "l"(db), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-// 32 columns of the warp's 32 rows; the whole warp takes part
+// 16 or 32 columns of the warp's 32 rows; the whole warp takes part
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&f)[16]) {
+  uint32_t r[16];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&f)[32]) {
   uint32_t r[32];
   __syncwarp();
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr) : "memory");
 #pragma unroll
   for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
@@ -121,10 +129,16 @@ struct MmaTile {
   uint32_t m, n, k0, k1;
 };
 
-// Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; epilogue(i, tile, tmem, row, col0) is called by
-// every epilogue warp with the tensor-memory address of its quarter and half: lane l holds row `row` + l of the tile, columns
-// col0 .. col0 + 127 follow `tmem`.  A tile without K blocks calls epilogue with tmem = kNone (all sums zero).
-template <bool kAMn, bool kBMn, class TileAt, class Epilogue>
+// Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; every epilogue warp calls
+// epilogue(tile, i, tmem, row, col0, last, release): tensor memory from `tmem` on holds 128 columns of its 32 rows, lane l the
+// row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() once it has read them (it is called behind it
+// otherwise).  A tile without K blocks has tmem = kNone: all sums are zero.
+//
+// kPart > 0: the sums of every kPart blocks of K are handed over by themselves (the final ones with `last`), for an
+// epilogue that adds them up in registers.  The tensor cores add with truncation, K / 16 times a sum, so a long K drifts
+// towards zero (2.6e-6 of a logit over 3584); a part of 8 blocks truncates 32 times, and the parts are added with rounding
+// to nearest.
+template <bool kAMn, bool kBMn, uint32_t kPart, class TileAt, class Epilogue>
 __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, uint64_t limit_ns, bool* lost_out,
                                                TileAt tile_at, Epilogue epilogue) {
   extern __shared__ uint8_t smem_raw[];
@@ -150,78 +164,96 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = bar->tmem;
   bool lost = false;
-
-  if (warp == 0 && lane == 0) {
-    uint32_t it = 0;  // stages filled so far
-    const uint32_t base = smem_u32(stages);
-    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
-      const MmaTile t = tile_at(i);
-      const int32_t a0 = (int32_t)(t.m + rank * 128), b0 = (int32_t)(t.n + rank * 128);
-      for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
-        const uint32_t s = it % kMmaStages, ph = (it / kMmaStages) & 1;
-        if (!mbar_wait_bounded(&bar->empty[s], ph ^ 1, limit_ns)) { lost = true; break; }
-        if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * kMmaStage);
-        const uint32_t full = in_even_cta(&bar->full[s]), sa = base + s * kMmaStage, sb = sa + kMmaOperand;
-        const int32_t kk = (int32_t)(k * kMmaK);
+  // An epilogue that keeps 128 sums a lane gets 216 registers for its two warpgroups, the other warpgroup 64: 63488 of the
+  // 384 x 168 = 64512 that the block was launched with.
+  if (warp < 4) {
+    if constexpr (kPart > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 0 && lane == 0) {
+      uint32_t it = 0;  // stages filled so far
+      const uint32_t base = smem_u32(stages);
+      for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
+        const MmaTile t = tile_at(i);
+        const int32_t a0 = (int32_t)(t.m + rank * 128), b0 = (int32_t)(t.n + rank * 128);
+        for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
+          const uint32_t s = it % kMmaStages, ph = (it / kMmaStages) & 1;
+          if (!mbar_wait_bounded(&bar->empty[s], ph ^ 1, limit_ns)) { lost = true; break; }
+          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * kMmaStage);
+          const uint32_t full = in_even_cta(&bar->full[s]), sa = base + s * kMmaStage, sb = sa + kMmaOperand;
+          const int32_t kk = (int32_t)(k * kMmaK);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (kAMn) tma_box(sa + h * kMmaBox, &map_a, a0 + 64 * h, kk, full);
-          else tma_box(sa + h * kMmaBox, &map_a, kk, a0 + 64 * h, full);
-          if (kBMn) tma_box(sb + h * kMmaBox, &map_b, b0 + 64 * h, kk, full);
-          else tma_box(sb + h * kMmaBox, &map_b, kk, b0 + 64 * h, full);
+          for (int h = 0; h < 2; ++h) {
+            if (kAMn) tma_box(sa + h * kMmaBox, &map_a, a0 + 64 * h, kk, full);
+            else tma_box(sa + h * kMmaBox, &map_a, kk, a0 + 64 * h, full);
+            if (kBMn) tma_box(sb + h * kMmaBox, &map_b, b0 + 64 * h, kk, full);
+            else tma_box(sb + h * kMmaBox, &map_b, kk, b0 + 64 * h, full);
+          }
         }
       }
-    }
-    // what still arrives in this CTA's shared memory: the loads of the last stages (both CTAs' bytes are counted in the
-    // even one), and the even CTA's signals that it is done with them
-    const uint32_t j0 = it > kMmaStages ? it - kMmaStages : 0;
-    if (lost && rank == 0)
-      for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
-    for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
-  } else if (warp == 1 && lane == 0 && rank == 0) {
-    uint32_t it = 0, local = 0;
-    const uint32_t base = smem_u32(stages);
-    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
-      const MmaTile t = tile_at(i);
-      if (t.k0 == t.k1) continue;
-      const uint32_t acc = local & 1, aph = (local >> 1) & 1;
-      ++local;
-      if (!mbar_wait_bounded(&bar->acc_empty[acc], aph ^ 1, limit_ns)) { lost = true; break; }
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
-        const uint32_t s = it % kMmaStages;
-        if (!mbar_wait_bounded(&bar->full[s], (it / kMmaStages) & 1, limit_ns)) { lost = true; break; }
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t sa = base + s * kMmaStage, sb = sa + kMmaOperand;
+      // what still arrives in this CTA's shared memory: the loads of the last stages (both CTAs' bytes are counted in the
+      // even one), and the even CTA's signals that it is done with them
+      const uint32_t j0 = it > kMmaStages ? it - kMmaStages : 0;
+      if (lost && rank == 0)
+        for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
+      for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+      uint32_t it = 0, local = 0;
+      const uint32_t base = smem_u32(stages);
+      for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
+        const MmaTile t = tile_at(i);
+        for (uint32_t k = t.k0; k < t.k1 && !lost;) {
+          const uint32_t acc = local & 1, aph = (local >> 1) & 1, kp = kPart ? min(k + kPart, t.k1) : t.k1, first = k;
+          ++local;
+          if (!mbar_wait_bounded(&bar->acc_empty[acc], aph ^ 1, limit_ns)) { lost = true; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          for (; k < kp; ++k, ++it) {
+            const uint32_t s = it % kMmaStages;
+            if (!mbar_wait_bounded(&bar->full[s], (it / kMmaStages) & 1, limit_ns)) { lost = true; break; }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t sa = base + s * kMmaStage, sb = sa + kMmaOperand;
 #pragma unroll
-        for (uint32_t j = 0; j < kMmaK / 16; ++j)
-          mma_issue(tmem + acc * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>), kMmaInstr<kAMn, kBMn>,
-                    k > t.k0 || j > 0);
-        mma_commit(&bar->empty[s]);
+            for (uint32_t j = 0; j < kMmaK / 16; ++j)
+              mma_issue(tmem + acc * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>), kMmaInstr<kAMn, kBMn>,
+                        k > first || j > 0);
+            mma_commit(&bar->empty[s]);
+          }
+          if (!lost) mma_commit(&bar->acc_full[acc]);
+        }
       }
-      if (!lost) mma_commit(&bar->acc_full[acc]);
+      if (lost) {  // products under way still read shared memory and write tensor memory
+        mma_commit(&bar->drain);
+        mbar_wait_bounded(&bar->drain, 0, limit_ns);
+      }
     }
-    if (lost) {  // products under way still read shared memory and write tensor memory
-      mma_commit(&bar->drain);
-      mbar_wait_bounded(&bar->drain, 0, limit_ns);
-    }
-  } else if (warp >= 4) {
-    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;
-    uint32_t local = 0;
-    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
-      const MmaTile t = tile_at(i);
-      const uint32_t row = rank * 128 + quarter * 32, col0 = half * 128;
-      if (t.k0 == t.k1) { epilogue(i, t, kNone, row, col0); continue; }
-      const uint32_t acc = local & 1, aph = (local >> 1) & 1;
-      ++local;
-      lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], aph, limit_ns));
-      if (lost) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      epilogue(i, t, tmem + acc * 256 + col0 + (quarter << 21), row, col0);
-      __syncwarp();
+  } else {
+    if constexpr (kPart > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2, row = rank * 128 + quarter * 32, col0 = half * 128;
+    uint32_t local = 0, acc = 0;
+    bool held = false;
+    const auto release = [&] {
+      if (!held) return;
+      held = false;
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive_at(in_even_cta(&bar->acc_empty[acc]));
+    };
+    for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
+      const MmaTile t = tile_at(i);
+      uint32_t k = t.k0;
+      do {
+        uint32_t at = kNone;
+        if (t.k0 < t.k1) {
+          acc = local & 1;
+          lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], (local >> 1) & 1, limit_ns));
+          if (lost) break;
+          ++local;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          at = tmem + acc * 256 + col0 + (quarter << 21);
+          held = true;
+        }
+        k = kPart ? min(k + kPart, t.k1) : t.k1;
+        epilogue(t, i, at, row, col0, k >= t.k1, release);
+        release();
+      } while (k < t.k1);
     }
   }
   if (lost) bar->lost = 1;
