@@ -25,13 +25,14 @@
 namespace ft {
 
 constexpr uint32_t kStatCols = 128;  // columns of the vocabulary that share a row's sum
-constexpr uint32_t kTileCost = 8;    // a tile's epilogue and start, in blocks of K
-constexpr uint32_t kPartBlocks = 8;  // blocks of K whose logits are summed by the tensor cores alone
+constexpr uint32_t kTileCost = 6;    // what a tile of dx costs beside its products, in blocks of K
+constexpr uint32_t kPartBlocks = 16; // blocks of K whose logits are summed by the tensor cores alone: 64 truncations, 7e-7 of a logit
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSumLimit = 0x1p60f;  // a row's sum outside [1 / limit, limit] wants another reference
 constexpr int32_t kNoLabel = -100;
 constexpr uint32_t kPieceRowsMost = 65536;
-constexpr uint32_t kMinSlots = 296;  // few rows: room for four tiles a pair
+constexpr uint32_t kHighRows = 2 * kMmaTile;  // rows of a tile of dx and dw
+constexpr uint32_t kMinSlots = 148;  // few rows: room for two tiles a pair
 
 struct LossPiece {
   uint32_t rows, hidden, vocab, ld_p, tiles, slots;  // tiles: of kStatCols columns; slots: tiles that dx_slots holds
@@ -54,7 +55,7 @@ struct LossPiece {
   float2* stat;            // [tiles][rows] maximum of z and sum of e of a row in a tile
   __nv_bfloat16* xc;       // [padded][hidden]
   __nv_bfloat16* p;        // [padded][ld_p] e
-  float* dx_slots;         // [slots][256][256] dx by tiles and slices of the vocabulary
+  float* dx_slots;         // [slots][512][256] dx by slices of the vocabulary and tiles
   float* dw_acc;           // [vocab][hidden]: bf16 dw of several pieces
 };
 
@@ -151,7 +152,7 @@ __device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp; results below 2
   return y;
 }
 // 32 bytes in one access: a whole sector a lane, where 16 bytes would write it in halves
-__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
@@ -188,21 +189,23 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
   float z[kStatCols];  // zero between tiles
 #pragma unroll
   for (uint32_t j = 0; j < kStatCols; ++j) z[j] = 0.f;
-  mma_pair_tiles<false, false, kPartBlocks>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+  mma_pair_tiles<false, false, 1, kPartBlocks>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
     [&](uint32_t i) {
       // bands of eight row tiles, all columns of a band before the next: a band's rows (8 x 256 x hidden) stay in L2
       const uint32_t band = i / (8 * n_tiles), in = i - band * 8 * n_tiles, high = min(8u, m_tiles - band * 8), m = band * 8 + in % high;
-      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m) * kMmaTile, in / high * kMmaTile, 0, k_blocks};
+      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m) * kMmaTile, in / high * kMmaTile, 0, k_blocks, 1};
     },
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, bool last, auto&& release) {
       const uint32_t c0 = t.n + col0;
       if (c0 >= a.vocab) return;
 #pragma unroll
-      for (uint32_t c = 0; c < kStatCols; c += 16) {
-        float s[16];
-        tmem_load16(tmem + c, s);
+      for (uint32_t c = 0; c < kStatCols; c += 64) {  // 64 columns in flight: a wait for each 16 made this the bottleneck
+        uint32_t s0[32], s1[32];
+        tmem_load32(tmem + c, s0);
+        tmem_load32(tmem + c + 32, s1);
+        tmem_wait();
 #pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) z[c + j] += s[j];
+        for (uint32_t j = 0; j < 32; ++j) { z[c + j] += __uint_as_float(s0[j]); z[c + 32 + j] += __uint_as_float(s1[j]); }
       }
       if (!last) return;
       release();
@@ -333,13 +336,38 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
   }
 }
 
-// Slices of K = vocab for dx's tiles: hidden / 256 columns of tiles rarely divide among the pairs, and few rows have few
-// tiles at all.  Taken is the number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile
-// costs beside its products; every CTA (and the kernel that joins the slices) computes the same number.
-__device__ __forceinline__ uint32_t dx_slices(uint32_t tiles, uint32_t k_blocks, uint32_t pairs, uint32_t slots) {
+// The work of a product in 512-row tiles.  Tile `t` of `all` = m_tiles x n_tiles (columns first) x slices of K; where the last
+// round has tiles for at most half the pairs, those are dealt out as two 256-row halves.
+struct HighTiles {
+  uint32_t blocks, n_tiles, tiles, all, split;  // blocks: of 256 rows; tiles: of one slice; split: whole tiles in front of the halves
+  __device__ __forceinline__ HighTiles(uint32_t rows, uint32_t cols, uint32_t slices, uint32_t pairs) {
+    blocks = (rows + kMmaTile - 1) / kMmaTile;
+    n_tiles = (cols + kMmaTile - 1) / kMmaTile;
+    tiles = (blocks + 1) / 2 * n_tiles;
+    all = tiles * slices;
+    const uint32_t rest = all % pairs;
+    split = rest * 2 <= pairs ? all - rest : all;
+  }
+  __device__ __forceinline__ uint32_t items() const { return split + 2 * (all - split); }
+  __device__ __forceinline__ uint32_t tile_of(uint32_t i) const { return i < split ? i : split + (i - split) / 2; }
+  __device__ __forceinline__ MmaTile at(uint32_t i, uint32_t k_each, uint32_t k_blocks) const {
+    const uint32_t tile = tile_of(i), slice = tile / tiles, t = tile - slice * tiles, half = i < split ? 0 : (i - split) & 1;
+    const uint32_t block = t / n_tiles * 2 + half, left = blocks > block ? blocks - block : 0;
+    return MmaTile{block * kMmaTile, t % n_tiles * kMmaTile, min(slice * k_each, k_blocks), min((slice + 1) * k_each, k_blocks), min(i < split ? 2u : 1u, left)};
+  }
+};
+
+// Slices of K = vocab for dx's tiles: they rarely divide among the pairs, and few rows have few tiles at all.  Taken is the
+// number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile costs beside its products; every
+// CTA (and the kernel that joins the slices) works out the same number.
+__device__ __forceinline__ uint32_t dx_slices(const LossPiece& a, uint32_t n, uint32_t pairs) {
+  const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK;
   uint32_t best = 1, best_cost = 0xFFFFFFFFu;
-  for (uint32_t s = 1; s <= 32 && s <= k_blocks && (s == 1 || (uint64_t)tiles * s <= slots); ++s) {
-    const uint32_t cost = (tiles * s + pairs - 1) / pairs * ((k_blocks + s - 1) / s + kTileCost);
+  for (uint32_t s = 1; s <= 32 && s <= k_blocks; ++s) {
+    const HighTiles h(n, a.hidden, s, pairs);
+    if (s > 1 && h.all > a.slots) break;
+    const uint32_t halves = 2 * ((h.split + pairs - 1) / pairs) + (h.split < h.all ? 1 : 0);  // rounds of 256 rows
+    const uint32_t cost = halves * ((k_blocks + s - 1) / s + kTileCost);
     if (cost < best_cost) { best = s; best_cost = cost; }
   }
   return best;
@@ -348,38 +376,33 @@ __device__ __forceinline__ uint32_t dx_slices(uint32_t tiles, uint32_t k_blocks,
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
 k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
      const __grid_constant__ LossPiece a) {
-  const uint32_t n = *a.count, m_tiles = (n + kMmaTile - 1) / kMmaTile, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile;
-  const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK, tiles = m_tiles * n_tiles;
-  const uint32_t slices = dx_slices(tiles, k_blocks, gridDim.x >> 1, a.slots), each = (k_blocks + slices - 1) / slices;
+  const uint32_t n = *a.count, k_blocks = (a.vocab + kMmaK - 1) / kMmaK, pairs = gridDim.x >> 1;
+  const uint32_t slices = dx_slices(a, n, pairs), each = (k_blocks + slices - 1) / slices;
+  const HighTiles work(n, a.hidden, slices, pairs);
   bool lost;
-  mma_pair_tiles<false, true, 0>(map_p, map_w, tiles * slices, v.bulk_wait_ns, &lost,
-    [&](uint32_t i) {
-      const uint32_t s = i / tiles, t = i - s * tiles;
-      return MmaTile{t / n_tiles * kMmaTile, t % n_tiles * kMmaTile, min(s * each, k_blocks), min((s + 1) * each, k_blocks)};
-    },
+  mma_pair_tiles<false, true, 2, 0>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
+    [&](uint32_t i) { return work.at(i, each, k_blocks); },
     [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, bool, auto&&) {
-      const uint32_t r = row + (threadIdx.x & 31), m = t.m + r, c0 = t.n + col0;
+      const uint32_t r = t.m % kHighRows + row + (threadIdx.x & 31), m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
       const uint32_t cols = min(128u, a.hidden - c0);
-      float* slot = a.dx_slots + ((uint64_t)i * kMmaTile + r) * kMmaTile + col0;
-      float d[32];
+      float* slot = a.dx_slots + ((uint64_t)work.tile_of(i) * kHighRows + r) * kMmaTile + col0;
+      uint32_t d[32];
 #pragma unroll
       for (uint32_t c = 0; c < 128; c += 32) {
         if (c >= cols) break;
         if (tmem == kNone) {
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j) d[j] = 0.f;
+          for (uint32_t j = 0; j < 32; ++j) d[j] = 0;
         } else {
           tmem_load32(tmem + c, d);
+          tmem_wait();
         }
         if (m >= n) continue;
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {
           if (c + q * 8 >= cols) break;
-          uint32_t w[8];
-#pragma unroll
-          for (uint32_t j = 0; j < 8; ++j) w[j] = __float_as_uint(d[q * 8 + j]);
-          store32(slot + c + q * 8, w);
+          store32(slot + c + q * 8, d + q * 8);
         }
       }
     });
@@ -388,17 +411,17 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
 
 // dx of a counted row: f times the sum of the slices, in slice order, rounded once
 __global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
-  const uint32_t n = *a.count, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile, tiles = (n + kMmaTile - 1) / kMmaTile * n_tiles;
-  const uint32_t slices = dx_slices(tiles, (a.vocab + kMmaK - 1) / kMmaK, pairs, a.slots), vecs = a.hidden / 8;
+  const uint32_t n = *a.count, slices = dx_slices(a, n, pairs), vecs = a.hidden / 8;
+  const HighTiles work(n, a.hidden, slices, pairs);
   const uint64_t all = (uint64_t)n * vecs;
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
     const uint32_t m = (uint32_t)(i / vecs), c = (uint32_t)(i % vecs) * 8;
-    const float* slot = a.dx_slots + (((uint64_t)(m / kMmaTile) * n_tiles + c / kMmaTile) * kMmaTile + m % kMmaTile) * kMmaTile + c % kMmaTile;
+    const float* slot = a.dx_slots + (((uint64_t)(m / kHighRows) * work.n_tiles + c / kMmaTile) * kHighRows + m % kHighRows) * kMmaTile + c % kMmaTile;
     const float f = a.factor[m];
     float s[8], t[8];
     load32(slot, s);
     for (uint32_t k = 1; k < slices; ++k) {
-      load32(slot + (uint64_t)k * tiles * kMmaTile * kMmaTile, t);
+      load32(slot + (uint64_t)k * work.tiles * kHighRows * kMmaTile, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += t[j];
     }
@@ -411,11 +434,11 @@ __global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
 k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PoolView v,
      const __grid_constant__ LossPiece a) {
-  const uint32_t n = *a.count, m_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, n_tiles = (a.hidden + kMmaTile - 1) / kMmaTile;
-  const uint32_t k_blocks = (n + kMmaK - 1) / kMmaK;
+  const uint32_t n = *a.count, k_blocks = (n + kMmaK - 1) / kMmaK;
+  const HighTiles work(a.vocab, a.hidden, 1, gridDim.x >> 1);
   bool lost;
-  mma_pair_tiles<true, true, 0>(map_p, map_x, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
-    [&](uint32_t i) { return MmaTile{i / n_tiles * kMmaTile, i % n_tiles * kMmaTile, 0, k_blocks}; },
+  mma_pair_tiles<true, true, 2, 0>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
+    [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); },
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, bool, auto&&) {
       const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
@@ -424,21 +447,24 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
       const float* base = a.add_dw ? (a.dw_dtype == FT_F32 ? static_cast<const float*>(a.dw) : a.dw_acc) : nullptr;
       const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;
       float* out = a.dw_dtype == FT_F32 ? static_cast<float*>(a.dw) : a.dw_acc;
-      float d[32];
+      uint32_t d[32];
 #pragma unroll
       for (uint32_t c = 0; c < 128; c += 32) {
         if (c >= cols) break;
         if (tmem == kNone) {
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j) d[j] = 0.f;
+          for (uint32_t j = 0; j < 32; ++j) d[j] = 0;
         } else {
           tmem_load32(tmem + c, d);
+          tmem_wait();
         }
         if (m >= a.vocab) continue;
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {
           if (c + q * 8 >= cols) break;
-          float (&f)[8] = *reinterpret_cast<float (*)[8]>(d + q * 8);
+          float f[8];
+#pragma unroll
+          for (uint32_t j = 0; j < 8; ++j) f[j] = __uint_as_float(d[q * 8 + j]);
           if (base) {
             const float4 b0 = *reinterpret_cast<const float4*>(base + at + c + q * 8), b1 = *reinterpret_cast<const float4*>(base + at + c + q * 8 + 4);
             f[0] += b0.x; f[1] += b0.y; f[2] += b0.z; f[3] += b0.w; f[4] += b1.x; f[5] += b1.y; f[6] += b1.z; f[7] += b1.w;
@@ -466,7 +492,7 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
   a->padded = (uint32_t)padded;
   a->tiles = (vocab + kStatCols - 1) / kStatCols;
   a->ld_p = (uint32_t)align_up_sz(vocab, 128);  // an epilogue lane's 32-byte stores stay inside its row
-  const uint64_t dx_tiles = padded / kMmaTile * ((hidden + kMmaTile - 1) / kMmaTile);
+  const uint64_t dx_tiles = (padded + kHighRows - 1) / kHighRows * ((hidden + kMmaTile - 1) / kMmaTile);
   a->slots = (uint32_t)std::max<uint64_t>(dx_tiles, kMinSlots);
   a->count = reinterpret_cast<uint32_t*>(take(4));
   a->row_of = reinterpret_cast<int32_t*>(take(4ull * rows));
@@ -478,7 +504,7 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
   a->stat = reinterpret_cast<float2*>(take(8ull * rows * a->tiles));
   a->xc = reinterpret_cast<__nv_bfloat16*>(take(2ull * padded * hidden));
   a->p = reinterpret_cast<__nv_bfloat16*>(take(grad ? 2ull * padded * a->ld_p : 0));
-  a->dx_slots = reinterpret_cast<float*>(take(grad ? 4ull * a->slots * kMmaTile * kMmaTile : 0));
+  a->dx_slots = reinterpret_cast<float*>(take(grad ? 4ull * a->slots * kHighRows * kMmaTile : 0));
   a->dw_acc = reinterpret_cast<float*>(take(acc ? 4ull * vocab * hidden : 0));
   return off;
 }

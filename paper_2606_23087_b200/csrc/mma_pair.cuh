@@ -1,11 +1,15 @@
-// A persistent bf16 matrix product on CTA pairs: 256 x 256 tiles of D = A B^T, fp32 sums in tensor memory, the epilogue
-// supplied by the caller.
+// A persistent bf16 matrix product on CTA pairs: tiles of D = A B^T, 256 columns wide and 256 or 512 rows high, fp32 sums in
+// tensor memory, the epilogue supplied by the caller.
 //
-// Two CTAs of a cluster (two SMs) work on one tile.  Each holds half of A's rows and half of B's: 16 KiB + 16 KiB a stage of
-// 64 columns of K, brought by TMA (128-byte swizzle) into a ring of kStages stages.  One thread of the even CTA issues the
-// matrix instructions of both (M 256, N 256, K 16); each CTA's tensor memory receives its 128 rows, in one of two
-// accumulators of 256 columns, so the epilogue of one tile runs beside the products of the next.  With a pair a stage
-// carries 64 KiB for 2 x 64 KiB of operands used: shared-memory traffic per product is half of a single CTA's 128 x 256.
+// Two CTAs of a cluster (two SMs) work on one tile.  Each holds half of A's rows and half of B's: 16 KiB for each 256 rows
+// of the tile and 16 KiB of B a stage of 64 columns of K, brought by TMA (128-byte swizzle) into a ring of stages.  One thread
+// of the even CTA issues the matrix instructions of both (M 256, N 256, K 16); each CTA's tensor memory receives its 128 rows
+// of each 256, in one of two accumulators of 256 columns.
+//
+//   kHigh = 1  256 rows: the accumulators alternate, the epilogue of one runs beside the products into the other
+//   kHigh = 2  512 rows: both accumulators belong to one tile and share its B, which takes 48 KiB from L2 where two lower
+//              tiles take 64.  A long product runs at the card's power limit, and bytes moved from L2 are what is left to
+//              save there; the epilogue stands alone, so this is for long K
 //
 // Operands need not be stored with K innermost: `kMn` operands have the tile's own dimension innermost (a row of the matrix
 // in memory per K index), as P and x in dW = P^T x; TMA brings 64 x 64 boxes either way and the descriptor says which.
@@ -23,21 +27,22 @@
 
 namespace ft {
 
-constexpr uint32_t kMmaTile = 256;    // rows and columns of a pair's tile
+constexpr uint32_t kMmaTile = 256;    // rows of an accumulator over the pair, columns of a tile
 constexpr uint32_t kMmaK = 64;        // K a stage: 128 bytes of bf16
-constexpr int kMmaStages = 6;
 constexpr uint32_t kMmaBox = 64 * kMmaK * 2;         // one TMA box, 8 KiB
-constexpr uint32_t kMmaOperand = 2 * kMmaBox;        // a CTA's half of an operand, a stage
-constexpr uint32_t kMmaStage = 2 * kMmaOperand;
+constexpr uint32_t kMmaOperand = 2 * kMmaBox;        // a CTA's half of 256 rows of an operand, a stage
+template <int kHigh>
+constexpr int kMmaStages = kHigh == 1 ? 6 : 4;
 constexpr int kMmaThreads = 384;
 constexpr int kMmaEpilogueWarps = 8;
-constexpr size_t kMmaSmem = (size_t)kMmaStages * kMmaStage + 1024 + 256;  // tiles on a 1 KiB boundary, then the barriers
+constexpr size_t kMmaRing = 6 * 2 * kMmaOperand;     // the stages of either height: 192 KiB
+constexpr size_t kMmaSmem = kMmaRing + 1024 + 256;   // on a 1 KiB boundary, then the barriers
 
 struct MmaBarriers {
-  uint64_t full[kMmaStages], empty[kMmaStages], acc_full[2], acc_empty[2], drain;
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
   uint32_t tmem, lost;
 };
-static_assert(sizeof(MmaBarriers) <= 256, "kMmaSmem");
+static_assert(sizeof(MmaBarriers) <= 256 && kMmaStages<2> * 3 * kMmaOperand <= kMmaRing, "kMmaSmem");
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ void cluster_sync() {
@@ -82,29 +87,15 @@ __device__ __forceinline__ void mma_issue(uint32_t tmem, uint64_t da, uint64_t d
                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                ::"r"(tmem), "l"(da), "l"(db), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-// 16 or 32 columns of the warp's 32 rows; the whole warp takes part
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&f)[16]) {
-  uint32_t r[16];
+// Columns of the warp's 32 rows, 32 a load; the whole warp takes part.  The values are there behind tmem_wait().
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
   __syncwarp();
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr) : "memory");
-#pragma unroll
-  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(r[i]);
-}
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&f)[32]) {
-  uint32_t r[32];
-  __syncwarp();
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-      "tcgen05.wait::ld.sync.aligned;"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr) : "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory descriptor (PTX ISA, "matrix descriptor"): bits 0-13 address / 16, 16-29 leading offset / 16, 32-45 stride
 // offset / 16, 46-47 = 1, 61-63 = 2 for the 128-byte swizzle.
@@ -124,30 +115,32 @@ constexpr uint32_t kMmaStep = kMn ? 2048 : 32;
 template <bool kAMn, bool kBMn>
 constexpr uint32_t kMmaInstr = 1u << 4 | 1u << 7 | 1u << 10 | (kAMn ? 1u << 15 : 0) | (kBMn ? 1u << 16 : 0) | (256 >> 3) << 17 | (256 >> 4) << 24;
 
-// One tile of work: rows from m, columns from n, K blocks [k0, k1).
+// One tile of work: rows from m (256 times `high` of them; none: nothing to do), columns from n, K blocks [k0, k1).
 struct MmaTile {
-  uint32_t m, n, k0, k1;
+  uint32_t m, n, k0, k1, high;
 };
 
 // Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; every epilogue warp calls
-// epilogue(tile, i, tmem, row, col0, last, release): tensor memory from `tmem` on holds 128 columns of its 32 rows, lane l the
-// row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() once it has read them (it is called behind it
-// otherwise).  A tile without K blocks has tmem = kNone: all sums are zero.
+// epilogue(tile, i, tmem, row, col0, last, release) for each 256 rows: tensor memory from `tmem` on holds 128 columns of its 32 rows,
+// lane l the row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() once it has read them (it is called
+// behind it otherwise).  A tile without K blocks has tmem = kNone: all sums are zero.
 //
-// kPart > 0: the sums of every kPart blocks of K are handed over by themselves (the final ones with `last`), for an
+// kPart > 0 (kHigh = 1): the sums of every kPart blocks of K are handed over by themselves (the final ones with `last`), for an
 // epilogue that adds them up in registers.  The tensor cores add with truncation, K / 16 times a sum, so a long K drifts
-// towards zero (2.6e-6 of a logit over 3584); a part of 8 blocks truncates 32 times, and the parts are added with rounding
-// to nearest.
-template <bool kAMn, bool kBMn, uint32_t kPart, class TileAt, class Epilogue>
+// towards zero (2.6e-6 of a logit over 3584); parts bound the number of truncations and are added with rounding to nearest.
+// Reading an accumulator holds the products up by some 800 cycles, so parts are not shorter than the error asks for.
+template <bool kAMn, bool kBMn, int kHigh, uint32_t kPart, class TileAt, class Epilogue>
 __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, uint64_t limit_ns, bool* lost_out,
                                                TileAt tile_at, Epilogue epilogue) {
+  static_assert(kHigh == 1 || kPart == 0, "parts alternate between the accumulators");
   extern __shared__ uint8_t smem_raw[];
+  constexpr uint32_t kStages = kMmaStages<kHigh>, kStageBytes = (kHigh + 1) * kMmaOperand;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  MmaBarriers* bar = reinterpret_cast<MmaBarriers*>(stages + (size_t)kMmaStages * kMmaStage);
+  MmaBarriers* bar = reinterpret_cast<MmaBarriers*>(stages + kMmaRing);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kMmaStages; ++s) { mbar_init(&bar->full[s], 1); mbar_init(&bar->empty[s], 1); }
+    for (uint32_t s = 0; s < kStages; ++s) { mbar_init(&bar->full[s], 1); mbar_init(&bar->empty[s], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&bar->acc_full[i], 1); mbar_init(&bar->acc_empty[i], 2 * kMmaEpilogueWarps); }
     mbar_init(&bar->drain, 1);
     bar->lost = 0;
@@ -162,61 +155,79 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   cluster_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const uint32_t tmem = bar->tmem;
+  const uint32_t tmem = bar->tmem, base = smem_u32(stages);
   bool lost = false;
+  uint32_t it = 0;            // stages used so far
+  uint32_t used[2] = {0, 0};  // times each accumulator was used so far
+  uint32_t turn = 0;          // kHigh = 1: the accumulator that is next
   // An epilogue that keeps 128 sums a lane gets 216 registers for its two warpgroups, the other warpgroup 64: 63488 of the
   // 384 x 168 = 64512 that the block was launched with.
   if (warp < 4) {
     if constexpr (kPart > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 && lane == 0) {
-      uint32_t it = 0;  // stages filled so far
-      const uint32_t base = smem_u32(stages);
       for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
         const MmaTile t = tile_at(i);
+        if (t.high == 0) continue;
         const int32_t a0 = (int32_t)(t.m + rank * 128), b0 = (int32_t)(t.n + rank * 128);
         for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
-          const uint32_t s = it % kMmaStages, ph = (it / kMmaStages) & 1;
-          if (!mbar_wait_bounded(&bar->empty[s], ph ^ 1, limit_ns)) { lost = true; break; }
-          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * kMmaStage);
-          const uint32_t full = in_even_cta(&bar->full[s]), sa = base + s * kMmaStage, sb = sa + kMmaOperand;
+          const uint32_t s = it % kStages;
+          if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
+          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * (t.high + 1) * kMmaOperand);
+          const uint32_t full = in_even_cta(&bar->full[s]), sb = base + s * kStageBytes;
           const int32_t kk = (int32_t)(k * kMmaK);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            if (kAMn) tma_box(sa + h * kMmaBox, &map_a, a0 + 64 * h, kk, full);
-            else tma_box(sa + h * kMmaBox, &map_a, kk, a0 + 64 * h, full);
             if (kBMn) tma_box(sb + h * kMmaBox, &map_b, b0 + 64 * h, kk, full);
             else tma_box(sb + h * kMmaBox, &map_b, kk, b0 + 64 * h, full);
+          }
+#pragma unroll
+          for (int h = 0; h < 2 * kHigh; ++h) {
+            if (h >= 2 && t.high < 2) break;
+            const int32_t row = a0 + 64 * (h & 1) + (int32_t)kMmaTile * (h >> 1);
+            if (kAMn) tma_box(sb + kMmaOperand + h * kMmaBox, &map_a, row, kk, full);
+            else tma_box(sb + kMmaOperand + h * kMmaBox, &map_a, kk, row, full);
           }
         }
       }
       // what still arrives in this CTA's shared memory: the loads of the last stages (both CTAs' bytes are counted in the
       // even one), and the even CTA's signals that it is done with them
-      const uint32_t j0 = it > kMmaStages ? it - kMmaStages : 0;
+      const uint32_t j0 = it > kStages ? it - kStages : 0;
       if (lost && rank == 0)
-        for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
-      for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kMmaStages], (j / kMmaStages) & 1, limit_ns);
+        for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kStages], (j / kStages) & 1, limit_ns);
+      for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kStages], (j / kStages) & 1, limit_ns);
     } else if (warp == 1 && lane == 0 && rank == 0) {
-      uint32_t it = 0, local = 0;
-      const uint32_t base = smem_u32(stages);
+      const auto take = [&](uint32_t acc) {  // waits until the accumulator's last user has read it
+        if (!mbar_wait_bounded(&bar->acc_empty[acc], (used[acc]++ & 1) ^ 1, limit_ns)) lost = true;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      };
       for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
         const MmaTile t = tile_at(i);
+        if (t.high == 0) continue;
         for (uint32_t k = t.k0; k < t.k1 && !lost;) {
-          const uint32_t acc = local & 1, aph = (local >> 1) & 1, kp = kPart ? min(k + kPart, t.k1) : t.k1, first = k;
-          ++local;
-          if (!mbar_wait_bounded(&bar->acc_empty[acc], aph ^ 1, limit_ns)) { lost = true; break; }
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          for (; k < kp; ++k, ++it) {
-            const uint32_t s = it % kMmaStages;
-            if (!mbar_wait_bounded(&bar->full[s], (it / kMmaStages) & 1, limit_ns)) { lost = true; break; }
+          const uint32_t kp = kPart ? min(k + kPart, t.k1) : t.k1, first = k, acc0 = kHigh == 1 ? turn : 0;
+          take(acc0);
+          for (; k < kp && !lost; ++k, ++it) {
+            const uint32_t s = it % kStages;
+            if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t sa = base + s * kMmaStage, sb = sa + kMmaOperand;
+            const uint32_t sb = base + s * kStageBytes;
 #pragma unroll
-            for (uint32_t j = 0; j < kMmaK / 16; ++j)
-              mma_issue(tmem + acc * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>), kMmaInstr<kAMn, kBMn>,
-                        k > first || j > 0);
+            for (uint32_t h = 0; h < kHigh; ++h) {
+              if (h == 1) {
+                if (t.high < 2) break;
+                if (k == first) take(1);
+                if (lost) break;
+              }
+              const uint32_t sa = sb + (1 + h) * kMmaOperand;
+#pragma unroll
+              for (uint32_t j = 0; j < kMmaK / 16; ++j)
+                mma_issue(tmem + (acc0 + h) * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>),
+                          kMmaInstr<kAMn, kBMn>, k > first || j > 0);
+              if (k + 1 == kp) mma_commit(&bar->acc_full[acc0 + h]);
+            }
             mma_commit(&bar->empty[s]);
           }
-          if (!lost) mma_commit(&bar->acc_full[acc]);
+          turn ^= 1;
         }
       }
       if (lost) {  // products under way still read shared memory and write tensor memory
@@ -226,8 +237,8 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
     }
   } else {
     if constexpr (kPart > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2, row = rank * 128 + quarter * 32, col0 = half * 128;
-    uint32_t local = 0, acc = 0;
+    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2, col0 = half * 128;
+    uint32_t acc = 0;
     bool held = false;
     const auto release = [&] {
       if (!held) return;
@@ -238,22 +249,25 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
     };
     for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
       const MmaTile t = tile_at(i);
-      uint32_t k = t.k0;
-      do {
-        uint32_t at = kNone;
-        if (t.k0 < t.k1) {
-          acc = local & 1;
-          lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], (local >> 1) & 1, limit_ns));
-          if (lost) break;
-          ++local;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          at = tmem + acc * 256 + col0 + (quarter << 21);
-          held = true;
-        }
-        k = kPart ? min(k + kPart, t.k1) : t.k1;
-        epilogue(t, i, at, row, col0, k >= t.k1, release);
-        release();
-      } while (k < t.k1);
+      for (uint32_t h = 0; h < t.high && !lost; ++h) {
+        uint32_t k = t.k0;
+        do {
+          uint32_t at = kNone;
+          if (t.k0 < t.k1) {
+            acc = kHigh == 1 ? turn : h;
+            lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], used[acc] & 1, limit_ns));
+            if (lost) break;
+            ++used[acc];
+            turn ^= 1;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            at = tmem + acc * 256 + col0 + (quarter << 21);
+            held = true;
+          }
+          k = kPart ? min(k + kPart, t.k1) : t.k1;
+          epilogue(t, i, at, h * kMmaTile + rank * 128 + quarter * 32, col0, k >= t.k1, release);
+          release();
+        } while (k < t.k1);
+      }
     }
   }
   if (lost) bar->lost = 1;
