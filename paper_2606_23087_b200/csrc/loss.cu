@@ -5,19 +5,21 @@
 //
 //   k_pick    takes the rows that count out of a piece of the rows: a dense copy of their x, their labels and row
 //             numbers.  Rows labelled -100 cost no products, and what they hold cannot reach dW as 0 * NaN.  It also
-//             takes each row's reference: the label's logit, x . W[label]
-//   k_logits  z by tiles; a row of a tile gives the sum of e = exp(z - reference), and with gradients e itself in bf16
-//             (rounding e costs 2^-8 of a probability, where rounding z would cost 2^-8 of z)
-//   k_join    adds a row's sums: lse = reference + log(sum)
+//             takes each row's reference: the label's logit, x . W[label], by fp32 FMAs
+//   k_logits  z by tiles; a row of a tile gives the sum of e = exp(z - reference) over the columns that are not its label,
+//             and with gradients e itself in bf16 (rounding e costs 2^-8 of a probability, rounding z would cost 2^-8 of z)
+//   k_join    adds a row's sums to S: loss = log(1 + S), lse = reference + loss
 //   k_finish  d = f e with one factor f = g exp(reference - lse) a row: f goes to the row's x for dW (rounded to bf16) and to
-//             the row's sums for dx, so e is not touched again but for the label's element, (exp(z - lse) - 1) exp(lse - reference)
+//             the row's sums for dx, so e is not touched again but for the label's element, (exp(-loss) - 1) exp(lse - reference)
 //   k_dx, k_dw  the two products
 //
 // Why a reference known before any logit: with each tile's own maximum, the usual choice, e has to be read, scaled and
-// written again once lse is known (1.1 ms of 10.7 for 16384 rows x 32768).  bf16 has fp32's range, so any reference within
-// 2^60 of exp(lse) serves as well as the maximum; the label's logit is that, unless a row's loss is above 41.  Such a row
-// (and one whose reference is far above everything or not finite) gets its maximum as reference, and its row tile's logits
-// are worked out once more (k_logits<., true>, which returns at once where there is none).
+// written again once lse is known (1.1 ms of 10.7 for 16384 rows x 32768).  bf16 has fp32's range, so any reference that is not
+// far below lse serves as well as the maximum; the label's logit is that, unless a row's loss is above 41.  Such a row gets its
+// maximum as reference, and its row tile's logits are worked out once more (k_logits<., true, .>, which returns at once where
+// there is none).  And it makes small losses exact: the label's term of the sum is 1, not a difference of two large numbers,
+// and the tensor cores' truncating additions (2.6e-6 of a logit over 3584) do not touch the one logit that a loss
+// depends on most: 2.6e-6 -> 3e-7 of the loss.
 #include <algorithm>
 
 #include "mma_pair.cuh"
@@ -26,9 +28,9 @@ namespace ft {
 
 constexpr uint32_t kStatCols = 128;  // columns of the vocabulary that share a row's sum
 constexpr uint32_t kTileCost = 6;    // what a tile of dx costs beside its products, in blocks of K
-constexpr uint32_t kPartBlocks = 16; // blocks of K whose logits are summed by the tensor cores alone: 64 truncations, 7e-7 of a logit
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSumLimit = 0x1p60f;  // a row's sum outside [1 / limit, limit] wants another reference
+constexpr uint32_t kMinusInf = 0xFF800000u;
+constexpr float kSumLimit = 0x1p60f;  // a row's sum above this wants another reference
 constexpr int32_t kNoLabel = -100;
 constexpr uint32_t kPieceRowsMost = 65536;
 constexpr uint32_t kHighRows = 2 * kMmaTile;  // rows of a tile of dx and dw
@@ -50,9 +52,9 @@ struct LossPiece {
   uint32_t* count;         // rows of the piece that count
   int32_t *row_of, *label; // [count] row in the piece, label
   uint32_t* redo;          // [1 + row tiles] whether any, and which row tiles need another reference
-  float *ref, *target;     // [count] the reference, and the label's logit as the product gives it
-  float* factor;           // [count] f
-  float2* stat;            // [tiles][rows] maximum of z and sum of e of a row in a tile
+  float *ref, *target;     // [count] the reference, and the label's logit
+  float* factor;           // [count] lse - reference, then f
+  float2* stat;            // [tiles][rows] maximum of z and sum of e of a row in a tile, the label's column apart
   __nv_bfloat16* xc;       // [padded][hidden]
   __nv_bfloat16* p;        // [padded][ld_p] e
   float* dx_slots;         // [slots][512][256] dx by slices of the vocabulary and tiles
@@ -136,7 +138,7 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
         dst[c] = xv;
       }
       dot = warp_sum(dot);
-      if (lane == 0) a.ref[dest[k]] = dot;
+      if (lane == 0) a.ref[dest[k]] = a.target[dest[k]] = dot;
     } else if (a.dx) {
       uint4* dst = reinterpret_cast<uint4*>(a.dx + (a.row0 + r0 + k) * a.lddx);
       for (uint32_t c = lane; c < vecs; c += 32) dst[c] = zero;
@@ -165,84 +167,77 @@ __device__ __forceinline__ void give_up(const PoolView& v, uint64_t call_seq, bo
   if (lost && threadIdx.x == 0) note_error(v, call_seq, FT_ERR_TIMEOUT, blockIdx.x);
 }
 
-// z by tiles.  A lane owns a row's 128 columns, whose sums it adds up in registers from parts of K.
-template <bool kKeep, bool kRedo>
+// z by tiles; a lane owns a row's 128 columns.  kRedo: only the row tiles whose reference has changed.
+template <bool kKeep, bool kRedo, int kHigh>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
 k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
          const __grid_constant__ LossPiece a) {
   __shared__ uint8_t s_tile[kRedo ? kPieceRowsMost / kMmaTile : 1];
   __shared__ uint32_t s_tiles;
   const uint32_t n = *a.count, n_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
-  uint32_t m_tiles = (n + kMmaTile - 1) / kMmaTile;
+  uint32_t blocks = (n + kMmaTile - 1) / kMmaTile;
   if constexpr (kRedo) {
     if (a.redo[0] == 0) return;
     if (threadIdx.x == 0) {
       uint32_t c = 0;
-      for (uint32_t t = 0; t < m_tiles; ++t)
+      for (uint32_t t = 0; t < blocks; ++t)
         if (a.redo[1 + t]) s_tile[c++] = (uint8_t)t;
       s_tiles = c;
     }
     __syncthreads();
-    m_tiles = s_tiles;
+    blocks = s_tiles;
   }
+  const uint32_t m_tiles = (blocks + kHigh - 1) / kHigh;
   bool lost;
-  float z[kStatCols];  // zero between tiles
-#pragma unroll
-  for (uint32_t j = 0; j < kStatCols; ++j) z[j] = 0.f;
-  mma_pair_tiles<false, false, 1, kPartBlocks>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+  mma_pair_tiles<false, false, kHigh>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
     [&](uint32_t i) {
-      // bands of eight row tiles, all columns of a band before the next: a band's rows (8 x 256 x hidden) stay in L2
-      const uint32_t band = i / (8 * n_tiles), in = i - band * 8 * n_tiles, high = min(8u, m_tiles - band * 8), m = band * 8 + in % high;
-      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m) * kMmaTile, in / high * kMmaTile, 0, k_blocks, 1};
+      // bands of 2048 rows, all columns of a band before the next: a band's x stays in L2
+      constexpr uint32_t kBand = 8 / kHigh;
+      const uint32_t band = i / (kBand * n_tiles), in = i - band * kBand * n_tiles, rows = min(kBand, m_tiles - band * kBand), m = band * kBand + in % rows;
+      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m * kHigh) * kMmaTile, in / rows * kMmaTile, 0, k_blocks, min((uint32_t)kHigh, blocks - m * kHigh)};
     },
-    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, bool last, auto&& release) {
+    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t c0 = t.n + col0;
       if (c0 >= a.vocab) return;
+      uint32_t z[kStatCols / 32][32];
 #pragma unroll
-      for (uint32_t c = 0; c < kStatCols; c += 64) {  // 64 columns in flight: a wait for each 16 made this the bottleneck
-        uint32_t s0[32], s1[32];
-        tmem_load32(tmem + c, s0);
-        tmem_load32(tmem + c + 32, s1);
-        tmem_wait();
-#pragma unroll
-        for (uint32_t j = 0; j < 32; ++j) { z[c + j] += __uint_as_float(s0[j]); z[c + 32 + j] += __uint_as_float(s1[j]); }
-      }
-      if (!last) return;
-      release();
+      for (uint32_t c = 0; c < kStatCols / 32; ++c) tmem_load32(tmem + 32 * c, z[c]);
+      tmem_wait();
+      release();  // the products go on while the exponentials are taken
       const uint32_t m = t.m + row + (threadIdx.x & 31), cols = min(kStatCols, a.vocab - c0);
       const uint32_t label_at = m < n ? (uint32_t)a.label[m] - c0 : kNone;
       const float ref = m < n ? a.ref[m] : 0.f;
+      [[maybe_unused]] const uint32_t keep = m < n ? 0xFFFFFFFFu : 0u;  // rows beyond the last one that counts: zeros, which the product over rows adds
       if (label_at < kStatCols) {
 #pragma unroll
         for (uint32_t j = 0; j < kStatCols; ++j)
-          if (j == label_at) a.target[m] = z[j];
+          if (j == label_at) z[j / 32][j % 32] = kMinusInf;
       }
-      float top = -INFINITY, sum = 0.f;
-      if (cols < kStatCols) {  // beyond the vocabulary: e = 0
+      if (cols < kStatCols) {  // beyond the vocabulary
 #pragma unroll
         for (uint32_t j = 0; j < kStatCols; ++j)
-          if (j >= cols) z[j] = -INFINITY;
+          if (j >= cols) z[j / 32][j % 32] = kMinusInf;
       }
+      float top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (uint32_t c = 0; c < kStatCols; c += 16) {
+        float e[16];
 #pragma unroll
         for (uint32_t j = 0; j < 16; ++j) {
-          top = fmaxf(top, z[c + j]);
-          z[c + j] = exp2_fast((z[c + j] - ref) * kLog2e);
-          sum += z[c + j];
+          const float x = __uint_as_float(z[(c + j) / 32][(c + j) % 32]);
+          top = fmaxf(top, x);
+          e[j] = exp2_fast((x - ref) * kLog2e);
+          sum += e[j];
         }
         if constexpr (kKeep) {
-          // rows beyond the last one that counts: zeros, which the product over rows adds
-          const uint32_t keep = m < n ? 0xFFFFFFFFu : 0u;
+          if (c >= cols) continue;
           uint32_t w[8];
 #pragma unroll
-          for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(z[c + 2 * j], z[c + 2 * j + 1]) & keep;
+          for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(e[2 * j], e[2 * j + 1]) & keep;
           store32(a.p + (uint64_t)m * a.ld_p + c0 + c, w);
         }
       }
       if (m < n) a.stat[(uint64_t)(c0 / kStatCols) * a.rows + m] = make_float2(top, sum);
-#pragma unroll
-      for (uint32_t j = 0; j < kStatCols; ++j) z[j] = 0.f;
     });
   give_up(v, a.call_seq, lost);
 }
@@ -271,12 +266,15 @@ __device__ __forceinline__ float2 join_tiles(const LossPiece& a, uint32_t n, uin
   }
   return make_float2(top, sum);
 }
+// loss and lse from the sum over the columns that are not the label, and lse - reference for k_finish (in factor); returns the loss
 __device__ __forceinline__ float store_loss(const LossPiece& a, uint32_t m, float sum) {
-  const float lse = a.ref[m] + logf(sum);
+  const float ref = a.ref[m], target = a.target[m];
+  const float above = ref == target ? log1pf(sum) : logf(sum + expf(target - ref)), loss = (ref - target) + above;
   const uint64_t row = a.row0 + a.row_of[m];
-  a.lse[row] = lse;
-  a.loss[row] = lse - a.target[m];
-  return lse;
+  a.loss[row] = loss;
+  a.lse[row] = target + loss;
+  a.factor[m] = above;
+  return loss;
 }
 
 __global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
@@ -284,8 +282,7 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
   if (blockIdx.x * 32 >= n) return;
   const float2 s = join_tiles(a, n, m);
   if (threadIdx.x >= 32 || m >= n) return;
-  const bool other = (s.y > kSumLimit || s.y < 1.f / kSumLimit || isinf(a.ref[m])) && s.x < INFINITY && s.x > -INFINITY;
-  if (other) {
+  if (s.y > kSumLimit && s.x < INFINITY) {
     a.ref[m] = s.x;
     a.redo[1 + m / kMmaTile] = 1;
     a.redo[0] = 1;
@@ -305,14 +302,15 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
   float sum = 0.f;
   if (again) sum = join_tiles(a, n, m).y;
   if (warp == 0 && m < n) {
-    const float lse = again ? store_loss(a, m, sum) : a.lse[a.row0 + a.row_of[m]];
+    const float loss = again ? store_loss(a, m, sum) : a.loss[a.row0 + a.row_of[m]];
     if constexpr (kGrad) {
       const float g = a.grad_loss ? a.grad_loss[(a.row0 + a.row_of[m]) * a.grad_stride] : 1.f;
+      const float above = a.factor[m];
       // The label's element outweighs the row's others together, so f takes up its rounding (at most 2^-8): f q is the label's d,
-      // and dw's error that of f x's rounding alone (2.4e-3 of its norm instead of 2.7e-3, the output's own 1.7e-3 included).
-      const float e = expm1f(a.target[m] - lse) * expf(lse - a.ref[m]);
+      // and dw's error that of f x's rounding alone (2.3e-3 of its norm instead of 2.7e-3, the output's own 1.7e-3 included).
+      const float e = expm1f(-loss) * expf(above);
       const __nv_bfloat16 q = __float2bfloat16_rn(e);
-      const float r = e / __bfloat162float(q), f = g * expf(a.ref[m] - lse) * (r > 0.99f && r < 1.01f ? r : 1.f);
+      const float r = e / __bfloat162float(q), f = g * expf(-above) * (r > 0.99f && r < 1.01f ? r : 1.f);
       a.factor[m] = f;
       s_f[lane] = f;
       a.p[(uint64_t)m * a.ld_p + a.label[m]] = q;
@@ -380,9 +378,9 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   const uint32_t slices = dx_slices(a, n, pairs), each = (k_blocks + slices - 1) / slices;
   const HighTiles work(n, a.hidden, slices, pairs);
   bool lost;
-  mma_pair_tiles<false, true, 2, 0>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
+  mma_pair_tiles<false, true, 2>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
     [&](uint32_t i) { return work.at(i, each, k_blocks); },
-    [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, bool, auto&&) {
+    [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, auto&&) {
       const uint32_t r = t.m % kHighRows + row + (threadIdx.x & 31), m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
       const uint32_t cols = min(128u, a.hidden - c0);
@@ -437,9 +435,9 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   const uint32_t n = *a.count, k_blocks = (n + kMmaK - 1) / kMmaK;
   const HighTiles work(a.vocab, a.hidden, 1, gridDim.x >> 1);
   bool lost;
-  mma_pair_tiles<true, true, 2, 0>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
+  mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
     [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); },
-    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, bool, auto&&) {
+    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&&) {
       const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
       const uint32_t cols = min(128u, a.hidden - c0);
@@ -551,7 +549,8 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   const unsigned pairs = (unsigned)p->sm_count / 2, grid = 2 * pairs;
   if (!p->loss_attr_set) {  // once per pool, hence once per device the pool lives on
-    for (auto k : {k_logits<false, false>, k_logits<false, true>, k_logits<true, false>, k_logits<true, true>})
+    for (auto k : {k_logits<false, false, 1>, k_logits<false, false, 2>, k_logits<false, true, 1>, k_logits<true, false, 1>, k_logits<true, false, 2>,
+                   k_logits<true, true, 1>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
     FT_CUDA(cudaFuncSetAttribute(k_dx, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
     FT_CUDA(cudaFuncSetAttribute(k_dw, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
@@ -564,18 +563,19 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     a.last = r0 + a.rows == rows;
     k_pick<<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
     const unsigned joins = (a.rows + 31) / 32;
+    const bool high = a.rows > kMmaTile;
     if (grad) {
-      k_logits<true, false><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      (high ? k_logits<true, false, 2> : k_logits<true, false, 1>)<<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
       k_join<<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
-      k_logits<true, true><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      k_logits<true, true, 1><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
       k_finish<true><<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
       k_dx<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_w, p->view, a);
       k_dx_join<<<(unsigned)p->sm_count * 4, 256, 0, st>>>(a, pairs);
       k_dw<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_x, p->view, a);
     } else {
-      k_logits<false, false><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      (high ? k_logits<false, false, 2> : k_logits<false, false, 1>)<<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
       k_join<<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
-      k_logits<false, true><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
+      k_logits<false, true, 1><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
       k_finish<false><<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
     }
     p->gpu_launches += grad ? 8 : 5;

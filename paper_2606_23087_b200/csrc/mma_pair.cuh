@@ -121,18 +121,12 @@ struct MmaTile {
 };
 
 // Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; every epilogue warp calls
-// epilogue(tile, i, tmem, row, col0, last, release) for each 256 rows: tensor memory from `tmem` on holds 128 columns of its 32 rows,
-// lane l the row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() once it has read them (it is called
-// behind it otherwise).  A tile without K blocks has tmem = kNone: all sums are zero.
-//
-// kPart > 0 (kHigh = 1): the sums of every kPart blocks of K are handed over by themselves (the final ones with `last`), for an
-// epilogue that adds them up in registers.  The tensor cores add with truncation, K / 16 times a sum, so a long K drifts
-// towards zero (2.6e-6 of a logit over 3584); parts bound the number of truncations and are added with rounding to nearest.
-// Reading an accumulator holds the products up by some 800 cycles, so parts are not shorter than the error asks for.
-template <bool kAMn, bool kBMn, int kHigh, uint32_t kPart, class TileAt, class Epilogue>
+// epilogue(tile, i, tmem, row, col0, release) for each 256 rows: tensor memory from `tmem` on holds 128 columns of its 32 rows, lane
+// l the row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() as soon as it has read them.  A tile
+// without K blocks has tmem = kNone: all sums are zero.
+template <bool kAMn, bool kBMn, int kHigh, class TileAt, class Epilogue>
 __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, uint64_t limit_ns, bool* lost_out,
                                                TileAt tile_at, Epilogue epilogue) {
-  static_assert(kHigh == 1 || kPart == 0, "parts alternate between the accumulators");
   extern __shared__ uint8_t smem_raw[];
   constexpr uint32_t kStages = kMmaStages<kHigh>, kStageBytes = (kHigh + 1) * kMmaOperand;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -160,10 +154,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   uint32_t it = 0;            // stages used so far
   uint32_t used[2] = {0, 0};  // times each accumulator was used so far
   uint32_t turn = 0;          // kHigh = 1: the accumulator that is next
-  // An epilogue that keeps 128 sums a lane gets 216 registers for its two warpgroups, the other warpgroup 64: 63488 of the
-  // 384 x 168 = 64512 that the block was launched with.
   if (warp < 4) {
-    if constexpr (kPart > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 && lane == 0) {
       for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
         const MmaTile t = tile_at(i);
@@ -202,32 +193,30 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
       };
       for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
         const MmaTile t = tile_at(i);
-        if (t.high == 0) continue;
-        for (uint32_t k = t.k0; k < t.k1 && !lost;) {
-          const uint32_t kp = kPart ? min(k + kPart, t.k1) : t.k1, first = k, acc0 = kHigh == 1 ? turn : 0;
-          take(acc0);
-          for (; k < kp && !lost; ++k, ++it) {
-            const uint32_t s = it % kStages;
-            if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t sb = base + s * kStageBytes;
+        if (t.high == 0 || t.k0 == t.k1) continue;
+        const uint32_t acc0 = kHigh == 1 ? turn : 0;
+        turn ^= 1;
+        take(acc0);
+        for (uint32_t k = t.k0; k < t.k1 && !lost; ++k, ++it) {
+          const uint32_t s = it % kStages;
+          if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t sb = base + s * kStageBytes;
 #pragma unroll
-            for (uint32_t h = 0; h < kHigh; ++h) {
-              if (h == 1) {
-                if (t.high < 2) break;
-                if (k == first) take(1);
-                if (lost) break;
-              }
-              const uint32_t sa = sb + (1 + h) * kMmaOperand;
-#pragma unroll
-              for (uint32_t j = 0; j < kMmaK / 16; ++j)
-                mma_issue(tmem + (acc0 + h) * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>),
-                          kMmaInstr<kAMn, kBMn>, k > first || j > 0);
-              if (k + 1 == kp) mma_commit(&bar->acc_full[acc0 + h]);
+          for (uint32_t h = 0; h < kHigh; ++h) {
+            if (h == 1) {
+              if (t.high < 2) break;
+              if (k == t.k0) take(1);
+              if (lost) break;
             }
-            mma_commit(&bar->empty[s]);
+            const uint32_t sa = sb + (1 + h) * kMmaOperand;
+#pragma unroll
+            for (uint32_t j = 0; j < kMmaK / 16; ++j)
+              mma_issue(tmem + (acc0 + h) * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>),
+                        kMmaInstr<kAMn, kBMn>, k > t.k0 || j > 0);
+            if (k + 1 == t.k1) mma_commit(&bar->acc_full[acc0 + h]);
           }
-          turn ^= 1;
+          mma_commit(&bar->empty[s]);
         }
       }
       if (lost) {  // products under way still read shared memory and write tensor memory
@@ -236,7 +225,6 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
       }
     }
   } else {
-    if constexpr (kPart > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const uint32_t quarter = warp & 3, half = (warp - 4) >> 2, col0 = half * 128;
     uint32_t acc = 0;
     bool held = false;
@@ -250,23 +238,18 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
     for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
       const MmaTile t = tile_at(i);
       for (uint32_t h = 0; h < t.high && !lost; ++h) {
-        uint32_t k = t.k0;
-        do {
-          uint32_t at = kNone;
-          if (t.k0 < t.k1) {
-            acc = kHigh == 1 ? turn : h;
-            lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], used[acc] & 1, limit_ns));
-            if (lost) break;
-            ++used[acc];
-            turn ^= 1;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            at = tmem + acc * 256 + col0 + (quarter << 21);
-            held = true;
-          }
-          k = kPart ? min(k + kPart, t.k1) : t.k1;
-          epilogue(t, i, at, h * kMmaTile + rank * 128 + quarter * 32, col0, k >= t.k1, release);
-          release();
-        } while (k < t.k1);
+        uint32_t at = kNone;
+        if (t.k0 < t.k1) {
+          acc = kHigh == 1 ? turn : h;
+          turn ^= 1;
+          lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], used[acc]++ & 1, limit_ns));
+          if (lost) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          at = tmem + acc * 256 + col0 + (quarter << 21);
+        }
+        held = at != kNone;
+        epilogue(t, i, at, h * kMmaTile + rank * 128 + quarter * 32, col0, release);
+        release();
       }
     }
   }
