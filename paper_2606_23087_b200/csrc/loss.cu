@@ -57,7 +57,7 @@ struct LossPiece {
   float2* stat;            // [tiles][rows] maximum of z and sum of e of a row in a tile, the label's column apart
   __nv_bfloat16* xc;       // [padded][hidden]
   __nv_bfloat16* p;        // [padded][ld_p] e
-  float* dx_slots;         // [slots][512][256] dx by slices of the vocabulary and tiles
+  float* dx_slots;         // [slots][256][512] dx by slices of the vocabulary and tiles, columns first
   float* dw_acc;           // [vocab][hidden]: bf16 dw of several pieces
 };
 
@@ -86,6 +86,8 @@ __device__ __forceinline__ uint32_t count_labels(const int32_t* labels, uint32_t
 __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
   __shared__ uint32_t warp_count[8];
   __shared__ int32_t dest[kPickRows], s_label[kPickRows];
+  __shared__ uint8_t s_from[kPickRows];  // the rows of the CTA that count, in order
+  let_next_start();
   const uint32_t r0 = blockIdx.x * kPickRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t* labels = a.labels + a.row0;
   if (blockIdx.x == 0)
@@ -104,6 +106,7 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
     dest[lane] = counts ? (int32_t)pos : -1;
     s_label[lane] = l;
     if (counts) {
+      s_from[pos - before] = (uint8_t)lane;
       a.row_of[pos] = (int32_t)r;
       a.label[pos] = l;
     } else if (r < a.rows) {
@@ -121,27 +124,42 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
     uint4* tail = reinterpret_cast<uint4*>(a.xc + (uint64_t)total * a.hidden);
     for (uint32_t c = threadIdx.x; c < (end - total) * vecs; c += blockDim.x) tail[c] = zero;
   }
-  for (uint32_t k = warp; k < rows; k += 8) {
-    if (dest[k] >= 0) {
-      const uint4* __restrict__ src = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
-      const uint4* __restrict__ wl = reinterpret_cast<const uint4*>(a.w + (uint64_t)s_label[k] * a.ldw);
-      uint4* __restrict__ dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)dest[k] * a.hidden);
-      float dot = 0.f;
-#pragma unroll 4
-      for (uint32_t c = lane; c < vecs; c += 32) {
-        const uint4 xv = src[c], wv = wl[c];
-        float f[8], g[8];
-        Pack<__nv_bfloat16>::widen(xv, f);
-        Pack<__nv_bfloat16>::widen(wv, g);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dot = fmaf(f[e], g[e], dot);
-        dst[c] = xv;
-      }
-      dot = warp_sum(dot);
-      if (lane == 0) a.ref[dest[k]] = a.target[dest[k]] = dot;
-    } else if (a.dx) {
+  for (uint32_t k = warp; k < rows; k += 8)
+    if (a.dx && dest[k] < 0) {
       uint4* dst = reinterpret_cast<uint4*>(a.dx + (a.row0 + r0 + k) * a.lddx);
       for (uint32_t c = lane; c < vecs; c += 32) dst[c] = zero;
+    }
+  // the rows that count, two a warp at a time (a short row's loads alone do not cover memory's latency)
+  for (uint32_t q = 2 * warp; q < total - before; q += 16) {
+    const uint4 *src[2], *wl[2];
+    float dot[2] = {0.f, 0.f};
+    const uint32_t two = min(2u, total - before - q);
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+      const uint32_t k = s_from[q + (i < two ? i : 0)];
+      src[i] = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
+      wl[i] = reinterpret_cast<const uint4*>(a.w + (uint64_t)s_label[k] * a.ldw);
+    }
+    uint4* __restrict__ dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)(before + q) * a.hidden);
+#pragma unroll 2
+    for (uint32_t c = lane; c < vecs; c += 32) {
+      uint4 xv[2], wv[2];
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) { xv[i] = __ldg(src[i] + c); wv[i] = __ldg(wl[i] + c); }
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        float f[8], g[8];
+        Pack<__nv_bfloat16>::widen(xv[i], f);
+        Pack<__nv_bfloat16>::widen(wv[i], g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot[i] = fmaf(f[e], g[e], dot[i]);
+        if (i < two) dst[i * vecs + c] = xv[i];
+      }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+      const float d = warp_sum(dot[i]);
+      if (lane == 0 && i < two) a.ref[before + q + i] = a.target[before + q + i] = d;
     }
   }
 }
@@ -174,6 +192,8 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
          const __grid_constant__ LossPiece a) {
   __shared__ uint8_t s_tile[kRedo ? kPieceRowsMost / kMmaTile : 1];
   __shared__ uint32_t s_tiles;
+  let_next_start();
+  after_previous();
   const uint32_t n = *a.count, n_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
   uint32_t blocks = (n + kMmaTile - 1) / kMmaTile;
   if constexpr (kRedo) {
@@ -278,6 +298,8 @@ __device__ __forceinline__ float store_loss(const LossPiece& a, uint32_t m, floa
 }
 
 __global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
+  let_next_start();
+  after_previous();
   const uint32_t n = *a.count, m = blockIdx.x * 32 + (threadIdx.x & 31);
   if (blockIdx.x * 32 >= n) return;
   const float2 s = join_tiles(a, n, m);
@@ -295,6 +317,8 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
 template <bool kGrad>
 __global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
   __shared__ float s_f[32];
+  let_next_start();
+  after_previous();
   const uint32_t n = *a.count, r0 = blockIdx.x * 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = r0 + lane;
   if (r0 >= n) return;
   const bool again = a.redo[1 + r0 / kMmaTile] != 0;
@@ -356,8 +380,9 @@ struct HighTiles {
 };
 
 // Slices of K = vocab for dx's tiles: they rarely divide among the pairs, and few rows have few tiles at all.  Taken is the
-// number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile costs beside its products; every
-// CTA (and the kernel that joins the slices) works out the same number.
+// number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile costs beside its products and
+// what the slices cost in traffic (in blocks of K of 256 rows, some 0.35 us); every CTA (and the kernel that joins the
+// slices) works out the same number.
 __device__ __forceinline__ uint32_t dx_slices(const LossPiece& a, uint32_t n, uint32_t pairs) {
   const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK;
   uint32_t best = 1, best_cost = 0xFFFFFFFFu;
@@ -365,115 +390,160 @@ __device__ __forceinline__ uint32_t dx_slices(const LossPiece& a, uint32_t n, ui
     const HighTiles h(n, a.hidden, s, pairs);
     if (s > 1 && h.all > a.slots) break;
     const uint32_t halves = 2 * ((h.split + pairs - 1) / pairs) + (h.split < h.all ? 1 : 0);  // rounds of 256 rows
-    const uint32_t cost = halves * ((k_blocks + s - 1) / s + kTileCost);
+    const uint32_t cost = halves * ((k_blocks + s - 1) / s + kTileCost) + (s > 1 ? s * h.blocks * h.n_tiles / 4 : 0);
     if (cost < best_cost) { best = s; best_cost = cost; }
   }
   return best;
 }
 
+// 16 values of a row, rounded to bf16; `left` of them exist (a multiple of 8)
+__device__ __forceinline__ void store_bf16x16(__nv_bfloat16* p, const float* f, uint32_t left, bool wide) {
+  uint32_t w[8];
+#pragma unroll
+  for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(f[2 * j], f[2 * j + 1]);
+  if (wide && left >= 16) {
+    store32(p, w);
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (left >= 16) *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+// a lane's 128 columns out of tensor memory, and the accumulator given back
+template <class Release>
+__device__ __forceinline__ void take_columns(uint32_t tmem, uint32_t (&z)[4][32], Release&& release) {
+#pragma unroll
+  for (uint32_t c = 0; c < 4; ++c) {
+    if (tmem == kNone) {
+#pragma unroll
+      for (uint32_t j = 0; j < 32; ++j) z[c][j] = 0;
+    } else {
+      tmem_load32(tmem + 32 * c, z[c]);
+    }
+  }
+  tmem_wait();
+  release();
+}
+
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
 k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
      const __grid_constant__ LossPiece a) {
+  let_next_start();
+  after_previous();
   const uint32_t n = *a.count, k_blocks = (a.vocab + kMmaK - 1) / kMmaK, pairs = gridDim.x >> 1;
   const uint32_t slices = dx_slices(a, n, pairs), each = (k_blocks + slices - 1) / slices;
   const HighTiles work(n, a.hidden, slices, pairs);
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.dx) | a.lddx * 2) & 31) == 0;
   bool lost;
   mma_pair_tiles<false, true, 2>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
     [&](uint32_t i) { return work.at(i, each, k_blocks); },
-    [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, auto&&) {
+    [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t r = t.m % kHighRows + row + (threadIdx.x & 31), m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
-      const uint32_t cols = min(128u, a.hidden - c0);
-      float* slot = a.dx_slots + ((uint64_t)work.tile_of(i) * kHighRows + r) * kMmaTile + col0;
-      uint32_t d[32];
+      uint32_t z[4][32];
+      take_columns(tmem, z, release);
+      if (slices > 1) {  // columns first: a warp's store is one line
+        float* slot = a.dx_slots + ((uint64_t)work.tile_of(i) * kMmaTile + col0) * kHighRows + r;
 #pragma unroll
-      for (uint32_t c = 0; c < 128; c += 32) {
-        if (c >= cols) break;
-        if (tmem == kNone) {
+        for (uint32_t c = 0; c < 128; ++c) slot[c * kHighRows] = __uint_as_float(z[c / 32][c % 32]);
+      } else if (m < n) {
+        const uint32_t cols = min(128u, a.hidden - c0);
+        const float f = a.factor[m];
+        __nv_bfloat16* dx = a.dx + (a.row0 + a.row_of[m]) * a.lddx + c0;
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j) d[j] = 0;
-        } else {
-          tmem_load32(tmem + c, d);
-          tmem_wait();
-        }
-        if (m >= n) continue;
+        for (uint32_t c = 0; c < 128; c += 16) {
+          if (c >= cols) break;
+          float d[16];
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          if (c + q * 8 >= cols) break;
-          store32(slot + c + q * 8, d + q * 8);
+          for (uint32_t j = 0; j < 16; ++j) d[j] = f * __uint_as_float(z[(c + j) / 32][(c + j) % 32]);
+          store_bf16x16(dx + c, d, cols - c, wide);
         }
       }
     });
   give_up(v, a.call_seq, lost);
 }
 
-// dx of a counted row: f times the sum of the slices, in slice order, rounded once
+// dx of a counted row from several slices: f times their sum, in slice order, rounded once.  A CTA takes 32 rows of a
+// tile's 256 columns and turns them over in shared memory: the slices hold columns, dx rows.
 __global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
-  const uint32_t n = *a.count, slices = dx_slices(a, n, pairs), vecs = a.hidden / 8;
+  __shared__ float turned[32][kMmaTile + 4];
+  let_next_start();
+  after_previous();
+  const uint32_t n = *a.count, slices = dx_slices(a, n, pairs), r0 = blockIdx.y * 32;
+  if (r0 >= n || slices == 1) return;
   const HighTiles work(n, a.hidden, slices, pairs);
-  const uint64_t all = (uint64_t)n * vecs;
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
-    const uint32_t m = (uint32_t)(i / vecs), c = (uint32_t)(i % vecs) * 8;
-    const float* slot = a.dx_slots + (((uint64_t)(m / kHighRows) * work.n_tiles + c / kMmaTile) * kHighRows + m % kHighRows) * kMmaTile + c % kMmaTile;
-    const float f = a.factor[m];
-    float s[8], t[8];
-    load32(slot, s);
-    for (uint32_t k = 1; k < slices; ++k) {
-      load32(slot + (uint64_t)k * work.tiles * kHighRows * kMmaTile, t);
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = r0 + lane;
+  const float* slot = a.dx_slots + (((uint64_t)(r0 / kHighRows) * work.n_tiles + blockIdx.x) * kMmaTile + warp * 32) * kHighRows + r0 % kHighRows + lane;
+  const uint64_t slice = (uint64_t)work.tiles * kMmaTile * kHighRows;
+  const float f = m < n ? a.factor[m] : 0.f;
+  for (uint32_t c = 0; c < 32; c += 8) {
+    float s[8] = {};
+    for (uint32_t k = 0; k < slices; ++k) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] += t[j];
+      for (uint32_t j = 0; j < 8; ++j) s[j] += slot[k * slice + (c + j) * kHighRows];
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] *= f;
-    *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[m]) * a.lddx + c) = Pack<__nv_bfloat16>::narrow(s);
+    for (uint32_t j = 0; j < 8; ++j) turned[lane][warp * 32 + c + j] = f * s[j];
   }
+  __syncthreads();
+  const uint32_t c = blockIdx.x * kMmaTile + lane * 8;
+  if (c >= a.hidden) return;
+  for (uint32_t r = warp; r < 32 && r0 + r < n; r += 8)
+    *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[r0 + r]) * a.lddx + c) = Pack<__nv_bfloat16>::narrow(&turned[r][lane * 8]);
 }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
 k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PoolView v,
      const __grid_constant__ LossPiece a) {
+  let_next_start();
+  after_previous();
   const uint32_t n = *a.count, k_blocks = (n + kMmaK - 1) / kMmaK;
   const HighTiles work(a.vocab, a.hidden, 1, gridDim.x >> 1);
+  // sums in fp32 go to dw itself, or for a bf16 dw to the accumulators until the last piece
+  float* sums = a.dw_dtype == FT_F32 ? static_cast<float*>(a.dw) : a.dw_acc;
+  const float* base = a.add_dw ? sums : nullptr;
+  float* out = a.dw_dtype == FT_F32 || !a.last ? sums : nullptr;
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.dw) | (out ? 0 : a.hidden * 2)) & 31) == 0;  // rows of 8 fp32 are 32-byte multiples
   bool lost;
   mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
     [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); },
-    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&&) {
+    [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
+      uint32_t z[4][32];
+      take_columns(tmem, z, release);
+      if (m >= a.vocab) return;
       const uint32_t cols = min(128u, a.hidden - c0);
       const uint64_t at = (uint64_t)m * a.hidden + c0;
-      const float* base = a.add_dw ? (a.dw_dtype == FT_F32 ? static_cast<const float*>(a.dw) : a.dw_acc) : nullptr;
-      const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;
-      float* out = a.dw_dtype == FT_F32 ? static_cast<float*>(a.dw) : a.dw_acc;
-      uint32_t d[32];
 #pragma unroll
-      for (uint32_t c = 0; c < 128; c += 32) {
+      for (uint32_t c = 0; c < 128; c += 16) {
         if (c >= cols) break;
-        if (tmem == kNone) {
+        float d[16];
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j) d[j] = 0;
-        } else {
-          tmem_load32(tmem + c, d);
-          tmem_wait();
-        }
-        if (m >= a.vocab) continue;
+        for (uint32_t j = 0; j < 16; ++j) d[j] = __uint_as_float(z[(c + j) / 32][(c + j) % 32]);
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          if (c + q * 8 >= cols) break;
-          float f[8];
-#pragma unroll
-          for (uint32_t j = 0; j < 8; ++j) f[j] = __uint_as_float(d[q * 8 + j]);
+        for (uint32_t q = 0; q < 16; q += 8) {
+          if (c + q >= cols) break;
           if (base) {
-            const float4 b0 = *reinterpret_cast<const float4*>(base + at + c + q * 8), b1 = *reinterpret_cast<const float4*>(base + at + c + q * 8 + 4);
-            f[0] += b0.x; f[1] += b0.y; f[2] += b0.z; f[3] += b0.w; f[4] += b1.x; f[5] += b1.y; f[6] += b1.z; f[7] += b1.w;
+            float b[8];
+            if (wide) {
+              load32(base + at + c + q, b);
+            } else {
+              Pack<float>::widen(*reinterpret_cast<const uint4*>(base + at + c + q), b);
+              Pack<float>::widen(*reinterpret_cast<const uint4*>(base + at + c + q + 4), b + 4);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) d[q + j] += b[j];
           }
-          if (in_fp32) {
-            *reinterpret_cast<uint4*>(out + at + c + q * 8) = Pack<float>::narrow(f);
-            *reinterpret_cast<uint4*>(out + at + c + q * 8 + 4) = Pack<float>::narrow(f + 4);
-          } else {
-            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dw) + at + c + q * 8) = Pack<__nv_bfloat16>::narrow(f);
+          if (out) {
+            if (wide) {
+              store32(out + at + c + q, reinterpret_cast<const uint32_t*>(d + q));
+            } else {
+              *reinterpret_cast<uint4*>(out + at + c + q) = Pack<float>::narrow(d + q);
+              *reinterpret_cast<uint4*>(out + at + c + q + 4) = Pack<float>::narrow(d + q + 4);
+            }
           }
         }
+        if (!out) store_bf16x16(static_cast<__nv_bfloat16*>(a.dw) + at + c, d, cols - c, wide);
       }
     });
   give_up(v, a.call_seq, lost);
@@ -561,25 +631,26 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     a.rows = (uint32_t)std::min<uint64_t>(piece, rows - r0);
     a.add_dw = r0 > 0 || accumulate;
     a.last = r0 + a.rows == rows;
-    k_pick<<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
-    const unsigned joins = (a.rows + 31) / 32;
+    const dim3 joins((a.rows + 31) / 32);
+    const uint32_t join_threads = 32 * kJoinRowWarps;
     const bool high = a.rows > kMmaTile;
+    k_pick<<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
+    FT_CUDA(cudaGetLastError());
     if (grad) {
-      (high ? k_logits<true, false, 2> : k_logits<true, false, 1>)<<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
-      k_join<<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
-      k_logits<true, true, 1><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
-      k_finish<true><<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
-      k_dx<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_w, p->view, a);
-      k_dx_join<<<(unsigned)p->sm_count * 4, 256, 0, st>>>(a, pairs);
-      k_dw<<<grid, kMmaThreads, kMmaSmem, st>>>(map_p, map_x, p->view, a);
+      FT_CUDA(launch_chained(high ? k_logits<true, false, 2> : k_logits<true, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_join, joins, join_threads, 0, st, a));
+      FT_CUDA(launch_chained(k_logits<true, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_finish<true>, joins, join_threads, 0, st, a));
+      FT_CUDA(launch_chained(k_dx, grid, kMmaThreads, kMmaSmem, st, map_p, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_dx_join, dim3((a.hidden + kMmaTile - 1) / kMmaTile, joins.x), 256, 0, st, a, pairs));
+      FT_CUDA(launch_chained(k_dw, grid, kMmaThreads, kMmaSmem, st, map_p, map_x, p->view, a));
     } else {
-      (high ? k_logits<false, false, 2> : k_logits<false, false, 1>)<<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
-      k_join<<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
-      k_logits<false, true, 1><<<grid, kMmaThreads, kMmaSmem, st>>>(map_x, map_w, p->view, a);
-      k_finish<false><<<joins, 32 * kJoinRowWarps, 0, st>>>(a);
+      FT_CUDA(launch_chained(high ? k_logits<false, false, 2> : k_logits<false, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_join, joins, join_threads, 0, st, a));
+      FT_CUDA(launch_chained(k_logits<false, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_finish<false>, joins, join_threads, 0, st, a));
     }
     p->gpu_launches += grad ? 8 : 5;
-    FT_CUDA(cudaGetLastError());
   }
   return FT_OK;
 }
