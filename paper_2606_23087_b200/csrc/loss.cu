@@ -39,6 +39,7 @@ constexpr uint32_t kMinSlots = 148;  // few rows: room for two tiles a pair
 struct LossPiece {
   uint32_t rows, hidden, vocab, ld_p, tiles, slots;  // tiles: of kStatCols columns; slots: tiles that dx_slots holds
   uint32_t padded;  // rows of xc and p: `rows` in whole tiles
+  uint32_t pairs;   // CTA pairs of the products
   uint64_t row0, ldx, ldw, lddx;
   const __nv_bfloat16 *x, *w;
   const int32_t* labels;
@@ -49,7 +50,7 @@ struct LossPiece {
   void* dw;
   uint64_t call_seq;
   // workspace
-  uint32_t* count;         // rows of the piece that count
+  uint32_t* count;         // rows of the piece that count; slices of dx's product
   int32_t *row_of, *label; // [count] row in the piece, label
   uint32_t* redo;          // [1 + row tiles] whether any, and which row tiles need another reference
   float *ref, *target;     // [count] the reference, and the label's logit
@@ -61,7 +62,9 @@ struct LossPiece {
   float* dw_acc;           // [vocab][hidden]: bf16 dw of several pieces
 };
 
-constexpr uint32_t kPickRows = 32;
+constexpr uint32_t kPickRows = 32;    // rows of a CTA; 8 where that alone fills the device, a row a warp
+constexpr uint32_t kPickFew = 8;
+constexpr uint32_t kPickFewUpTo = 4096;
 
 __device__ __forceinline__ bool has_label(int32_t l, uint32_t vocab) { return (uint32_t)l < vocab; }
 
@@ -81,14 +84,15 @@ __device__ __forceinline__ uint32_t count_labels(const int32_t* labels, uint32_t
   return c;
 }
 
-// A CTA takes 32 rows; where they go it learns by counting the labels before them itself (a piece's labels stay in L2),
+// A CTA takes kRows rows; where they go it learns by counting the labels before them itself (a piece's labels stay in L2),
 // so nothing has to wait for another CTA.
+template <uint32_t kRows>
 __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
   __shared__ uint32_t warp_count[8];
-  __shared__ int32_t dest[kPickRows], s_label[kPickRows];
-  __shared__ uint8_t s_from[kPickRows];  // the rows of the CTA that count, in order
+  __shared__ int32_t dest[32], s_label[32];
+  __shared__ uint8_t s_from[32];  // the rows of the CTA that count, in order
   let_next_start();
-  const uint32_t r0 = blockIdx.x * kPickRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t r0 = blockIdx.x * kRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t* labels = a.labels + a.row0;
   if (blockIdx.x == 0)
     for (uint32_t i = threadIdx.x; i <= a.padded / kMmaTile; i += blockDim.x) a.redo[i] = 0;
@@ -99,7 +103,7 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
 #pragma unroll
   for (int w = 0; w < 8; ++w) before += warp_count[w];
   const uint32_t r = r0 + lane;
-  const int32_t l = r < a.rows ? labels[r] : kNoLabel;
+  const int32_t l = lane < kRows && r < a.rows ? labels[r] : kNoLabel;
   const bool counts = has_label(l, a.vocab);
   const uint32_t mask = __ballot_sync(0xFFFFFFFFu, counts), pos = before + __popc(mask & ((1u << lane) - 1)), total = before + __popc(mask);
   if (warp == 0) {
@@ -109,7 +113,7 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
       s_from[pos - before] = (uint8_t)lane;
       a.row_of[pos] = (int32_t)r;
       a.label[pos] = l;
-    } else if (r < a.rows) {
+    } else if (lane < kRows && r < a.rows) {
       a.loss[a.row0 + r] = 0.f;
       a.lse[a.row0 + r] = 0.f;
       if (l != kNoLabel) note_error(v, a.call_seq, FT_ERR_BAD_TOKEN_ID, (uint32_t)(a.row0 + r));
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
     if (blockIdx.x == gridDim.x - 1 && lane == 0) *a.count = total;
   }
   __syncthreads();
-  const uint32_t vecs = a.hidden / 8, rows = min(kPickRows, a.rows - r0);
+  const uint32_t vecs = a.hidden / 8, rows = min(kRows, a.rows - r0);
   const uint4 zero = make_uint4(0, 0, 0, 0);
   if (blockIdx.x == gridDim.x - 1) {  // the product over rows runs to a whole block of K: those rows' x must be finite
     const uint32_t end = (total + kMmaK - 1) / kMmaK * kMmaK;
@@ -129,25 +133,26 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
       uint4* dst = reinterpret_cast<uint4*>(a.dx + (a.row0 + r0 + k) * a.lddx);
       for (uint32_t c = lane; c < vecs; c += 32) dst[c] = zero;
     }
-  // the rows that count, two a warp at a time (a short row's loads alone do not cover memory's latency)
-  for (uint32_t q = 2 * warp; q < total - before; q += 16) {
-    const uint4 *src[2], *wl[2];
-    float dot[2] = {0.f, 0.f};
-    const uint32_t two = min(2u, total - before - q);
+  // the rows that count, two a warp at a time (a short row's loads alone do not cover memory's latency) where there are many
+  constexpr uint32_t kAtOnce = kRows == kPickFew ? 1 : 2;
+  for (uint32_t q = kAtOnce * warp; q < total - before; q += kAtOnce * 8) {
+    const uint4 *src[kAtOnce], *wl[kAtOnce];
+    float dot[kAtOnce] = {};
+    const uint32_t two = min(kAtOnce, total - before - q);
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kAtOnce; ++i) {
       const uint32_t k = s_from[q + (i < two ? i : 0)];
       src[i] = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
       wl[i] = reinterpret_cast<const uint4*>(a.w + (uint64_t)s_label[k] * a.ldw);
     }
     uint4* __restrict__ dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)(before + q) * a.hidden);
-#pragma unroll 2
+#pragma unroll(4 / kAtOnce)
     for (uint32_t c = lane; c < vecs; c += 32) {
-      uint4 xv[2], wv[2];
+      uint4 xv[kAtOnce], wv[kAtOnce];
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) { xv[i] = __ldg(src[i] + c); wv[i] = __ldg(wl[i] + c); }
+      for (uint32_t i = 0; i < kAtOnce; ++i) { xv[i] = __ldg(src[i] + c); wv[i] = __ldg(wl[i] + c); }
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
+      for (uint32_t i = 0; i < kAtOnce; ++i) {
         float f[8], g[8];
         Pack<__nv_bfloat16>::widen(xv[i], f);
         Pack<__nv_bfloat16>::widen(wv[i], g);
@@ -157,7 +162,7 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
       }
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kAtOnce; ++i) {
       const float d = warp_sum(dot[i]);
       if (lane == 0 && i < two) a.ref[before + q + i] = a.target[before + q + i] = d;
     }
@@ -188,8 +193,8 @@ __device__ __forceinline__ void give_up(const PoolView& v, uint64_t call_seq, bo
 // z by tiles; a lane owns a row's 128 columns.  kRedo: only the row tiles whose reference has changed.
 template <bool kKeep, bool kRedo, int kHigh>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
-k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
-         const __grid_constant__ LossPiece a) {
+k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_e,
+         const __grid_constant__ PoolView v, const __grid_constant__ LossPiece a) {
   __shared__ uint8_t s_tile[kRedo ? kPieceRowsMost / kMmaTile : 1];
   __shared__ uint32_t s_tiles;
   let_next_start();
@@ -209,12 +214,19 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
   }
   const uint32_t m_tiles = (blocks + kHigh - 1) / kHigh;
   bool lost;
+  int32_t label = kNoLabel;
+  float ref = 0.f;
   mma_pair_tiles<false, false, kHigh>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
     [&](uint32_t i) {
       // bands of 2048 rows, all columns of a band before the next: a band's x stays in L2
       constexpr uint32_t kBand = 8 / kHigh;
       const uint32_t band = i / (kBand * n_tiles), in = i - band * kBand * n_tiles, rows = min(kBand, m_tiles - band * kBand), m = band * kBand + in % rows;
       return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m * kHigh) * kMmaTile, in / rows * kMmaTile, 0, k_blocks, min((uint32_t)kHigh, blocks - m * kHigh)};
+    },
+    [&](const MmaTile& t, uint32_t row) {
+      const uint32_t m = t.m + row + (threadIdx.x & 31);
+      label = m < n ? a.label[m] : kNoLabel;
+      ref = m < n ? a.ref[m] : 0.f;
     },
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t c0 = t.n + col0;
@@ -225,8 +237,7 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
       tmem_wait();
       release();  // the products go on while the exponentials are taken
       const uint32_t m = t.m + row + (threadIdx.x & 31), cols = min(kStatCols, a.vocab - c0);
-      const uint32_t label_at = m < n ? (uint32_t)a.label[m] - c0 : kNone;
-      const float ref = m < n ? a.ref[m] : 0.f;
+      const uint32_t label_at = (uint32_t)label - c0;
       [[maybe_unused]] const uint32_t keep = m < n ? 0xFFFFFFFFu : 0u;  // rows beyond the last one that counts: zeros, which the product over rows adds
       if (label_at < kStatCols) {
 #pragma unroll
@@ -239,33 +250,76 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
           if (j >= cols) z[j / 32][j % 32] = kMinusInf;
       }
       float top = -INFINITY, sum = 0.f;
+      const auto take_exp = [&](uint32_t c) {
+        const float x = __uint_as_float(z[c / 32][c % 32]), e = exp2_fast((x - ref) * kLog2e);
+        top = fmaxf(top, x);
+        sum += e;
+        return e;
+      };
+      if constexpr (kKeep) {
 #pragma unroll
-      for (uint32_t c = 0; c < kStatCols; c += 16) {
-        float e[16];
+        for (uint32_t c = 0; c < kStatCols; c += 64) {
+          if (c >= cols) break;
+          MmaOut().put<false>(&map_e, (int32_t)(c0 + c), (int32_t)(t.m + row), [&](uint32_t j) {
+            float e[8];
 #pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) {
-          const float x = __uint_as_float(z[(c + j) / 32][(c + j) % 32]);
-          top = fmaxf(top, x);
-          e[j] = exp2_fast((x - ref) * kLog2e);
-          sum += e[j];
+            for (uint32_t k = 0; k < 8; ++k) e[k] = take_exp(c + 8 * j + k);
+            const uint4 w = Pack<__nv_bfloat16>::narrow(e);
+            return make_uint4(w.x & keep, w.y & keep, w.z & keep, w.w & keep);
+          });
         }
-        if constexpr (kKeep) {
-          if (c >= cols) continue;
-          uint32_t w[8];
+      } else {
 #pragma unroll
-          for (uint32_t j = 0; j < 8; ++j) w[j] = bf16x2(e[2 * j], e[2 * j + 1]) & keep;
-          store32(a.p + (uint64_t)m * a.ld_p + c0 + c, w);
-        }
+        for (uint32_t c = 0; c < kStatCols; ++c) take_exp(c);
       }
       if (m < n) a.stat[(uint64_t)(c0 / kStatCols) * a.rows + m] = make_float2(top, sum);
     });
   give_up(v, a.call_seq, lost);
 }
 
+// The work of a product in tiles of kHigh x 256 rows.  Tile `t` of `all` = m_tiles x n_tiles (columns first) x slices of K;
+// where the last round has 512-row tiles for at most half the pairs, those are dealt out as two 256-row halves.
+template <int kHigh>
+struct HighTiles {
+  uint32_t blocks, n_tiles, tiles, all, split;  // blocks: of 256 rows; tiles: of one slice; split: whole tiles in front of the halves
+  __device__ __forceinline__ HighTiles(uint32_t rows, uint32_t cols, uint32_t slices, uint32_t pairs) {
+    blocks = (rows + kMmaTile - 1) / kMmaTile;
+    n_tiles = (cols + kMmaTile - 1) / kMmaTile;
+    tiles = (blocks + kHigh - 1) / kHigh * n_tiles;
+    all = split = tiles * slices;
+    const uint32_t rest = all % pairs;
+    if (kHigh == 2 && blocks > 1 && rest * 2 <= pairs) split -= rest;
+  }
+  __device__ __forceinline__ uint32_t items() const { return split + 2 * (all - split); }
+  // rounds of all pairs, in tiles of 256 rows
+  __device__ __forceinline__ uint32_t rounds(uint32_t pairs) const {
+    return min((uint32_t)kHigh, blocks) * ((split + pairs - 1) / pairs) + (split < all ? 1 : 0);
+  }
+  __device__ __forceinline__ uint32_t tile_of(uint32_t i) const { return i < split ? i : split + (i - split) / 2; }
+  __device__ __forceinline__ MmaTile at(uint32_t i, uint32_t k_each, uint32_t k_blocks) const {
+    const uint32_t tile = tile_of(i), slice = tile / tiles, t = tile - slice * tiles, half = i < split ? 0 : (i - split) & 1;
+    const uint32_t block = t / n_tiles * kHigh + half, left = blocks > block ? blocks - block : 0;
+    return MmaTile{block * kMmaTile, t % n_tiles * kMmaTile, min(slice * k_each, k_blocks), min((slice + 1) * k_each, k_blocks),
+                   min(i < split ? (uint32_t)kHigh : 1u, left)};
+  }
+};
+
+// Slices of K = vocab for dx's tiles: they rarely divide among the pairs, and few rows have few tiles at all.  Taken is the
+// number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile costs beside its products and
+// what the slices cost in traffic (in blocks of K of 256 rows, some 0.35 us); every
+__device__ __forceinline__ uint32_t dx_slices(const LossPiece& a, uint32_t n) {  // a whole warp: a lane a number of slices
+  const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK, s = (threadIdx.x & 31) + 1;
+  const HighTiles<2> h(n, a.hidden, s, a.pairs);
+  uint32_t cost = h.rounds(a.pairs) * ((k_blocks + s - 1) / s + kTileCost) + (s > 1 ? s * h.blocks * h.n_tiles / 4 : 0);
+  if (s > k_blocks || (s > 1 && h.all > a.slots)) cost = 0x7FFFFFFu;
+  const uint32_t best = __reduce_min_sync(0xFFFFFFFFu, cost);
+  return __ffs(__ballot_sync(0xFFFFFFFFu, cost == best));
+}
+
 // ---- joining the tiles of a row -------------------------------------------------------------------------------------
 
 // 32 rows a CTA, a lane a row, the CTA's warps share the tiles; warp 0 gets the result.
-constexpr int kJoinRowWarps = 8;
+constexpr int kJoinRowWarps = 16;
 __device__ __forceinline__ float2 join_tiles(const LossPiece& a, uint32_t n, uint32_t m) {
   __shared__ float2 part[kJoinRowWarps][32];
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -302,6 +356,10 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
   after_previous();
   const uint32_t n = *a.count, m = blockIdx.x * 32 + (threadIdx.x & 31);
   if (blockIdx.x * 32 >= n) return;
+  if (a.dx && blockIdx.x == 0 && threadIdx.x / 32 == 1) {
+    const uint32_t slices = dx_slices(a, n);
+    if (threadIdx.x == 32) a.count[1] = slices;
+  }
   const float2 s = join_tiles(a, n, m);
   if (threadIdx.x >= 32 || m >= n) return;
   if (s.y > kSumLimit && s.x < INFINITY) {
@@ -358,44 +416,6 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
   }
 }
 
-// The work of a product in 512-row tiles.  Tile `t` of `all` = m_tiles x n_tiles (columns first) x slices of K; where the last
-// round has tiles for at most half the pairs, those are dealt out as two 256-row halves.
-struct HighTiles {
-  uint32_t blocks, n_tiles, tiles, all, split;  // blocks: of 256 rows; tiles: of one slice; split: whole tiles in front of the halves
-  __device__ __forceinline__ HighTiles(uint32_t rows, uint32_t cols, uint32_t slices, uint32_t pairs) {
-    blocks = (rows + kMmaTile - 1) / kMmaTile;
-    n_tiles = (cols + kMmaTile - 1) / kMmaTile;
-    tiles = (blocks + 1) / 2 * n_tiles;
-    all = tiles * slices;
-    const uint32_t rest = all % pairs;
-    split = rest * 2 <= pairs ? all - rest : all;
-  }
-  __device__ __forceinline__ uint32_t items() const { return split + 2 * (all - split); }
-  __device__ __forceinline__ uint32_t tile_of(uint32_t i) const { return i < split ? i : split + (i - split) / 2; }
-  __device__ __forceinline__ MmaTile at(uint32_t i, uint32_t k_each, uint32_t k_blocks) const {
-    const uint32_t tile = tile_of(i), slice = tile / tiles, t = tile - slice * tiles, half = i < split ? 0 : (i - split) & 1;
-    const uint32_t block = t / n_tiles * 2 + half, left = blocks > block ? blocks - block : 0;
-    return MmaTile{block * kMmaTile, t % n_tiles * kMmaTile, min(slice * k_each, k_blocks), min((slice + 1) * k_each, k_blocks), min(i < split ? 2u : 1u, left)};
-  }
-};
-
-// Slices of K = vocab for dx's tiles: they rarely divide among the pairs, and few rows have few tiles at all.  Taken is the
-// number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile costs beside its products and
-// what the slices cost in traffic (in blocks of K of 256 rows, some 0.35 us); every CTA (and the kernel that joins the
-// slices) works out the same number.
-__device__ __forceinline__ uint32_t dx_slices(const LossPiece& a, uint32_t n, uint32_t pairs) {
-  const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK;
-  uint32_t best = 1, best_cost = 0xFFFFFFFFu;
-  for (uint32_t s = 1; s <= 32 && s <= k_blocks; ++s) {
-    const HighTiles h(n, a.hidden, s, pairs);
-    if (s > 1 && h.all > a.slots) break;
-    const uint32_t halves = 2 * ((h.split + pairs - 1) / pairs) + (h.split < h.all ? 1 : 0);  // rounds of 256 rows
-    const uint32_t cost = halves * ((k_blocks + s - 1) / s + kTileCost) + (s > 1 ? s * h.blocks * h.n_tiles / 4 : 0);
-    if (cost < best_cost) { best = s; best_cost = cost; }
-  }
-  return best;
-}
-
 // 16 values of a row, rounded to bf16; `left` of them exist (a multiple of 8)
 __device__ __forceinline__ void store_bf16x16(__nv_bfloat16* p, const float* f, uint32_t left, bool wide) {
   uint32_t w[8];
@@ -429,13 +449,13 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
      const __grid_constant__ LossPiece a) {
   let_next_start();
   after_previous();
-  const uint32_t n = *a.count, k_blocks = (a.vocab + kMmaK - 1) / kMmaK, pairs = gridDim.x >> 1;
-  const uint32_t slices = dx_slices(a, n, pairs), each = (k_blocks + slices - 1) / slices;
-  const HighTiles work(n, a.hidden, slices, pairs);
+  const uint32_t n = *a.count, k_blocks = (a.vocab + kMmaK - 1) / kMmaK;
+  const uint32_t slices = n ? a.count[1] : 1, each = (k_blocks + slices - 1) / slices;
+  const HighTiles<2> work(n, a.hidden, slices, a.pairs);
   const bool wide = ((reinterpret_cast<uintptr_t>(a.dx) | a.lddx * 2) & 31) == 0;
   bool lost;
   mma_pair_tiles<false, true, 2>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
-    [&](uint32_t i) { return work.at(i, each, k_blocks); },
+    [&](uint32_t i) { return work.at(i, each, k_blocks); }, [](const MmaTile&, uint32_t) {},
     [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t r = t.m % kHighRows + row + (threadIdx.x & 31), m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
       if (c0 >= a.hidden) return;
@@ -462,88 +482,90 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   give_up(v, a.call_seq, lost);
 }
 
-// dx of a counted row from several slices: f times their sum, in slice order, rounded once.  A CTA takes 32 rows of a
-// tile's 256 columns and turns them over in shared memory: the slices hold columns, dx rows.
-__global__ void __launch_bounds__(256) k_dx_join(LossPiece a, uint32_t pairs) {
-  __shared__ float turned[32][kMmaTile + 4];
+// dx of a counted row from several slices: f times their sum, in slice order, rounded once.  A CTA takes 32 rows and 64
+// columns and turns them over in shared memory: the slices hold columns, dx rows.
+constexpr uint32_t kJoinCols = 64;
+__global__ void __launch_bounds__(256) k_dx_join(LossPiece a) {
+  __shared__ float turned[32][kJoinCols + 4];
   let_next_start();
   after_previous();
-  const uint32_t n = *a.count, slices = dx_slices(a, n, pairs), r0 = blockIdx.y * 32;
-  if (r0 >= n || slices == 1) return;
-  const HighTiles work(n, a.hidden, slices, pairs);
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = r0 + lane;
-  const float* slot = a.dx_slots + (((uint64_t)(r0 / kHighRows) * work.n_tiles + blockIdx.x) * kMmaTile + warp * 32) * kHighRows + r0 % kHighRows + lane;
-  const uint64_t slice = (uint64_t)work.tiles * kMmaTile * kHighRows;
-  const float f = m < n ? a.factor[m] : 0.f;
-  for (uint32_t c = 0; c < 32; c += 8) {
+  const uint32_t n = *a.count;
+  if (n == 0) return;
+  const uint32_t slices = a.count[1], col_parts = (a.hidden + kJoinCols - 1) / kJoinCols, parts = (n + 31) / 32 * col_parts;
+  if (slices == 1) return;
+  const HighTiles<2> work(n, a.hidden, slices, a.pairs);
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (uint32_t i = blockIdx.x; i < parts; i += gridDim.x) {
+    const uint32_t r0 = i / col_parts * 32, c0 = i % col_parts * kJoinCols, m = r0 + lane;
+    const uint64_t tile = (uint64_t)(r0 / kHighRows) * work.n_tiles + c0 / kMmaTile, slice = (uint64_t)work.tiles * kMmaTile * kHighRows;
+    const float* __restrict__ slot = a.dx_slots + (tile * kMmaTile + c0 % kMmaTile + warp * 8) * kHighRows + r0 % kHighRows + lane;
+    const float f = m < n ? a.factor[m] : 0.f;
     float s[8] = {};
+#pragma unroll 4
     for (uint32_t k = 0; k < slices; ++k) {
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) s[j] += slot[k * slice + (c + j) * kHighRows];
+      for (uint32_t j = 0; j < 8; ++j) s[j] += slot[k * slice + j * kHighRows];
     }
+    __syncthreads();  // the part before this one has been written out
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) turned[lane][warp * 32 + c + j] = f * s[j];
+    for (uint32_t j = 0; j < 8; ++j) turned[lane][warp * 8 + j] = f * s[j];
+    __syncthreads();
+    const uint32_t r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+    if (r0 + r < n && c0 + c < a.hidden)
+      *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[r0 + r]) * a.lddx + c0 + c) = Pack<__nv_bfloat16>::narrow(&turned[r][c]);
   }
-  __syncthreads();
-  const uint32_t c = blockIdx.x * kMmaTile + lane * 8;
-  if (c >= a.hidden) return;
-  for (uint32_t r = warp; r < 32 && r0 + r < n; r += 8)
-    *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[r0 + r]) * a.lddx + c) = Pack<__nv_bfloat16>::narrow(&turned[r][lane * 8]);
 }
 
+// dw leaves by TMA.  fp32 sums that are added to (accumulation, or later pieces) are added on their way out, each element once.
+// 200 rows x 32768 x 3584: 83 us, 93 us with direct stores of 32 bytes a lane.
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
-k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PoolView v,
-     const __grid_constant__ LossPiece a) {
+k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_out,
+     const __grid_constant__ PoolView v, const __grid_constant__ LossPiece a) {
   let_next_start();
   after_previous();
   const uint32_t n = *a.count, k_blocks = (n + kMmaK - 1) / kMmaK;
-  const HighTiles work(a.vocab, a.hidden, 1, gridDim.x >> 1);
-  // sums in fp32 go to dw itself, or for a bf16 dw to the accumulators until the last piece
-  float* sums = a.dw_dtype == FT_F32 ? static_cast<float*>(a.dw) : a.dw_acc;
-  const float* base = a.add_dw ? sums : nullptr;
-  float* out = a.dw_dtype == FT_F32 || !a.last ? sums : nullptr;
-  const bool wide = ((reinterpret_cast<uintptr_t>(a.dw) | (out ? 0 : a.hidden * 2)) & 31) == 0;  // rows of 8 fp32 are 32-byte multiples
+  const HighTiles<2> work(a.vocab, a.hidden, 1, a.pairs);
+  const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;  // a bf16 dw of several pieces is summed in fp32 until the last one
   bool lost;
   mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
-    [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); },
+    [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); }, [](const MmaTile&, uint32_t) {},
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
-      const uint32_t m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
-      if (c0 >= a.hidden) return;
+      const int32_t c0 = (int32_t)(t.n + col0), m0 = (int32_t)(t.m + row);
+      if (c0 >= (int32_t)a.hidden) return;
       uint32_t z[4][32];
       take_columns(tmem, z, release);
-      if (m >= a.vocab) return;
-      const uint32_t cols = min(128u, a.hidden - c0);
-      const uint64_t at = (uint64_t)m * a.hidden + c0;
+      if (m0 >= (int32_t)a.vocab) return;
+      const MmaOut out;
+      if (in_fp32) {
 #pragma unroll
-      for (uint32_t c = 0; c < 128; c += 16) {
-        if (c >= cols) break;
-        float d[16];
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) d[j] = __uint_as_float(z[(c + j) / 32][(c + j) % 32]);
-#pragma unroll
-        for (uint32_t q = 0; q < 16; q += 8) {
-          if (c + q >= cols) break;
-          if (base) {
-            float b[8];
-            if (wide) {
-              load32(base + at + c + q, b);
-            } else {
-              Pack<float>::widen(*reinterpret_cast<const uint4*>(base + at + c + q), b);
-              Pack<float>::widen(*reinterpret_cast<const uint4*>(base + at + c + q + 4), b + 4);
-            }
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) d[q + j] += b[j];
-          }
-          if (out) {
-            if (wide) {
-              store32(out + at + c + q, reinterpret_cast<const uint32_t*>(d + q));
-            } else {
-              *reinterpret_cast<uint4*>(out + at + c + q) = Pack<float>::narrow(d + q);
-              *reinterpret_cast<uint4*>(out + at + c + q + 4) = Pack<float>::narrow(d + q + 4);
-            }
-          }
+        for (uint32_t c = 0; c < 128; c += 32) {
+          if (c0 + c >= a.hidden) break;
+          const auto quad = [&](uint32_t j) { return make_uint4(z[c / 32][4 * j], z[c / 32][4 * j + 1], z[c / 32][4 * j + 2], z[c / 32][4 * j + 3]); };
+          if (a.add_dw) out.put<true>(&map_out, c0 + (int32_t)c, m0, quad);
+          else out.put<false>(&map_out, c0 + (int32_t)c, m0, quad);
         }
-        if (!out) store_bf16x16(static_cast<__nv_bfloat16*>(a.dw) + at + c, d, cols - c, wide);
+        return;
+      }
+      if (a.add_dw) {  // the last of several pieces
+        const uint32_t m = (uint32_t)m0 + (threadIdx.x & 31);
+        const float* sums = a.dw_acc + (uint64_t)m * a.hidden + c0;
+#pragma unroll
+        for (uint32_t c = 0; c < 128; c += 8) {
+          float b[8] = {};
+          if (m < a.vocab && c0 + c < a.hidden) load32(sums + c, b);
+#pragma unroll
+          for (uint32_t j = 0; j < 8; ++j) z[c / 32][c % 32 + j] = __float_as_uint(__uint_as_float(z[c / 32][c % 32 + j]) + b[j]);
+        }
+      }
+#pragma unroll
+      for (uint32_t c = 0; c < 128; c += 64) {
+        if (c0 + c >= a.hidden) break;
+        out.put<false>(&map_out, c0 + (int32_t)c, m0, [&](uint32_t j) {
+          float d[8];
+#pragma unroll
+          for (uint32_t k = 0; k < 8; ++k) d[k] = __uint_as_float(z[(c + 8 * j + k) / 32][(c + 8 * j + k) % 32]);
+          return Pack<__nv_bfloat16>::narrow(d);
+        });
       }
     });
   give_up(v, a.call_seq, lost);
@@ -559,10 +581,10 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
   a->rows = rows;
   a->padded = (uint32_t)padded;
   a->tiles = (vocab + kStatCols - 1) / kStatCols;
-  a->ld_p = (uint32_t)align_up_sz(vocab, 128);  // an epilogue lane's 32-byte stores stay inside its row
+  a->ld_p = (uint32_t)align_up_sz(vocab, 64);  // whole lines
   const uint64_t dx_tiles = (padded + kHighRows - 1) / kHighRows * ((hidden + kMmaTile - 1) / kMmaTile);
   a->slots = (uint32_t)std::max<uint64_t>(dx_tiles, kMinSlots);
-  a->count = reinterpret_cast<uint32_t*>(take(4));
+  a->count = reinterpret_cast<uint32_t*>(take(8));
   a->row_of = reinterpret_cast<int32_t*>(take(4ull * rows));
   a->label = reinterpret_cast<int32_t*>(take(4ull * rows));
   a->redo = reinterpret_cast<uint32_t*>(take(4ull * (1 + padded / kMmaTile)));
@@ -613,11 +635,12 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
   const uint32_t piece = work.piece_for(workspace_bytes);
   loss_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, grad, grad && a.dw_dtype == FT_BF16 && piece < rows);
   a.call_seq = status_seq(p);
-  CUtensorMap map_x, map_w, map_p;
+  CUtensorMap map_x, map_w, map_p = {}, map_e = {}, map_dw = {};
   if (mma_map(&map_x, a.xc, a.hidden, a.padded, a.hidden) != CUDA_SUCCESS || mma_map(&map_w, a.w, a.hidden, a.vocab, a.ldw) != CUDA_SUCCESS ||
-      (grad && mma_map(&map_p, a.p, a.vocab, a.padded, a.ld_p) != CUDA_SUCCESS))
+      (grad && (mma_map(&map_p, a.p, a.vocab, a.padded, a.ld_p) != CUDA_SUCCESS || mma_map(&map_e, a.p, a.vocab, a.padded, a.ld_p, 32) != CUDA_SUCCESS)))
     return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
-  const unsigned pairs = (unsigned)p->sm_count / 2, grid = 2 * pairs;
+  a.pairs = (uint32_t)p->sm_count / 2;
+  const unsigned grid = 2 * a.pairs;
   if (!p->loss_attr_set) {  // once per pool, hence once per device the pool lives on
     for (auto k : {k_logits<false, false, 1>, k_logits<false, false, 2>, k_logits<false, true, 1>, k_logits<true, false, 1>, k_logits<true, false, 2>,
                    k_logits<true, true, 1>})
@@ -631,23 +654,29 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     a.rows = (uint32_t)std::min<uint64_t>(piece, rows - r0);
     a.add_dw = r0 > 0 || accumulate;
     a.last = r0 + a.rows == rows;
+    if (grad) {
+      const bool fp32 = a.dw_dtype == FT_F32 || !a.last;
+      if (mma_map(&map_dw, a.dw_dtype == FT_F32 || a.last ? a.dw : a.dw_acc, a.hidden, a.vocab, a.hidden, 32, fp32) != CUDA_SUCCESS)
+        return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    }
     const dim3 joins((a.rows + 31) / 32);
     const uint32_t join_threads = 32 * kJoinRowWarps;
     const bool high = a.rows > kMmaTile;
-    k_pick<<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
+    if (a.rows <= kPickFewUpTo) k_pick<kPickFew><<<(a.rows + kPickFew - 1) / kPickFew, 256, 0, st>>>(p->view, a);
+    else k_pick<kPickRows><<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
     FT_CUDA(cudaGetLastError());
     if (grad) {
-      FT_CUDA(launch_chained(high ? k_logits<true, false, 2> : k_logits<true, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(high ? k_logits<true, false, 2> : k_logits<true, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, map_e, p->view, a));
       FT_CUDA(launch_chained(k_join, joins, join_threads, 0, st, a));
-      FT_CUDA(launch_chained(k_logits<true, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_logits<true, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, map_e, p->view, a));
       FT_CUDA(launch_chained(k_finish<true>, joins, join_threads, 0, st, a));
       FT_CUDA(launch_chained(k_dx, grid, kMmaThreads, kMmaSmem, st, map_p, map_w, p->view, a));
-      FT_CUDA(launch_chained(k_dx_join, dim3((a.hidden + kMmaTile - 1) / kMmaTile, joins.x), 256, 0, st, a, pairs));
-      FT_CUDA(launch_chained(k_dw, grid, kMmaThreads, kMmaSmem, st, map_p, map_x, p->view, a));
+      FT_CUDA(launch_chained(k_dx_join, dim3((unsigned)p->sm_count * 8), 256, 0, st, a));
+      FT_CUDA(launch_chained(k_dw, grid, kMmaThreads, kMmaSmem, st, map_p, map_x, map_dw, p->view, a));
     } else {
-      FT_CUDA(launch_chained(high ? k_logits<false, false, 2> : k_logits<false, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(high ? k_logits<false, false, 2> : k_logits<false, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, map_e, p->view, a));
       FT_CUDA(launch_chained(k_join, joins, join_threads, 0, st, a));
-      FT_CUDA(launch_chained(k_logits<false, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
+      FT_CUDA(launch_chained(k_logits<false, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, map_e, p->view, a));
       FT_CUDA(launch_chained(k_finish<false>, joins, join_threads, 0, st, a));
     }
     p->gpu_launches += grad ? 8 : 5;

@@ -36,7 +36,8 @@ constexpr int kMmaStages = kHigh == 1 ? 6 : 4;
 constexpr int kMmaThreads = 384;
 constexpr int kMmaEpilogueWarps = 8;
 constexpr size_t kMmaRing = 6 * 2 * kMmaOperand;     // the stages of either height: 192 KiB
-constexpr size_t kMmaSmem = kMmaRing + 1024 + 256;   // on a 1 KiB boundary, then the barriers
+constexpr uint32_t kMmaOut = 32 * 128;                // an epilogue warp's staging: its 32 rows, 128 bytes each
+constexpr size_t kMmaSmem = kMmaRing + kMmaEpilogueWarps * kMmaOut + 1024 + 256;  // on a 1 KiB boundary; last the barriers
 
 struct MmaBarriers {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
@@ -97,6 +98,44 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// An epilogue warp's way out: 32 rows of 128 bytes (64 bf16 or 32 fp32 columns) are written into its staging in the 128-byte
+// swizzle, and one TMA store takes them to the matrix, clipped at its extents.  Direct stores put a warp's 32 rows into 32 lines
+// an instruction and cost more cycles than the rest of the epilogue (see k_dw).
+struct MmaOut {
+  uint32_t stage;  // shared-memory address of the warp's staging
+  __device__ __forceinline__ MmaOut() {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u;
+    stage = ring + (uint32_t)kMmaRing + ((threadIdx.x >> 5) & 7) * kMmaOut;  // warps 4..11
+  }
+  // the lane's row: value v(j) gives 16 bytes of it, j = 0..7.  kAdd: the fp32 values are added to what the matrix holds
+  template <bool kAdd, class F>
+  __device__ __forceinline__ void put(const CUtensorMap* map, int32_t x, int32_t y, F&& v) const {
+    const uint32_t lane = threadIdx.x & 31;
+    if (lane == 0) bulk_wait_read<0>();  // the staging's last store has read it
+    __syncwarp();
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) {
+      const uint4 w = v(j);
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+    }
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if constexpr (kAdd)
+        asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(stage), "r"(x), "r"(y) : "memory");
+      else
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(stage), "r"(x), "r"(y) : "memory");
+      bulk_commit();
+    }
+  }
+  // all stores of the warp have reached memory
+  __device__ __forceinline__ void done() const {
+    if ((threadIdx.x & 31) == 0) bulk_wait_all<0>();
+    __syncwarp();
+  }
+};
+
 // Shared-memory descriptor (PTX ISA, "matrix descriptor"): bits 0-13 address / 16, 16-29 leading offset / 16, 32-45 stride
 // offset / 16, 46-47 = 1, 61-63 = 2 for the 128-byte swizzle.
 //   K innermost: rows of 128 bytes, groups of eight rows 1 KiB apart (stride offset); the leading offset is not used
@@ -123,14 +162,15 @@ struct MmaTile {
 // Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; every epilogue warp calls
 // epilogue(tile, i, tmem, row, col0, release) for each 256 rows: tensor memory from `tmem` on holds 128 columns of its 32 rows, lane
 // l the row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() as soon as it has read them.  A tile
-// without K blocks has tmem = kNone: all sums are zero.
-template <bool kAMn, bool kBMn, int kHigh, class TileAt, class Epilogue>
+// without K blocks has tmem = kNone: all sums are zero.  before(tile, row) is called ahead of the wait for the products, for
+// what the epilogue reads from memory.
+template <bool kAMn, bool kBMn, int kHigh, class TileAt, class Before, class Epilogue>
 __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, uint64_t limit_ns, bool* lost_out,
-                                               TileAt tile_at, Epilogue epilogue) {
+                                               TileAt tile_at, Before before, Epilogue epilogue) {
   extern __shared__ uint8_t smem_raw[];
   constexpr uint32_t kStages = kMmaStages<kHigh>, kStageBytes = (kHigh + 1) * kMmaOperand;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  MmaBarriers* bar = reinterpret_cast<MmaBarriers*>(stages + kMmaRing);
+  MmaBarriers* bar = reinterpret_cast<MmaBarriers*>(stages + kMmaRing + kMmaEpilogueWarps * kMmaOut);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   if (threadIdx.x == 0) {
@@ -239,6 +279,8 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
       const MmaTile t = tile_at(i);
       for (uint32_t h = 0; h < t.high && !lost; ++h) {
         uint32_t at = kNone;
+        const uint32_t row = h * kMmaTile + rank * 128 + quarter * 32;
+        before(t, row);
         if (t.k0 < t.k1) {
           acc = kHigh == 1 ? turn : h;
           turn ^= 1;
@@ -248,10 +290,11 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
           at = tmem + acc * 256 + col0 + (quarter << 21);
         }
         held = at != kNone;
-        epilogue(t, i, at, h * kMmaTile + rank * 128 + quarter * 32, col0, release);
+        epilogue(t, i, at, row, col0, release);
         release();
       }
     }
+    MmaOut().done();
   }
   if (lost) bar->lost = 1;
   __syncwarp();
@@ -262,8 +305,9 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   *lost_out = bar->lost != 0;
 }
 
-// A matrix of bf16 rows, brought in 64 x 64 boxes; reads beyond its extents give zeros.
-inline CUresult mma_map(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t ld) {
+// A matrix of bf16 rows, brought in 64 x 64 boxes; reads beyond its extents give zeros.  With box_rows = 32 the map of a store,
+// whose values may be fp32 (32 columns a box).
+inline CUresult mma_map(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows = 64, bool fp32 = false) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static const Encode encode = [] {
@@ -273,9 +317,9 @@ inline CUresult mma_map(CUtensorMap* map, const void* base, uint64_t inner, uint
     return reinterpret_cast<Encode>(f);
   }();
   if (!encode) return CUDA_ERROR_NOT_FOUND;
-  const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
-  const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * (fp32 ? 4 : 2)};
+  const cuuint32_t box[2] = {fp32 ? 32u : 64u, box_rows}, step[2] = {1, 1};
+  return encode(map, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
