@@ -6,14 +6,16 @@
 //
 // Both are bound by HBM: a row is read once (two rows backward) and written once, with a dozen operations an element.
 //
-//   k_norm          a CTA holds one row at a time in registers: the variance is taken about the mean, not from a difference
-//                   of sums.  16-byte chunks of the following rows are on their way into shared memory meanwhile
-//   k_norm_grad     the same walk; a thread always owns the same columns, so the sums over rows stay in its registers
-//                   until the CTA has seen its last row.  No atomics: partial sums go to the workspace, one line a CTA
+//   k_norm          a few warps (one for rows up to 4096 elements, where there are rows enough) hold a row in registers: the
+//                   variance is taken about the mean, not from a difference of sums
+//   k_norm_grad     groups of warps hold a row each; a thread always owns the same columns, so the sums over rows stay in
+//                   its registers until its last row, while 16-byte chunks of the following rows are on their way into
+//                   shared memory.  No atomics: partial sums go to the workspace, one line a CTA
 //   k_norm_join     adds the lines of partial sums in line order
-//   k_norm_wide, k_norm_grad_sums, k_norm_grad_cols   rows too long for a CTA's registers
+//   k_norm_wide, k_norm_grad_sums, k_norm_grad_cols   rows too long for that
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "operators.cuh"
 
@@ -37,198 +39,302 @@ struct NormGradArgs {
   float* partial;  // [lines][2][cols]
 };
 
-constexpr int kNormMaxThreads = 512;
-// Rows in shared memory or under way to it: four, or two where the backward pass holds two operands of 64 bytes a thread
-// (four stages of those would take 256 KiB at 512 threads).
-template <int kOperands, int V>
-constexpr int kNormStages = kOperands * V <= 4 ? 4 : 2;
+// ---- forward ------------------------------------------------------------------------------------------------------
 
-// sum over the block of N values a thread; every thread gets them.  `red` is one of two buffers used in turn: a buffer
-// is written again only behind the barrier of the other one's use.
-template <int N>
-__device__ __forceinline__ void block_sum(float (&v)[N], float (*red)[kNormMaxThreads / 32]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-  const int nw = blockDim.x >> 5;
-  if (nw == 1) return;
-  if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) red[i][threadIdx.x >> 5] = v[i];
-  }
+// Sum over a block of kN threads, for every thread.  `red` is one of two zeroed buffers used in turn: a buffer is written
+// again only behind the barrier of the other one's use.
+template <int kN>
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  v = warp_sum(v);
+  if constexpr (kN == 32) return v;
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
+  const float4* r = reinterpret_cast<const float4*>(red);
+  v = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float s = red[i][0];
-    for (int w = 1; w < nw; ++w) s += red[i][w];
-    v[i] = s;
-  }
+  for (int w = 0; w < (kN + 127) / 128; ++w) v += (r[w].x + r[w].y) + (r[w].z + r[w].w);
+  return v;
 }
 
-// Rows as this thread sees them: chunk k of thread t holds the E elements from (k * blockDim + t) * E on.  With 16-byte
-// chunks (kVec) a row travels through a ring of kStages rows in shared memory, filled by asynchronous copies that the
-// same thread issues and waits for, so the ring needs no barrier.  Otherwise (odd widths, odd strides) E = 1 and the
-// chunks come straight into registers.
-template <typename T, int V, bool kVec, int kStages>
-struct RowRing {
+// A thread's chunks of the rows that its group of kN threads goes through: chunk k of thread t holds the E elements from
+// (k kN + t) E on.  Where the rows allow it (kVec) a chunk is 16 bytes, and the following rows' chunks are on their way into a
+// ring in shared memory: a thread reads only what it has fetched itself, so the ring needs no barrier.  Otherwise a chunk is
+// one element and the next row's are fetched into registers.  Where the row has no such chunk the values are zero.  kN is a
+// constant, so that chunks are offsets in the instructions; a quarter of the first version's instructions were addresses.
+template <typename T, int V, bool kVec, int kN, int kThreads, int kStages>
+struct RowFeed {
   static constexpr int E = kVec ? Pack<T>::kElems : 1;
-  const T* base;
-  uint64_t ld, rows;
-  uint32_t cols;
-  uint4* ring;  // [kStages][V][blockDim], kVec only
+  const T* p;        // the thread's first chunk of the row to be fetched next
+  uint64_t step;     // elements from that row to the one after it
+  uint64_t left;     // rows still to be fetched
+  uint32_t chunks;   // chunks of this thread that the row has
+  uint4* slot;       // [kStages][V][kThreads]
+  T next[kVec ? 1 : V];
 
-  __device__ __forceinline__ uint32_t at(int k) const { return (k * blockDim.x + threadIdx.x) * E; }
-  __device__ __forceinline__ void fetch(uint64_t row, uint32_t stage) {
-    if constexpr (kVec) {
-      if (row < rows) {
-        const T* p = base + row * ld;
+  __device__ __forceinline__ void init(const void* base, uint64_t ld, uint64_t rows, uint64_t row, uint64_t row_step, uint32_t cols, uint32_t t, uint4* s) {
+    p = static_cast<const T*>(base) + row * ld + t * E;
+    step = row_step * ld;
+    left = row < rows ? (rows - row + row_step - 1) / row_step : 0;
+    const uint32_t n = cols / E;
+    chunks = n > t ? (n - t + kN - 1) / kN : 0;
+    slot = s;
+    if constexpr (kVec) {  // chunks that the rows do not have are never fetched
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-          if (at(k) < cols) copy16_async(ring + (stage * V + k) * blockDim.x + threadIdx.x, p + at(k));
-      }
+      for (int i = 0; i < kStages * V; ++i)
+        if (i % V >= (int)chunks) slot[i * kThreads] = make_uint4(0, 0, 0, 0);
     }
   }
-  __device__ __forceinline__ void take(uint64_t row, uint32_t stage, float (&f)[V * E]) const {
+  __device__ __forceinline__ bool has(int k) const { return k < (int)chunks; }
+  __device__ __forceinline__ void fetch(uint32_t stage) {
+    if (left == 0) return;
+    --left;
+    uint4* to = slot + stage * (V * kThreads);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if (at(k) < cols) {
-        if constexpr (kVec) Pack<T>::widen(ring[(stage * V + k) * blockDim.x + threadIdx.x], f + k * E);
-        else f[k] = widen1(base[row * ld + at(k)]);
+      if constexpr (kVec) {
+        if (has(k)) copy16_async(to + k * kThreads, p + k * kN * E);
       } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) f[k * E + e] = 0.f;
+        next[k] = has(k) ? p[k * kN] : narrow1<T>(0.f);
       }
     }
+    p += step;
   }
-  __device__ __forceinline__ void store(void* out, uint64_t row, uint64_t ldo, const float (&f)[V * E]) const {
-    T* p = static_cast<T*>(out) + row * ldo;
+  __device__ __forceinline__ void take(uint32_t stage, float (&f)[V * E]) const {
+    const uint4* from = slot + stage * (V * kThreads);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if (at(k) < cols) {
-        if constexpr (kVec) *reinterpret_cast<uint4*>(p + at(k)) = Pack<T>::narrow(f + k * E);
-        else p[at(k)] = narrow1<T>(f[k]);
-      }
+      if constexpr (kVec) Pack<T>::widen(from[k * kThreads], f + k * E);
+      else f[k] = widen1(next[k]);
+    }
+  }
+  __device__ __forceinline__ void store(T* q, const float (&f)[V * E]) const {  // q: the thread's first chunk of the output row
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if (!has(k)) continue;
+      if constexpr (kVec) *reinterpret_cast<uint4*>(q + k * kN * E) = Pack<T>::narrow(f + k * E);
+      else q[k * kN] = narrow1<T>(f[k]);
     }
   }
 };
 
-template <typename T, int V, bool kVec>
-__global__ void __launch_bounds__(kNormMaxThreads) k_norm(NormArgs a) {
-  extern __shared__ __align__(16) uint4 ring[];
-  __shared__ float red[2][1][kNormMaxThreads / 32];
-  constexpr int kStages = kNormStages<1, V>;
-  using Ring = RowRing<T, V, kVec, kStages>;
-  constexpr int E = Ring::E, N = V * E;
-  Ring in{static_cast<const T*>(a.x), a.ldx, a.rows, a.cols, ring};
+constexpr int kNormStages = 4;
+
+template <typename T, int V, bool kVec, int kN>
+__global__ void __launch_bounds__(kN, 512 / kN) k_norm(NormArgs a) {
+  extern __shared__ __align__(16) uint4 ring[];  // [kNormStages][V][kN]
+  __shared__ __align__(16) float red[2][kN < 128 ? 4 : kN / 32];
+  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E, kSums = N < 4 ? N : 4;
+  RowFeed<T, V, kVec, kN, kN, kNormStages> in;
   const uint64_t step = gridDim.x;
   uint64_t row = blockIdx.x;
+  in.init(a.x, a.ldx, a.rows, row, step, a.cols, threadIdx.x, ring + threadIdx.x);
+  if constexpr (kVec) {
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) { in.fetch(row + s * step, s); copy_async_commit(); }
+    for (int s = 0; s < kNormStages - 1; ++s) { in.fetch(s); copy_async_commit(); }
+  } else {
+    in.fetch(0);
+  }
+  if (kN > 32 && threadIdx.x < sizeof(red) / 4) (&red[0][0])[threadIdx.x] = 0.f;
   float w[N], b[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint32_t c = in.at(i / E) + i % E;
-    w[i] = c < a.cols ? (a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f) : 0.f;
+    const uint32_t c = (i / E * kN + threadIdx.x) * E + i % E;
+    w[i] = c < a.cols && a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f;
     b[i] = c < a.cols && a.bias ? load_as(a.bias, a.param_dtype, c) : 0.f;
   }
+  if (kN > 32) __syncthreads();
+  const float inv = 1.f / a.cols;
+  T* q = static_cast<T*>(a.y) + row * a.ldy + threadIdx.x * E;
   uint32_t stage = 0;
   for (; row < a.rows; row += step) {
-    in.fetch(row + (kStages - 1) * step, (stage + kStages - 1) % kStages);
-    copy_async_commit();
-    copy_async_wait<kStages - 1>();
-    float x[N];
-    in.take(row, stage, x);
-    float s[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[0] += x[i];
-    block_sum(s, red[0]);
-    const float mean = s[0] / a.cols;
-    s[0] = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      x[i] -= mean;
-      if (in.at(i / E) < a.cols) s[0] += x[i] * x[i];
+    float x[N], s[kSums] = {};
+    if constexpr (kVec) {
+      in.fetch((stage + kNormStages - 1) % kNormStages);
+      copy_async_commit();
+      copy_async_wait<kNormStages - 1>();
     }
-    block_sum(s, red[1]);
-    const float rstd = rsqrtf(s[0] / a.cols + a.eps);
+    in.take(stage, x);
+    if constexpr (!kVec) in.fetch(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i % kSums] += x[i];
+#pragma unroll
+    for (int i = 1; i < kSums; ++i) s[0] += s[i];
+    const float mean = block_sum<kN>(s[0], red[0]) * inv;
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if (!in.has(k)) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = k * E + e;
+        x[i] -= mean;
+        s[i % kSums] += x[i] * x[i];
+      }
+    }
+#pragma unroll
+    for (int i = 1; i < kSums; ++i) s[0] += s[i];
+    const float rstd = rsqrtf(block_sum<kN>(s[0], red[1]) * inv + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = x[i] * rstd * w[i] + b[i];
-    in.store(a.y, row, a.ldy, x);
-    stage = (stage + 1) % kStages;
+    in.store(q, x);
+    q += step * a.ldy;
+    stage = (stage + 1) % kNormStages;
   }
 }
 
-template <typename T, int V, bool kVec>
-__global__ void __launch_bounds__(kNormMaxThreads) k_norm_grad(NormGradArgs a) {
-  extern __shared__ __align__(16) uint4 ring[];
-  __shared__ float red[2][2][kNormMaxThreads / 32];
-  constexpr int kStages = kNormStages<2, V>;
-  using Ring = RowRing<T, V, kVec, kStages>;
-  constexpr int E = Ring::E, N = V * E;
-  Ring in_x{static_cast<const T*>(a.x), a.ldx, a.rows, a.cols, ring};
-  Ring in_g{static_cast<const T*>(a.dy), a.lddy, a.rows, a.cols, ring + kStages * V * blockDim.x};
-  const uint64_t step = gridDim.x;
-  uint64_t row = blockIdx.x;
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) {
-    in_x.fetch(row + s * step, s); in_g.fetch(row + s * step, s);
-    copy_async_commit();
+// ---- backward -----------------------------------------------------------------------------------------------------
+
+// Rows in shared memory or under way to it: four, or two where a row's two operands take 256 bytes a thread.
+template <int V>
+constexpr int kGradStages = V > 4 ? 2 : 4;
+constexpr int kGradGroups(int n) { return n >= 256 ? 1 : 384 / n; }  // 384 threads an SM hold 168 registers each
+
+// The CTA's threads form groups of kN; group i of the grid takes the rows i, i + groups, ...
+template <typename T, int V, bool kVec, int kN, int kGroups>
+__global__ void __launch_bounds__(kN * kGroups, 1) k_norm_grad(NormGradArgs a) {
+  extern __shared__ __align__(16) uint4 ring[];  // weights; then [2][kStages][V][kThreads], at the end the groups' sums
+  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E, kThreads = kN * kGroups, kStages = kGradStages<V>, nw = kN / 32;
+  __shared__ float2 red[2][kThreads / 32];
+  const uint32_t group = threadIdx.x / kN, t = threadIdx.x % kN;
+  // The weights stay in shared memory, a thread's registers being taken by its row and its sums: chunk by chunk, in quarters of
+  // four, so that the lanes of an access read one range.
+  constexpr int Q = kVec ? 4 : 1;
+  float* weights = reinterpret_cast<float*>(ring);  // [V][E / Q][kN][Q]
+  uint4* rows = ring + V * E * kN / 4;
+  for (uint32_t i = threadIdx.x; i < V * E * kN; i += kThreads) {
+    const uint32_t q = i % Q, th = i / Q % kN, part = i / Q / kN;  // part: chunk and quarter
+    const uint32_t c = (part / (E / Q) * kN + th) * E + part % (E / Q) * Q + q;
+    weights[i] = c < a.cols ? (a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f) : 0.f;
   }
-  float w[N], dw[N], db[N];
+  const uint64_t step = (uint64_t)gridDim.x * kGroups;
+  uint64_t row = (uint64_t)blockIdx.x * kGroups + group;
+  RowFeed<T, V, kVec, kN, kThreads, kStages> in_x, in_g;
+  in_x.init(a.x, a.ldx, a.rows, row, step, a.cols, t, rows + threadIdx.x);
+  in_g.init(a.dy, a.lddy, a.rows, row, step, a.cols, t, rows + kStages * V * kThreads + threadIdx.x);
+  if constexpr (kVec) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t c = in_x.at(i / E) + i % E;
-    w[i] = c < a.cols ? (a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f) : 0.f;
-    dw[i] = db[i] = 0.f;
+    for (int s = 0; s < kStages - 1; ++s) { in_x.fetch(s); in_g.fetch(s); copy_async_commit(); }
+  } else {
+    in_x.fetch(0); in_g.fetch(0);
   }
-  uint32_t stage = 0;
+  __syncthreads();
+  float dw[N], db[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+  const float inv = 1.f / a.cols;
+  T* q = static_cast<T*>(a.dx) + row * a.lddx + t * E;
+  uint32_t stage = 0, turn = 0;
+  float mean = 0.f, rstd = 0.f;
+  if (row < a.rows) { mean = a.mean[row]; rstd = a.rstd[row]; }
   for (; row < a.rows; row += step) {
-    in_x.fetch(row + (kStages - 1) * step, (stage + kStages - 1) % kStages);
-    in_g.fetch(row + (kStages - 1) * step, (stage + kStages - 1) % kStages);
-    copy_async_commit();
-    copy_async_wait<kStages - 1>();
-    const float mean = a.mean[row], rstd = a.rstd[row];
     float x[N], g[N];
-    in_x.take(row, stage, x);
-    in_g.take(row, stage, g);
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      x[i] = in_x.at(i / E) < a.cols ? (x[i] - mean) * rstd : 0.f;
-      dw[i] += g[i] * x[i];
-      db[i] += g[i];
-      g[i] *= w[i];
-      s[0] += g[i];
-      s[1] += g[i] * x[i];
+    if constexpr (kVec) {
+      in_x.fetch((stage + kStages - 1) % kStages);
+      in_g.fetch((stage + kStages - 1) % kStages);
+      copy_async_commit();
+      copy_async_wait<kStages - 1>();
     }
-    block_sum(s, red[stage & 1]);
-    const float c0 = s[0] / a.cols, c1 = s[1] / a.cols;
+    float next_mean = 0.f, next_rstd = 0.f;
+    if (row + step < a.rows) { next_mean = a.mean[row + step]; next_rstd = a.rstd[row + step]; }
+    in_x.take(stage, x);
+    in_g.take(stage, g);
+    if constexpr (!kVec) { in_x.fetch(0); in_g.fetch(0); }
+    float s0[2] = {0.f, 0.f}, s1[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      float w[E];
+#pragma unroll
+      for (int h = 0; h < E / Q; ++h) {
+        const float* p = weights + ((k * (E / Q) + h) * kN + t) * Q;
+        if constexpr (kVec) Pack<float>::widen(*reinterpret_cast<const uint4*>(p), w + h * Q);
+        else w[h] = *p;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {  // beyond the row dy and w are zero
+        const int i = k * E + e;
+        x[i] = (x[i] - mean) * rstd;
+        dw[i] += g[i] * x[i];
+        db[i] += g[i];
+        g[i] *= w[e];
+        s0[i & 1] += g[i];
+        s1[i & 1] += g[i] * x[i];
+      }
+    }
+    // both sums over the warp in five exchanges: the lower half of the lanes goes on with the first, the upper half with the second
+    const float a0 = s0[0] + s0[1], a1 = s1[0] + s1[1];
+    const bool upper = (threadIdx.x & 16) != 0;
+    float s = (upper ? a1 : a0) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a0 : a1, 16);
+#pragma unroll
+    for (int d = 8; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    float c0, c1;
+    if constexpr (nw == 1) {
+      c0 = __shfl_sync(0xFFFFFFFFu, s, 0);
+      c1 = __shfl_sync(0xFFFFFFFFu, s, 16);
+    } else {
+      if ((threadIdx.x & 15) == 0) reinterpret_cast<float*>(&red[turn][threadIdx.x >> 5])[upper ? 1 : 0] = s;
+      asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kN) : "memory");
+      const float2* r = &red[turn][group * nw];
+      c0 = r[0].x; c1 = r[0].y;
+#pragma unroll
+      for (int i = 1; i < nw; ++i) { c0 += r[i].x; c1 += r[i].y; }
+      turn ^= 1;  // written again only behind the next row's barrier
+    }
+    c0 *= inv;
+    c1 *= inv;
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = rstd * (g[i] - c0 - x[i] * c1);
-    in_x.store(a.dx, row, a.lddx, x);
+    in_x.store(q, x);
+    q += step * a.lddx;
+    mean = next_mean;
+    rstd = next_rstd;
     stage = (stage + 1) % kStages;
+  }
+  let_next_start();
+  // the groups' sums, in group order
+  if constexpr (kGroups > 1) {
+    float* sums = reinterpret_cast<float*>(rows);  // [kGroups - 1][2 N][kN]
+    copy_async_wait<0>();
+    __syncthreads();
+    if (group) {
+      float* mine = sums + (group - 1) * (2 * N * kN) + t;
+#pragma unroll
+      for (int i = 0; i < N; ++i) { mine[2 * i * kN] = dw[i]; mine[(2 * i + 1) * kN] = db[i]; }
+    }
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      for (int o = 0; o < kGroups - 1; ++o) {
+        dw[i] += sums[o * (2 * N * kN) + 2 * i * kN + t];
+        db[i] += sums[o * (2 * N * kN) + (2 * i + 1) * kN + t];
+      }
   }
   float* line = a.partial + (uint64_t)blockIdx.x * 2 * a.cols;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint32_t c = in_x.at(i / E) + i % E;
+    const uint32_t c = (i / E * kN + t) * E + i % E;
     if (c < a.cols) { line[c] = dw[i]; line[a.cols + c] = db[i]; }
   }
 }
 
-// dw and db from the lines of partial sums: 32 columns a CTA, eight warps over the lines, joined in a fixed order
-constexpr int kJoinWarps = 8;
+// dw and db from the lines of partial sums: 32 columns a CTA, its warps over the lines, joined in a fixed order
+constexpr int kJoinWarps = 16;
 __global__ void __launch_bounds__(32 * kJoinWarps) k_norm_join(const float* __restrict__ partial, uint32_t lines, uint32_t cols,
                                                                float* dweight, float* dbias, uint32_t accumulate) {
   __shared__ float part[kJoinWarps][32];
+  after_previous();
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;  // column of [dw | db]
   float s = 0.f;
-  if (c < 2ull * cols)
+  if (c < 2ull * cols) {
+#pragma unroll 5
     for (uint32_t l = warp; l < lines; l += kJoinWarps) s += partial[(uint64_t)l * 2 * cols + c];
+  }
   part[warp][lane] = s;
   __syncthreads();
   if (warp || c >= 2ull * cols) return;
@@ -240,22 +346,22 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_norm_join(const float* __re
   out[i] = accumulate ? out[i] + s : s;
 }
 
-// ---- rows beyond a CTA's registers: every pass reads the row again (from L2, a row at a time a CTA) ----------------
+// ---- long rows: every pass reads the row again (from L2, a row at a time a CTA) ---------------------------------------
+
+constexpr int kWideThreads = 512;
 
 template <typename T>
-__global__ void __launch_bounds__(kNormMaxThreads) k_norm_wide(NormArgs a) {
-  __shared__ float red[2][1][kNormMaxThreads / 32];
+__global__ void __launch_bounds__(kWideThreads) k_norm_wide(NormArgs a) {
+  __shared__ __align__(16) float red[2][kWideThreads / 32];
   for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     T* y = static_cast<T*>(a.y) + row * a.ldy;
-    float s[1] = {0.f};
-    for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) s[0] += widen1(x[c]);
-    block_sum(s, red[0]);
-    const float mean = s[0] / a.cols;
-    s[0] = 0.f;
-    for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) { const float d = widen1(x[c]) - mean; s[0] += d * d; }
-    block_sum(s, red[1]);
-    const float rstd = rsqrtf(s[0] / a.cols + a.eps);
+    float s = 0.f;
+    for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) s += widen1(x[c]);
+    const float mean = block_sum<kWideThreads>(s, red[0]) / a.cols;
+    s = 0.f;
+    for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) { const float d = widen1(x[c]) - mean; s += d * d; }
+    const float rstd = rsqrtf(block_sum<kWideThreads>(s, red[1]) / a.cols + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -269,20 +375,20 @@ __global__ void __launch_bounds__(kNormMaxThreads) k_norm_wide(NormArgs a) {
 
 // sums[row] = (sum(a), sum(a xhat)) / cols
 template <typename T>
-__global__ void __launch_bounds__(kNormMaxThreads) k_norm_grad_sums(NormGradArgs a, float2* sums) {
-  __shared__ float red[2][2][kNormMaxThreads / 32];
-  uint32_t turn = 0;
-  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+__global__ void __launch_bounds__(kWideThreads) k_norm_grad_sums(NormGradArgs a, float2* sums) {
+  __shared__ __align__(16) float red[2][kWideThreads / 32];
+  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T *x = static_cast<const T*>(a.x) + row * a.ldx, *dy = static_cast<const T*>(a.dy) + row * a.lddy;
     const float mean = a.mean[row], rstd = a.rstd[row];
-    float s[2] = {0.f, 0.f};
+    float s0 = 0.f, s1 = 0.f;
     for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) {
       const float g = widen1(dy[c]) * (a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f);
-      s[0] += g;
-      s[1] += g * ((widen1(x[c]) - mean) * rstd);
+      s0 += g;
+      s1 += g * ((widen1(x[c]) - mean) * rstd);
     }
-    block_sum(s, red[turn]);
-    if (threadIdx.x == 0) sums[row] = make_float2(s[0] / a.cols, s[1] / a.cols);
+    s0 = block_sum<kWideThreads>(s0, red[0]);
+    s1 = block_sum<kWideThreads>(s1, red[1]);
+    if (threadIdx.x == 0) sums[row] = make_float2(s0 / a.cols, s1 / a.cols);
   }
 }
 
@@ -308,103 +414,101 @@ __global__ void __launch_bounds__(256) k_norm_grad_cols(NormGradArgs a, const fl
 
 // ---- launch geometry ----------------------------------------------------------------------------------------------
 
-constexpr uint32_t kNormHeld = 16;  // elements of a row a thread holds at most
-constexpr uint32_t kNormMaxCols = kNormHeld * kNormMaxThreads;
-constexpr uint32_t kNormMaxLines = 1024;  // lines of partial sums: the grid of the backward kernel at most
 constexpr uint32_t kNormWideLines = 64;
 constexpr uint32_t kNormColsLimit = 1u << 30;  // column counters are 32-bit
 
-struct NormShape {
-  uint32_t threads, chunks;  // chunks a thread
-  bool vec;
-};
-
-// A row in 16-byte chunks where every row of every operand starts on a 16-byte boundary, else element by element.
-static NormShape norm_shape(uint32_t cols, bool vec, uint32_t elems, bool few_rows) {
-  NormShape s;
-  s.vec = vec;
-  const uint32_t n = vec ? cols / elems : cols, most = vec ? kNormHeld / elems : kNormHeld;
-  s.chunks = 1;
-  while (s.chunks < most && (n + s.chunks - 1) / s.chunks > (few_rows ? kNormMaxThreads : 128u)) s.chunks *= 2;
-  s.threads = ((n + s.chunks - 1) / s.chunks + 31) / 32 * 32;
-  return s;
+// f with the number n of `list` as a constant
+template <typename F, int... N>
+static void with_number(uint32_t n, std::integer_sequence<int, N...>, F&& f) {
+  (void)((n == (uint32_t)N && (f(std::integral_constant<int, N>{}), true)) || ...);
 }
-
-template <typename T, typename F>
-static void with_chunks(const NormShape& s, F&& f) {
-  if (s.vec) {
-    switch (s.chunks) {
-      case 1: f(std::integral_constant<int, 1>{}, std::true_type{}); return;
-      case 2: f(std::integral_constant<int, 2>{}, std::true_type{}); return;
-      default:
-        if constexpr (Pack<T>::kElems == 4) f(std::integral_constant<int, 4>{}, std::true_type{});
-        return;
-    }
-  }
-  switch (s.chunks) {
-    case 1: f(std::integral_constant<int, 1>{}, std::false_type{}); return;
-    case 2: f(std::integral_constant<int, 2>{}, std::false_type{}); return;
-    case 4: f(std::integral_constant<int, 4>{}, std::false_type{}); return;
-    case 8: f(std::integral_constant<int, 8>{}, std::false_type{}); return;
-    default: f(std::integral_constant<int, 16>{}, std::false_type{}); return;
-  }
+static uint32_t pow2_at_least(uint32_t x) {
+  uint32_t p = 32;
+  while (p < x) p *= 2;
+  return p;
 }
-
 template <typename K>
-static cudaError_t ctas_per_sm(K kernel, uint32_t threads, size_t smem, int* n) {
-  cudaError_t e = cudaSuccess;
-  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(n, kernel, (int)threads, smem);
-  *n = std::max(1, *n);
-  return e;
+static cudaError_t allow_smem(K kernel, size_t smem) {
+  return smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
 }
 
-template <typename T>
-static cudaError_t norm_launch(const ft_pool* p, const NormArgs& a, bool vec, cudaStream_t st) {
-  if (a.cols > kNormMaxCols) {
-    k_norm_wide<T><<<(unsigned)std::min<uint64_t>(a.rows, 4ull * p->sm_count), kNormMaxThreads, 0, st>>>(a);
-    return cudaGetLastError();
-  }
-  const NormShape s = norm_shape(a.cols, vec, Pack<T>::kElems, a.rows <= (uint64_t)p->sm_count);
+// Chunks a thread: 32 elements (16 single ones, which come with an address each), so that a row's two sums over its threads
+// weigh little; one chunk (four) where there are few rows, which are a matter of latency: 32768 rows x 3584 take 90 us with
+// 32 elements a thread and 120 us with 16.
+template <typename T, bool kVec>
+static constexpr int kMany = kVec ? 32 / Pack<T>::kElems : 16;
+template <bool kVec>
+static constexpr int kFew = kVec ? 1 : 4;
+
+template <typename T, bool kVec, int V>
+static cudaError_t norm_rows(const ft_pool* p, const NormArgs& a, cudaStream_t st) {
+  const uint32_t n = a.cols / (kVec ? Pack<T>::kElems : 1), threads = pow2_at_least((n + V - 1) / V);
   cudaError_t e = cudaSuccess;
-  with_chunks<T>(s, [&](auto v, auto is_vec) {
-    auto kernel = k_norm<T, decltype(v)::value, decltype(is_vec)::value>;
-    const size_t smem = s.vec ? (size_t)kNormStages<1, decltype(v)::value> * s.chunks * s.threads * 16 : 0;
+  with_number(threads, std::integer_sequence<int, 32, 64, 128, 256, 512>{}, [&](auto k) {
+    constexpr int kN = decltype(k)::value;
+    auto kernel = k_norm<T, V, kVec, kN>;
+    constexpr size_t smem = kVec ? (size_t)kNormStages * V * kN * 16 : 0;
+    if ((e = allow_smem(kernel, smem)) != cudaSuccess) return;
     int per_sm = 1;
-    if ((e = ctas_per_sm(kernel, s.threads, smem, &per_sm)) != cudaSuccess) return;
-    kernel<<<(unsigned)std::min<uint64_t>(a.rows, (uint64_t)per_sm * p->sm_count), s.threads, smem, st>>>(a);
+    if (a.rows > (uint64_t)p->sm_count) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kN, smem);
+    if (e != cudaSuccess) return;
+    kernel<<<(unsigned)std::min<uint64_t>(a.rows, (uint64_t)std::max(1, per_sm) * p->sm_count), kN, smem, st>>>(a);
     e = cudaGetLastError();
   });
   return e;
 }
 
-template <typename T>
-static cudaError_t norm_grad_launch(const ft_pool* p, const NormGradArgs& a, bool vec, float2* sums, uint32_t* lines, cudaStream_t st) {
-  if (a.cols > kNormMaxCols) {
-    k_norm_grad_sums<T><<<(unsigned)std::min<uint64_t>(a.rows, 4ull * p->sm_count), kNormMaxThreads, 0, st>>>(a, sums);
+template <typename T, bool kVec>
+static cudaError_t norm_launch(const ft_pool* p, const NormArgs& a, cudaStream_t st) {
+  constexpr uint32_t E = kVec ? Pack<T>::kElems : 1, kMost = 512 * E;
+  if (a.cols > kMany<T, kVec> * kMost) {
+    k_norm_wide<T><<<(unsigned)std::min<uint64_t>(a.rows, 4ull * p->sm_count), kWideThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  const uint64_t warps = a.rows * ((a.cols / E + 32 * kMany<T, kVec> - 1) / (32 * kMany<T, kVec>));
+  const bool few = warps < 8ull * p->sm_count && a.cols <= kFew<kVec> * kMost;
+  return few ? norm_rows<T, kVec, kFew<kVec>>(p, a, st) : norm_rows<T, kVec, kMany<T, kVec>>(p, a, st);
+}
+
+template <typename T, bool kVec, int V, int kN, int kGroups>
+static cudaError_t norm_grad_rows(ft_pool* p, const NormGradArgs& a, uint32_t* lines, cudaStream_t st) {
+  constexpr int E = kVec ? Pack<T>::kElems : 1;
+  constexpr size_t kRows = kVec ? 2ull * kGradStages<V> * V * kN * kGroups * 16 : 0, kSums = (kGroups - 1) * 2ull * V * E * kN * 4;
+  constexpr size_t smem = (size_t)V * E * kN * 4 + (kRows > kSums ? kRows : kSums);
+  auto kernel = k_norm_grad<T, V, kVec, kN, kGroups>;
+  const cudaError_t e = allow_smem(kernel, smem);
+  if (e != cudaSuccess) return e;
+  *lines = (uint32_t)std::min<uint64_t>((a.rows + kGroups - 1) / kGroups, (uint64_t)p->sm_count);
+  kernel<<<*lines, kN * kGroups, smem, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T, bool kVec>
+static cudaError_t norm_grad_launch(ft_pool* p, const NormGradArgs& a, float2* sums, uint32_t* lines, cudaStream_t st) {
+  constexpr uint32_t E = kVec ? Pack<T>::kElems : 1;
+  constexpr int kV = kMany<T, kVec>;
+  const uint32_t n = a.cols / E;
+  if (n > kV * 256) {
+    k_norm_grad_sums<T><<<(unsigned)std::min<uint64_t>(a.rows, 4ull * p->sm_count), kWideThreads, 0, st>>>(a, sums);
     *lines = (uint32_t)std::min<uint64_t>(a.rows, kNormWideLines);
     k_norm_grad_cols<T><<<dim3((a.cols + 255u) / 256u, *lines), 256, 0, st>>>(a, sums);
+    p->gpu_launches += 1;
     return cudaGetLastError();
   }
-  const NormShape s = norm_shape(a.cols, vec, Pack<T>::kElems, a.rows <= (uint64_t)p->sm_count);
+  if (n <= 32u * kFew<kVec>) return norm_grad_rows<T, kVec, kFew<kVec>, 32, kGradGroups(32)>(p, a, lines, st);
   cudaError_t e = cudaSuccess;
-  with_chunks<T>(s, [&](auto v, auto is_vec) {
-    auto kernel = k_norm_grad<T, decltype(v)::value, decltype(is_vec)::value>;
-    const size_t smem = s.vec ? 2ull * kNormStages<2, decltype(v)::value> * s.chunks * s.threads * 16 : 0;
-    int per_sm = 1;
-    if ((e = ctas_per_sm(kernel, s.threads, smem, &per_sm)) != cudaSuccess) return;
-    *lines = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(a.rows, (uint64_t)per_sm * p->sm_count), kNormMaxLines);
-    kernel<<<*lines, s.threads, smem, st>>>(a);
-    e = cudaGetLastError();
+  with_number(pow2_at_least((n + kV - 1) / kV), std::integer_sequence<int, 32, 64, 128, 256>{}, [&](auto k) {
+    constexpr int kN = decltype(k)::value;
+    e = norm_grad_rows<T, kVec, kV, kN, kGradGroups(kN)>(p, a, lines, st);
   });
   return e;
 }
 
-// bytes of the backward pass's workspace: the lines of partial sums, and for wide rows two numbers a row
+// bytes of the backward pass's workspace: the lines of partial sums, and for long rows two numbers a row (which rows those are
+// depends on the operands' alignment too: 4096 elements are the least)
 static uint64_t norm_grad_ws(const ft_pool* p, uint64_t rows, uint32_t cols) {
-  const bool wide = cols > kNormMaxCols;
-  const uint64_t lines = wide ? kNormWideLines : std::min<uint64_t>(std::min<uint64_t>(rows, 16ull * p->sm_count), kNormMaxLines);
-  return align_up_sz(lines * 2 * cols * sizeof(float), 256) + (wide ? rows * sizeof(float2) : 0);
+  const uint64_t lines = std::min<uint64_t>(rows, std::max<uint64_t>(p->sm_count, kNormWideLines));
+  return align_up_sz(lines * 2 * cols * sizeof(float), 256) + (cols > 4096 ? rows * sizeof(float2) : 0);
 }
 
 static bool rows_in_16(const void* p, uint64_t ld, uint32_t es) { return aligned_to(p, 16) && ld * es % 16 == 0; }
@@ -429,7 +533,9 @@ FT_EXPORT int32_t pool_layer_norm(ft_pool* p, uint64_t rows, uint32_t cols, cons
   a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.mean = mean; a.rstd = rstd; a.eps = eps;
   const bool vec = cols * es % 16 == 0 && rows_in_16(x, ldx, es) && rows_in_16(y, ldy, es);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  FT_CUDA(dtype == FT_F32 ? norm_launch<float>(p, a, vec, st) : norm_launch<__nv_bfloat16>(p, a, vec, st));
+  using B = __nv_bfloat16;
+  FT_CUDA(dtype == FT_F32 ? (vec ? norm_launch<float, true>(p, a, st) : norm_launch<float, false>(p, a, st))
+                          : (vec ? norm_launch<B, true>(p, a, st) : norm_launch<B, false>(p, a, st)));
   p->gpu_launches += 1;
   return FT_OK;
 }
@@ -464,14 +570,16 @@ FT_EXPORT int32_t pool_layer_norm_grad(ft_pool* p, uint64_t rows, uint32_t cols,
   NormGradArgs a;
   a.rows = rows; a.lddy = lddy; a.ldx = ldx; a.lddx = lddx; a.cols = cols; a.param_dtype = param_dtype;
   a.dy = dy; a.x = x; a.weight = weight; a.mean = mean; a.rstd = rstd; a.dx = dx; a.partial = static_cast<float*>(workspace);
-  float2* sums = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + align_up_sz((size_t)kNormWideLines * 2 * cols * sizeof(float), 256));
+  float2* sums = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + norm_grad_ws(p, rows, cols)) - rows;  // at the workspace's end
   const bool vec = cols * es % 16 == 0 && rows_in_16(dy, lddy, es) && rows_in_16(x, ldx, es) && rows_in_16(dx, lddx, es);
   uint32_t lines = 0;
-  FT_CUDA(dtype == FT_F32 ? norm_grad_launch<float>(p, a, vec, sums, &lines, st) : norm_grad_launch<__nv_bfloat16>(p, a, vec, sums, &lines, st));
-  p->gpu_launches += cols > kNormMaxCols ? 2 : 1;
+  using B = __nv_bfloat16;
+  FT_CUDA(dtype == FT_F32 ? (vec ? norm_grad_launch<float, true>(p, a, sums, &lines, st) : norm_grad_launch<float, false>(p, a, sums, &lines, st))
+                          : (vec ? norm_grad_launch<B, true>(p, a, sums, &lines, st) : norm_grad_launch<B, false>(p, a, sums, &lines, st)));
+  p->gpu_launches += 1;
   if (dweight || dbias) {
-    k_norm_join<<<(unsigned)((2ull * cols + 31) / 32), 32 * kJoinWarps, 0, st>>>(a.partial, lines, cols, dweight, dbias, accumulate);
-    FT_CUDA(cudaGetLastError());
+    FT_CUDA(launch_chained(k_norm_join, dim3((unsigned)((2ull * cols + 31) / 32)), 32 * kJoinWarps, 0, st, static_cast<const float*>(a.partial), lines, cols,
+                           dweight, dbias, accumulate));
     p->gpu_launches += 1;
   }
   return FT_OK;
