@@ -117,7 +117,7 @@ struct MmaOut {
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
       const uint4 w = v(j);
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+      store_shared16(stage + lane * 128 + ((j ^ (lane & 7)) << 4), w);
     }
     fence_async_smem();
     __syncwarp();

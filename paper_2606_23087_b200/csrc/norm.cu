@@ -68,31 +68,31 @@ struct RowFeed {
   uint64_t step;     // elements from that row to the one after it
   uint64_t left;     // rows still to be fetched
   uint32_t chunks;   // chunks of this thread that the row has
-  uint4* slot;       // [kStages][V][kThreads]
+  uint32_t slot;     // shared-memory address of this thread's places: [kStages][V][kThreads] of 16 bytes
   T next[kVec ? 1 : V];
 
-  __device__ __forceinline__ void init(const void* base, uint64_t ld, uint64_t rows, uint64_t row, uint64_t row_step, uint32_t cols, uint32_t t, uint4* s) {
+  __device__ __forceinline__ void init(const void* base, uint64_t ld, uint64_t rows, uint64_t row, uint64_t row_step, uint32_t cols, uint32_t t, const uint4* s) {
     p = static_cast<const T*>(base) + row * ld + t * E;
     step = row_step * ld;
     left = row < rows ? (rows - row + row_step - 1) / row_step : 0;
     const uint32_t n = cols / E;
     chunks = n > t ? (n - t + kN - 1) / kN : 0;
-    slot = s;
+    slot = shared_address(s);
     if constexpr (kVec) {  // chunks that the rows do not have are never fetched
 #pragma unroll
       for (int i = 0; i < kStages * V; ++i)
-        if (i % V >= (int)chunks) slot[i * kThreads] = make_uint4(0, 0, 0, 0);
+        if (i % V >= (int)chunks) store_shared16(slot + i * kThreads * 16, make_uint4(0, 0, 0, 0));
     }
   }
   __device__ __forceinline__ bool has(int k) const { return k < (int)chunks; }
   __device__ __forceinline__ void fetch(uint32_t stage) {
     if (left == 0) return;
     --left;
-    uint4* to = slot + stage * (V * kThreads);
+    const uint32_t to = slot + stage * (V * kThreads * 16);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       if constexpr (kVec) {
-        if (has(k)) copy16_async(to + k * kThreads, p + k * kN * E);
+        if (has(k)) copy16_async(to + k * kThreads * 16, p + k * kN * E);
       } else {
         next[k] = has(k) ? p[k * kN] : narrow1<T>(0.f);
       }
@@ -100,10 +100,10 @@ struct RowFeed {
     p += step;
   }
   __device__ __forceinline__ void take(uint32_t stage, float (&f)[V * E]) const {
-    const uint4* from = slot + stage * (V * kThreads);
+    const uint32_t from = slot + stage * (V * kThreads * 16);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if constexpr (kVec) Pack<T>::widen(from[k * kThreads], f + k * E);
+      if constexpr (kVec) Pack<T>::widen(load_shared16(from + k * kThreads * 16), f + k * E);
       else f[k] = widen1(next[k]);
     }
   }
