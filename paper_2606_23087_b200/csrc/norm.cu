@@ -56,6 +56,9 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return v;
 }
 
+// rows of all that a group takes: first, first + step, ...
+__device__ __forceinline__ uint32_t rows_from(uint64_t all, uint64_t first, uint64_t step) { return first < all ? (uint32_t)((all - first + step - 1) / step) : 0; }
+
 // A thread's chunks of the rows that its group of kN threads goes through: chunk k of thread t holds the E elements from
 // (k kN + t) E on.  Where the rows allow it (kVec) a chunk is 16 bytes, and the following rows' chunks are on their way into a
 // ring in shared memory: a thread reads only what it has fetched itself, so the ring needs no barrier.  Otherwise a chunk is
@@ -65,16 +68,16 @@ template <typename T, int V, bool kVec, int kN, int kThreads, int kStages>
 struct RowFeed {
   static constexpr int E = kVec ? Pack<T>::kElems : 1;
   const T* p;        // the thread's first chunk of the row to be fetched next
-  uint64_t step;     // elements from that row to the one after it
-  uint64_t left;     // rows still to be fetched
+  uint64_t step;     // elements from that row to the group's next one
+  uint32_t left;     // rows still to be fetched
   uint32_t chunks;   // chunks of this thread that the row has
   uint32_t slot;     // shared-memory address of this thread's places: [kStages][V][kThreads] of 16 bytes
   T next[kVec ? 1 : V];
 
-  __device__ __forceinline__ void init(const void* base, uint64_t ld, uint64_t rows, uint64_t row, uint64_t row_step, uint32_t cols, uint32_t t, const uint4* s) {
+  __device__ __forceinline__ void init(const void* base, uint64_t ld, uint64_t row, uint64_t row_step, uint32_t rows, uint32_t cols, uint32_t t, const uint4* s) {
     p = static_cast<const T*>(base) + row * ld + t * E;
     step = row_step * ld;
-    left = row < rows ? (rows - row + row_step - 1) / row_step : 0;
+    left = rows;
     const uint32_t n = cols / E;
     chunks = n > t ? (n - t + kN - 1) / kN : 0;
     slot = shared_address(s);
@@ -99,20 +102,26 @@ struct RowFeed {
     }
     p += step;
   }
-  __device__ __forceinline__ void take(uint32_t stage, float (&f)[V * E]) const {
+  __device__ __forceinline__ void take(uint32_t stage, F2 (&f)[V * E / 2]) const {
     const uint32_t from = slot + stage * (V * kThreads * 16);
+    if constexpr (kVec) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      if constexpr (kVec) Pack<T>::widen(load_shared16(from + k * kThreads * 16), f + k * E);
-      else f[k] = widen1(next[k]);
+      for (int k = 0; k < V; ++k) Pack<T>::widen(load_shared16(from + k * kThreads * 16), f + k * (E / 2));
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; k += 2) f[k / 2] = f2(widen1(next[k]), widen1(next[k + 1]));
     }
   }
-  __device__ __forceinline__ void store(T* q, const float (&f)[V * E]) const {  // q: the thread's first chunk of the output row
+  __device__ __forceinline__ void store(T* q, const F2 (&f)[V * E / 2]) const {  // q: the thread's first chunk of the output row
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       if (!has(k)) continue;
-      if constexpr (kVec) *reinterpret_cast<uint4*>(q + k * kN * E) = Pack<T>::narrow(f + k * E);
-      else q[k * kN] = narrow1<T>(f[k]);
+      if constexpr (kVec) {
+        *reinterpret_cast<uint4*>(q + k * kN * E) = Pack<T>::narrow(f + k * (E / 2));
+      } else {
+        const float2 p = parts(f[k / 2]);
+        q[k * kN] = narrow1<T>(k % 2 ? p.y : p.x);
+      }
     }
   }
 };
@@ -120,14 +129,13 @@ struct RowFeed {
 constexpr int kNormStages = 4;
 
 template <typename T, int V, bool kVec, int kN>
-__global__ void __launch_bounds__(kN, 512 / kN) k_norm(NormArgs a) {
+__global__ void __launch_bounds__(kN, kVec && V * Pack<T>::kElems <= 16 ? 896 / kN : 512 / kN) k_norm(NormArgs a) {
   extern __shared__ __align__(16) uint4 ring[];  // [kNormStages][V][kN]
-  __shared__ __align__(16) float red[2][kN < 128 ? 4 : kN / 32];
-  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E, kSums = N < 4 ? N : 4;
+  __shared__ __align__(16) float red[2][(kN / 32 + 3) / 4 * 4];
+  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E / 2;  // N pairs
   RowFeed<T, V, kVec, kN, kN, kNormStages> in;
-  const uint64_t step = gridDim.x;
-  uint64_t row = blockIdx.x;
-  in.init(a.x, a.ldx, a.rows, row, step, a.cols, threadIdx.x, ring + threadIdx.x);
+  const uint32_t n_rows = rows_from(a.rows, blockIdx.x, gridDim.x);
+  in.init(a.x, a.ldx, blockIdx.x, gridDim.x, n_rows, a.cols, threadIdx.x, ring + threadIdx.x);
   if constexpr (kVec) {
 #pragma unroll
     for (int s = 0; s < kNormStages - 1; ++s) { in.fetch(s); copy_async_commit(); }
@@ -135,19 +143,26 @@ __global__ void __launch_bounds__(kN, 512 / kN) k_norm(NormArgs a) {
     in.fetch(0);
   }
   if (kN > 32 && threadIdx.x < sizeof(red) / 4) (&red[0][0])[threadIdx.x] = 0.f;
-  float w[N], b[N];
+  F2 w[N], b[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint32_t c = (i / E * kN + threadIdx.x) * E + i % E;
-    w[i] = c < a.cols && a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f;
-    b[i] = c < a.cols && a.bias ? load_as(a.bias, a.param_dtype, c) : 0.f;
+    float wv[2], bv[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t c = ((2 * i + j) / E * kN + threadIdx.x) * E + (2 * i + j) % E;
+      wv[j] = c < a.cols && a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f;
+      bv[j] = c < a.cols && a.bias ? load_as(a.bias, a.param_dtype, c) : 0.f;
+    }
+    w[i] = f2(wv[0], wv[1]);
+    b[i] = f2(bv[0], bv[1]);
   }
   if (kN > 32) __syncthreads();
   const float inv = 1.f / a.cols;
-  T* q = static_cast<T*>(a.y) + row * a.ldy + threadIdx.x * E;
+  T* q = static_cast<T*>(a.y) + blockIdx.x * a.ldy + threadIdx.x * E;
+  const uint64_t q_step = gridDim.x * a.ldy;
   uint32_t stage = 0;
-  for (; row < a.rows; row += step) {
-    float x[N], s[kSums] = {};
+  for (uint32_t r = 0; r < n_rows; ++r) {
+    F2 x[N], s[2] = {f2(0.f), f2(0.f)};
     if constexpr (kVec) {
       in.fetch((stage + kNormStages - 1) % kNormStages);
       copy_async_commit();
@@ -156,117 +171,130 @@ __global__ void __launch_bounds__(kN, 512 / kN) k_norm(NormArgs a) {
     in.take(stage, x);
     if constexpr (!kVec) in.fetch(0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i % kSums] += x[i];
+    for (int i = 0; i < N; ++i) s[i & 1] = s[i & 1] + x[i];
+    const float mean = block_sum<kN>(sum(s[0] + s[1]), red[0]) * inv;
+    s[0] = s[1] = f2(0.f);
 #pragma unroll
-    for (int i = 1; i < kSums; ++i) s[0] += s[i];
-    const float mean = block_sum<kN>(s[0], red[0]) * inv;
-#pragma unroll
-    for (int i = 0; i < kSums; ++i) s[i] = 0.f;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      if (!in.has(k)) continue;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int i = k * E + e;
-        x[i] -= mean;
-        s[i % kSums] += x[i] * x[i];
+    for (int i = 0; i < N; ++i) {
+      x[i] = x[i] + f2(-mean);
+      if constexpr (kVec) {
+        if (in.has(i / (E / 2))) s[i & 1] = fma(x[i], x[i], s[i & 1]);
+      } else {  // a pair is two chunks
+        const float2 p = parts(x[i]);
+        const F2 d = f2(in.has(2 * i) ? p.x : 0.f, in.has(2 * i + 1) ? p.y : 0.f);
+        s[i & 1] = fma(d, d, s[i & 1]);
       }
     }
-#pragma unroll
-    for (int i = 1; i < kSums; ++i) s[0] += s[i];
-    const float rstd = rsqrtf(block_sum<kN>(s[0], red[1]) * inv + a.eps);
+    const float rstd = rsqrtf(block_sum<kN>(sum(s[0] + s[1]), red[1]) * inv + a.eps);
     if (threadIdx.x == 0) {
+      const uint64_t row = blockIdx.x + (uint64_t)r * gridDim.x;
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = x[i] * rstd * w[i] + b[i];
+    for (int i = 0; i < N; ++i) x[i] = fma(x[i] * f2(rstd), w[i], b[i]);
     in.store(q, x);
-    q += step * a.ldy;
+    q += q_step;
     stage = (stage + 1) % kNormStages;
   }
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------
 
-// Rows in shared memory or under way to it: four, or two where a row's two operands take 256 bytes a thread.
-template <int V>
-constexpr int kGradStages = V > 4 ? 2 : 4;
-constexpr int kGradGroups(int n) { return n >= 256 ? 1 : 384 / n; }  // 384 threads an SM hold 168 registers each
+// Rows in shared memory or under way to it: four, or three where those would not fit.
+template <int V, int kThreads>
+constexpr int kGradStages = V * kThreads <= 1024 ? 4 : 3;
+// Groups of n threads in a CTA, one CTA an SM: 512 threads of 128 registers, or 256 of 255 where a thread holds 32 elements.
+constexpr int kGradGroups(int elems, int n) { return elems > 16 ? 256 / n : 512 / n; }
 
 // The CTA's threads form groups of kN; group i of the grid takes the rows i, i + groups, ...
 template <typename T, int V, bool kVec, int kN, int kGroups>
 __global__ void __launch_bounds__(kN * kGroups, 1) k_norm_grad(NormGradArgs a) {
   extern __shared__ __align__(16) uint4 ring[];  // weights; then [2][kStages][V][kThreads], at the end the groups' sums
-  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E, kThreads = kN * kGroups, kStages = kGradStages<V>, nw = kN / 32;
-  __shared__ float2 red[2][kThreads / 32];
+  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E / 2, kThreads = kN * kGroups, kStages = kGradStages<V, kN * kGroups>, nw = kN / 32;  // N pairs
+  __shared__ float2 red[2][kThreads / 32], stats[4][kThreads / 32];
   const uint32_t group = threadIdx.x / kN, t = threadIdx.x % kN;
-  // The weights stay in shared memory, a thread's registers being taken by its row and its sums: chunk by chunk, in quarters of
-  // four, so that the lanes of an access read one range.
-  constexpr int Q = kVec ? 4 : 1;
-  float* weights = reinterpret_cast<float*>(ring);  // [V][E / Q][kN][Q]
+  // The weights stay in shared memory, a thread's registers being taken by its row and its sums: by fours (pairs of single
+  // elements), so that the lanes of an access read one range.
+  constexpr int Q = kVec ? 4 : 2;
+  float* weights = reinterpret_cast<float*>(ring);  // [V E / Q][kN][Q]
   uint4* rows = ring + V * E * kN / 4;
   for (uint32_t i = threadIdx.x; i < V * E * kN; i += kThreads) {
-    const uint32_t q = i % Q, th = i / Q % kN, part = i / Q / kN;  // part: chunk and quarter
-    const uint32_t c = (part / (E / Q) * kN + th) * E + part % (E / Q) * Q + q;
+    const uint32_t th = i / Q % kN, e = i / Q / kN * Q + i % Q;  // the thread and which of its V E elements
+    const uint32_t c = (e / E * kN + th) * E + e % E;
     weights[i] = c < a.cols ? (a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f) : 0.f;
   }
-  const uint64_t step = (uint64_t)gridDim.x * kGroups;
-  uint64_t row = (uint64_t)blockIdx.x * kGroups + group;
+  const uint64_t step = (uint64_t)gridDim.x * kGroups, first = (uint64_t)blockIdx.x * kGroups + group;
+  const uint32_t n_rows = rows_from(a.rows, first, step);
   RowFeed<T, V, kVec, kN, kThreads, kStages> in_x, in_g;
-  in_x.init(a.x, a.ldx, a.rows, row, step, a.cols, t, rows + threadIdx.x);
-  in_g.init(a.dy, a.lddy, a.rows, row, step, a.cols, t, rows + kStages * V * kThreads + threadIdx.x);
-  if constexpr (kVec) {
+  in_x.init(a.x, a.ldx, first, step, n_rows, a.cols, t, rows + threadIdx.x);
+  in_g.init(a.dy, a.lddy, first, step, n_rows, a.cols, t, rows + kStages * V * kThreads + threadIdx.x);
+  // A row's two statistics come three rows ahead as well, a copy a warp (taken one row ahead they cost 25 of 160 us: each
+  // row's are 4 bytes of a sector of their own).
+  const uint32_t lane = threadIdx.x & 31, stat_at = shared_address(&stats[0][threadIdx.x >> 5]);
+  const float* stat = (lane ? a.rstd : a.mean) + first;
+  uint32_t stat_row = 0;
+  const auto fetch_stats = [&] {
+    if (lane < 2 && stat_row < n_rows) {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(stat_at + (stat_row % 4) * (uint32_t)sizeof(stats[0]) + lane * 4), "l"(stat) : "memory");
+      stat += step;
+    }
+    ++stat_row;
+  };
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) { in_x.fetch(s); in_g.fetch(s); copy_async_commit(); }
-  } else {
-    in_x.fetch(0); in_g.fetch(0);
+  for (int s = 0; s < 3; ++s) {
+    fetch_stats();
+    if (kVec && s < kStages - 1) { in_x.fetch(s); in_g.fetch(s); }
+    copy_async_commit();
   }
+  if constexpr (!kVec) { in_x.fetch(0); in_g.fetch(0); }
   __syncthreads();
-  float dw[N], db[N];
+  F2 dw[N], db[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+  for (int i = 0; i < N; ++i) dw[i] = db[i] = f2(0.f);
   const float inv = 1.f / a.cols;
-  T* q = static_cast<T*>(a.dx) + row * a.lddx + t * E;
+  T* q = static_cast<T*>(a.dx) + first * a.lddx + t * E;
+  const uint64_t q_step = step * a.lddx;
   uint32_t stage = 0, turn = 0;
-  float mean = 0.f, rstd = 0.f;
-  if (row < a.rows) { mean = a.mean[row]; rstd = a.rstd[row]; }
-  for (; row < a.rows; row += step) {
-    float x[N], g[N];
+  for (uint32_t r = 0; r < n_rows; ++r) {
+    F2 x[N], g[N];
+    fetch_stats();
     if constexpr (kVec) {
       in_x.fetch((stage + kStages - 1) % kStages);
       in_g.fetch((stage + kStages - 1) % kStages);
-      copy_async_commit();
-      copy_async_wait<kStages - 1>();
     }
-    float next_mean = 0.f, next_rstd = 0.f;
-    if (row + step < a.rows) { next_mean = a.mean[row + step]; next_rstd = a.rstd[row + step]; }
+    copy_async_commit();
+    copy_async_wait<kVec ? kStages - 1 : 3>();
+    __syncwarp();
+    const float2 st = stats[r % 4][threadIdx.x >> 5];
+    const float mean = st.x, rstd = st.y;
     in_x.take(stage, x);
     in_g.take(stage, g);
     if constexpr (!kVec) { in_x.fetch(0); in_g.fetch(0); }
-    float s0[2] = {0.f, 0.f}, s1[2] = {0.f, 0.f};
+    F2 s0 = f2(0.f), s1 = f2(0.f);
+    const F2 by = f2(rstd), less = f2(-mean);
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      float w[E];
-#pragma unroll
-      for (int h = 0; h < E / Q; ++h) {
-        const float* p = weights + ((k * (E / Q) + h) * kN + t) * Q;
-        if constexpr (kVec) Pack<float>::widen(*reinterpret_cast<const uint4*>(p), w + h * Q);
-        else w[h] = *p;
+    for (int i = 0; i < N; i += Q / 2) {
+      F2 w[Q / 2];
+      const float* p = weights + (i / (Q / 2) * kN + t) * Q;
+      if constexpr (kVec) {
+        Pack<float>::widen(*reinterpret_cast<const uint4*>(p), w);
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(p);
+        w[0] = f2(v.x, v.y);
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) {  // beyond the row dy and w are zero
-        const int i = k * E + e;
-        x[i] = (x[i] - mean) * rstd;
-        dw[i] += g[i] * x[i];
-        db[i] += g[i];
-        g[i] *= w[e];
-        s0[i & 1] += g[i];
-        s1[i & 1] += g[i] * x[i];
+      for (int j = 0; j < Q / 2; ++j) {  // beyond the row dy and w are zero
+        x[i + j] = (x[i + j] + less) * by;
+        dw[i + j] = fma(g[i + j], x[i + j], dw[i + j]);
+        db[i + j] = db[i + j] + g[i + j];
+        g[i + j] = g[i + j] * w[j];
+        s0 = s0 + g[i + j];
+        s1 = fma(g[i + j], x[i + j], s1);
       }
     }
     // both sums over the warp in five exchanges: the lower half of the lanes goes on with the first, the upper half with the second
-    const float a0 = s0[0] + s0[1], a1 = s1[0] + s1[1];
+    const float a0 = sum(s0), a1 = sum(s1);
     const bool upper = (threadIdx.x & 16) != 0;
     float s = (upper ? a1 : a0) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a0 : a1, 16);
 #pragma unroll
@@ -287,38 +315,40 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_norm_grad(NormGradArgs a) {
     c0 *= inv;
     c1 *= inv;
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = rstd * (g[i] - c0 - x[i] * c1);
+    for (int i = 0; i < N; ++i) x[i] = fma(x[i], f2(-c1), g[i] + f2(-c0)) * by;
     in_x.store(q, x);
-    q += step * a.lddx;
-    mean = next_mean;
-    rstd = next_rstd;
+    q += q_step;
     stage = (stage + 1) % kStages;
   }
   let_next_start();
   // the groups' sums, in group order
   if constexpr (kGroups > 1) {
-    float* sums = reinterpret_cast<float*>(rows);  // [kGroups - 1][2 N][kN]
+    uint64_t* sums = reinterpret_cast<uint64_t*>(rows);  // [kGroups - 1][2 N][kN] pairs
     copy_async_wait<0>();
     __syncthreads();
     if (group) {
-      float* mine = sums + (group - 1) * (2 * N * kN) + t;
+      uint64_t* mine = sums + (group - 1) * (2 * N * kN) + t;
 #pragma unroll
-      for (int i = 0; i < N; ++i) { mine[2 * i * kN] = dw[i]; mine[(2 * i + 1) * kN] = db[i]; }
+      for (int i = 0; i < N; ++i) { mine[2 * i * kN] = dw[i].v; mine[(2 * i + 1) * kN] = db[i].v; }
     }
     __syncthreads();
     if (group) return;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       for (int o = 0; o < kGroups - 1; ++o) {
-        dw[i] += sums[o * (2 * N * kN) + 2 * i * kN + t];
-        db[i] += sums[o * (2 * N * kN) + (2 * i + 1) * kN + t];
+        dw[i] = dw[i] + F2{sums[o * (2 * N * kN) + 2 * i * kN + t]};
+        db[i] = db[i] + F2{sums[o * (2 * N * kN) + (2 * i + 1) * kN + t]};
       }
   }
   float* line = a.partial + (uint64_t)blockIdx.x * 2 * a.cols;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint32_t c = (i / E * kN + t) * E + i % E;
-    if (c < a.cols) { line[c] = dw[i]; line[a.cols + c] = db[i]; }
+    const float2 w2 = parts(dw[i]), b2 = parts(db[i]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t c = ((2 * i + j) / E * kN + t) * E + (2 * i + j) % E;
+      if (c < a.cols) { line[c] = j ? w2.y : w2.x; line[a.cols + c] = j ? b2.y : b2.x; }
+    }
   }
 }
 
@@ -422,29 +452,25 @@ template <typename F, int... N>
 static void with_number(uint32_t n, std::integer_sequence<int, N...>, F&& f) {
   (void)((n == (uint32_t)N && (f(std::integral_constant<int, N>{}), true)) || ...);
 }
-static uint32_t pow2_at_least(uint32_t x) {
-  uint32_t p = 32;
-  while (p < x) p *= 2;
-  return p;
-}
 template <typename K>
 static cudaError_t allow_smem(K kernel, size_t smem) {
   return smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
 }
 
-// Chunks a thread: 32 elements (16 single ones, which come with an address each), so that a row's two sums over its threads
-// weigh little; one chunk (four) where there are few rows, which are a matter of latency: 32768 rows x 3584 take 90 us with
-// 32 elements a thread and 120 us with 16.
-template <typename T, bool kVec>
-static constexpr int kMany = kVec ? 32 / Pack<T>::kElems : 16;
-template <bool kVec>
-static constexpr int kFew = kVec ? 1 : 4;
+// Threads a row: multiples of 32, so that few of them have nothing (3584 bf16 elements are 224 threads x 2 chunks of 8).
+template <typename F>
+static void with_threads(uint32_t n, F&& f) {
+  with_number(n <= 256 ? (n + 31) / 32 * 32 : (n + 127) / 128 * 128, std::integer_sequence<int, 32, 64, 96, 128, 160, 192, 224, 256, 384, 512>{}, f);
+}
+
+template <typename T, bool kVec, int kElems>
+static constexpr int kChunks = kVec ? (kElems < Pack<T>::kElems ? 1 : kElems / Pack<T>::kElems) : kElems;
 
 template <typename T, bool kVec, int V>
 static cudaError_t norm_rows(const ft_pool* p, const NormArgs& a, cudaStream_t st) {
-  const uint32_t n = a.cols / (kVec ? Pack<T>::kElems : 1), threads = pow2_at_least((n + V - 1) / V);
-  cudaError_t e = cudaSuccess;
-  with_number(threads, std::integer_sequence<int, 32, 64, 128, 256, 512>{}, [&](auto k) {
+  const uint32_t n = a.cols / (kVec ? Pack<T>::kElems : 1);
+  cudaError_t e = cudaErrorInvalidConfiguration;
+  with_threads((n + V - 1) / V, [&](auto k) {
     constexpr int kN = decltype(k)::value;
     auto kernel = k_norm<T, V, kVec, kN>;
     constexpr size_t smem = kVec ? (size_t)kNormStages * V * kN * 16 : 0;
@@ -458,22 +484,25 @@ static cudaError_t norm_rows(const ft_pool* p, const NormArgs& a, cudaStream_t s
   return e;
 }
 
+// Elements a thread: 16 (90 us for 32768 rows x 3584 in bf16), 32 for rows beyond 256 x 16 (80 us for 14336 x 8192, 99 with
+// 16); few where there are few rows, which are a matter of latency.
 template <typename T, bool kVec>
 static cudaError_t norm_launch(const ft_pool* p, const NormArgs& a, cudaStream_t st) {
-  constexpr uint32_t E = kVec ? Pack<T>::kElems : 1, kMost = 512 * E;
-  if (a.cols > kMany<T, kVec> * kMost) {
+  constexpr uint32_t E = kVec ? Pack<T>::kElems : 1;
+  constexpr int kFew = kChunks<T, kVec, 4>, kMany = kChunks<T, kVec, 16>, kLong = kChunks<T, kVec, 32>;
+  const uint32_t n = a.cols / E;
+  if (n > kLong * 512u) {
     k_norm_wide<T><<<(unsigned)std::min<uint64_t>(a.rows, 4ull * p->sm_count), kWideThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
-  const uint64_t warps = a.rows * ((a.cols / E + 32 * kMany<T, kVec> - 1) / (32 * kMany<T, kVec>));
-  const bool few = warps < 8ull * p->sm_count && a.cols <= kFew<kVec> * kMost;
-  return few ? norm_rows<T, kVec, kFew<kVec>>(p, a, st) : norm_rows<T, kVec, kMany<T, kVec>>(p, a, st);
+  if (a.rows <= 2ull * p->sm_count && n <= kFew * 512u) return norm_rows<T, kVec, kFew>(p, a, st);
+  return n <= kMany * 256u ? norm_rows<T, kVec, kMany>(p, a, st) : norm_rows<T, kVec, kLong>(p, a, st);
 }
 
-template <typename T, bool kVec, int V, int kN, int kGroups>
+template <typename T, bool kVec, int V, int kN>
 static cudaError_t norm_grad_rows(ft_pool* p, const NormGradArgs& a, uint32_t* lines, cudaStream_t st) {
-  constexpr int E = kVec ? Pack<T>::kElems : 1;
-  constexpr size_t kRows = kVec ? 2ull * kGradStages<V> * V * kN * kGroups * 16 : 0, kSums = (kGroups - 1) * 2ull * V * E * kN * 4;
+  constexpr int E = kVec ? Pack<T>::kElems : 1, kGroups = kGradGroups(V * E, kN);
+  constexpr size_t kRows = kVec ? 2ull * kGradStages<V, kN * kGroups> * V * kN * kGroups * 16 : 0, kSums = (kGroups - 1) * 2ull * V * E * kN * 4;
   constexpr size_t smem = (size_t)V * E * kN * 4 + (kRows > kSums ? kRows : kSums);
   auto kernel = k_norm_grad<T, V, kVec, kN, kGroups>;
   const cudaError_t e = allow_smem(kernel, smem);
@@ -483,24 +512,31 @@ static cudaError_t norm_grad_rows(ft_pool* p, const NormGradArgs& a, uint32_t* l
   return cudaGetLastError();
 }
 
+// 16 elements a thread (121 us for 32768 rows x 3584 in bf16, 135 with 32), which 256 threads make 4096; 32 up to 8192.
 template <typename T, bool kVec>
 static cudaError_t norm_grad_launch(ft_pool* p, const NormGradArgs& a, float2* sums, uint32_t* lines, cudaStream_t st) {
   constexpr uint32_t E = kVec ? Pack<T>::kElems : 1;
-  constexpr int kV = kMany<T, kVec>;
+  constexpr int kFew = kChunks<T, kVec, 4>, kMany = kChunks<T, kVec, 16>, kLong = kChunks<T, true, 32>;
   const uint32_t n = a.cols / E;
-  if (n > kV * 256) {
+  if (n <= 32u * kFew) return norm_grad_rows<T, kVec, kFew, 32>(p, a, lines, st);
+  cudaError_t e = cudaErrorInvalidConfiguration;
+  if (n <= kMany * 256u) {
+    with_threads((n + kMany - 1) / kMany, [&](auto k) {
+      constexpr int kN = decltype(k)::value;
+      if constexpr (kN <= 256) e = norm_grad_rows<T, kVec, kMany, kN>(p, a, lines, st);
+    });
+  } else if (kVec && n <= kLong * 256u) {
+    with_threads((n + kLong - 1) / kLong, [&](auto k) {
+      constexpr int kN = decltype(k)::value;
+      if constexpr (kVec && kN > 128 && kN <= 256) e = norm_grad_rows<T, true, kLong, kN>(p, a, lines, st);
+    });
+  } else {
     k_norm_grad_sums<T><<<(unsigned)std::min<uint64_t>(a.rows, 4ull * p->sm_count), kWideThreads, 0, st>>>(a, sums);
     *lines = (uint32_t)std::min<uint64_t>(a.rows, kNormWideLines);
     k_norm_grad_cols<T><<<dim3((a.cols + 255u) / 256u, *lines), 256, 0, st>>>(a, sums);
     p->gpu_launches += 1;
-    return cudaGetLastError();
+    e = cudaGetLastError();
   }
-  if (n <= 32u * kFew<kVec>) return norm_grad_rows<T, kVec, kFew<kVec>, 32, kGradGroups(32)>(p, a, lines, st);
-  cudaError_t e = cudaSuccess;
-  with_number(pow2_at_least((n + kV - 1) / kV), std::integer_sequence<int, 32, 64, 128, 256>{}, [&](auto k) {
-    constexpr int kN = decltype(k)::value;
-    e = norm_grad_rows<T, kVec, kV, kN, kGradGroups(kN)>(p, a, lines, st);
-  });
   return e;
 }
 

@@ -7,6 +7,26 @@
 
 namespace ft {
 
+// Two fp32 values that one instruction takes through an operation, each rounded by itself.
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float both) { return f2(both, both); }
+__device__ __forceinline__ float2 parts(F2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ float sum(F2 a) { const float2 p = parts(a); return p.x + p.y; }
+
 // 16 bytes of a row in its stored type <-> fp32.  Widening bf16 is exact; narrowing rounds to nearest even.
 template <typename T>
 struct Pack;
@@ -18,6 +38,14 @@ struct Pack<float> {
   }
   static __device__ __forceinline__ uint4 narrow(const float* f) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+  static __device__ __forceinline__ void widen(const uint4 v, F2* f) {
+    f[0] = f2(__uint_as_float(v.x), __uint_as_float(v.y));
+    f[1] = f2(__uint_as_float(v.z), __uint_as_float(v.w));
+  }
+  static __device__ __forceinline__ uint4 narrow(const F2* f) {
+    const float2 a = parts(f[0]), b = parts(f[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
   }
 };
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
@@ -34,6 +62,15 @@ struct Pack<__nv_bfloat16> {
   }
   static __device__ __forceinline__ uint4 narrow(const float* f) {
     return make_uint4(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]), bf16x2(f[4], f[5]), bf16x2(f[6], f[7]));
+  }
+  static __device__ __forceinline__ void widen(const uint4 v, F2* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint4 narrow(const F2* f) {
+    const float2 a = parts(f[0]), b = parts(f[1]), c = parts(f[2]), d = parts(f[3]);
+    return make_uint4(bf16x2(a.x, a.y), bf16x2(b.x, b.y), bf16x2(c.x, c.y), bf16x2(d.x, d.y));
   }
 };
 __device__ __forceinline__ float widen1(float x) { return x; }
