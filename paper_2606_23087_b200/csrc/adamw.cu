@@ -5,8 +5,8 @@
 //   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Bound by HBM: every array is read and written once, 16 operations an element.  One launch serves up to kAdamwPerLaunch
-// tensors: their descriptors travel as kernel arguments (no upload, nothing for the caller to keep), a CTA finds its
-// tensor by a binary search over the tensors' first chunks, and a warp takes 256 elements at a time.
+// tensors of one kind: their descriptors travel as kernel arguments (no upload, nothing for the caller to keep), a CTA finds its
+// tensor by a binary search over the tensors' first chunks, and a warp takes blocks of 256 elements.
 //
 // 8-bit states.  A block of 256 elements of a tensor holds m and r = sqrt(v) as float8 (e4m3) values times one scale a
 // block and state.  Keeping r instead of v halves the range that the format has to cover: its 18 octaves are 36 octaves of
@@ -17,6 +17,8 @@
 // bytes the same on every launch shape.  A block that holds a value that is not finite reads back as NaN.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
+#include <type_traits>
 
 #include <cuda_fp8.h>
 
@@ -24,9 +26,8 @@
 
 namespace ft {
 
-constexpr uint32_t kAdamwBlock = 256;      // elements that share a scale; a warp's share of a round
+constexpr uint32_t kAdamwBlock = 256;      // elements that share a scale
 constexpr int kAdamwThreads = 256;
-constexpr uint32_t kAdamwChunk = 8 * 256;  // elements a CTA updates: one block a warp
 constexpr uint32_t kAdamwPerLaunch = 320;  // tensors a launch takes at most (kernel arguments hold 32 KiB)
 constexpr uint32_t kAdamwFew = 8;          // tensors of the launch with a small argument block
 
@@ -37,13 +38,12 @@ struct AdamwTensorArg {
   uint64_t n;
   uint64_t first_chunk;  // chunks of the tensors before this one
   float keep;            // 1 - lr * weight decay
-  uint16_t kind;         // see adamw_kind
-  uint16_t pad;
 };
 
-struct AdamwConst {
-  float b1, c1, b2, c2;   // c: 1 - b
-  float step, inv, eps;   // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+struct AdamwConst {         // pairs of equal values, as the kernel's operations take them
+  float2 b1, c1, b2, c2;    // c: 1 - b
+  float2 step, inv, eps;    // -lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  float2 minus_zero;        // see rounded_product
   const float* grad_scale;
 };
 
@@ -63,29 +63,35 @@ enum { kParamBf16 = 1, kGradBf16 = 2, kState8 = 4, kVec = 8 };
 template <bool kV>
 __device__ __forceinline__ uint32_t elem_of(uint32_t lane, int i) { return kV ? lane * 8 + i : lane + 32 * i; }
 
+// A lane's eight elements as they are stored; those beyond the tensor are zero.
 template <typename T, bool kV>
-__device__ __forceinline__ void load8(const T* p, uint32_t lane, uint32_t left, float (&f)[8]) {
-  if constexpr (kV) {
-    if (lane * 8 + 8 <= left) {
-      if constexpr (sizeof(T) == 4) {
-        Pack<float>::widen(*reinterpret_cast<const uint4*>(p + lane * 8), f);
-        Pack<float>::widen(*reinterpret_cast<const uint4*>(p + lane * 8 + 4), f + 4);
-      } else {
-        Pack<__nv_bfloat16>::widen(*reinterpret_cast<const uint4*>(p + lane * 8), f);
-      }
+struct Raw8 {
+  static constexpr int kQuads = sizeof(T) == 4 ? 2 : 1;
+  uint4 q[kQuads];
+  __device__ __forceinline__ void load(const T* p, uint32_t lane, uint32_t left) {
+    if (kV && lane * 8 + 8 <= left) {
+#pragma unroll
+      for (int i = 0; i < kQuads; ++i) q[i] = *reinterpret_cast<const uint4*>(p + lane * 8 + i * (8 / kQuads));
       return;
     }
-  }
+    T v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = elem_of<kV>(lane, i) < left ? widen1(p[elem_of<kV>(lane, i)]) : 0.f;
-}
+    for (int i = 0; i < 8; ++i) v[i] = elem_of<kV>(lane, i) < left ? p[elem_of<kV>(lane, i)] : narrow1<T>(0.f);
+    memcpy(q, v, sizeof(v));
+  }
+  // (every operation below is taken by pairs, each value rounded by itself)
+  __device__ __forceinline__ void widen(F2 (&f)[4]) const {
+#pragma unroll
+    for (int i = 0; i < kQuads; ++i) Pack<T>::widen(q[i], f + i * (4 / kQuads));
+  }
+};
 template <typename T, bool kV>
-__device__ __forceinline__ void store8(T* p, uint32_t lane, uint32_t left, const float (&f)[8]) {
+__device__ __forceinline__ void store8(T* p, uint32_t lane, uint32_t left, const F2 (&f)[4]) {
   if constexpr (kV) {
     if (lane * 8 + 8 <= left) {
       if constexpr (sizeof(T) == 4) {
         *reinterpret_cast<uint4*>(p + lane * 8) = Pack<float>::narrow(f);
-        *reinterpret_cast<uint4*>(p + lane * 8 + 4) = Pack<float>::narrow(f + 4);
+        *reinterpret_cast<uint4*>(p + lane * 8 + 4) = Pack<float>::narrow(f + 2);
       } else {
         *reinterpret_cast<uint4*>(p + lane * 8) = Pack<__nv_bfloat16>::narrow(f);
       }
@@ -93,44 +99,42 @@ __device__ __forceinline__ void store8(T* p, uint32_t lane, uint32_t left, const
     }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (elem_of<kV>(lane, i) < left) p[elem_of<kV>(lane, i)] = narrow1<T>(f[i]);
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = parts(f[i]);
+    if (elem_of<kV>(lane, 2 * i) < left) p[elem_of<kV>(lane, 2 * i)] = narrow1<T>(v.x);
+    if (elem_of<kV>(lane, 2 * i + 1) < left) p[elem_of<kV>(lane, 2 * i + 1)] = narrow1<T>(v.y);
+  }
 }
 
-__device__ __forceinline__ void widen_fp8x2(uint16_t q, float* f) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(q, __NV_E4M3);
-  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h));
-  f[0] = x.x;
-  f[1] = x.y;
-}
 template <bool kV>
-__device__ __forceinline__ void load_state8(const uint8_t* p, uint32_t lane, uint32_t left, float scale, float (&f)[8]) {
-  uint16_t q[4];
-  if (kV && lane * 8 + 8 <= left) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p + lane * 8);
-    q[0] = (uint16_t)v.x; q[1] = (uint16_t)(v.x >> 16); q[2] = (uint16_t)v.y; q[3] = (uint16_t)(v.y >> 16);
-  } else {
+struct RawState8 {
+  uint2 q;
+  float scale;
+  __device__ __forceinline__ void load(const uint8_t* p, const float* scale_of_block, uint32_t lane, uint32_t left) {
+    scale = *scale_of_block;
+    if (kV && lane * 8 + 8 <= left) {
+      q = *reinterpret_cast<const uint2*>(p + lane * 8);
+      return;
+    }
+    uint8_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = elem_of<kV>(lane, i) < left ? p[elem_of<kV>(lane, i)] : 0;
+    memcpy(&q, v, sizeof(v));
+  }
+  __device__ __forceinline__ void widen(F2 (&f)[4]) const {
+    const uint16_t pair[4] = {(uint16_t)q.x, (uint16_t)(q.x >> 16), (uint16_t)q.y, (uint16_t)(q.y >> 16)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t e0 = elem_of<kV>(lane, 2 * i), e1 = elem_of<kV>(lane, 2 * i + 1);
-      q[i] = (uint16_t)((e0 < left ? p[e0] : 0) | ((e1 < left ? p[e1] : 0) << 8));
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(pair[i], __NV_E4M3);
+      const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h));
+      f[i] = f2(x.x, x.y);
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) widen_fp8x2(q[i], f + 2 * i);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(f[i], scale);
-}
+};
 
-// the block's scale (lane 0 stores it) and its values rounded to float8
-template <bool kV, bool kFloor>
-__device__ __forceinline__ void store_state8(uint8_t* p, float* scale_out, uint32_t lane, uint32_t left, const float (&f)[8]) {
-  // fmaxf drops a NaN: not finite is looked for in the bits, whose order is that of the magnitudes
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (elem_of<kV>(lane, i) < left) top = max(top, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-  top = __reduce_max_sync(0xFFFFFFFFu, top);
+// the block's scale (lane 0 stores it) and its values rounded to float8; `top`: bits of its largest magnitude
+template <bool kV, bool kRoot>
+__device__ __forceinline__ void store_state8(uint8_t* p, float* scale_out, uint32_t lane, uint32_t left, uint32_t top, const F2 (&f)[4]) {
   float scale = 0.f, inv = 0.f;
   if (top >= 0x7F800000u) {
     scale = __uint_as_float(0x7FC00000u);
@@ -142,120 +146,222 @@ __device__ __forceinline__ void store_state8(uint8_t* p, float* scale_out, uint3
     inv = __uint_as_float((uint32_t)(127 - x) << 23);
   }
   if (lane == 0) *scale_out = scale;
-  uint16_t q[4];
+  uint32_t q[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float a = f[2 * i] * inv, b = f[2 * i + 1] * inv;
-    if (kFloor) {
-      a = a > 0.f ? fmaxf(a, 0.001953125f) : a;
-      b = b > 0.f ? fmaxf(b, 0.001953125f) : b;
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(parts(f[2 * i] * f2(inv)), __NV_SATFINITE, __NV_E4M3);
+    q[i] = lo | (uint32_t)__nv_cvt_float2_to_fp8x2(parts(f[2 * i + 1] * f2(inv)), __NV_SATFINITE, __NV_E4M3) << 16;
+    if (kRoot && ((q[i] - 0x01010101u) & ~q[i] & 0x80808080u)) {  // some byte is zero: a positive root takes the smallest value, 1
+      const float2 a = parts(f[2 * i]), b = parts(f[2 * i + 1]);
+      const float r[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (r[j] > 0.f && !(q[i] >> 8 * j & 0xFF)) q[i] |= 1u << 8 * j;
     }
-    q[i] = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
   }
   if (kV && lane * 8 + 8 <= left) {
-    *reinterpret_cast<uint2*>(p + lane * 8) = make_uint2(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16);
+    *reinterpret_cast<uint2*>(p + lane * 8) = make_uint2(q[0], q[1]);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t e0 = elem_of<kV>(lane, 2 * i), e1 = elem_of<kV>(lane, 2 * i + 1);
-    if (e0 < left) p[e0] = (uint8_t)q[i];
-    if (e1 < left) p[e1] = (uint8_t)(q[i] >> 8);
-  }
+  for (int i = 0; i < 8; ++i)
+    if (elem_of<kV>(lane, i) < left) p[elem_of<kV>(lane, i)] = (uint8_t)(q[i / 4] >> 8 * (i % 4));
 }
 
+// a b rounded by itself: the assembler makes one operation of a product of pairs and the sum that follows, .rn or not, but
+// not of a multiply-add with an addend that it does not know (-0, which changes nothing)
+__device__ __forceinline__ F2 f2(float2 v) { return f2(v.x, v.y); }
+__device__ __forceinline__ F2 rounded_product(F2 a, F2 b, const AdamwConst& k) { return fma(a, b, f2(k.minus_zero)); }
+
+__device__ __forceinline__ float reciprocal(float x) {  // 1 ulp; x is zero or normal
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float inverse_root(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Square roots of pairs by one step of Heron's method from an approximate inverse root, the residual taken exactly by a
+// multiply-add: r = s + (v - s s) / (2 s), off by less than 2^-43 of r before its one rounding (eight of __fsqrt_rn a lane were a
+// third of the kernel's instructions).  v lies in [2^-100, 2^126] or is zero.
+__device__ __forceinline__ F2 root(F2 v) {
+  const float2 a = parts(v);
+  const F2 y = f2(inverse_root(fmaxf(a.x, 0x1p-126f)), inverse_root(fmaxf(a.y, 0x1p-126f)));
+  const F2 s = v * y;
+  return fma(fma(s * f2(-1.f), s, v), y * f2(0.5f), s);
+}
+
+// what a block is made from
 template <typename P, typename G, bool k8, bool kV>
-__device__ __forceinline__ void adamw_block(const AdamwTensorArg& t, const AdamwConst& k, uint64_t e0, uint32_t lane) {
+struct AdamwLoads {
+  Raw8<G, kV> g;
+  Raw8<P, kV> w;
+  std::conditional_t<k8, RawState8<kV>, Raw8<float, kV>> m, v;
+  __device__ __forceinline__ void load(const AdamwTensorArg& t, uint64_t e0, uint32_t lane) {
+    const uint32_t left = (uint32_t)min((uint64_t)kAdamwBlock, t.n - e0);
+    g.load(static_cast<const G*>(t.grad) + e0, lane, left);
+    w.load(static_cast<const P*>(t.param) + e0, lane, left);
+    if constexpr (k8) {
+      m.load(static_cast<const uint8_t*>(t.m) + e0, t.m_scale + e0 / kAdamwBlock, lane, left);
+      v.load(static_cast<const uint8_t*>(t.v) + e0, t.v_scale + e0 / kAdamwBlock, lane, left);
+    } else {
+      m.load(static_cast<const float*>(t.m) + e0, lane, left);
+      v.load(static_cast<const float*>(t.v) + e0, lane, left);
+    }
+  }
+};
+
+template <typename P, typename G, bool k8, bool kV>
+__device__ __forceinline__ void adamw_block(const AdamwLoads<P, G, k8, kV>& in, const AdamwTensorArg& t, const AdamwConst& k, uint64_t e0, uint32_t lane) {
   const uint32_t left = (uint32_t)min((uint64_t)kAdamwBlock, t.n - e0);
-  float g[8], m[8], r[8], w[8];
-  load8<G, kV>(static_cast<const G*>(t.grad) + e0, lane, left, g);
-  load8<P, kV>(static_cast<const P*>(t.param) + e0, lane, left, w);
+  F2 g[4], m[4], v[4], r[4], w[4];
+  in.g.widen(g);
+  in.w.widen(w);
+  in.m.widen(m);
+  F2 b1 = f2(k.b1);
   if constexpr (k8) {
-    load_state8<kV>(static_cast<const uint8_t*>(t.m) + e0, lane, left, t.m_scale[e0 / kAdamwBlock], m);
-    load_state8<kV>(static_cast<const uint8_t*>(t.v) + e0, lane, left, t.v_scale[e0 / kAdamwBlock], r);
+    b1 = b1 * f2(in.m.scale);  // the scale is a power of two: b1 (scale q) and (b1 scale) q round alike
+    in.v.widen(r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = __fmul_rn(r[i], r[i]);
+    for (int i = 0; i < 4; ++i) { r[i] = r[i] * f2(in.v.scale); v[i] = r[i] * r[i]; }
   } else {
-    load8<float, kV>(static_cast<const float*>(t.m) + e0, lane, left, m);
-    load8<float, kV>(static_cast<const float*>(t.v) + e0, lane, left, r);
+    in.v.widen(v);
   }
   const float s = k.grad_scale ? *k.grad_scale : 1.f;
-  float v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = __fmul_rn(g[i], s);
-    m[i] = __fadd_rn(__fmul_rn(k.b1, m[i]), __fmul_rn(k.c1, x));
-    v[i] = __fadd_rn(__fmul_rn(k.b2, r[i]), __fmul_rn(k.c2, __fmul_rn(x, x)));
-    r[i] = __fsqrt_rn(v[i]);
-    w[i] = w[i] * t.keep - k.step * __fdividef(m[i], fmaf(r[i], k.inv, k.eps));
+  for (int i = 0; i < 4; ++i) {
+    const F2 x = g[i] * f2(s);
+    m[i] = rounded_product(b1, m[i], k) + rounded_product(f2(k.c1), x, k);
+    v[i] = rounded_product(f2(k.b2), v[i], k) + rounded_product(f2(k.c2), x * x, k);
+  }
+  uint32_t most = 0;  // bits of the largest v of the warp; a NaN's are above all
+  if constexpr (k8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = parts(v[i]);
+      most = max(most, max(__float_as_uint(a.x), __float_as_uint(a.y)));
+    }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    // small v are brought up by an even power of two, so that root() sees no subnormal number; beside a large one they
+    // matter neither to the block's float8 values nor, below eps, to the step
+    const bool small = most < __float_as_uint(0x1p40f);
+    const float up = small ? 0x1p64f : 1.f, down = small ? 0x1p-32f : 1.f;
+    if (most < 0x7F800000u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = root(v[i] * f2(up)) * f2(down);
+    }
+  }
+  if (!k8 || most >= 0x7F800000u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = parts(v[i]);
+      r[i] = f2(sqrtf(a.x), sqrtf(a.y));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 d = parts(fma(r[i], f2(k.inv), f2(k.eps)));
+    w[i] = fma(m[i] * f2(reciprocal(d.x), reciprocal(d.y)), f2(k.step), w[i] * f2(t.keep));
   }
   store8<P, kV>(static_cast<P*>(t.param) + e0, lane, left, w);
   if (t.copy) store8<__nv_bfloat16, kV>(static_cast<__nv_bfloat16*>(t.copy) + e0, lane, left, w);
   if constexpr (k8) {
-    store_state8<kV, false>(static_cast<uint8_t*>(t.m) + e0, t.m_scale + e0 / kAdamwBlock, lane, left, m);
-    store_state8<kV, true>(static_cast<uint8_t*>(t.v) + e0, t.v_scale + e0 / kAdamwBlock, lane, left, r);
+    uint32_t top = 0;  // bits of the largest |m|, whose order is that of the magnitudes and which keep a NaN in sight
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = parts(m[i]);
+      top = max(top, max(__float_as_uint(a.x) & 0x7FFFFFFFu, __float_as_uint(a.y) & 0x7FFFFFFFu));
+    }
+    store_state8<kV, false>(static_cast<uint8_t*>(t.m) + e0, t.m_scale + e0 / kAdamwBlock, lane, left, __reduce_max_sync(0xFFFFFFFFu, top), m);
+    // the largest root is the largest v's
+    store_state8<kV, true>(static_cast<uint8_t*>(t.v) + e0, t.v_scale + e0 / kAdamwBlock, lane, left, __float_as_uint(__fsqrt_rn(__uint_as_float(most))), r);
   } else {
     store8<float, kV>(static_cast<float*>(t.m) + e0, lane, left, m);
     store8<float, kV>(static_cast<float*>(t.v) + e0, lane, left, v);
   }
 }
 
-template <uint32_t kCap>
-__global__ void __launch_bounds__(kAdamwThreads) k_adamw(const __grid_constant__ AdamwArgs<kCap> a) {
+// Blocks of a warp whose loads go out together.  8-bit states bring little in a block: with one block a warp, 32 warps an SM
+// keep some 25 KiB on their way, which held the kernel at 3.7 TB/s.
+template <bool k8>
+constexpr uint32_t kAdamwAtOnce = k8 ? 2 : 1;
+template <bool k8>
+constexpr uint32_t kAdamwChunk = kAdamwAtOnce<k8> * (kAdamwThreads / 32) * kAdamwBlock;  // elements of a CTA
+
+template <typename P, typename G, bool k8, bool kV, uint32_t kCap>
+__device__ __forceinline__ void adamw_cta(const AdamwArgs<kCap>& a) {
   uint32_t lo = 0, hi = a.n;  // the last tensor whose first chunk is not behind this one
   while (hi - lo > 1) {
     const uint32_t mid = (lo + hi) >> 1;
     if (a.t[mid].first_chunk <= blockIdx.x) lo = mid; else hi = mid;
   }
   const AdamwTensorArg& t = a.t[lo];
-  const uint64_t e0 = (blockIdx.x - t.first_chunk) * kAdamwChunk + (threadIdx.x >> 5) * kAdamwBlock;
-  if (e0 >= t.n) return;
+  const uint64_t e0 = (blockIdx.x - t.first_chunk) * kAdamwChunk<k8> + (threadIdx.x >> 5) * kAdamwBlock;
   const uint32_t lane = threadIdx.x & 31;
-  using B = __nv_bfloat16;
-  switch (t.kind) {
-    case 0: adamw_block<float, float, false, false>(t, a.k, e0, lane); break;
-    case 1: adamw_block<B, float, false, false>(t, a.k, e0, lane); break;
-    case 2: adamw_block<float, B, false, false>(t, a.k, e0, lane); break;
-    case 3: adamw_block<B, B, false, false>(t, a.k, e0, lane); break;
-    case 4: adamw_block<float, float, true, false>(t, a.k, e0, lane); break;
-    case 5: adamw_block<B, float, true, false>(t, a.k, e0, lane); break;
-    case 6: adamw_block<float, B, true, false>(t, a.k, e0, lane); break;
-    case 7: adamw_block<B, B, true, false>(t, a.k, e0, lane); break;
-    case 8: adamw_block<float, float, false, true>(t, a.k, e0, lane); break;
-    case 9: adamw_block<B, float, false, true>(t, a.k, e0, lane); break;
-    case 10: adamw_block<float, B, false, true>(t, a.k, e0, lane); break;
-    case 11: adamw_block<B, B, false, true>(t, a.k, e0, lane); break;
-    case 12: adamw_block<float, float, true, true>(t, a.k, e0, lane); break;
-    case 13: adamw_block<B, float, true, true>(t, a.k, e0, lane); break;
-    case 14: adamw_block<float, B, true, true>(t, a.k, e0, lane); break;
-    default: adamw_block<B, B, true, true>(t, a.k, e0, lane); break;
-  }
+  constexpr uint32_t kAtOnce = kAdamwAtOnce<k8>, kNext = kAdamwThreads / 32 * kAdamwBlock;
+  AdamwLoads<P, G, k8, kV> in[kAtOnce];
+#pragma unroll
+  for (uint32_t i = 0; i < kAtOnce; ++i)
+    if (e0 + i * kNext < t.n) in[i].load(t, e0 + i * kNext, lane);
+#pragma unroll
+  for (uint32_t i = 0; i < kAtOnce; ++i)
+    if (e0 + i * kNext < t.n) adamw_block(in[i], t, a.k, e0 + i * kNext, lane);
 }
 
-static uint16_t adamw_kind(const ft_adamw_tensor& t) {
+template <typename P, typename G, bool k8, bool kV, uint32_t kCap>
+__global__ void __launch_bounds__(kAdamwThreads, 4) k_adamw(const __grid_constant__ AdamwArgs<kCap> a) {
+  adamw_cta<P, G, k8, kV>(a);
+}
+
+static uint32_t adamw_kind(const ft_adamw_tensor& t) {
   const bool s8 = t.state_bits == 8;
   const bool vec = aligned_to(t.param, 16) && aligned_to(t.grad, 16) && aligned_to(t.copy, 16) && aligned_to(t.m, s8 ? 8 : 16) &&
                    aligned_to(t.v, s8 ? 8 : 16);
-  return (uint16_t)((t.param_dtype == FT_BF16 ? kParamBf16 : 0) | (t.grad_dtype == FT_BF16 ? kGradBf16 : 0) | (s8 ? kState8 : 0) | (vec ? kVec : 0));
+  return (t.param_dtype == FT_BF16 ? kParamBf16 : 0) | (t.grad_dtype == FT_BF16 ? kGradBf16 : 0) | (s8 ? kState8 : 0) | (vec ? kVec : 0);
 }
 
-template <uint32_t kCap>
-static cudaError_t adamw_launch(const AdamwConst& k, double lr, const ft_adamw_tensor* t, uint32_t n, uint64_t chunks, cudaStream_t st) {
+template <typename P, typename G, bool k8, bool kV, uint32_t kCap>
+static cudaError_t adamw_launch(const AdamwConst& k, double lr, const ft_adamw_tensor* t, uint32_t n, uint32_t kind, uint64_t chunks, cudaStream_t st) {
   AdamwArgs<kCap> a;
   a.k = k;
   a.n = 0;
   uint64_t at = 0;
   for (uint32_t i = 0; i < n; ++i) {
-    if (t[i].n == 0) continue;
+    if (t[i].n == 0 || adamw_kind(t[i]) != kind) continue;
     AdamwTensorArg& d = a.t[a.n++];
     d.param = t[i].param; d.m = t[i].m; d.v = t[i].v; d.copy = t[i].copy; d.grad = t[i].grad;
     d.m_scale = t[i].m_scale; d.v_scale = t[i].v_scale; d.n = t[i].n; d.first_chunk = at;
     d.keep = (float)(1.0 - lr * t[i].weight_decay);
-    d.kind = adamw_kind(t[i]); d.pad = 0;
-    at += (t[i].n + kAdamwChunk - 1) / kAdamwChunk;
+    at += (t[i].n + kAdamwChunk<k8> - 1) / kAdamwChunk<k8>;
   }
-  k_adamw<kCap><<<(unsigned)chunks, kAdamwThreads, 0, st>>>(a);
+  k_adamw<P, G, k8, kV, kCap><<<(unsigned)chunks, kAdamwThreads, 0, st>>>(a);
   return cudaGetLastError();
+}
+
+// The tensors of one kind: as many a launch as its arguments hold and its grid can index.  (One kernel for all kinds, with a
+// branch in it, has the registers of its most demanding kind.)
+template <typename P, typename G, bool k8, bool kV>
+static int32_t adamw_tensors(ft_pool* p, const AdamwConst& k, double lr, const ft_adamw_tensor* t, uint32_t n, uint32_t kind, cudaStream_t st) {
+  for (uint32_t i0 = 0; i0 < n;) {
+    uint32_t i1 = i0, used = 0;
+    uint64_t chunks = 0;
+    while (i1 < n && used < kAdamwPerLaunch) {
+      const uint64_t c = adamw_kind(t[i1]) == kind ? (t[i1].n + kAdamwChunk<k8> - 1) / kAdamwChunk<k8> : 0;
+      if (chunks + c > 0x7FFFFFFFull) break;
+      chunks += c;
+      used += c != 0;
+      ++i1;
+    }
+    if (chunks) {
+      FT_CUDA(used <= kAdamwFew ? (adamw_launch<P, G, k8, kV, kAdamwFew>(k, lr, t + i0, i1 - i0, kind, chunks, st))
+                                : (adamw_launch<P, G, k8, kV, kAdamwPerLaunch>(k, lr, t + i0, i1 - i0, kind, chunks, st)));
+      p->gpu_launches += 1;
+    }
+    i0 = i1;
+  }
+  return FT_OK;
 }
 
 }  // namespace ft
@@ -281,31 +387,30 @@ FT_EXPORT int32_t pool_adamw_step(ft_pool* p, const ft_adamw_tensor* tensors, ui
     if (t.state_bits == 8 && (!t.m_scale || !t.v_scale || !aligned_to(t.m_scale, 4) || !aligned_to(t.v_scale, 4))) return FT_ERR_INVALID_ARG;
     if (t.n > (1ull << 40)) return FT_ERR_CAPACITY;
   }
+  const auto both = [](double x) { return make_float2((float)x, (float)x); };
   AdamwConst k;
-  k.b1 = (float)cfg->beta1; k.c1 = (float)(1.0 - cfg->beta1);
-  k.b2 = (float)cfg->beta2; k.c2 = (float)(1.0 - cfg->beta2);
-  k.step = (float)(cfg->lr / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
-  k.inv = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)cfg->step)));
-  k.eps = (float)cfg->eps;
+  k.b1 = both(cfg->beta1); k.c1 = both(1.0 - cfg->beta1);
+  k.b2 = both(cfg->beta2); k.c2 = both(1.0 - cfg->beta2);
+  k.step = both(-cfg->lr / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
+  k.inv = both(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)cfg->step)));
+  k.eps = both(cfg->eps);
+  k.minus_zero = both(-0.0);
   k.grad_scale = cfg->grad_scale;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // as many tensors a launch as its arguments hold and its grid can index
-  for (uint32_t i0 = 0; i0 < n_tensors;) {
-    uint32_t i1 = i0, used = 0;
-    uint64_t chunks = 0;
-    while (i1 < n_tensors && used < kAdamwPerLaunch) {
-      const uint64_t c = (tensors[i1].n + kAdamwChunk - 1) / kAdamwChunk;
-      if (chunks + c > 0x7FFFFFFFull) break;
-      chunks += c;
-      used += c != 0;
-      ++i1;
+  uint32_t kinds = 0;  // a bit a kind that the list has
+  for (uint32_t i = 0; i < n_tensors; ++i)
+    if (tensors[i].n) kinds |= 1u << adamw_kind(tensors[i]);
+  using B = __nv_bfloat16;
+  using Run = int32_t (*)(ft_pool*, const AdamwConst&, double, const ft_adamw_tensor*, uint32_t, uint32_t, cudaStream_t);
+  static const Run run[16] = {  // by kind
+      adamw_tensors<float, float, false, false>, adamw_tensors<B, float, false, false>, adamw_tensors<float, B, false, false>, adamw_tensors<B, B, false, false>,
+      adamw_tensors<float, float, true, false>,  adamw_tensors<B, float, true, false>,  adamw_tensors<float, B, true, false>,  adamw_tensors<B, B, true, false>,
+      adamw_tensors<float, float, false, true>,  adamw_tensors<B, float, false, true>,  adamw_tensors<float, B, false, true>,  adamw_tensors<B, B, false, true>,
+      adamw_tensors<float, float, true, true>,   adamw_tensors<B, float, true, true>,   adamw_tensors<float, B, true, true>,   adamw_tensors<B, B, true, true>};
+  for (uint32_t kind = 0; kind < 16; ++kind)
+    if (kinds >> kind & 1) {
+      const int32_t rc = run[kind](p, k, cfg->lr, tensors, n_tensors, kind, st);
+      if (rc != FT_OK) return rc;
     }
-    if (chunks) {
-      FT_CUDA(used <= kAdamwFew ? adamw_launch<kAdamwFew>(k, cfg->lr, tensors + i0, i1 - i0, chunks, st)
-                                : adamw_launch<kAdamwPerLaunch>(k, cfg->lr, tensors + i0, i1 - i0, chunks, st));
-      p->gpu_launches += 1;
-    }
-    i0 = i1;
-  }
   return FT_OK;
 }
