@@ -249,11 +249,15 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
         for (uint32_t j = 0; j < kStatCols; ++j)
           if (j >= cols) z[j / 32][j % 32] = kMinusInf;
       }
-      float top = -INFINITY, sum = 0.f;
-      const auto take_exp = [&](uint32_t c) {
-        const float x = __uint_as_float(z[c / 32][c % 32]), e = exp2_fast((x - ref) * kLog2e);
-        top = fmaxf(top, x);
-        sum += e;
+      float top = -INFINITY;
+      F2 sums = f2(0.f);
+      const F2 minus_ref = f2(-ref), scale = f2(kLog2e);
+      const auto take_exp = [&](uint32_t c) {  // of two columns
+        const float x0 = __uint_as_float(z[c / 32][c % 32]), x1 = __uint_as_float(z[c / 32][c % 32 + 1]);
+        const float2 t = parts((f2(x0, x1) + minus_ref) * scale);
+        const F2 e = f2(exp2_fast(t.x), exp2_fast(t.y));
+        top = fmaxf(top, fmaxf(x0, x1));
+        sums = sums + e;
         return e;
       };
       if constexpr (kKeep) {
@@ -261,18 +265,18 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
         for (uint32_t c = 0; c < kStatCols; c += 64) {
           if (c >= cols) break;
           MmaOut().put<false>(&map_e, (int32_t)(c0 + c), (int32_t)(t.m + row), [&](uint32_t j) {
-            float e[8];
+            F2 e[4];
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) e[k] = take_exp(c + 8 * j + k);
+            for (uint32_t k = 0; k < 4; ++k) e[k] = take_exp(c + 8 * j + 2 * k);
             const uint4 w = Pack<__nv_bfloat16>::narrow(e);
             return make_uint4(w.x & keep, w.y & keep, w.z & keep, w.w & keep);
           });
         }
       } else {
 #pragma unroll
-        for (uint32_t c = 0; c < kStatCols; ++c) take_exp(c);
+        for (uint32_t c = 0; c < kStatCols; c += 2) take_exp(c);
       }
-      if (m < n) a.stat[(uint64_t)(c0 / kStatCols) * a.rows + m] = make_float2(top, sum);
+      if (m < n) a.stat[(uint64_t)(c0 / kStatCols) * a.rows + m] = make_float2(top, sum(sums));
     });
   give_up(v, a.call_seq, lost);
 }

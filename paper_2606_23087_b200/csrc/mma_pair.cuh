@@ -9,7 +9,7 @@
 //   kHigh = 1  256 rows: the accumulators alternate, the epilogue of one runs beside the products into the other
 //   kHigh = 2  512 rows: both accumulators belong to one tile and share its B, which takes 48 KiB from L2 where two lower
 //              tiles take 64.  A long product runs at the card's power limit, and bytes moved from L2 are what is left to
-//              save there; the epilogue stands alone, so this is for long K
+//              save there; the epilogues of its halves run beside kMmaLead stages of products of the other half
 //
 // Operands need not be stored with K innermost: `kMn` operands have the tile's own dimension innermost (a row of the matrix
 // in memory per K index), as P and x in dW = P^T x; TMA brings 64 x 64 boxes either way and the descriptor says which.
@@ -31,6 +31,9 @@ constexpr uint32_t kMmaTile = 256;    // rows of an accumulator over the pair, c
 constexpr uint32_t kMmaK = 64;        // K a stage: 128 bytes of bf16
 constexpr uint32_t kMmaBox = 64 * kMmaK * 2;         // one TMA box, 8 KiB
 constexpr uint32_t kMmaOperand = 2 * kMmaBox;        // a CTA's half of 256 rows of an operand, a stage
+// Stages by which a high tile's rows 0..255 run ahead of the others at its beginning and its end: the epilogue of one half then
+// runs beside products of the other on both sides.  2460 rows x 32768 x 1024: 128 us, 135 without it; 4, the whole ring, is no better.
+constexpr uint32_t kMmaLead = 3;
 template <int kHigh>
 constexpr int kMmaStages = kHigh == 1 ? 6 : 4;
 constexpr int kMmaThreads = 384;
@@ -70,8 +73,10 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* b, uint32_t parity, 
     if ((++spins & 1023u) == 0 && global_timer_ns() - t0 > limit_ns) return false;
   return true;
 }
+// Relaxed: what it stands for is a read of tensor memory that tcgen05.wait::ld has seen complete and tcgen05.fence orders.  With
+// release it also waits for the stores that the thread has under way, 1300 cycles a time.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // one 64 x 64 box to this CTA, its bytes counted on the even CTA's barrier
 __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
@@ -237,27 +242,46 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
         const uint32_t acc0 = kHigh == 1 ? turn : 0;
         turn ^= 1;
         take(acc0);
-        for (uint32_t k = t.k0; k < t.k1 && !lost; ++k, ++it) {
-          const uint32_t s = it % kStages;
-          if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
+        const auto arrived = [&](uint32_t i) {  // the stage's operands are in both CTAs
+          if (!mbar_wait_bounded(&bar->full[i % kStages], (i / kStages) & 1, limit_ns)) lost = true;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t sb = base + s * kStageBytes;
+          return !lost;
+        };
+        const auto products = [&](uint32_t h, uint32_t i, bool add) {
+          const uint32_t sb = base + i % kStages * kStageBytes, sa = sb + (1 + h) * kMmaOperand;
 #pragma unroll
-          for (uint32_t h = 0; h < kHigh; ++h) {
-            if (h == 1) {
-              if (t.high < 2) break;
-              if (k == t.k0) take(1);
-              if (lost) break;
-            }
-            const uint32_t sa = sb + (1 + h) * kMmaOperand;
-#pragma unroll
-            for (uint32_t j = 0; j < kMmaK / 16; ++j)
-              mma_issue(tmem + (acc0 + h) * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>),
-                        kMmaInstr<kAMn, kBMn>, k > t.k0 || j > 0);
-            if (k + 1 == t.k1) mma_commit(&bar->acc_full[acc0 + h]);
+          for (uint32_t j = 0; j < kMmaK / 16; ++j)
+            mma_issue(tmem + (acc0 + h) * 256, mma_desc<kAMn>(sa + j * kMmaStep<kAMn>), mma_desc<kBMn>(sb + j * kMmaStep<kBMn>),
+                      kMmaInstr<kAMn, kBMn>, add || j > 0);
+        };
+        const uint32_t ks = t.k1 - t.k0;
+        uint32_t k = 0;  // K blocks whose products have been issued
+        const auto ahead = [&](uint32_t blocks) {
+          for (uint32_t g = 0; g < blocks && arrived(it + g); ++g) products(0, it + g, k + g > 0);
+          if (lost) return;
+          if (k + blocks == ks) mma_commit(&bar->acc_full[0]);
+          if (k == 0) take(1);
+          if (lost) return;
+          for (uint32_t g = 0; g < blocks; ++g) {
+            products(1, it + g, k + g > 0);
+            mma_commit(&bar->empty[(it + g) % kStages]);
           }
-          mma_commit(&bar->empty[s]);
+          if (k + blocks == ks) mma_commit(&bar->acc_full[1]);
+          it += blocks;
+          k += blocks;
+        };
+        const bool two = kHigh == 2 && t.high == 2;
+        if (two) ahead(min(kMmaLead, ks));
+        const uint32_t last = two ? min(kMmaLead, ks - k) : 0;
+        for (; k + last < ks && !lost; ++k, ++it) {
+          if (!arrived(it)) break;
+          products(0, it, k > 0);
+          if (two) products(1, it, true);
+          mma_commit(&bar->empty[it % kStages]);
         }
+        if (lost) break;
+        if (!two) mma_commit(&bar->acc_full[acc0]);
+        else if (last) ahead(last);
       }
       if (lost) {  // products under way still read shared memory and write tensor memory
         mma_commit(&bar->drain);
