@@ -281,39 +281,39 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
   give_up(v, a.call_seq, lost);
 }
 
-// The work of a product in tiles of kHigh x 256 rows.  Tile `t` of `all` = m_tiles x n_tiles (columns first) x slices of K;
+// The work of a product in tiles of 512 rows.  Tile `t` of `all` = m_tiles x n_tiles (columns first) x slices of K;
 // where the last round has 512-row tiles for at most half the pairs, those are dealt out as two 256-row halves.
-template <int kHigh>
 struct HighTiles {
   uint32_t blocks, n_tiles, tiles, all, split;  // blocks: of 256 rows; tiles: of one slice; split: whole tiles in front of the halves
   __device__ __forceinline__ HighTiles(uint32_t rows, uint32_t cols, uint32_t slices, uint32_t pairs) {
     blocks = (rows + kMmaTile - 1) / kMmaTile;
     n_tiles = (cols + kMmaTile - 1) / kMmaTile;
-    tiles = (blocks + kHigh - 1) / kHigh * n_tiles;
+    tiles = (blocks + 1) / 2 * n_tiles;
     all = split = tiles * slices;
     const uint32_t rest = all % pairs;
-    if (kHigh == 2 && blocks > 1 && rest * 2 <= pairs) split -= rest;
+    if (blocks > 1 && rest * 2 <= pairs) split -= rest;
   }
   __device__ __forceinline__ uint32_t items() const { return split + 2 * (all - split); }
   // rounds of all pairs, in tiles of 256 rows
   __device__ __forceinline__ uint32_t rounds(uint32_t pairs) const {
-    return min((uint32_t)kHigh, blocks) * ((split + pairs - 1) / pairs) + (split < all ? 1 : 0);
+    return min(2u, blocks) * ((split + pairs - 1) / pairs) + (split < all ? 1 : 0);
   }
   __device__ __forceinline__ uint32_t tile_of(uint32_t i) const { return i < split ? i : split + (i - split) / 2; }
   __device__ __forceinline__ MmaTile at(uint32_t i, uint32_t k_each, uint32_t k_blocks) const {
     const uint32_t tile = tile_of(i), slice = tile / tiles, t = tile - slice * tiles, half = i < split ? 0 : (i - split) & 1;
-    const uint32_t block = t / n_tiles * kHigh + half, left = blocks > block ? blocks - block : 0;
+    const uint32_t block = t / n_tiles * 2 + half, left = blocks > block ? blocks - block : 0;
     return MmaTile{block * kMmaTile, t % n_tiles * kMmaTile, min(slice * k_each, k_blocks), min((slice + 1) * k_each, k_blocks),
-                   min(i < split ? (uint32_t)kHigh : 1u, left)};
+                   min(i < split ? 2u : 1u, left)};
   }
 };
 
 // Slices of K = vocab for dx's tiles: they rarely divide among the pairs, and few rows have few tiles at all.  Taken is the
 // number of slices with the least rounds of tiles times blocks of K a tile, plus what a tile costs beside its products and
-// what the slices cost in traffic (in blocks of K of 256 rows, some 0.35 us); every
+// what the slices cost in traffic (in blocks of K of 256 rows, some 0.35 us).  Not sensitive: kTileCost from 1 to 10 is within
+// 1 % at 200 to 5000 rows.
 __device__ __forceinline__ uint32_t dx_slices(const LossPiece& a, uint32_t n) {  // a whole warp: a lane a number of slices
   const uint32_t k_blocks = (a.vocab + kMmaK - 1) / kMmaK, s = (threadIdx.x & 31) + 1;
-  const HighTiles<2> h(n, a.hidden, s, a.pairs);
+  const HighTiles h(n, a.hidden, s, a.pairs);
   uint32_t cost = h.rounds(a.pairs) * ((k_blocks + s - 1) / s + kTileCost) + (s > 1 ? s * h.blocks * h.n_tiles / 4 : 0);
   if (s > k_blocks || (s > 1 && h.all > a.slots)) cost = 0x7FFFFFFu;
   const uint32_t best = __reduce_min_sync(0xFFFFFFFFu, cost);
@@ -455,7 +455,7 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   after_previous();
   const uint32_t n = *a.count, k_blocks = (a.vocab + kMmaK - 1) / kMmaK;
   const uint32_t slices = n ? a.count[1] : 1, each = (k_blocks + slices - 1) / slices;
-  const HighTiles<2> work(n, a.hidden, slices, a.pairs);
+  const HighTiles work(n, a.hidden, slices, a.pairs);
   const bool wide = ((reinterpret_cast<uintptr_t>(a.dx) | a.lddx * 2) & 31) == 0;
   bool lost;
   mma_pair_tiles<false, true, 2>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
@@ -486,36 +486,38 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   give_up(v, a.call_seq, lost);
 }
 
-// dx of a counted row from several slices: f times their sum, in slice order, rounded once.  A CTA takes 32 rows and 64
-// columns and turns them over in shared memory: the slices hold columns, dx rows.
-constexpr uint32_t kJoinCols = 64;
+// dx of a counted row from several slices: f times their sum, in slice order, rounded once.  A CTA takes 32 rows and kCols
+// columns and turns them over in shared memory: the slices hold columns, dx rows.  64 columns, a line of dx, unless that
+// gives fewer CTAs than SMs; then 16 (8 rows x 1024, 32 slices: 20.7 -> 12.0 us; 2460 rows x 1024: 16.7 us, 21.7 with 16).
+template <uint32_t kCols>
 __global__ void __launch_bounds__(256) k_dx_join(LossPiece a) {
-  __shared__ float turned[32][kJoinCols + 4];
+  constexpr uint32_t kEach = kCols / 8;  // columns of a warp
+  __shared__ float turned[32][kCols + 4];
   let_next_start();
   after_previous();
   const uint32_t n = *a.count;
   if (n == 0) return;
-  const uint32_t slices = a.count[1], col_parts = (a.hidden + kJoinCols - 1) / kJoinCols, parts = (n + 31) / 32 * col_parts;
+  const uint32_t slices = a.count[1], col_parts = (a.hidden + kCols - 1) / kCols, parts = (n + 31) / 32 * col_parts;
   if (slices == 1) return;
-  const HighTiles<2> work(n, a.hidden, slices, a.pairs);
+  const HighTiles work(n, a.hidden, slices, a.pairs);
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (uint32_t i = blockIdx.x; i < parts; i += gridDim.x) {
-    const uint32_t r0 = i / col_parts * 32, c0 = i % col_parts * kJoinCols, m = r0 + lane;
+    const uint32_t r0 = i / col_parts * 32, c0 = i % col_parts * kCols, m = r0 + lane;
     const uint64_t tile = (uint64_t)(r0 / kHighRows) * work.n_tiles + c0 / kMmaTile, slice = (uint64_t)work.tiles * kMmaTile * kHighRows;
-    const float* __restrict__ slot = a.dx_slots + (tile * kMmaTile + c0 % kMmaTile + warp * 8) * kHighRows + r0 % kHighRows + lane;
+    const float* __restrict__ slot = a.dx_slots + (tile * kMmaTile + c0 % kMmaTile + warp * kEach) * kHighRows + r0 % kHighRows + lane;
     const float f = m < n ? a.factor[m] : 0.f;
-    float s[8] = {};
-#pragma unroll 4
+    float s[kEach] = {};
+#pragma unroll(32 / kEach)
     for (uint32_t k = 0; k < slices; ++k) {
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) s[j] += slot[k * slice + j * kHighRows];
+      for (uint32_t j = 0; j < kEach; ++j) s[j] += slot[k * slice + j * kHighRows];
     }
     __syncthreads();  // the part before this one has been written out
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) turned[lane][warp * 8 + j] = f * s[j];
+    for (uint32_t j = 0; j < kEach; ++j) turned[lane][warp * kEach + j] = f * s[j];
     __syncthreads();
-    const uint32_t r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
-    if (r0 + r < n && c0 + c < a.hidden)
+    const uint32_t r = threadIdx.x / kEach, c = threadIdx.x % kEach * 8;
+    if (r < 32 && r0 + r < n && c0 + c < a.hidden)
       *reinterpret_cast<uint4*>(a.dx + (a.row0 + a.row_of[r0 + r]) * a.lddx + c0 + c) = Pack<__nv_bfloat16>::narrow(&turned[r][c]);
   }
 }
@@ -528,7 +530,7 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   let_next_start();
   after_previous();
   const uint32_t n = *a.count, k_blocks = (n + kMmaK - 1) / kMmaK;
-  const HighTiles<2> work(a.vocab, a.hidden, 1, a.pairs);
+  const HighTiles work(a.vocab, a.hidden, 1, a.pairs);
   const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;  // a bf16 dw of several pieces is summed in fp32 until the last one
   bool lost;
   mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
@@ -675,7 +677,9 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
       FT_CUDA(launch_chained(k_logits<true, true, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, map_e, p->view, a));
       FT_CUDA(launch_chained(k_finish<true>, joins, join_threads, 0, st, a));
       FT_CUDA(launch_chained(k_dx, grid, kMmaThreads, kMmaSmem, st, map_p, map_w, p->view, a));
-      FT_CUDA(launch_chained(k_dx_join, dim3((unsigned)p->sm_count * 8), 256, 0, st, a));
+      const uint64_t parts = (uint64_t)joins.x * ((a.hidden + 63) / 64), most = (uint64_t)p->sm_count * 8;
+      if (parts < (uint64_t)p->sm_count) FT_CUDA(launch_chained(k_dx_join<16>, dim3((unsigned)parts * 4), 256, 0, st, a));
+      else FT_CUDA(launch_chained(k_dx_join<64>, dim3((unsigned)std::min(parts, most)), 256, 0, st, a));
       FT_CUDA(launch_chained(k_dw, grid, kMmaThreads, kMmaSmem, st, map_p, map_x, map_dw, p->view, a));
     } else {
       FT_CUDA(launch_chained(high ? k_logits<false, false, 2> : k_logits<false, false, 1>, grid, kMmaThreads, kMmaSmem, st, map_x, map_w, map_e, p->view, a));
