@@ -316,13 +316,15 @@ int32_t pool_free(ft_pool* pool, const uint32_t* sample_slot, uint32_t n, void* 
 
 /*
  * FT_ERR_TIMEOUT is the one asynchronous error that is not about the caller's data.  The host-tier kernels move pages
- * with bulk-asynchronous copies and wait for each staged load on an mbarrier; that wait, the library's only device-side
- * spin, gives up after 2 s of wall clock (a host link that has stopped answering; ft_tuning.bulk_wait_limit_us).  The
+ * with bulk-asynchronous copies and wait for each staged load on an mbarrier; that wait
+ * gives up after 2 s of wall clock (a host link that has stopped answering; ft_tuning.bulk_wait_limit_us).  The
  * CTA then issues no further copy, waits once more -- again at most that long -- for the loads it had already issued,
  * and returns; detail = CTA index (low 16 bits) | loads that had still not arrived when it returned (high 16 bits; 0
  * means that none can land later).  The bytes of that call are incomplete and the pool's state is no longer
  * trustworthy: after FT_ERR_TIMEOUT the only call a pool still supports is pool_destroy.  (Under the test hook
  * ft_tuning.bulk_timeout_test nothing was lost: the call's output is incomplete, the pool is intact.)
+ * The library's only other device-side spins are those of pool_token_loss*: a CTA pair's warps wait on mbarriers for
+ * operands and for one another, with the same limit and the same end (detail = CTA index).
  */
 /* First asynchronous error since the last call of pool_status (smallest call, then smallest code, then smallest
  * detail), then cleared.  Synchronises the device.  Calls are numbered from the last read, on 28 bits: read the
@@ -517,7 +519,7 @@ int32_t pool_layer_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const 
  * rows at a time has its probabilities there in bf16, and *best stops at pieces of 4 GiB); any size between the two works.
  * Errors: hidden or vocab 0 or a size that is no multiple of 8, a NULL or misaligned operand, a stride below hidden,
  * grad_stride > 1, accumulate with FT_BF16 INVALID_ARG; rows or vocab >= 2^31 CAPACITY; workspace NULL or misaligned
- * INVALID_ARG, below *least CAPACITY.  rows = 0: dw becomes zero unless accumulating.
+ * INVALID_ARG, below *least CAPACITY.  rows = 0: dw becomes zero unless accumulating.  Asynchronous: TIMEOUT (see there).
  */
 int32_t pool_token_loss_workspace(ft_pool* pool, uint64_t rows, uint32_t hidden, uint32_t vocab, uint32_t with_grad,
                                   uint32_t dw_dtype, uint64_t* least, uint64_t* best);
@@ -627,7 +629,8 @@ int32_t pool_profile_read(ft_pool* pool, ft_kernel_time* out /* host [FT_K_COUNT
  *                        engine serves its queue in order, so these copies wait behind any bulk copy the application
  *                        has queued in the same direction, and the application's behind them; the kernels share
  *                        the link but no queue.  Hence off by default
- *   bulk_wait_limit_us   bound, in microseconds, of every wait of the bulk-copy kernels for a staged load (default
+ *   bulk_wait_limit_us   bound, in microseconds, of every wait of the bulk-copy kernels for a staged load, and of every
+ *                        wait inside pool_token_loss* (default
  *                        2 000 000; 100..10 000 000).  A load not seen within it is declared lost and the call
  *                        reports FT_ERR_TIMEOUT through the status word (see FT_ERR_TIMEOUT above)
  *   bulk_timeout_test    test hook for that path, 0 in use.  1: every staged load announces 16 bytes more to its
@@ -636,7 +639,8 @@ int32_t pool_profile_read(ft_pool* pool, ft_kernel_time* out /* host [FT_K_COUNT
  *                        (bounded) for the loads it had issued, and returns; the call stores nothing from those
  *                        frames and reports FT_ERR_TIMEOUT.  Nothing faults and nothing spins beyond twice the
  *                        limit; accepted only with bulk_wait_limit_us set to at most 100 000.  This is the one knob
- *                        that changes results
+ *                        that changes results.  The loads of pool_token_loss* announce the 16 bytes too, and its
+ *                        kernels end the same way, the loads under way being waited for stage by stage
  */
 typedef struct {
   uint32_t dev_ctas_per_sm, scatter_ctas_per_sm, scatter_group, chunk_shift;

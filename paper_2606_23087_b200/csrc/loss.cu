@@ -216,7 +216,7 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
   bool lost;
   int32_t label = kNoLabel;
   float ref = 0.f;
-  mma_pair_tiles<false, false, kHigh>(map_x, map_w, m_tiles * n_tiles, v.bulk_wait_ns, &lost,
+  mma_pair_tiles<false, false, kHigh>(map_x, map_w, m_tiles * n_tiles, v, &lost,
     [&](uint32_t i) {
       // bands of 2048 rows, all columns of a band before the next: a band's x stays in L2
       constexpr uint32_t kBand = 8 / kHigh;
@@ -458,7 +458,7 @@ k_dx(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   const HighTiles work(n, a.hidden, slices, a.pairs);
   const bool wide = ((reinterpret_cast<uintptr_t>(a.dx) | a.lddx * 2) & 31) == 0;
   bool lost;
-  mma_pair_tiles<false, true, 2>(map_p, map_w, work.items(), v.bulk_wait_ns, &lost,
+  mma_pair_tiles<false, true, 2>(map_p, map_w, work.items(), v, &lost,
     [&](uint32_t i) { return work.at(i, each, k_blocks); }, [](const MmaTile&, uint32_t) {},
     [&](const MmaTile& t, uint32_t i, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t r = t.m % kHighRows + row + (threadIdx.x & 31), m = t.m + row + (threadIdx.x & 31), c0 = t.n + col0;
@@ -533,7 +533,7 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
   const HighTiles work(a.vocab, a.hidden, 1, a.pairs);
   const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;  // a bf16 dw of several pieces is summed in fp32 until the last one
   bool lost;
-  mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v.bulk_wait_ns, &lost,
+  mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v, &lost,
     [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); }, [](const MmaTile&, uint32_t) {},
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const int32_t c0 = (int32_t)(t.n + col0), m0 = (int32_t)(t.m + row);

@@ -170,7 +170,7 @@ struct MmaTile {
 // without K blocks has tmem = kNone: all sums are zero.  before(tile, row) is called ahead of the wait for the products, for
 // what the epilogue reads from memory.
 template <bool kAMn, bool kBMn, int kHigh, class TileAt, class Before, class Epilogue>
-__device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, uint64_t limit_ns, bool* lost_out,
+__device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t n_tiles, const PoolView& v, bool* lost_out,
                                                TileAt tile_at, Before before, Epilogue epilogue) {
   extern __shared__ uint8_t smem_raw[];
   constexpr uint32_t kStages = kMmaStages<kHigh>, kStageBytes = (kHigh + 1) * kMmaOperand;
@@ -199,6 +199,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   uint32_t it = 0;            // stages used so far
   uint32_t used[2] = {0, 0};  // times each accumulator was used so far
   uint32_t turn = 0;          // kHigh = 1: the accumulator that is next
+  const uint64_t limit_ns = v.bulk_wait_ns;
   if (warp < 4) {
     if (warp == 0 && lane == 0) {
       for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
@@ -208,7 +209,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
         for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
           const uint32_t s = it % kStages;
           if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
-          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * (t.high + 1) * kMmaOperand);
+          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * (t.high + 1) * kMmaOperand + v.bulk_tx_slack);  // the slack: a test hook, 0
           const uint32_t full = in_even_cta(&bar->full[s]), sb = base + s * kStageBytes;
           const int32_t kk = (int32_t)(k * kMmaK);
 #pragma unroll
