@@ -18,8 +18,8 @@
 // far below lse serves as well as the maximum; the label's logit is that, unless a row's loss is above 41.  Such a row gets its
 // maximum as reference, and its row tile's logits are worked out once more (k_logits<., true, .>, which returns at once where
 // there is none).  And it makes small losses exact: the label's term of the sum is 1, not a difference of two large numbers,
-// and the tensor cores' truncating additions (2.6e-6 of a logit over 3584) do not touch the one logit that a loss
-// depends on most: 2.6e-6 -> 3e-7 of the loss.
+// and the tensor cores' truncating additions do not touch the one logit that a loss depends on most (2.6e-6 -> 0.7e-6 of the loss
+// over 3584; see kPartBlocks for the rest).
 #include <algorithm>
 
 #include "mma_pair.cuh"
@@ -28,6 +28,13 @@ namespace ft {
 
 constexpr uint32_t kStatCols = 128;  // columns of the vocabulary that share a row's sum
 constexpr uint32_t kTileCost = 6;    // what a tile of dx costs beside its products, in blocks of K
+// The tensor cores truncate at every addition of 16 products, all one way, which shows in a loss as 0.24e-6 of it for each 1024 of K.
+// Tiles of 256 rows are summed in parts of kPartBlocks blocks of K, the parts joined in registers: 0.2e-6 at any K, for 3 to 5 % of a call
+// (200 rows x 32768 x 3584 76.6 -> 80.4 us; parts of 8 blocks 83.8).  Tiles of 512 rows have no registers for that: they are for
+// rows beyond 256 and K up to kHighBlocks blocks, where a loss comes to be off by 1e-6 (3000 rows x 32768 x 5120, with gradients: 2.39 ms
+// in parts, 2.24 ms in high tiles and off by 1.2e-6).
+constexpr uint32_t kPartBlocks = 16;
+constexpr uint32_t kHighBlocks = 66;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kMinusInf = 0xFF800000u;
 constexpr float kSumLimit = 0x1p60f;  // a row's sum above this wants another reference
@@ -212,16 +219,23 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
     __syncthreads();
     blocks = s_tiles;
   }
-  const uint32_t m_tiles = (blocks + kHigh - 1) / kHigh;
+  const uint32_t m_tiles = (blocks + kHigh - 1) / kHigh, tiles = m_tiles * n_tiles;
+  // A pair takes the parts of a tile's K one after the other.
+  constexpr uint32_t kPart = kHigh == 1 ? kPartBlocks : 0xFFFFFFu;
+  const uint32_t k_parts = (k_blocks + kPart - 1) / kPart;
   bool lost;
+  uint32_t z[kStatCols / 32][32];
   int32_t label = kNoLabel;
   float ref = 0.f;
-  mma_pair_tiles<false, false, kHigh>(map_x, map_w, m_tiles * n_tiles, v, &lost,
-    [&](uint32_t i) {
+  mma_pair_tiles<false, false, kHigh>(map_x, map_w, (tiles + a.pairs - 1) / a.pairs * a.pairs * k_parts, v, &lost,
+    [&](uint32_t item) {
+      const uint32_t round = item / a.pairs, i = item % a.pairs + round / k_parts * a.pairs, part = round % k_parts;
+      if (i >= tiles) return MmaTile{0, 0, 0, 0, 0};
       // bands of 2048 rows, all columns of a band before the next: a band's x stays in L2
       constexpr uint32_t kBand = 8 / kHigh;
       const uint32_t band = i / (kBand * n_tiles), in = i - band * kBand * n_tiles, rows = min(kBand, m_tiles - band * kBand), m = band * kBand + in % rows;
-      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m * kHigh) * kMmaTile, in / rows * kMmaTile, 0, k_blocks, min((uint32_t)kHigh, blocks - m * kHigh)};
+      return MmaTile{(kRedo ? (uint32_t)s_tile[m] : m * kHigh) * kMmaTile, in / rows * kMmaTile, part * kPart, min((part + 1) * kPart, k_blocks),
+                     min((uint32_t)kHigh, blocks - m * kHigh)};
     },
     [&](const MmaTile& t, uint32_t row) {
       const uint32_t m = t.m + row + (threadIdx.x & 31);
@@ -231,11 +245,22 @@ k_logits(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUte
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t c0 = t.n + col0;
       if (c0 >= a.vocab) return;
-      uint32_t z[kStatCols / 32][32];
+      if (kHigh == 2 || t.k0 == 0) {
 #pragma unroll
-      for (uint32_t c = 0; c < kStatCols / 32; ++c) tmem_load32(tmem + 32 * c, z[c]);
-      tmem_wait();
+        for (uint32_t c = 0; c < kStatCols / 32; ++c) tmem_load32(tmem + 32 * c, z[c]);
+        tmem_wait();
+      } else {
+#pragma unroll
+        for (uint32_t c = 0; c < kStatCols / 32; ++c) {
+          uint32_t part[32];
+          tmem_load32(tmem + 32 * c, part);
+          tmem_wait();
+#pragma unroll
+          for (uint32_t j = 0; j < 32; ++j) z[c][j] = __float_as_uint(__uint_as_float(z[c][j]) + __uint_as_float(part[j]));
+        }
+      }
       release();  // the products go on while the exponentials are taken
+      if (kHigh == 1 && t.k1 < k_blocks) return;
       const uint32_t m = t.m + row + (threadIdx.x & 31), cols = min(kStatCols, a.vocab - c0);
       const uint32_t label_at = (uint32_t)label - c0;
       [[maybe_unused]] const uint32_t keep = m < n ? 0xFFFFFFFFu : 0u;  // rows beyond the last one that counts: zeros, which the product over rows adds
@@ -667,7 +692,7 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     }
     const dim3 joins((a.rows + 31) / 32);
     const uint32_t join_threads = 32 * kJoinRowWarps;
-    const bool high = a.rows > kMmaTile;
+    const bool high = a.rows > kMmaTile && a.hidden <= kHighBlocks * kMmaK;
     if (a.rows <= kPickFewUpTo) k_pick<kPickFew><<<(a.rows + kPickFew - 1) / kPickFew, 256, 0, st>>>(p->view, a);
     else k_pick<kPickRows><<<(a.rows + kPickRows - 1) / kPickRows, 256, 0, st>>>(p->view, a);
     FT_CUDA(cudaGetLastError());
