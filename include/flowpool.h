@@ -512,7 +512,7 @@ int32_t pool_layer_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const 
  *   dw[v] = sum over i of d_iv * x[i]     device [vocab, hidden] contiguous, FT_F32 or FT_BF16 (dw_dtype);
  *                                         accumulate != 0 (FT_F32 only) adds to what it holds, as pool_embed_grad does
  * The products run on the tensor cores with fp32 sums; for them d is rounded to bf16, as a probability over a factor of its
- * row, and for dw that factor times x as well.
+ * row, and for dw that factor times x as well (up to 128 rows as two bf16 values).
  *
  * hidden, ldx, ldw, lddx are multiples of 8; x, w, dx and dw start on 16-byte boundaries.  pool_token_loss_workspace
  * gives the smallest workspace (*least) and the one from which more brings nothing (*best; with gradients a piece of the

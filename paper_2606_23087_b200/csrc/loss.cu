@@ -9,7 +9,7 @@
 //   k_logits  z by tiles; a row of a tile gives the sum of e = exp(z - reference) over the columns that are not its label,
 //             and with gradients e itself in bf16 (rounding e costs 2^-8 of a probability, rounding z would cost 2^-8 of z)
 //   k_join    adds a row's sums to S: loss = log(1 + S), lse = reference + loss
-//   k_finish  d = f e with one factor f = g exp(reference - lse) a row: f goes to the row's x for dW (rounded to bf16) and to
+//   k_finish  d = f e with one factor f = g exp(reference - lse) a row: f goes to the row's x for dW (rounded to bf16; for few rows as two bf16 values) and to
 //             the row's sums for dx, so e is not touched again but for the label's element, (exp(-loss) - 1) exp(lse - reference)
 //   k_dx, k_dw  the two products
 //
@@ -34,6 +34,11 @@ constexpr uint32_t kTileCost = 6;    // what a tile of dx costs beside its produ
 // rows beyond 256 and K up to kHighBlocks blocks, where a loss comes to be off by 1e-6 (3000 rows x 32768 x 5120, with gradients: 2.39 ms
 // in parts, 2.24 ms in high tiles and off by 1.2e-6).
 constexpr uint32_t kPartBlocks = 16;
+// Rounding f x to bf16 makes dW's error 2.3e-3 of its norm, where the rounding of a bf16 dW alone is 1.7e-3.  Up to kTwiceUpTo rows, where
+// dW's bytes and not the product take the time, x goes in as two bf16 values, over twice the K: 1.7e-3, for 2 to 3 % of the call (60 rows x
+// 32768 x 3584 195 -> 199 us); 250 rows would pay 17 % (219 -> 256 us).
+constexpr uint32_t kTwiceUpTo = 128;
+static_assert(2 * kTwiceUpTo <= kMmaTile, "both values of f x fit in xc");
 constexpr uint32_t kHighBlocks = 66;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kMinusInf = 0xFF800000u;
@@ -46,6 +51,7 @@ constexpr uint32_t kMinSlots = 148;  // few rows: room for two tiles a pair
 struct LossPiece {
   uint32_t rows, hidden, vocab, ld_p, tiles, slots;  // tiles: of kStatCols columns; slots: tiles that dx_slots holds
   uint32_t padded;  // rows of xc and p: `rows` in whole tiles
+  uint32_t twice;   // dw takes f x as two bf16 values, the second one behind the whole blocks of K of the first
   uint32_t pairs;   // CTA pairs of the products
   uint64_t row0, ldx, ldw, lddx;
   const __nv_bfloat16 *x, *w;
@@ -133,7 +139,10 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
   if (blockIdx.x == gridDim.x - 1) {  // the product over rows runs to a whole block of K: those rows' x must be finite
     const uint32_t end = (total + kMmaK - 1) / kMmaK * kMmaK;
     uint4* tail = reinterpret_cast<uint4*>(a.xc + (uint64_t)total * a.hidden);
-    for (uint32_t c = threadIdx.x; c < (end - total) * vecs; c += blockDim.x) tail[c] = zero;
+    for (uint32_t c = threadIdx.x; c < (end - total) * vecs; c += blockDim.x) {
+      tail[c] = zero;
+      if (a.twice) tail[(uint64_t)end * vecs + c] = zero;
+    }
   }
   for (uint32_t k = warp; k < rows; k += 8)
     if (a.dx && dest[k] < 0) {
@@ -429,7 +438,7 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
   }
   if constexpr (kGrad) {
     __syncthreads();
-    const uint32_t vecs = a.hidden / 8;
+    const uint32_t vecs = a.hidden / 8, second = (n + kMmaK - 1) / kMmaK * kMmaK;
     for (uint32_t k = warp; k < 32 && r0 + k < n; k += kJoinRowWarps) {
       uint4* x = reinterpret_cast<uint4*>(a.xc + (uint64_t)(r0 + k) * a.hidden);
       const float f = s_f[k];
@@ -439,7 +448,14 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_finish(LossPiece a) {
         Pack<__nv_bfloat16>::widen(x[c], t);
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] *= f;
-        x[c] = Pack<__nv_bfloat16>::narrow(t);
+        const uint4 first = x[c] = Pack<__nv_bfloat16>::narrow(t);
+        if (a.twice) {
+          float b[8];
+          Pack<__nv_bfloat16>::widen(first, b);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[e] -= b[e];
+          x[(uint64_t)second * vecs + c] = Pack<__nv_bfloat16>::narrow(t);
+        }
       }
     }
   }
@@ -554,12 +570,17 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
      const __grid_constant__ PoolView v, const __grid_constant__ LossPiece a) {
   let_next_start();
   after_previous();
-  const uint32_t n = *a.count, k_blocks = (n + kMmaK - 1) / kMmaK;
+  const uint32_t n = *a.count, blocks = (n + kMmaK - 1) / kMmaK, k_blocks = a.twice ? 2 * blocks : blocks;
   const HighTiles work(a.vocab, a.hidden, 1, a.pairs);
   const bool in_fp32 = a.dw_dtype == FT_F32 || !a.last;  // a bf16 dw of several pieces is summed in fp32 until the last one
   bool lost;
   mma_pair_tiles<true, true, 2>(map_p, map_x, work.items(), v, &lost,
-    [&](uint32_t i) { return work.at(i, k_blocks, k_blocks); }, [](const MmaTile&, uint32_t) {},
+    [&](uint32_t i) {
+      MmaTile t = work.at(i, k_blocks, k_blocks);
+      if (a.twice) t.again = blocks;
+      return t;
+    },
+    [](const MmaTile&, uint32_t) {},
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const int32_t c0 = (int32_t)(t.n + col0), m0 = (int32_t)(t.m + row);
       if (c0 >= (int32_t)a.hidden) return;
@@ -685,6 +706,7 @@ static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, voi
     a.rows = (uint32_t)std::min<uint64_t>(piece, rows - r0);
     a.add_dw = r0 > 0 || accumulate;
     a.last = r0 + a.rows == rows;
+    a.twice = grad && a.rows <= kTwiceUpTo;
     if (grad) {
       const bool fp32 = a.dw_dtype == FT_F32 || !a.last;
       if (mma_map(&map_dw, a.dw_dtype == FT_F32 || a.last ? a.dw : a.dw_acc, a.hidden, a.vocab, a.hidden, 32, fp32) != CUDA_SUCCESS)

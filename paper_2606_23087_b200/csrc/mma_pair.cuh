@@ -159,9 +159,10 @@ constexpr uint32_t kMmaStep = kMn ? 2048 : 32;
 template <bool kAMn, bool kBMn>
 constexpr uint32_t kMmaInstr = 1u << 4 | 1u << 7 | 1u << 10 | (kAMn ? 1u << 15 : 0) | (kBMn ? 1u << 16 : 0) | (256 >> 3) << 17 | (256 >> 4) << 24;
 
-// One tile of work: rows from m (256 times `high` of them; none: nothing to do), columns from n, K blocks [k0, k1).
+// One tile of work: rows from m (256 times `high` of them; none: nothing to do), columns from n, K blocks [k0, k1).  From block
+// `again` on, A begins once more at its first block.
 struct MmaTile {
-  uint32_t m, n, k0, k1, high;
+  uint32_t m, n, k0, k1, high, again = kNone;
 };
 
 // Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; every epilogue warp calls
@@ -211,7 +212,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
           if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
           if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * (t.high + 1) * kMmaOperand + v.bulk_tx_slack);  // the slack: a test hook, 0
           const uint32_t full = in_even_cta(&bar->full[s]), sb = base + s * kStageBytes;
-          const int32_t kk = (int32_t)(k * kMmaK);
+          const int32_t kk = (int32_t)(k * kMmaK), ka = (int32_t)((k < t.again ? k : k - t.again) * kMmaK);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (kBMn) tma_box(sb + h * kMmaBox, &map_b, b0 + 64 * h, kk, full);
@@ -221,8 +222,8 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
           for (int h = 0; h < 2 * kHigh; ++h) {
             if (h >= 2 && t.high < 2) break;
             const int32_t row = a0 + 64 * (h & 1) + (int32_t)kMmaTile * (h >> 1);
-            if (kAMn) tma_box(sb + kMmaOperand + h * kMmaBox, &map_a, row, kk, full);
-            else tma_box(sb + kMmaOperand + h * kMmaBox, &map_a, kk, row, full);
+            if (kAMn) tma_box(sb + kMmaOperand + h * kMmaBox, &map_a, row, ka, full);
+            else tma_box(sb + kMmaOperand + h * kMmaBox, &map_a, ka, row, full);
           }
         }
       }
