@@ -13,6 +13,9 @@
 //             the row's sums for dx, so e is not touched again but for the label's element, (exp(-loss) - 1) exp(lse - reference)
 //   k_dx, k_dw  the two products
 //
+// Bound by the tensor cores, long calls by the card's power limit: 16384 rows that count x 32768 x 3584 with gradients 8.4 to 8.9 ms (1.3 to
+// 1.37 PFLOP/s), 2460 x 32768 x 1024 470 us (1.05 PFLOP/s); few rows by W and launches: 24 x 32768 x 1024 forward 33 us.
+//
 // Why a reference known before any logit: with each tile's own maximum, the usual choice, e has to be read, scaled and
 // written again once lse is known (1.1 ms of 10.7 for 16384 rows x 32768).  bf16 has fp32's range, so any reference that is not
 // far below lse serves as well as the maximum; the label's logit is that, unless a row's loss is above 41.  Such a row gets its
