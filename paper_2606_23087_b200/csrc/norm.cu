@@ -127,19 +127,22 @@ struct RowFeed {
   }
 };
 
-constexpr int kNormStages = 4;
+// Rows in shared memory or under way to it: four, or three where those would not fit (fp32 rows beyond 12288 columns).
+template <int V, int kN>
+constexpr int kNormStages = V * kN <= 3072 ? 4 : 3;
+constexpr size_t kSmemMost = 227 * 1024;  // of a CTA
 
 template <typename T, int V, bool kVec, int kN>
 __global__ void __launch_bounds__(kN, kVec && V * Pack<T>::kElems <= 16 ? 896 / kN : 512 / kN) k_norm(NormArgs a) {
-  extern __shared__ __align__(16) uint4 ring[];  // [kNormStages][V][kN]
+  extern __shared__ __align__(16) uint4 ring[];  // [kStages][V][kN]
   __shared__ __align__(16) float red[2][(kN / 32 + 3) / 4 * 4];
-  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E / 2;  // N pairs
-  RowFeed<T, V, kVec, kN, kN, kNormStages> in;
+  constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E / 2, kStages = kNormStages<V, kN>;  // N pairs
+  RowFeed<T, V, kVec, kN, kN, kStages> in;
   const uint32_t n_rows = rows_from(a.rows, blockIdx.x, gridDim.x);
   in.init(a.x, a.ldx, blockIdx.x, gridDim.x, n_rows, a.cols, threadIdx.x, ring + threadIdx.x);
   if constexpr (kVec) {
 #pragma unroll
-    for (int s = 0; s < kNormStages - 1; ++s) { in.fetch(s); copy_async_commit(); }
+    for (int s = 0; s < kStages - 1; ++s) { in.fetch(s); copy_async_commit(); }
   } else {
     in.fetch(0);
   }
@@ -165,9 +168,9 @@ __global__ void __launch_bounds__(kN, kVec && V * Pack<T>::kElems <= 16 ? 896 / 
   for (uint32_t r = 0; r < n_rows; ++r) {
     F2 x[N], s[2] = {f2(0.f), f2(0.f)};
     if constexpr (kVec) {
-      in.fetch((stage + kNormStages - 1) % kNormStages);
+      in.fetch((stage + kStages - 1) % kStages);
       copy_async_commit();
-      copy_async_wait<kNormStages - 1>();
+      copy_async_wait<kStages - 1>();
     }
     in.take(stage, x);
     if constexpr (!kVec) in.fetch(0);
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(kN, kVec && V * Pack<T>::kElems <= 16 ? 896 / 
     for (int i = 0; i < N; ++i) x[i] = fma(x[i] * f2(rstd), w[i], b[i]);
     in.store(q, x);
     q += q_step;
-    stage = (stage + 1) % kNormStages;
+    stage = (stage + 1) % kStages;
   }
 }
 
@@ -474,7 +477,8 @@ static cudaError_t norm_rows(const ft_pool* p, const NormArgs& a, cudaStream_t s
   with_threads((n + V - 1) / V, [&](auto k) {
     constexpr int kN = decltype(k)::value;
     auto kernel = k_norm<T, V, kVec, kN>;
-    constexpr size_t smem = kVec ? (size_t)kNormStages * V * kN * 16 : 0;
+    constexpr size_t smem = kVec ? (size_t)kNormStages<V, kN> * V * kN * 16 : 0;
+    static_assert(smem + 2 * (kN / 32 + 3) / 4 * 16 <= kSmemMost, "every instance can be launched");
     if ((e = allow_smem(kernel, smem)) != cudaSuccess) return;
     int per_sm = 1;
     if (a.rows > (uint64_t)p->sm_count) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kN, smem);
@@ -505,6 +509,7 @@ static cudaError_t norm_grad_rows(ft_pool* p, const NormGradArgs& a, uint32_t* l
   constexpr int E = kVec ? Pack<T>::kElems : 1, kGroups = kGradGroups(V * E, kN);
   constexpr size_t kRows = kVec ? 2ull * kGradStages<V, kN * kGroups> * V * kN * kGroups * 16 : 0, kSums = (kGroups - 1) * 2ull * V * E * kN * 4;
   constexpr size_t smem = (size_t)V * E * kN * 4 + (kRows > kSums ? kRows : kSums);
+  static_assert(smem + 6 * (kN * kGroups / 32) * sizeof(float2) <= kSmemMost, "every instance can be launched");
   auto kernel = k_norm_grad<T, V, kVec, kN, kGroups>;
   const cudaError_t e = allow_smem(kernel, smem);
   if (e != cudaSuccess) return e;
