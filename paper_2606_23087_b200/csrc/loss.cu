@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(256) k_dx_join(LossPiece a) {
   for (uint32_t i = blockIdx.x; i < parts; i += gridDim.x) {
     const uint32_t r0 = i / col_parts * 32, c0 = i % col_parts * kCols, m = r0 + lane;
     const uint64_t tile = (uint64_t)(r0 / kHighRows) * work.n_tiles + c0 / kMmaTile, slice = (uint64_t)work.tiles * kMmaTile * kHighRows;
-    const float* __restrict__ slot = a.dx_slots + (tile * kMmaTile + c0 % kMmaTile + warp * kEach) * kHighRows + r0 % kHighRows + lane;
+    const float* slot = a.dx_slots + (tile * kMmaTile + c0 % kMmaTile + warp * kEach) * kHighRows + r0 % kHighRows + lane;
     const float f = m < n ? a.factor[m] : 0.f;
     float s[kEach] = {};
 #pragma unroll(32 / kEach)

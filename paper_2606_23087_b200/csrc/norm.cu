@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_norm_grad(NormGradArgs a) {
 
 // dw and db from the lines of partial sums: 32 columns a CTA, its warps over the lines, joined in a fixed order
 constexpr int kJoinWarps = 16;
-__global__ void __launch_bounds__(32 * kJoinWarps) k_norm_join(const float* __restrict__ partial, uint32_t lines, uint32_t cols,
+__global__ void __launch_bounds__(32 * kJoinWarps) k_norm_join(const float* partial, uint32_t lines, uint32_t cols,
                                                                float* dweight, float* dbias, uint32_t accumulate) {
   __shared__ float part[kJoinWarps][32];
   after_previous();

@@ -113,7 +113,8 @@ template <int N>
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // A chain of kernels of one call: each lets the next one be set up while it runs, and waits at its start for the one before
-// (which has waited for the one before it) to have ended with its stores visible.
+// (which has waited for the one before it) to have ended with its stores visible.  Such a kernel takes no `const __restrict__`
+// pointer and no __ldg to memory that the one before writes: those loads need not stay behind the wait.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... P, typename... A>
