@@ -324,7 +324,7 @@ int32_t pool_free(ft_pool* pool, const uint32_t* sample_slot, uint32_t n, void* 
  * trustworthy: after FT_ERR_TIMEOUT the only call a pool still supports is pool_destroy.  (Under the test hook
  * ft_tuning.bulk_timeout_test nothing was lost: the call's output is incomplete, the pool is intact.)
  * The library's only other device-side spins are those of pool_token_loss*: a CTA pair's warps wait on mbarriers for
- * operands and for one another, with the same limit and the same end (detail = CTA index).
+ * operands and for one another, with that limit or a tile's own time if that is longer, and the same end (detail = CTA index).
  */
 /* First asynchronous error since the last call of pool_status (smallest call, then smallest code, then smallest
  * detail), then cleared.  Synchronises the device.  Calls are numbered from the last read, on 28 bits: read the
@@ -629,9 +629,10 @@ int32_t pool_profile_read(ft_pool* pool, ft_kernel_time* out /* host [FT_K_COUNT
  *                        engine serves its queue in order, so these copies wait behind any bulk copy the application
  *                        has queued in the same direction, and the application's behind them; the kernels share
  *                        the link but no queue.  Hence off by default
- *   bulk_wait_limit_us   bound, in microseconds, of every wait of the bulk-copy kernels for a staged load, and of every
- *                        wait inside pool_token_loss* (default
- *                        2 000 000; 100..10 000 000).  A load not seen within it is declared lost and the call
+ *   bulk_wait_limit_us   bound, in microseconds, of every wait of the bulk-copy kernels for a staged load (default
+ *                        2 000 000; 100..10 000 000), and of every wait inside pool_token_loss*, where it counts as 1 ms
+ *                        plus 4 us for each 64 of the dimension that a tile sums over (the products of a tile are waited
+ *                        for as a whole) if it is set below that.  A load not seen within it is declared lost and the call
  *                        reports FT_ERR_TIMEOUT through the status word (see FT_ERR_TIMEOUT above)
  *   bulk_timeout_test    test hook for that path, 0 in use.  1: every staged load announces 16 bytes more to its
  *                        completion barrier than it requests, so that no load is ever SEEN complete although all of

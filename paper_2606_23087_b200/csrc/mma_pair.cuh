@@ -17,7 +17,7 @@
 // Warps: 0 TMA, 1 matrix instructions (even CTA), 2 tensor memory, 4..11 epilogue: quarter w % 4 of the rows, columns
 // [0, 128) for 4..7 and [128, 256) for 8..11.
 //
-// Every wait is bounded (PoolView::bulk_wait_ns).  A role that gives up stops issuing; before the pair leaves, the loads
+// Every wait is bounded (mma_wait_limit).  A role that gives up stops issuing; before the pair leaves, the loads
 // and products under way are waited for once more, bounded again, and the tensor memory is freed.
 #pragma once
 #include <cuda.h>
@@ -165,6 +165,13 @@ struct MmaTile {
   uint32_t m, n, k0, k1, high, again = kNone;
 };
 
+// Bound of a wait inside a tile: the pool's limit, which is meant for one load, but never less than what the tile's products may take.
+// A block of K of 512 rows takes a pair 0.52 us at the card's highest clock (1024 cycles), 0.8 at its power limit; 4 leave room for a
+// device that others use too, the millisecond for an epilogue behind other traffic.  The test hook's waits are to run out: the limit itself.
+__device__ __forceinline__ uint64_t mma_wait_limit(const PoolView& v, uint32_t k_blocks) {
+  return v.bulk_tx_slack ? v.bulk_wait_ns : max(v.bulk_wait_ns, (uint64_t)1000000 + (uint64_t)k_blocks * 4000);
+}
+
 // Runs the tiles pair, pair + pairs, ... below `n_tiles`.  tile_at(i) -> MmaTile; every epilogue warp calls
 // epilogue(tile, i, tmem, row, col0, release) for each 256 rows: tensor memory from `tmem` on holds 128 columns of its 32 rows, lane
 // l the row `row` + l of the tile, columns col0 .. col0 + 127.  It may call release() as soon as it has read them.  A tile
@@ -200,12 +207,13 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   uint32_t it = 0;            // stages used so far
   uint32_t used[2] = {0, 0};  // times each accumulator was used so far
   uint32_t turn = 0;          // kHigh = 1: the accumulator that is next
-  const uint64_t limit_ns = v.bulk_wait_ns;
+  const uint64_t last_limit_ns = mma_wait_limit(v, 0);  // behind the last tile
   if (warp < 4) {
     if (warp == 0 && lane == 0) {
       for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
         const MmaTile t = tile_at(i);
         if (t.high == 0) continue;
+        const uint64_t limit_ns = mma_wait_limit(v, t.k1 - t.k0);
         const int32_t a0 = (int32_t)(t.m + rank * 128), b0 = (int32_t)(t.n + rank * 128);
         for (uint32_t k = t.k0; k < t.k1; ++k, ++it) {
           const uint32_t s = it % kStages;
@@ -231,9 +239,10 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
       // even one), and the even CTA's signals that it is done with them
       const uint32_t j0 = it > kStages ? it - kStages : 0;
       if (lost && rank == 0)
-        for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kStages], (j / kStages) & 1, limit_ns);
-      for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kStages], (j / kStages) & 1, limit_ns);
+        for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kStages], (j / kStages) & 1, last_limit_ns);
+      for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kStages], (j / kStages) & 1, last_limit_ns);
     } else if (warp == 1 && lane == 0 && rank == 0) {
+      uint64_t limit_ns = 0;
       const auto take = [&](uint32_t acc) {  // waits until the accumulator's last user has read it
         if (!mbar_wait_bounded(&bar->acc_empty[acc], (used[acc]++ & 1) ^ 1, limit_ns)) lost = true;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -243,6 +252,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
         if (t.high == 0 || t.k0 == t.k1) continue;
         const uint32_t acc0 = kHigh == 1 ? turn : 0;
         turn ^= 1;
+        limit_ns = mma_wait_limit(v, t.k1 - t.k0);
         take(acc0);
         const auto arrived = [&](uint32_t i) {  // the stage's operands are in both CTAs
           if (!mbar_wait_bounded(&bar->full[i % kStages], (i / kStages) & 1, limit_ns)) lost = true;
@@ -287,7 +297,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
       }
       if (lost) {  // products under way still read shared memory and write tensor memory
         mma_commit(&bar->drain);
-        mbar_wait_bounded(&bar->drain, 0, limit_ns);
+        mbar_wait_bounded(&bar->drain, 0, last_limit_ns);
       }
     }
   } else {
@@ -303,6 +313,7 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
     };
     for (uint32_t i = pair; i < n_tiles && !lost; i += pairs) {
       const MmaTile t = tile_at(i);
+      const uint64_t limit_ns = mma_wait_limit(v, t.k1 - t.k0);
       for (uint32_t h = 0; h < t.high && !lost; ++h) {
         uint32_t at = kNone;
         const uint32_t row = h * kMmaTile + rank * 128 + quarter * 32;
