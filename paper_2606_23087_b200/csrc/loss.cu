@@ -387,7 +387,7 @@ __device__ __forceinline__ float store_loss(const LossPiece& a, uint32_t m, floa
   const float above = ref == target ? log1pf(sum) : logf(sum + expf(target - ref)), loss = (ref - target) + above;
   const uint64_t row = a.row0 + a.row_of[m];
   a.loss[row] = loss;
-  a.lse[row] = target + loss;
+  a.lse[row] = ref + above;  // not target + loss, which is no number where the label's logit is -inf
   a.factor[m] = above;
   return loss;
 }
@@ -403,7 +403,8 @@ __global__ void __launch_bounds__(32 * kJoinRowWarps) k_join(LossPiece a) {
   }
   const float2 s = join_tiles(a, n, m);
   if (threadIdx.x >= 32 || m >= n) return;
-  if (s.y > kSumLimit && s.x < INFINITY) {
+  // (a label's logit of -inf is no reference either: z - reference is inf or no number)
+  if ((s.y > kSumLimit || a.ref[m] == -INFINITY) && s.x < INFINITY && s.x > -INFINITY) {
     a.ref[m] = s.x;
     a.redo[1 + m / kMmaTile] = 1;
     a.redo[0] = 1;
