@@ -186,13 +186,15 @@ __device__ __forceinline__ float inverse_root(float x) {
 }
 // Square roots of pairs by one step of Heron's method from an approximate inverse root, the residual taken exactly by a
 // multiply-add: r = s + (v - s s) / (2 s), off by less than 2^-43 of r before its one rounding (eight of __fsqrt_rn a lane were a
-// third of the kernel's instructions).  v lies in [2^-100, 2^126] or is zero.
+// third of the kernel's instructions).  v lies in [2^-100, 2^104] or is zero.
 __device__ __forceinline__ F2 root(F2 v) {
   const float2 a = parts(v);
   const F2 y = f2(inverse_root(fmaxf(a.x, 0x1p-126f)), inverse_root(fmaxf(a.y, 0x1p-126f)));
   const F2 s = v * y;
   return fma(fma(s * f2(-1.f), s, v), y * f2(0.5f), s);
 }
+
+constexpr uint32_t kRootBelow = 0x53800000u;  // bits of 2^40
 
 // what a block is made from
 template <typename P, typename G, bool k8, bool kV>
@@ -245,16 +247,14 @@ __device__ __forceinline__ void adamw_block(const AdamwLoads<P, G, k8, kV>& in, 
       most = max(most, max(__float_as_uint(a.x), __float_as_uint(a.y)));
     }
     most = __reduce_max_sync(0xFFFFFFFFu, most);
-    // small v are brought up by an even power of two, so that root() sees no subnormal number; beside a large one they
-    // matter neither to the block's float8 values nor, below eps, to the step
-    const bool small = most < __float_as_uint(0x1p40f);
-    const float up = small ? 0x1p64f : 1.f, down = small ? 0x1p-32f : 1.f;
-    if (most < 0x7F800000u) {
+    // v is brought up by an even power of two, so that root() sees no subnormal number; blocks with a v too large for that (a
+    // gradient above some 10^6) or not finite take the function
+    if (most < kRootBelow) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = root(v[i] * f2(up)) * f2(down);
+      for (int i = 0; i < 4; ++i) r[i] = root(v[i] * f2(0x1p64f)) * f2(0x1p-32f);
     }
   }
-  if (!k8 || most >= 0x7F800000u) {
+  if (!k8 || most >= kRootBelow) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 a = parts(v[i]);
