@@ -537,7 +537,7 @@ int32_t pool_token_loss_grad(ft_pool* pool, uint64_t rows, uint32_t hidden, uint
  * g = *grad_scale * grad (device fp32, e.g. a clipping factor; NULL = 1):
  *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * g^2
  *   param = param * (1 - lr * weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in fp32 (the factors that depend on the step in double, on the host); param is rounded once to its type, `copy` (bf16
+ * in fp32 (the factors that depend on the step in double, on the host; an eps between 0 and 2^-126 counts as 2^-126); param is rounded once to its type, `copy` (bf16
  * [n], may be NULL) receives the new parameters as well, as the 16-bit table that pool_gather_* reads beside 32-bit
  * master weights.
  *   state_bits 32   m, v fp32 [n]

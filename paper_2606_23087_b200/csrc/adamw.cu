@@ -17,6 +17,7 @@
 // be a step without bound.  m, v and r are taken with one rounding an operation (no contraction), which makes the stored
 // bytes the same on every launch shape.  A block that holds a value that is not finite reads back as NaN.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -394,7 +395,8 @@ FT_EXPORT int32_t pool_adamw_step(ft_pool* p, const ft_adamw_tensor* tensors, ui
   k.b2 = both(cfg->beta2); k.c2 = both(1.0 - cfg->beta2);
   k.step = both(-cfg->lr / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
   k.inv = both(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)cfg->step)));
-  k.eps = both(cfg->eps);
+  // the quotient flushes divisors below the normal numbers to zero: m = r = 0 would be 0 / 0
+  k.eps = both(cfg->eps > 0.0 ? std::max(cfg->eps, (double)FLT_MIN) : 0.0);
   k.minus_zero = both(-0.0);
   k.grad_scale = cfg->grad_scale;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -31,3 +31,9 @@ def first_step(pool, bits, eps, empty):  # noqa: F811
 @pytest.mark.parametrize("bits", [32, 8])
 def test_second_moments_below_the_normal_numbers(pool, bits):  # noqa: F811
     first_step(pool, bits, 0.0, False)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-42, 1e-50])
+def test_an_epsilon_below_the_normal_numbers(pool, bits, eps):  # noqa: F811
+    first_step(pool, bits, eps, True)
