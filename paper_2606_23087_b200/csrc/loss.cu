@@ -49,7 +49,6 @@ constexpr float kSumLimit = 0x1p60f;  // a row's sum above this wants another re
 constexpr int32_t kNoLabel = -100;
 constexpr uint32_t kPieceRowsMost = 65536;
 constexpr uint32_t kHighRows = 2 * kMmaTile;  // rows of a tile of dx and dw
-constexpr uint32_t kMinSlots = 148;  // few rows: room for two tiles a pair
 
 struct LossPiece {
   uint32_t rows, hidden, vocab, ld_p, tiles, slots;  // tiles: of kStatCols columns; slots: tiles that dx_slots holds
@@ -629,8 +628,9 @@ k_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensor
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
 
-// Carves the workspace for pieces of `rows` rows; returns its bytes.  `several`: more than one piece.
-static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, bool grad, bool acc) {
+// Carves the workspace for pieces of `rows` rows; returns its bytes.  `acc`: a bf16 dw of several pieces.  Few rows have room for
+// slices of dx that give each pair two tiles: `sms` of them, 512 KiB each.
+static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, uint32_t sms, bool grad, bool acc) {
   uint64_t off = 0;
   auto take = [&](uint64_t bytes) { const uint64_t o = off; off += align_up_sz(bytes, 256); return base + o; };
   const uint64_t padded = align_up_sz(rows, kMmaTile);
@@ -639,7 +639,7 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
   a->tiles = (vocab + kStatCols - 1) / kStatCols;
   a->ld_p = (uint32_t)align_up_sz(vocab, 64);  // whole lines
   const uint64_t dx_tiles = (padded + kHighRows - 1) / kHighRows * ((hidden + kMmaTile - 1) / kMmaTile);
-  a->slots = (uint32_t)std::max<uint64_t>(dx_tiles, kMinSlots);
+  a->slots = (uint32_t)std::max<uint64_t>(dx_tiles, sms);
   a->count = reinterpret_cast<uint32_t*>(take(8));
   a->row_of = reinterpret_cast<int32_t*>(take(4ull * rows));
   a->label = reinterpret_cast<int32_t*>(take(4ull * rows));
@@ -656,12 +656,12 @@ static uint64_t loss_carve(LossPiece* a, uint8_t* base, uint32_t rows, uint32_t 
 }
 
 struct LossWork {
-  uint32_t hidden, vocab;
+  uint32_t hidden, vocab, sms;
   bool grad, bf16_dw;
   uint64_t rows;
   uint64_t bytes(uint32_t piece) const {
     LossPiece a;
-    return loss_carve(&a, nullptr, piece, hidden, vocab, grad, grad && bf16_dw && piece < rows);
+    return loss_carve(&a, nullptr, piece, hidden, vocab, sms, grad, grad && bf16_dw && piece < rows);
   }
   uint32_t least_rows() const { return (uint32_t)std::min<uint64_t>(rows, 256); }
   // pieces of the rows whose probabilities take 4 GiB
@@ -685,11 +685,11 @@ struct LossWork {
 
 static int32_t token_loss(ft_pool* p, LossPiece a, uint64_t rows, bool grad, void* workspace, uint64_t workspace_bytes, uint32_t accumulate,
                           cudaStream_t st) {
-  const LossWork work{a.hidden, a.vocab, grad, a.dw_dtype == FT_BF16, rows};
+  const LossWork work{a.hidden, a.vocab, (uint32_t)p->sm_count, grad, a.dw_dtype == FT_BF16, rows};
   if (!workspace || !aligned_to(workspace, 256)) return FT_ERR_INVALID_ARG;
   if (workspace_bytes < work.least()) return FT_ERR_CAPACITY;
   const uint32_t piece = work.piece_for(workspace_bytes);
-  loss_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, grad, grad && a.dw_dtype == FT_BF16 && piece < rows);
+  loss_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, (uint32_t)p->sm_count, grad, grad && a.dw_dtype == FT_BF16 && piece < rows);
   a.call_seq = status_seq(p);
   CUtensorMap map_x, map_w, map_p = {}, map_e = {}, map_dw = {};
   if (mma_map(&map_x, a.xc, a.hidden, a.padded, a.hidden) != CUDA_SUCCESS || mma_map(&map_w, a.w, a.hidden, a.vocab, a.ldw) != CUDA_SUCCESS ||
@@ -762,7 +762,7 @@ FT_EXPORT int32_t pool_token_loss_workspace(ft_pool* p, uint64_t rows, uint32_t 
                                             uint64_t* least, uint64_t* best) {
   if (!p || hidden == 0 || hidden % 8 || vocab == 0 || !dtype_ok(dw_dtype) || !least || !best) return FT_ERR_INVALID_ARG;
   if (rows >> 31 || vocab >> 31) return FT_ERR_CAPACITY;
-  const LossWork work{hidden, vocab, with_grad != 0, dw_dtype == FT_BF16, rows};
+  const LossWork work{hidden, vocab, (uint32_t)p->sm_count, with_grad != 0, dw_dtype == FT_BF16, rows};
   *least = rows ? work.least() : 0;
   *best = rows ? work.best() : 0;
   return FT_OK;
