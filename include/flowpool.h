@@ -468,11 +468,12 @@ int32_t pool_embed_grad(ft_pool* pool, const ft_plan* plan, uint32_t mb_begin, u
 /*
  * pool_layer_norm -- y = (x - mean) * rstd * weight + bias for each row, mean = sum(x) / cols,
  * rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps); statistics and products in fp32, y rounded once.
- *   x, y          device [rows, cols] of `dtype` (FT_BF16 or FT_F32), strides ldx, ldy >= cols; y may be x
+ *   x, y          device [rows, cols] of `dtype` (FT_BF16 or FT_F32), strides ldx, ldy >= cols; y may be x with x's stride
  *   weight, bias  device [cols] of `param_dtype`; NULL = ones, zeros
  *   mean, rstd    device fp32 [rows], what the backward pass reads; may be NULL
  * A row's result depends on that row alone (a NaN stays in its row).  Rows whose operands all start on 16-byte boundaries
- * take wide accesses; any other width and stride works element by element.
+ * take wide accesses; any other width and stride works element by element (bf16 at 2/3 of the rate, fp32 at 9/10).  Rows
+ * beyond 16384 elements are read three times, from cache, at a fifth to a fourth of the rate.
  * Errors: cols 0, a type, eps negative or not finite, a NULL or misaligned operand, a stride below cols INVALID_ARG;
  * cols > 2^30 CAPACITY.  rows = 0 does nothing.
  */
@@ -482,11 +483,13 @@ int32_t pool_layer_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void*
 
 /*
  * pool_layer_norm_grad -- with xhat = (x - mean) * rstd and a = weight * dy:
- *   dx = rstd * (a - sum(a) / cols - xhat * sum(a * xhat) / cols)     device [rows, cols] of `dtype`; dx may be dy or x
+ *   dx = rstd * (a - sum(a) / cols - xhat * sum(a * xhat) / cols)     device [rows, cols] of `dtype`; dx may be dy or x,
+ *                                                                     with that one's stride
  *   dweight = sum over rows of dy * xhat, dbias = sum over rows of dy  device fp32 [cols], either may be NULL;
  *             accumulate != 0 adds to what they hold
  * mean and rstd as pool_layer_norm gave them.  Sums over rows are fp32, in an order fixed by the shapes and the device.
  * pool_layer_norm_grad_workspace gives the workspace's size.  rows = 0: dweight and dbias become zero unless accumulating.
+ * Rows beyond 8192 elements (4096 where an operand is off 16 bytes) are read twice, a fourth to a third as fast.
  * Errors as pool_layer_norm; workspace NULL or misaligned INVALID_ARG, too small CAPACITY.
  */
 int32_t pool_layer_norm_grad_workspace(ft_pool* pool, uint64_t rows, uint32_t cols, uint64_t* bytes);
@@ -512,11 +515,16 @@ int32_t pool_layer_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const 
  *   dw[v] = sum over i of d_iv * x[i]     device [vocab, hidden] contiguous, FT_F32 or FT_BF16 (dw_dtype);
  *                                         accumulate != 0 (FT_F32 only) adds to what it holds, as pool_embed_grad does
  * The products run on the tensor cores with fp32 sums; for them d is rounded to bf16, as a probability over a factor of its
- * row, and for dw that factor times x as well (up to 128 rows as two bf16 values).
+ * row, and for dw that factor times x as well (up to 128 rows as two bf16 values).  So is an FT_F32 dw: it is off by some
+ * 1.7e-3 of its norm, where fp32 products would be off by 1e-6.
+ *
+ * The time depends on the values in one way: a row whose loss is above 41 has the logits of its 256 rows that count worked
+ * out once more.  One such row in every 256 makes a long pool_token_loss 2.4 times as long, pool_token_loss_grad 1.25 times.
  *
  * hidden, ldx, ldw, lddx are multiples of 8; x, w, dx and dw start on 16-byte boundaries.  pool_token_loss_workspace
  * gives the smallest workspace (*least) and the one from which more brings nothing (*best; with gradients a piece of the
- * rows at a time has its probabilities there in bf16, and *best stops at pieces of 4 GiB); any size between the two works.
+ * rows at a time has its probabilities there in bf16, and *best stops at pieces of 4 GiB; *least is some 0.6 MiB an SM for a
+ * single row); any size between the two works.
  * Errors: hidden or vocab 0 or a size that is no multiple of 8, a NULL or misaligned operand, a stride below hidden,
  * grad_stride > 1, accumulate with FT_BF16 INVALID_ARG; rows or vocab >= 2^31 CAPACITY; workspace NULL or misaligned
  * INVALID_ARG, below *least CAPACITY.  rows = 0: dw becomes zero unless accumulating.  Asynchronous: TIMEOUT (see there).
@@ -545,7 +553,8 @@ int32_t pool_token_loss_grad(ft_pool* pool, uint64_t rows, uint32_t hidden, uint
  *                   [ceil(n / 256)]), the smallest power of two that brings the block's largest value to 448 or less, from
  *                   2^-100 to 2^100; a positive sqrt(v) is held as at least 2^-9 of its scale.  All zero = no history.
  *                   A block with a value that is not finite reads back as NaN
- * Any alignment of a tensor's elements works; 16-byte starts (8 for float8 states) take wide accesses.  No array of the
+ * Any alignment of a tensor's elements works; 16-byte starts (8 for float8 states) take wide accesses (8-bit states in 0.6 of
+ * the time; fp32 states take the same either way).  No array of the
  * list may overlap another.
  * Errors: lr, eps or a weight_decay not finite, eps < 0, a beta outside [0, 1), step 0, a type, a NULL or misaligned array of
  * a tensor with n > 0 INVALID_ARG; n > 2^40 CAPACITY.
@@ -558,7 +567,7 @@ typedef struct {
   void* copy;
   uint64_t n;
   double weight_decay;
-  uint32_t param_dtype, grad_dtype, state_bits, reserved;
+  uint32_t param_dtype, grad_dtype, state_bits, reserved; /* reserved: not read; 0 */
 } ft_adamw_tensor;
 typedef struct {
   double lr, beta1, beta2, eps;

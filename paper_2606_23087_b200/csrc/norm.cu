@@ -5,7 +5,8 @@
 //              dx = rstd (a - sum(a)/c - xhat sum(a xhat)/c),  dw = sum over rows of dy xhat,  db = sum over rows of dy
 //
 // Both are bound by HBM: a row is read once (two rows backward) and written once, with a dozen operations an element.  32768 rows x
-// 3584 in bf16: forward 82 us (5.7 TB/s; 60 % of the issue slots), backward 125 us (5.6 TB/s, 7 us of it for joining the lines).
+// 3584 in bf16: forward 83 to 90 us (5.2 to 5.7 TB/s; 60 % of the issue slots), backward 122 to 129 us (5.5 to 5.8 TB/s, 7 us of it for joining
+// the lines).  Rows off 16-byte boundaries go element by element: 127 and 198 us in bf16, 94 and 124 for half the rows in fp32.
 //
 //   k_norm          a few warps (one for rows up to 4096 elements, where there are rows enough) hold a row in registers: the
 //                   variance is taken about the mean, not from a difference of sums
@@ -13,7 +14,8 @@
 //                   its registers until its last row, while 16-byte chunks of the following rows are on their way into
 //                   shared memory.  No atomics: partial sums go to the workspace, one line a CTA
 //   k_norm_join     adds the lines of partial sums in line order
-//   k_norm_wide, k_norm_grad_sums, k_norm_grad_cols   rows too long for that
+//   k_norm_wide, k_norm_grad_sums, k_norm_grad_cols   rows too long for that: forward beyond 16384 elements, backward beyond 8192 (4096
+//                   where they are off 16 bytes), at 1 to 1.5 and 1.2 to 2 TB/s of the bytes that must move
 #include <algorithm>
 #include <cmath>
 #include <utility>
