@@ -578,6 +578,124 @@ int32_t pool_adamw_step(ft_pool* pool, const ft_adamw_tensor* tensors, uint32_t 
                         void* stream);
 
 /*
+ * pool_rotary -- rotary positions over the heads of queries, keys or their gradients, with the positions of several axes as
+ * pool_gather_padded writes them (out_pos3) or a single one:
+ *   angle_i = pos[axis_i][row] * freq_i;   (a, b) becomes (a cos - b sin, a sin + b cos) for the pair i of every head
+ *   pos     device int32, row r of axis x at pos[x * pos_ld + r]; any value (the angle is taken modulo a turn in 64-bit
+ *           fixed point: a far position's is off by 2^-33 of a turn at most)
+ *   cfg     host.  freq: host [pairs], radians per position, at most 2^32; axis: host [pairs], 0..2, NULL = all 0 (sections in any
+ *           order are a table); the first 2 * pairs elements of a head are turned, element i with i + pairs (interleaved = 0) or
+ *           2i with 2i + 1; the rest is copied.  inverse != 0 turns back: the backward pass of the same call
+ *   tensors host [n_tensors]: element e of head h of row r lies at src[r * src_row + h * src_head + e] (strides in elements, so
+ *           that heads may be read out of a projection's rows), likewise dst; dst may be src with src's strides.  What is
+ *           written overlaps nothing else of the call
+ * Products in fp32, rounded once.  Heads off 16-byte boundaries, and pairs that are no multiple of 8 (4 in fp32), go element by
+ * element.
+ * Errors: freq NULL, not finite or beyond 2^32, an axis above 2, pairs 0 or more than half of head_dim, a type, a NULL or misaligned
+ * operand, pos_ld < rows with several axes, heads or rows of dst that overlap INVALID_ARG; head_dim > 512, more than 8192 heads, rows >=
+ * 2^31 CAPACITY.  rows = 0 does nothing.
+ */
+#define FT_ROTARY_MAX_DIM 512u
+#define FT_ROTARY_MAX_PAIRS (FT_ROTARY_MAX_DIM / 2)
+#define FT_ROTARY_MAX_HEADS 8192u
+typedef struct {
+  const double* freq;
+  const uint8_t* axis;
+  uint32_t pairs, head_dim, interleaved, inverse;
+} ft_rotary_config;
+typedef struct {
+  const void* src;
+  void* dst;
+  uint64_t src_row, src_head, dst_row, dst_head;
+  uint32_t heads, dtype;
+} ft_rotary_tensor;
+int32_t pool_rotary(ft_pool* pool, uint64_t rows, const int32_t* pos, uint64_t pos_ld, const ft_rotary_config* cfg,
+                    const ft_rotary_tensor* tensors, uint32_t n_tensors, void* stream);
+
+/*
+ * pool_rms_norm -- root-mean-square norm with the residual's addition.  For each row, in fp32:
+ *   s = x + residual,  rstd = 1 / sqrt(sum(s^2) / cols + eps),  y = s * rstd * weight
+ *   x, residual, sum, y   device [rows, cols] of `dtype`, each with its stride; residual NULL = none; sum (receives s) and y may be
+ *                         NULL, and may be x or residual with its stride (not both the same one)
+ *   weight                device [cols] of `param_dtype`; NULL = ones
+ *   q, q_scale            y in 8 bits: device e4m3 [rows, cols] and fp32 [rows, ceil(cols / 128)], strides ldq and ldqs; both or
+ *                         neither.  Of every 128 columns scale = max|y| / 448 (y as fp32 gives it, no less than 2^-110) and
+ *                         q = y / scale; all zero: scale 0; a value that is not finite: scale NaN.  They overlap nothing else
+ *   rstd                  device fp32 [rows], what the backward pass reads; may be NULL
+ * s is normalised as fp32 holds it, before it is rounded into `sum`.  Rows whose operands all start on 16-byte boundaries (q: 8, fp32
+ * input 4) take wide accesses; others go element by element, those with q and rows beyond 16384 elements (fp32 with a residual 12288)
+ * from cache in three passes.
+ * Errors: cols 0, a type, eps negative or not finite, x NULL, none of sum, y and q, q without q_scale or the reverse, a misaligned
+ * operand, a stride below what a row needs INVALID_ARG; cols > 2^30 CAPACITY.  rows = 0 does nothing.
+ */
+int32_t pool_rms_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void* x, uint64_t ldx, const void* residual, uint64_t ldr,
+                      uint32_t dtype, const void* weight, uint32_t param_dtype, float eps, void* sum, uint64_t lds, void* y,
+                      uint64_t ldy, void* q, uint64_t ldq, float* q_scale, uint64_t ldqs, float* rstd, void* stream);
+
+/*
+ * pool_rms_norm_grad -- with s what was normalised (`sum`, or x where there was no residual), xhat = s * rstd and a = weight * dy:
+ *   dx = rstd * (a - xhat * sum(a * xhat) / cols) + dsum   device [rows, cols] of `dtype`: the gradient of x and of the residual
+ *                                                          alike; dsum (NULL = none) is what arrives at `sum` from behind; dx may
+ *                                                          be dy, s or dsum, with that one's stride
+ *   dweight = sum over rows of dy * xhat                   device fp32 [cols], may be NULL; accumulate != 0 adds to what it holds
+ * Sums over rows are fp32, in an order fixed by the shapes and the device.  pool_rms_norm_grad_workspace gives the workspace's size.
+ * rows = 0: dweight becomes zero unless accumulating.  Rows beyond 8192 elements (4096 off 16-byte boundaries) are read twice.
+ * Errors as pool_rms_norm; workspace NULL or misaligned INVALID_ARG, too small CAPACITY.
+ */
+int32_t pool_rms_norm_grad_workspace(ft_pool* pool, uint64_t rows, uint32_t cols, uint64_t* bytes);
+int32_t pool_rms_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const void* dy, uint64_t lddy, const void* s, uint64_t lds,
+                           const void* dsum, uint64_t lddsum, uint32_t dtype, const void* weight, uint32_t param_dtype,
+                           const float* rstd, void* dx, uint64_t lddx, float* dweight, uint32_t accumulate, void* workspace,
+                           uint64_t workspace_bytes, void* stream);
+
+/*
+ * pool_grad_norm -- the 2-norm over a list of gradients (host array, read before the call returns) and the factor that pool_adamw_step
+ * takes as grad_scale to clip them to max_norm:
+ *   total = more + sum over all elements of g^2;  norm = sqrt(total);  factor = norm > max_norm ? max_norm / norm : 1
+ *   more    device double, or NULL: squares that others have summed (another call's, or other ranks')
+ *   sumsq   device double, may be NULL and may be `more`: receives total.  Ranks that hold parts of the gradients take sumsq of
+ *           their parts, add them up, and get norm and factor by a call with no tensors and more = that sum
+ *   norm, factor  device fp32 [1], may be NULL.  A norm that is no number makes the factor none either
+ * Squares are added in fp32 over 64 bytes a thread, in fp64 beyond that and wherever they leave fp32's range.  Any alignment works at
+ * the same rate.
+ * Errors: a type, a NULL or misaligned gradient with n > 0, max_norm negative or NaN where factor is wanted, a misaligned output,
+ * workspace NULL or misaligned INVALID_ARG; n > 2^40, workspace too small CAPACITY.
+ */
+typedef struct {
+  const void* grad;
+  uint64_t n;
+  uint32_t dtype, reserved; /* reserved: not read; 0 */
+} ft_grad_tensor;
+int32_t pool_grad_norm_workspace(ft_pool* pool, uint64_t* bytes);
+int32_t pool_grad_norm(ft_pool* pool, const ft_grad_tensor* tensors, uint32_t n_tensors, double max_norm, const double* more,
+                       double* sumsq, float* norm, float* factor, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * pool_token_logprobs -- how likely a model holds given tokens, without the matrix of logits: scoring, evaluation, the next token's
+ * alternatives.  With z = logit_scale * x[i] . W^T (bf16 operands, fp32 sums; logit_scale: 1 / temperature) and p = softmax(z):
+ *   logprob[i] = z_token - log(sum over v of exp(z_v))     device fp32 [rows], where tokens are given
+ *   entropy[i] = - sum over v of p_v log p_v               device fp32 [rows], may be NULL
+ *   top_ids, top_logprobs   device int32 and fp32 [rows, top], the `top` largest logits' ids and log probabilities, largest first,
+ *                           equal logits by ascending id; top = 0: neither
+ *   tokens  device int32 [rows], -100: the row counts nothing (logprob, entropy and top_logprobs 0, top_ids -1), costs next to
+ *           nothing and its x reaches no result.  NULL: every row counts and logprob must be NULL.  Asynchronous: any
+ *           other token outside [0, vocab) BAD_TOKEN_ID (detail = row; the row is treated as -100)
+ * Places beyond the vocabulary have id -1 and log probability -inf.  A logit that is NaN or +inf makes logprob, entropy and top_logprobs NaN;
+ * as an alternative a NaN counts as -inf.
+ * The gradient of the log probability is pool_token_loss_grad's with -grad_loss.
+ * x, w, hidden, ldx, ldw as in pool_token_loss.  pool_token_logprobs_workspace gives the smallest workspace and the one from which more
+ * brings nothing; any size between the two works (alternatives keep a piece of the rows' logits in the workspace, up to 4 GiB).
+ * Errors: as pool_token_loss; logit_scale not positive or not finite, logprob NULL with tokens or the reverse, top without top_ids and
+ * top_logprobs INVALID_ARG; top > 32 CAPACITY.  rows = 0 does nothing.  Asynchronous: TIMEOUT, as pool_token_loss.
+ */
+#define FT_LOGPROBS_MAX_TOP 32u
+int32_t pool_token_logprobs_workspace(ft_pool* pool, uint64_t rows, uint32_t hidden, uint32_t vocab, uint32_t top, uint64_t* least,
+                                      uint64_t* best);
+int32_t pool_token_logprobs(ft_pool* pool, uint64_t rows, uint32_t hidden, uint32_t vocab, const void* x, uint64_t ldx, const void* w,
+                            uint64_t ldw, const int32_t* tokens, float logit_scale, float* logprob, float* entropy, uint32_t top,
+                            int32_t* top_ids, float* top_logprobs, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
  * Kernel timing for benchmarks.  While enabled, the library brackets each of its copy kernels with CUDA
  * events on the stream that kernel is launched on (the host-tier kernels run on the pool's side stream).
  * pool_profile_read synchronises the device, adds up the elapsed time and launch count per kernel class

@@ -26,7 +26,9 @@ EXPORTS = (
     "pool_create", "pool_register_samples", "pool_write_embeddings", "pool_write_embeddings_noalloc",
     "pool_plan_microbatches", "plan_summary",
     "plan_arrays", "plan_destroy", "pool_gather_packed", "pool_gather_list", "pool_set_span_grids", "pool_gather_padded", "pool_embed_grad", "pool_layer_norm", "pool_layer_norm_grad", "pool_layer_norm_grad_workspace", "pool_token_loss",
-    "pool_token_loss_grad", "pool_token_loss_workspace", "pool_adamw_step", "pool_free", "pool_status", "pool_stats",
+    "pool_token_loss_grad", "pool_token_loss_workspace", "pool_adamw_step",
+    "pool_rotary", "pool_rms_norm", "pool_rms_norm_grad", "pool_rms_norm_grad_workspace", "pool_grad_norm", "pool_grad_norm_workspace",
+    "pool_token_logprobs", "pool_token_logprobs_workspace", "pool_free", "pool_status", "pool_stats",
     "pool_ready_count", "pool_take_ready", "pool_backing", "pool_ipc_export", "pool_ipc_open", "pool_ipc_close", "pool_export_mapping", "pool_import_mapping", "pool_export_samples", "pool_import_samples",
     "pool_get_tuning", "pool_set_tuning", "pool_profile_enable", "pool_profile_read", "pool_debug_span_pages", "pool_debug_ring", "pool_debug_translate", "pool_destroy", "flowpool_last_cuda_error",
 )
@@ -79,6 +81,32 @@ class AdamwConfig(C.Structure):
                 ("grad_scale", C.c_void_p), ("step", C.c_uint64)]
 
 
+class RotaryConfig(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("axis", C.c_void_p), ("pairs", C.c_uint32), ("head_dim", C.c_uint32),
+                ("interleaved", C.c_uint32), ("inverse", C.c_uint32)]
+
+
+class RotaryTensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("src_row", C.c_uint64), ("src_head", C.c_uint64),
+                ("dst_row", C.c_uint64), ("dst_head", C.c_uint64), ("heads", C.c_uint32), ("dtype", C.c_uint32)]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("n", C.c_uint64), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+def rotary_config(freqs, axes, head_dim, interleaved=False, inverse=False):
+    """A RotaryConfig that keeps its host arrays alive; `axes` None = one axis."""
+    f = np.ascontiguousarray(freqs, dtype=np.float64)
+    a = None if axes is None else np.ascontiguousarray(axes, dtype=np.uint8)
+    if a is not None and len(a) != len(f):
+        raise ValueError("one axis for each frequency")
+    cfg = RotaryConfig(freq=f.ctypes.data, axis=None if a is None else a.ctypes.data, pairs=len(f), head_dim=head_dim,
+                       interleaved=1 if interleaved else 0, inverse=1 if inverse else 0)
+    cfg.keep = (f, a)
+    return cfg
+
+
 TUNING_FIELDS = ("dev_ctas_per_sm", "scatter_ctas_per_sm", "scatter_group", "chunk_shift", "host_ctas", "host_store_ctas",
                  "gather_unroll", "grad_ctas_per_sm", "grad_hot_threshold", "remote_ctas", "peers_remote", "scatter_smem_carveout", "gather_smem_carveout",
                  "bulk_wait_limit_us", "bulk_timeout_test", "host_copy_engine")
@@ -119,7 +147,7 @@ def lib():
         if not os.path.exists(SO):
             build()
         _lib = C.CDLL(SO)
-        P, u32, u64, i32, f32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32, C.c_float
+        P, u32, u64, i32, f32, f64 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32, C.c_float, C.c_double
         sig = {
             "pool_create": [P, P, P, P],
             "pool_register_samples": [P, u32, P, P, P, P, P, P, P],
@@ -141,6 +169,14 @@ def lib():
             "pool_token_loss": [P, u64, u32, u32, P, u64, P, u64, P, P, P, P, u64, P],
             "pool_token_loss_grad": [P, u64, u32, u32, P, u64, P, u64, P, P, u32, P, P, P, u64, P, u32, u32, P, u64, P],
             "pool_adamw_step": [P, P, u32, P, P],
+            "pool_rotary": [P, u64, P, u64, P, P, u32, P],
+            "pool_rms_norm": [P, u64, u32, P, u64, P, u64, u32, P, u32, f32, P, u64, P, u64, P, u64, P, u64, P, P],
+            "pool_rms_norm_grad_workspace": [P, u64, u32, P],
+            "pool_rms_norm_grad": [P, u64, u32, P, u64, P, u64, P, u64, u32, P, u32, P, P, u64, P, u32, P, u64, P],
+            "pool_grad_norm_workspace": [P, P],
+            "pool_grad_norm": [P, P, u32, f64, P, P, P, P, P, u64, P],
+            "pool_token_logprobs_workspace": [P, u64, u32, u32, u32, P, P],
+            "pool_token_logprobs": [P, u64, u32, u32, P, u64, P, u64, P, f32, P, P, u32, P, P, P, u64, P],
             "pool_free": [P, P, u32, P],
             "pool_status": [P, P, P],
             "pool_stats": [P, P],
@@ -327,6 +363,60 @@ class Pool:
         if not isinstance(tensors, C.Array):
             tensors = (AdamwTensor * len(tensors))(*tensors)
         return lib().pool_adamw_step(self.h, tensors, len(tensors), C.byref(cfg), stream or None)
+
+    def rotary(self, rows, pos_ptr: int, pos_ld, cfg: RotaryConfig, tensors, stream: int = 0):
+        """pool_rotary; `tensors` is a ctypes array of RotaryTensor or a list of them."""
+        if not isinstance(tensors, C.Array):
+            tensors = (RotaryTensor * len(tensors))(*tensors)
+        return lib().pool_rotary(self.h, rows, pos_ptr or None, pos_ld, C.byref(cfg), tensors, len(tensors), stream or None)
+
+    def rms_norm(self, rows, cols, x_ptr: int, ldx, residual_ptr: int, ldr, dtype, weight_ptr: int, param_dtype, eps, sum_ptr: int, lds,
+                 y_ptr: int, ldy, q_ptr: int = 0, ldq=0, q_scale_ptr: int = 0, ldqs=0, rstd_ptr: int = 0, stream: int = 0):
+        return lib().pool_rms_norm(self.h, rows, cols, x_ptr or None, ldx, residual_ptr or None, ldr, dtype, weight_ptr or None, param_dtype,
+                                   eps, sum_ptr or None, lds, y_ptr or None, ldy, q_ptr or None, ldq, q_scale_ptr or None, ldqs,
+                                   rstd_ptr or None, stream or None)
+
+    def rms_norm_grad_workspace(self, rows, cols):
+        n = C.c_uint64()
+        rc = lib().pool_rms_norm_grad_workspace(self.h, rows, cols, C.byref(n))
+        if rc:
+            raise FlowpoolError(rc, "pool_rms_norm_grad_workspace")
+        return n.value
+
+    def rms_norm_grad(self, rows, cols, dy_ptr: int, lddy, s_ptr: int, lds, dsum_ptr: int, lddsum, dtype, weight_ptr: int, param_dtype,
+                      rstd_ptr: int, dx_ptr: int, lddx, dweight_ptr: int, accumulate, ws_ptr: int, ws_bytes, stream: int = 0):
+        return lib().pool_rms_norm_grad(self.h, rows, cols, dy_ptr or None, lddy, s_ptr or None, lds, dsum_ptr or None, lddsum, dtype,
+                                        weight_ptr or None, param_dtype, rstd_ptr or None, dx_ptr or None, lddx, dweight_ptr or None,
+                                        1 if accumulate else 0, ws_ptr or None, ws_bytes, stream or None)
+
+    def grad_norm_workspace(self):
+        n = C.c_uint64()
+        rc = lib().pool_grad_norm_workspace(self.h, C.byref(n))
+        if rc:
+            raise FlowpoolError(rc, "pool_grad_norm_workspace")
+        return n.value
+
+    def grad_norm(self, tensors, max_norm, more_ptr: int, sumsq_ptr: int, norm_ptr: int, factor_ptr: int, ws_ptr: int, ws_bytes,
+                  stream: int = 0):
+        """pool_grad_norm; `tensors` is a ctypes array of GradTensor (kept by the caller from step to step) or a list of them."""
+        if not isinstance(tensors, C.Array):
+            tensors = (GradTensor * len(tensors))(*tensors)
+        return lib().pool_grad_norm(self.h, tensors, len(tensors), max_norm, more_ptr or None, sumsq_ptr or None, norm_ptr or None,
+                                    factor_ptr or None, ws_ptr or None, ws_bytes, stream or None)
+
+    def token_logprobs_workspace(self, rows, hidden, vocab, top=0):
+        """(least, best) workspace bytes of token_logprobs."""
+        a, b = C.c_uint64(), C.c_uint64()
+        rc = lib().pool_token_logprobs_workspace(self.h, rows, hidden, vocab, top, C.byref(a), C.byref(b))
+        if rc:
+            raise FlowpoolError(rc, "pool_token_logprobs_workspace")
+        return a.value, b.value
+
+    def token_logprobs(self, rows, hidden, vocab, x_ptr: int, ldx, w_ptr: int, ldw, tokens_ptr: int, logit_scale, logprob_ptr: int,
+                       entropy_ptr: int, top, top_ids_ptr: int, top_logprobs_ptr: int, ws_ptr: int, ws_bytes, stream: int = 0):
+        return lib().pool_token_logprobs(self.h, rows, hidden, vocab, x_ptr or None, ldx, w_ptr or None, ldw, tokens_ptr or None,
+                                         logit_scale, logprob_ptr or None, entropy_ptr or None, top, top_ids_ptr or None,
+                                         top_logprobs_ptr or None, ws_ptr or None, ws_bytes, stream or None)
 
     def free(self, slots, stream: int = 0):
         slots = _u32(slots)

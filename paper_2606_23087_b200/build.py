@@ -6,7 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SO = os.path.join(HERE, "libflowpool.so")
-SOURCES = ["pool.cu", "plan.cu", "gather.cu", "peer.cu", "backbone.cu", "norm.cu", "adamw.cu", "loss.cu"]
+SOURCES = ["pool.cu", "plan.cu", "gather.cu", "peer.cu", "backbone.cu", "norm.cu", "adamw.cu", "loss.cu",
+           "rotary.cu", "rms.cu", "grad_norm.cu", "logprobs.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-fvisibility=hidden"]
 

@@ -372,6 +372,7 @@ struct ft_pool {
   int scatter_ctas_per_sm = 0;  // resident CTAs per SM of the device-tier scatter kernel; 0 = the measured default
   bool grad_attr_set = false;   // k_embed_grad_hot's shared-memory opt-in done
   bool loss_attr_set = false;   // the token loss's products' shared-memory opt-in done
+  bool score_attr_set = false;  // the same for the log probabilities
   int grad_hot_threshold = 0;   // rows from which an id takes k_embed_grad_hot; 0 = rows / (8 x grid), at least 64
   int grad_ctas_per_sm = 6;     // CTAs per SM of k_embed_grad (each owns the table rows v with v % grid == its index)
   int gather_unroll = 0;        // 16-byte vectors per lane in flight in k_gather (4 or 8); 0 = chosen per launch

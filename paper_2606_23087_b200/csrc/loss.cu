@@ -47,7 +47,6 @@ constexpr uint32_t kHighBlocks = 66;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kMinusInf = 0xFF800000u;
 constexpr float kSumLimit = 0x1p60f;  // a row's sum above this wants another reference
-constexpr int32_t kNoLabel = -100;
 constexpr uint32_t kPieceRowsMost = 65536;
 constexpr uint32_t kHighRows = 2 * kMmaTile;  // rows of a tile of dx and dw
 
@@ -81,24 +80,6 @@ struct LossPiece {
 constexpr uint32_t kPickRows = 32;    // rows of a CTA; 8 where that alone fills the device, a row a warp
 constexpr uint32_t kPickFew = 8;
 constexpr uint32_t kPickFewUpTo = 4096;
-
-__device__ __forceinline__ bool has_label(int32_t l, uint32_t vocab) { return (uint32_t)l < vocab; }
-
-// this thread's share of the rows among the first n that count
-__device__ __forceinline__ uint32_t count_labels(const int32_t* labels, uint32_t n, uint32_t vocab) {
-  const uint32_t head = min(n, (uint32_t)((16 - (reinterpret_cast<uintptr_t>(labels) & 15)) & 15) / 4), quads = (n - head) / 4;
-  uint32_t c = 0;
-  if (threadIdx.x < head) c += has_label(labels[threadIdx.x], vocab);
-  const int4* q = reinterpret_cast<const int4*>(labels + head);
-#pragma unroll 8
-  for (uint32_t i = threadIdx.x; i < quads; i += blockDim.x) {
-    const int4 l = q[i];
-    c += has_label(l.x, vocab) + has_label(l.y, vocab) + has_label(l.z, vocab) + has_label(l.w, vocab);
-  }
-  const uint32_t r = head + 4 * quads + threadIdx.x;
-  if (r < n) c += has_label(labels[r], vocab);
-  return c;
-}
 
 // A CTA takes kRows rows; where they go it learns by counting the labels before them itself (a piece's labels stay in L2),
 // so nothing has to wait for another CTA.
@@ -190,11 +171,6 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
 
 // ---- the three products ---------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp; results below 2^-126 are zero
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // 32 bytes in one access: a whole sector a lane, where 16 bytes would write it in halves
 __device__ __forceinline__ void store32(void* p, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -203,10 +179,6 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* v) {
 __device__ __forceinline__ void load32(const float* p, float (&v)[8]) {
   asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p) : "memory");
-}
-
-__device__ __forceinline__ void give_up(const PoolView& v, uint64_t call_seq, bool lost) {
-  if (lost && threadIdx.x == 0) note_error(v, call_seq, FT_ERR_TIMEOUT, blockIdx.x);
 }
 
 // z by tiles; a lane owns a row's 128 columns.  kRedo: only the row tiles whose reference has changed.

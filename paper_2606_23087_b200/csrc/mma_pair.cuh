@@ -342,6 +342,10 @@ __device__ __forceinline__ void mma_pair_tiles(const CUtensorMap& map_a, const C
   *lost_out = bar->lost != 0;
 }
 
+__device__ __forceinline__ void give_up(const PoolView& v, uint64_t call_seq, bool lost) {
+  if (lost && threadIdx.x == 0) note_error(v, call_seq, FT_ERR_TIMEOUT, blockIdx.x);
+}
+
 // A matrix of bf16 rows, brought in 64 x 64 boxes; reads beyond its extents give zeros.  With box_rows = 32 the map of a store,
 // whose values may be fp32 (32 columns a box).
 inline CUresult mma_map(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows = 64, bool fp32 = false) {

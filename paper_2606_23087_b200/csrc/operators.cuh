@@ -95,6 +95,33 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
+__device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp; results below 2^-126 are zero
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// ---- rows with a label (a token of the vocabulary) and rows without one -------------------------------------------
+
+constexpr int32_t kNoLabel = -100;
+__device__ __forceinline__ bool has_label(int32_t l, uint32_t vocab) { return (uint32_t)l < vocab; }
+
+// this thread's share of the rows among the first n that count
+__device__ __forceinline__ uint32_t count_labels(const int32_t* labels, uint32_t n, uint32_t vocab) {
+  const uint32_t head = min(n, (uint32_t)((16 - (reinterpret_cast<uintptr_t>(labels) & 15)) & 15) / 4), quads = (n - head) / 4;
+  uint32_t c = 0;
+  if (threadIdx.x < head) c += has_label(labels[threadIdx.x], vocab);
+  const int4* q = reinterpret_cast<const int4*>(labels + head);
+#pragma unroll 8
+  for (uint32_t i = threadIdx.x; i < quads; i += blockDim.x) {
+    const int4 l = q[i];
+    c += has_label(l.x, vocab) + has_label(l.y, vocab) + has_label(l.z, vocab) + has_label(l.w, vocab);
+  }
+  const uint32_t r = head + 4 * quads + threadIdx.x;
+  if (r < n) c += has_label(labels[r], vocab);
+  return c;
+}
+
 // 16 bytes at a shared-memory address (32 bits: a generic pointer kept in a structure is read as one, at twice the latency)
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16_async(uint32_t shared_dst, const void* gmem_src) {
