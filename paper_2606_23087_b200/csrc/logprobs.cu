@@ -7,6 +7,8 @@
 //   k_score_pick  takes the rows that count out of a piece of the rows: a dense copy of their x, their tokens and row numbers
 //   k_score       z by tiles; a row of a tile gives max, S and U of 128 columns (a segment), each about the segment's own maximum: every
 //                 term of U is negative, so nothing cancels in an entropy; the token's logit; and with alternatives z itself in fp32
+//   k_score_few   the same for up to 64 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
+//                 of x in its columns, so that no product is spent on rows that are not there; segments of 32 columns
 //   k_score_join  joins a row's segments.  Alternatives: the `top` segments with the largest maxima (equal ones: the first) hold the `top`
 //                 largest logits, so only those are read again
 //
@@ -19,6 +21,8 @@
 namespace ft {
 
 constexpr uint32_t kSegCols = 128;     // columns of a segment: an epilogue warp's
+constexpr uint32_t kFewCols = 32;      // the same where the rows are few
+constexpr uint32_t kFewRows = 64;      // rows that count as few
 // The tensor cores truncate at every addition of 16 products, all one way: tiles of 256 rows are summed in parts of kScorePart blocks of K,
 // the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
 constexpr uint32_t kScorePart = 16, kScoreHigh = 66;
@@ -28,6 +32,8 @@ constexpr float kLeastExponent = -300.f;    // 2^-300 is zero; finite, so that i
 
 struct ScorePiece {
   uint32_t rows, hidden, vocab, segs, padded, pairs, top, ld_z;
+  uint32_t few;              // few rows: all of them are there, counted or not, and a row's segments lie side by side
+  uint32_t held;             // the join keeps its rows' maxima in shared memory
   uint64_t row0, ldx;
   const __nv_bfloat16* x;
   const int32_t* tokens;
@@ -39,7 +45,7 @@ struct ScorePiece {
   uint32_t* count;          // rows of the piece that count
   int32_t *row_of, *token;  // [count] row in the piece, token
   float* target;            // [count] the token's logit
-  float *most, *sum, *moment;  // [segs][rows] max, S, U of a row's segment
+  float *most, *sum, *moment;  // max, S, U of a row's segment: [segs][rows], few rows [rows][segs]
   __nv_bfloat16* xc;        // [padded][hidden]
   float* z;                 // [padded][ld_z]
 };
@@ -93,6 +99,28 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
   }
 }
 
+// max, S and U of a lane's segment, about its maximum
+struct SegStats {
+  float most, sum, moment;
+};
+template <uint32_t kCols, class Z>
+__device__ __forceinline__ SegStats segment_stats(Z&& z, float scale) {
+  float most = -INFINITY;
+#pragma unroll
+  for (uint32_t j = 0; j < kCols; j += 2) most = fmaxf(most, fmaxf(z(j), z(j + 1)));
+  F2 sums = f2(0.f), moments = f2(0.f);
+  const F2 less = f2(most == -INFINITY ? 0.f : -most), by = f2(scale * kScoreLog2e);
+#pragma unroll
+  for (uint32_t j = 0; j < kCols; j += 2) {
+    const float2 t = parts((f2(z(j), z(j + 1)) + less) * by);
+    const float u0 = max_with_nan(t.x, kLeastExponent), u1 = max_with_nan(t.y, kLeastExponent);
+    const F2 e = f2(exp2_fast(u0), exp2_fast(u1));
+    sums = sums + e;
+    moments = fma(e, f2(u0, u1), moments);
+  }
+  return SegStats{most, sum(sums), sum(moments)};
+}
+
 // z by tiles; a lane owns a row's segment
 template <bool kKeep, int kHigh>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
@@ -113,7 +141,9 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
       if (i >= tiles) return MmaTile{0, 0, 0, 0, 0};
       // bands of 2048 rows, all columns of a band before the next: a band's x stays in L2
       constexpr uint32_t kBand = 8 / kHigh;
-      const uint32_t band = i / (kBand * n_tiles), in = i - band * kBand * n_tiles, rows = min(kBand, m_tiles - band * kBand), m = band * kBand + in % rows;
+      const uint32_t band = i / (kBand * n_tiles), in = i - band * kBand * n_tiles, rows = min(kBand, m_tiles - band * kBand);
+      // the row tiles' order shifts from column to column: else a pair might meet the same ones again and again, and never the short last one
+      const uint32_t m = band * kBand + (in + in / rows) % rows;
       return MmaTile{m * kHigh * kMmaTile, in / rows * kMmaTile, part * kPart, min((part + 1) * kPart, k_blocks), min((uint32_t)kHigh, blocks - m * kHigh)};
     },
     [&](const MmaTile& t, uint32_t row) {
@@ -157,32 +187,197 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
           MmaOut().put<false>(&map_z, (int32_t)(c0 + c), (int32_t)(t.m + row),
                               [&](uint32_t j) { return make_uint4(z[c / 32][4 * j], z[c / 32][4 * j + 1], z[c / 32][4 * j + 2], z[c / 32][4 * j + 3]); });
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (uint32_t j = 0; j < kSegCols; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(z[j / 32][j % 32]), __uint_as_float(z[j / 32][j % 32 + 1])));
-      F2 sums = f2(0.f), moments = f2(0.f);
-      const F2 less = f2(top == -INFINITY ? 0.f : -top), scale = f2(a.scale * kScoreLog2e);
-#pragma unroll
-      for (uint32_t j = 0; j < kSegCols; j += 2) {
-        const float2 t2 = parts((f2(__uint_as_float(z[j / 32][j % 32]), __uint_as_float(z[j / 32][j % 32 + 1])) + less) * scale);
-        const float u0 = max_with_nan(t2.x, kLeastExponent), u1 = max_with_nan(t2.y, kLeastExponent);
-        const F2 e = f2(exp2_fast(u0), exp2_fast(u1));
-        sums = sums + e;
-        moments = fma(e, f2(u0, u1), moments);
-      }
+      const SegStats g = segment_stats<kSegCols>([&](uint32_t j) { return __uint_as_float(z[j / 32][j % 32]); }, a.scale);
       if (m < n) {
         const uint64_t at = (uint64_t)(c0 / kSegCols) * a.rows + m;
-        a.most[at] = top;
-        a.sum[at] = sum(sums);
-        a.moment[at] = sum(moments);
+        a.most[at] = g.most;
+        a.sum[at] = g.sum;
+        a.moment[at] = g.moment;
       }
     });
   give_up(v, a.call_seq, lost);
 }
 
+// ---- few rows -------------------------------------------------------------------------------------------------------
+
+// A CTA takes a contiguous run of W's rows, 128 of them (four segments) a tile: D = W x^T, a vocabulary entry a lane of the tensor
+// memory, a row of x a column.  The products of up to kScorePart blocks of K go into columns of their own, as many as half of the tensor
+// memory holds; its other half takes the next tile meanwhile.
+//
+// Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 4..7 epilogue.  Waits are bounded as in mma_pair_tiles, and given up the same way.
+constexpr int kFewThreads = 256;
+constexpr uint32_t kFewTile = 128;                       // W's rows of a tile
+constexpr uint32_t kFewBox = kFewCols * kMmaK * 2;       // bytes of a box of W: a segment's rows, 64 columns of K
+template <uint32_t kN>
+constexpr uint32_t kFewStage = kFewTile * kMmaK * 2 + kN * kMmaK * 2;
+template <uint32_t kN>
+constexpr uint32_t kFewStages = kN == 32 ? 10 : 8;
+constexpr uint32_t kFewTurn = 32 * 33 * 4;               // bytes of a warp's 32 x 32 logits, turned over
+template <uint32_t kN>
+constexpr size_t kFewSmem = kFewStages<kN> * (size_t)kFewStage<kN> + 4 * kFewTurn + 1024 + 256;
+
+struct FewBarriers {
+  uint64_t full[10], empty[10], acc_full[2], acc_empty[2], drain;
+  uint32_t tmem, lost;
+};
+static_assert(sizeof(FewBarriers) <= 256 && kFewSmem<32> <= 227 * 1024 && kFewSmem<64> <= 227 * 1024, "kFewSmem");
+
+__device__ __forceinline__ void few_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void few_commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void few_product(uint32_t tmem, uint64_t da, uint64_t db, uint32_t idesc, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(tmem), "l"(da), "l"(db), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+
+template <uint32_t kN, bool kKeep>
+__global__ void __launch_bounds__(kFewThreads, 1)
+k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
+            const __grid_constant__ ScorePiece a) {
+  extern __shared__ uint8_t smem_raw[];
+  constexpr uint32_t kStages = kFewStages<kN>, kStage = kFewStage<kN>;
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* turned = reinterpret_cast<float*>(stages + kStages * kStage);
+  FewBarriers* bar = reinterpret_cast<FewBarriers*>(stages + kStages * kStage + 4 * kFewTurn);
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  let_next_start();
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < kStages; ++s) { mbar_init(&bar->full[s], 1); mbar_init(&bar->empty[s], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar->acc_full[i], 1); mbar_init(&bar->acc_empty[i], 4); }
+    mbar_init(&bar->drain, 1);
+    bar->lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bar->tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  after_previous();
+  const uint32_t tmem = bar->tmem, base = smem_u32(stages);
+  const uint32_t k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
+  const uint32_t parts = min((k_blocks + kScorePart - 1) / kScorePart, 256 / kN), each = (k_blocks + parts - 1) / parts;
+  const uint32_t seg0 = (uint32_t)((uint64_t)a.segs * blockIdx.x / gridDim.x), seg1 = (uint32_t)((uint64_t)a.segs * (blockIdx.x + 1) / gridDim.x);
+  const uint64_t limit_ns = mma_wait_limit(v, k_blocks);
+  bool lost = false;
+  if (warp == 0 && lane == 0) {
+    uint32_t it = 0;
+    for (uint32_t seg = seg0; seg < seg1 && !lost; seg += 4) {
+      const uint32_t boxes = min(4u, seg1 - seg);
+      for (uint32_t k = 0; k < k_blocks; ++k, ++it) {
+        const uint32_t s = it % kStages, at = base + s * kStage;
+        if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
+        mbar_expect_tx(&bar->full[s], boxes * kFewBox + kN * kMmaK * 2 + v.bulk_tx_slack);  // the slack: a test hook, 0
+        for (uint32_t b = 0; b < boxes; ++b) few_box(at + b * kFewBox, &map_w, (int32_t)(k * kMmaK), (int32_t)((seg + b) * kFewCols), &bar->full[s]);
+        few_box(at + kFewTile * kMmaK * 2, &map_x, (int32_t)(k * kMmaK), 0, &bar->full[s]);
+      }
+    }
+    // what still arrives in shared memory: the loads of the last stages, and the signals that their products are done
+    const uint32_t j0 = it > kStages ? it - kStages : 0;
+    if (lost)
+      for (uint32_t j = j0; j < it; ++j) mbar_wait_bounded(&bar->full[j % kStages], (j / kStages) & 1, limit_ns);
+    for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kStages], (j / kStages) & 1, limit_ns);
+  } else if (warp == 1 && lane == 0) {
+    constexpr uint32_t kInstr = 1u << 4 | 1u << 7 | 1u << 10 | (kN >> 3) << 17 | (kFewTile >> 4) << 24;  // fp32 sums of bf16 x bf16
+    uint32_t it = 0, tile = 0;
+    for (uint32_t seg = seg0; seg < seg1 && !lost; seg += 4, ++tile) {
+      const uint32_t acc = tile & 1;
+      if (!mbar_wait_bounded(&bar->acc_empty[acc], ((tile >> 1) & 1) ^ 1, limit_ns)) { lost = true; break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      for (uint32_t k = 0; k < k_blocks; ++k, ++it) {
+        const uint32_t s = it % kStages, sa = base + s * kStage, sb = sa + kFewTile * kMmaK * 2;
+        if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t part = k / each;
+#pragma unroll
+        for (uint32_t j = 0; j < kMmaK / 16; ++j)
+          few_product(tmem + acc * 256 + part * kN, mma_desc<false>(sa + j * kMmaStep<false>), mma_desc<false>(sb + j * kMmaStep<false>), kInstr,
+                      k > part * each || j > 0);
+        few_commit(&bar->empty[s]);
+      }
+      if (!lost) few_commit(&bar->acc_full[acc]);
+    }
+    if (lost) {  // products under way still read shared memory and write tensor memory
+      few_commit(&bar->drain);
+      mbar_wait_bounded(&bar->drain, 0, limit_ns);
+    }
+  } else if (warp >= 4) {
+    const uint32_t quarter = warp & 3;
+    float* mine = turned + quarter * (kFewTurn / 4);
+    int32_t token[kN / 32];  // of the rows that the lane owns
+#pragma unroll
+    for (uint32_t g = 0; g < kN / 32; ++g) token[g] = a.tokens && g * 32 + lane < a.rows ? a.tokens[a.row0 + g * 32 + lane] : kNoLabel;
+    const uint32_t used = (k_blocks + each - 1) / each;  // parts that hold something
+    uint32_t tile = 0;
+    for (uint32_t s0 = seg0; s0 < seg1 && !lost; s0 += 4, ++tile) {
+      const uint32_t acc = tile & 1, seg = s0 + quarter;
+      lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], (tile >> 1) & 1, limit_ns));
+      if (lost) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      uint32_t z[kN / 32][32];
+#pragma unroll
+      for (uint32_t g = 0; g < kN / 32; ++g) {
+        const uint32_t at = tmem + acc * 256 + g * 32 + (quarter << 21);
+        tmem_load32(at, z[g]);
+        tmem_wait();
+        for (uint32_t p = 1; p < used; ++p) {
+          uint32_t more[32];
+          tmem_load32(at + p * kN, more);
+          tmem_wait();
+#pragma unroll
+          for (uint32_t j = 0; j < 32; ++j) z[g][j] = __float_as_uint(__uint_as_float(z[g][j]) + __uint_as_float(more[j]));
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(smem_u32(&bar->acc_empty[acc]));
+      if (seg >= seg1) continue;
+      const uint32_t id = seg * kFewCols + lane;
+#pragma unroll
+      for (uint32_t g = 0; g < kN / 32; ++g) {
+        if (g * 32 >= a.rows) break;
+        __syncwarp();
+#pragma unroll
+        for (uint32_t j = 0; j < 32; ++j) {
+          const float x = id < a.vocab ? __uint_as_float(z[g][j]) : -INFINITY;
+          if (kKeep && g * 32 + j < a.rows) a.z[(uint64_t)(g * 32 + j) * a.ld_z + id] = x;
+          mine[j * 33 + lane] = x;
+        }
+        __syncwarp();
+        const uint32_t m = g * 32 + lane;
+        if (m >= a.rows) continue;
+        const uint32_t token_at = (uint32_t)token[g] - seg * kFewCols;
+        if (token_at < kFewCols) a.target[m] = mine[lane * 33 + token_at];
+        const SegStats t = segment_stats<kFewCols>([&](uint32_t j) { return mine[lane * 33 + j]; }, a.scale);
+        const uint64_t at = (uint64_t)m * a.segs + seg;
+        a.most[at] = t.most;
+        a.sum[at] = t.sum;
+        a.moment[at] = t.moment;
+      }
+      __syncwarp();
+    }
+  }
+  if (lost) bar->lost = 1;
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  give_up(v, a.call_seq, bar->lost != 0);
+}
+
 // ---- joining the segments of a row ----------------------------------------------------------------------------------
 
-// An order of (value, place): larger values first, equal ones by place.  A NaN counts as -inf, -0 as 0.
+// An order of (value, place): larger values first, equal ones by place.  A NaN counts as -inf, -0 as 0.  No key is zero.
 __device__ __forceinline__ uint64_t order_key(float z, uint32_t place) {
   const uint32_t b = __float_as_uint(fmaxf(z, -INFINITY) + 0.f);
   return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~place;
@@ -198,116 +393,174 @@ __device__ __forceinline__ uint64_t warp_max(uint64_t key) {
   return (uint64_t)hi << 32 | lo;
 }
 
-constexpr uint32_t kScoreJoinWarps = 16;  // rows of a CTA: a sector of the segments' numbers serves eight of them
-constexpr uint32_t kFewPicks = 64;        // logits that a row's alternatives are usually among
+// The `top` first of many keys, by a warp: each(f) calls f(key) for every key of a lane, all lanes as often (0: no key); put(rank, key) is
+// called for each of the first.  `least`: a key that none of them is below, or 0.  Without one, or where it leaves too many, it is the
+// `top`-th largest of the lanes' own first keys.  What it leaves, usually little more than `top`, is ranked by counting.
+constexpr uint32_t kFewPicks = 64;  // keys that `room` holds
+template <class Each, class Put>
+__device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, uint64_t* room, Each&& each, Put&& put) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t found = kFewPicks + 1;
+  const auto collect = [&] {
+    found = 0;
+    __syncwarp();
+    each([&](uint64_t key) {
+      const bool take = key >= least && key;
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, take), at = found + __popc(mask & ((1u << lane) - 1));
+      if (take && at < kFewPicks) room[at] = key;
+      found += __popc(mask);
+    });
+    __syncwarp();
+  };
+  if (least) collect();
+  if (found > kFewPicks) {
+    uint64_t first = 0;
+    each([&](uint64_t key) { first = max(first, key); });
+    __syncwarp();
+    room[lane] = first;
+    __syncwarp();
+    uint32_t rank = 0;
+#pragma unroll 8
+    for (uint32_t i = 0; i < 32; ++i) rank += room[i] > first || (room[i] == first && i < lane);
+    least = max(least, __shfl_sync(0xFFFFFFFFu, first, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1));
+    collect();
+  }
+  if (found <= kFewPicks) {
+    for (uint32_t i = lane; i < found; i += 32) {
+      const uint64_t key = room[i];
+      uint32_t rank = 0;
+      for (uint32_t j = 0; j < found; ++j) rank += room[j] > key;
+      if (rank < top) put(rank, key);
+    }
+    __syncwarp();
+    return;
+  }
+  uint64_t last = ~0ull;  // very many equal ones: one after the other
+  for (uint32_t j = 0; j < top; ++j) {
+    uint64_t best = 0;
+    each([&](uint64_t key) {
+      if (key < last) best = max(best, key);
+    });
+    last = warp_max(best);
+    if (last == 0) break;
+    if (lane == 0) put(j, last);
+  }
+  __syncwarp();
+}
 
-// A warp a row.
-__global__ void __launch_bounds__(32 * kScoreJoinWarps) k_score_join(ScorePiece a) {
-  __shared__ uint64_t s_picks[kScoreJoinWarps][kFewPicks];
+constexpr uint32_t kJoinHeldMost = 96 * 1024;  // bytes of maxima in shared memory
+
+// kWarps warps a row.  Many rows: one, and 16 rows a CTA, since a sector of the segments' numbers serves eight of them.
+template <uint32_t kSeg, uint32_t kWarps>
+__global__ void __launch_bounds__(kWarps == 1 ? 512 : 32 * kWarps) k_score_join(const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
+  constexpr uint32_t kRows = kWarps == 1 ? 16 : 1;
+  extern __shared__ float s_most[];  // [kRows][segs]
+  __shared__ uint64_t s_room[kRows][kFewPicks];
+  __shared__ uint32_t s_seg[kRows][FT_LOGPROBS_MAX_TOP];
+  __shared__ float s_part[3][kWarps];
   after_previous();
-  const uint32_t n = a.tokens ? *a.count : a.rows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = blockIdx.x * kScoreJoinWarps + warp;
+  const uint32_t lane = threadIdx.x & 31, slot = kWarps == 1 ? threadIdx.x >> 5 : 0, m = blockIdx.x * kRows + slot;
+  const uint32_t n = a.tokens && !a.few ? *a.count : a.rows, t = kWarps == 1 ? lane : threadIdx.x;
   if (m >= n) return;
-  const uint64_t row = a.row0 + (a.tokens ? (uint32_t)a.row_of[m] : m);
+  const uint64_t row = a.row0 + (a.tokens && !a.few ? (uint32_t)a.row_of[m] : m);
+  if (a.few && a.tokens && !has_label(a.tokens[row], a.vocab)) {
+    if (t == 0) {
+      a.logprob[row] = 0.f;
+      if (a.entropy) a.entropy[row] = 0.f;
+      if (a.tokens[row] != kNoLabel) note_error(v, a.call_seq, FT_ERR_BAD_TOKEN_ID, (uint32_t)row);
+    }
+    if (t < a.top) { a.top_ids[row * a.top + t] = -1; a.top_logprobs[row * a.top + t] = 0.f; }
+    return;
+  }
+  const uint64_t seg_step = a.few ? 1 : a.rows, first = a.few ? (uint64_t)m * a.segs : m;
+  float* held = s_most + (a.held ? slot * a.segs : 0);
   float most = -INFINITY;
-  uint64_t seg_key = 0;  // the lane's first segment in the order
-  for (uint32_t s = lane; s < a.segs; s += 32) {
-    const float v = a.most[(uint64_t)s * a.rows + m];
-    most = fmaxf(most, v);
-    seg_key = max(seg_key, order_key(v, s));
+#pragma unroll 4
+  for (uint32_t s = t; s < a.segs; s += 32 * kWarps) {
+    const float x = a.most[first + s * seg_step];
+    if (a.held) held[s] = x;
+    most = fmaxf(most, x);
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+  if constexpr (kWarps > 1) {
+    if (lane == 0) s_part[0][threadIdx.x >> 5] = most;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) most = fmaxf(most, s_part[0][w]);
+  }
   const float about = most == -INFINITY ? 0.f : most, to_log2 = a.scale * kScoreLog2e;
   float sum = 0.f, moment = 0.f;
-  for (uint32_t s = lane; s < a.segs; s += 32) {
-    const uint64_t at = (uint64_t)s * a.rows + m;
-    const float v = a.most[at], u = max_with_nan(((v == -INFINITY ? 0.f : v) - about) * to_log2, kLeastExponent), e = exp2f(u), part = a.sum[at];
-    if (v == -INFINITY && part == 0.f) continue;  // nothing in it (a sum of NaN stays)
+#pragma unroll 4
+  for (uint32_t s = t; s < a.segs; s += 32 * kWarps) {
+    const uint64_t at = first + s * seg_step;
+    const float part = a.sum[at], part_moment = a.moment[at], x = a.held ? held[s] : a.most[at];
+    if (x == -INFINITY && part == 0.f) continue;  // nothing in it (a sum of NaN stays)
+    const float u = max_with_nan(((x == -INFINITY ? 0.f : x) - about) * to_log2, kLeastExponent), e = exp2f(u);
     sum = fmaf(part, e, sum);
-    moment = fmaf(e, fmaf(part, u, a.moment[at]), moment);
+    moment = fmaf(e, fmaf(part, u, part_moment), moment);
   }
   sum = warp_sum(sum);
   moment = warp_sum(moment);
+  if constexpr (kWarps > 1) {
+    if (lane == 0) { s_part[1][threadIdx.x >> 5] = sum; s_part[2][threadIdx.x >> 5] = moment; }
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    sum = moment = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) { sum += s_part[1][w]; moment += s_part[2][w]; }
+  }
   const float log_sum = logf(sum);
   if (lane == 0) {
     if (a.tokens) a.logprob[row] = (a.target[m] - about) * a.scale - log_sum;
     if (a.entropy) a.entropy[row] = log_sum - kScoreLn2 * moment / sum;
   }
   if (a.top == 0) return;
-  // the first `top` segments, lane j the j-th
+  __syncwarp();
+  uint64_t* room = s_room[slot];
+  uint32_t* seg_of = s_seg[slot];
   const uint32_t segs = min(a.top, a.segs);
-  uint32_t my_seg = 0;
-  float least = 0.f;
-  for (uint32_t j = 0; j < segs; ++j) {
-    const uint64_t key = warp_max(seg_key);
-    if (lane == j) my_seg = key_place(key);
-    least = key_value(key);
-    if (key == seg_key) {
-      seg_key = 0;
-      for (uint32_t s = lane; s < a.segs; s += 32) {
-        const uint64_t k = order_key(a.most[(uint64_t)s * a.rows + m], s);
-        if (k < key) seg_key = max(seg_key, k);
-      }
-    }
-  }
-  if (segs < a.top) least = -INFINITY;
-  // their logits that are not below the last one's maximum; where those are many, not below the `top`-th largest of the lanes' maxima either
-  const float* z = a.z + (uint64_t)m * a.ld_z;
-  const auto each = [&](auto&& f) {  // f(key) of the lane's logits in the segments
-    for (uint32_t j = 0; j < segs; ++j) {
-      const uint32_t c = __shfl_sync(0xFFFFFFFFu, my_seg, j) * kSegCols + lane * 4;
-      const float4 q = *reinterpret_cast<const float4*>(z + c);
-      f(order_key(q.x, c));
-      f(order_key(q.y, c + 1));
-      f(order_key(q.z, c + 2));
-      f(order_key(q.w, c + 3));
-    }
-  };
-  bool few = false;
-  uint32_t found = 0;
-  for (int round = 0; round < 2 && !few; ++round) {
-    found = 0;
-    uint64_t mine = 0;
-    each([&](uint64_t key) {
-      const bool take = key_value(key) >= least;
-      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, take), at = found + __popc(mask & ((1u << lane) - 1));
-      if (take && at < kFewPicks) s_picks[warp][at] = key;
-      found += __popc(mask);
-      mine = max(mine, key);
-    });
-    few = found <= kFewPicks;
-    if (few || round == 1) break;
-    for (uint32_t j = 0; j < a.top; ++j) {
-      const uint64_t key = warp_max(mine);
-      least = key_value(key);
-      if (mine == key) mine = 0;
-    }
-    __syncwarp();
+  uint64_t least = 0;
+  if (a.segs > a.top) {
+    first_keys(a.top, 0, room,
+      [&](auto&& f) {
+        for (uint32_t s0 = 0; s0 < a.segs; s0 += 32) {
+          const uint32_t s = s0 + lane;
+          f(s < a.segs ? order_key(a.held ? held[s] : a.most[first + s * seg_step], s) : 0);
+        }
+      },
+      [&](uint32_t rank, uint64_t key) { seg_of[rank] = key_place(key); });
+  } else if (lane < a.segs) {
+    seg_of[lane] = lane;
   }
   __syncwarp();
-  uint64_t pick[kFewPicks / 32] = {}, last = ~0ull;
-  if (few) {
-#pragma unroll
-    for (uint32_t i = 0; i < kFewPicks / 32; ++i) pick[i] = i * 32 + lane < found ? s_picks[warp][i * 32 + lane] : 0;
+  if (a.segs > a.top) {  // no logit below the last segment's maximum is among the first
+    const uint32_t s = seg_of[a.top - 1];
+    least = order_key(a.held ? held[s] : a.most[first + s * seg_step], 0xFFFFFFFFu);
   }
-  for (uint32_t j = 0; j < a.top; ++j) {
-    uint64_t best = 0;
-    if (few) {
-#pragma unroll
-      for (uint32_t i = 0; i < kFewPicks / 32; ++i)
-        if (pick[i] < last) best = max(best, pick[i]);
-    } else {  // many equal logits: all of the segments again
-      each([&](uint64_t key) {
-        if (key < last) best = max(best, key);
-      });
-    }
-    last = warp_max(best);
-    if (lane == 0) {
-      const bool there = last != 0 && key_place(last) < a.vocab;
-      a.top_ids[row * a.top + j] = there ? (int32_t)key_place(last) : -1;
-      a.top_logprobs[row * a.top + j] = there ? (key_value(last) - about) * a.scale - log_sum : -INFINITY;
-    }
-  }
+  const float* z = a.z + (uint64_t)m * a.ld_z;
+  for (uint32_t j = lane; j < a.top; j += 32) { a.top_ids[row * a.top + j] = -1; a.top_logprobs[row * a.top + j] = -INFINITY; }
+  __syncwarp();
+  first_keys(a.top, least, room,
+    [&](auto&& f) {
+      for (uint32_t j = 0; j < segs; ++j) {
+        const uint32_t c = seg_of[j] * kSeg + lane * (kSeg / 32);
+        if constexpr (kSeg == 128) {
+          const float4 q = *reinterpret_cast<const float4*>(z + c);
+          f(order_key(q.x, c));
+          f(order_key(q.y, c + 1));
+          f(order_key(q.z, c + 2));
+          f(order_key(q.w, c + 3));
+        } else {
+          f(order_key(z[c], c));
+        }
+      }
+    },
+    [&](uint32_t rank, uint64_t key) {
+      if (key_place(key) >= a.vocab) return;
+      a.top_ids[row * a.top + rank] = (int32_t)key_place(key);
+      a.top_logprobs[row * a.top + rank] = (key_value(key) - about) * a.scale - log_sum;
+    });
 }
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
@@ -315,11 +568,13 @@ __global__ void __launch_bounds__(32 * kScoreJoinWarps) k_score_join(ScorePiece 
 static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, uint32_t top) {
   uint64_t off = 0;
   auto take = [&](uint64_t bytes) { const uint64_t o = off; off += align_up_sz(bytes, 256); return base + o; };
-  const uint64_t padded = align_up_sz(rows, kMmaTile);
+  a->few = rows <= kFewRows;
+  const uint64_t padded = a->few ? rows : align_up_sz(rows, kMmaTile);
+  const uint32_t cols = a->few ? kFewCols : kSegCols;
   a->rows = rows;
   a->padded = (uint32_t)padded;
-  a->segs = (vocab + kSegCols - 1) / kSegCols;
-  a->ld_z = a->segs * kSegCols;
+  a->segs = (vocab + cols - 1) / cols;
+  a->ld_z = a->segs * cols;
   a->count = reinterpret_cast<uint32_t*>(take(4));
   a->row_of = reinterpret_cast<int32_t*>(take(4ull * rows));
   a->token = reinterpret_cast<int32_t*>(take(4ull * rows));
@@ -327,7 +582,7 @@ static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_
   a->most = reinterpret_cast<float*>(take(4ull * rows * a->segs));
   a->sum = reinterpret_cast<float*>(take(4ull * rows * a->segs));
   a->moment = reinterpret_cast<float*>(take(4ull * rows * a->segs));
-  a->xc = reinterpret_cast<__nv_bfloat16*>(take(2ull * padded * hidden));
+  a->xc = reinterpret_cast<__nv_bfloat16*>(take(a->few ? 0 : 2ull * padded * hidden));
   a->z = reinterpret_cast<float*>(take(top ? 4ull * padded * a->ld_z : 0));
   return off;
 }
@@ -367,13 +622,32 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   score_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, a.top);
   a.call_seq = status_seq(p);
   a.pairs = (uint32_t)p->sm_count / 2;
+  const uint32_t join_rows = a.few ? 1 : 16;
+  a.held = (uint64_t)join_rows * a.segs * sizeof(float) <= kJoinHeldMost;
+  const size_t join_smem = a.held ? (size_t)join_rows * a.segs * sizeof(float) : 0;
   CUtensorMap map_x, map_w, map_z = {};
-  if (mma_map(&map_w, w, a.hidden, a.vocab, ldw) != CUDA_SUCCESS || (a.top && mma_map(&map_z, a.z, a.ld_z, a.padded, a.ld_z, 32, true) != CUDA_SUCCESS))
+  if (mma_map(&map_w, w, a.hidden, a.vocab, ldw, a.few ? kFewCols : 64) != CUDA_SUCCESS ||
+      (a.top && !a.few && mma_map(&map_z, a.z, a.ld_z, a.padded, a.ld_z, 32, true) != CUDA_SUCCESS))
     return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   if (!p->score_attr_set) {  // once per pool, hence once per device the pool lives on
     for (auto k : {k_score<false, 1>, k_score<false, 2>, k_score<true, 1>, k_score<true, 2>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
+    for (auto k : {k_score_few<32, false>, k_score_few<32, true>})
+      FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<32>));
+    for (auto k : {k_score_few<64, false>, k_score_few<64, true>})
+      FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<64>));
+    FT_CUDA(cudaFuncSetAttribute(k_score_join<kSegCols, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
+    FT_CUDA(cudaFuncSetAttribute(k_score_join<kFewCols, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     p->score_attr_set = true;
+  }
+  if (a.few) {
+    const uint32_t n = a.rows <= 32 ? 32 : 64, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
+    if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    const auto kernel = n == 32 ? (a.top ? k_score_few<32, true> : k_score_few<32, false>) : (a.top ? k_score_few<64, true> : k_score_few<64, false>);
+    FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : kFewSmem<64>, st, map_x, map_w, p->view, a));
+    FT_CUDA(launch_chained(k_score_join<kFewCols, 8>, a.rows, 256, join_smem, st, p->view, a));
+    p->gpu_launches += 2;
+    return FT_OK;
   }
   for (uint64_t r0 = 0; r0 < rows; r0 += piece) {
     a.row0 = r0;
@@ -389,7 +663,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     const bool high = a.rows > kMmaTile && a.hidden <= kScoreHigh * kMmaK;
     const auto kernel = a.top ? (high ? k_score<true, 2> : k_score<true, 1>) : (high ? k_score<false, 2> : k_score<false, 1>);
     FT_CUDA(launch_chained(kernel, 2 * a.pairs, kMmaThreads, kMmaSmem, st, map_x, map_w, map_z, p->view, a));
-    FT_CUDA(launch_chained(k_score_join, dim3((a.rows + kScoreJoinWarps - 1) / kScoreJoinWarps), 32 * kScoreJoinWarps, 0, st, a));
+    FT_CUDA(launch_chained(k_score_join<kSegCols, 1>, dim3((a.rows + join_rows - 1) / join_rows), 512, join_smem, st, p->view, a));
     p->gpu_launches += 2;
   }
   return FT_OK;
