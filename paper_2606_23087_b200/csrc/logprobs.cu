@@ -57,7 +57,7 @@ __device__ __forceinline__ float max_with_nan(float a, float b) {
 }
 
 // A CTA takes kRows rows; where they go it learns by counting the tokens before them itself, so nothing has to wait for another CTA.
-constexpr uint32_t kScorePickRows = 32, kScorePickFew = 8, kScorePickFewUpTo = 4096;
+constexpr uint32_t kScorePickRows = 32, kScorePickFew = 8, kScorePickFewUpTo = 65536;
 template <uint32_t kRows>
 __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
   __shared__ uint32_t warp_count[8];
@@ -393,46 +393,77 @@ __device__ __forceinline__ uint64_t warp_max(uint64_t key) {
   return (uint64_t)hi << 32 | lo;
 }
 
-// The `top` first of many keys, by a warp: each(f) calls f(key) for every key of a lane, all lanes as often (0: no key); put(rank, key) is
-// called for each of the first.  `least`: a key that none of them is below, or 0.  Without one, or where it leaves too many, it is the
-// `top`-th largest of the lanes' own first keys.  What it leaves, usually little more than `top`, is ranked by counting.
-constexpr uint32_t kFewPicks = 64;  // keys that `room` holds
-template <class Each, class Put>
-__device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, uint64_t* room, Each&& each, Put&& put) {
-  const uint32_t lane = threadIdx.x & 31;
+template <uint32_t kWarps>
+__device__ __forceinline__ void row_sync() {  // of the warps that share a row
+  if constexpr (kWarps == 1) __syncwarp();
+  else __syncthreads();
+}
+
+// The `top` first of many keys, by the warps of a row: each(f) calls f(key) for every key of a thread, the lanes of a warp as often
+// (0: no key); put(rank, key) is called for each of the first.  `least`: a key that none of them is below, or 0.  Without one, or
+// where it leaves too many, it is the `top`-th largest of a warp's lanes' own first keys.  What it leaves, usually little more than
+// `top`, is ranked by counting.
+constexpr uint32_t kFewPicks = 64;  // keys that the room holds
+template <uint32_t kWarps>
+struct KeyRoom {
+  uint64_t key[kFewPicks], first[kWarps][32], least[kWarps];
+  uint32_t found;
+};
+template <uint32_t kWarps, class Each, class Put>
+__device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, KeyRoom<kWarps>& room, Each&& each, Put&& put) {
+  const uint32_t lane = threadIdx.x & 31, warp = kWarps == 1 ? 0 : threadIdx.x >> 5, t = kWarps == 1 ? lane : threadIdx.x;
   uint32_t found = kFewPicks + 1;
   const auto collect = [&] {
     found = 0;
-    __syncwarp();
+    if (kWarps > 1 && t == 0) room.found = 0;
+    row_sync<kWarps>();
     each([&](uint64_t key) {
       const bool take = key >= least && key;
-      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, take), at = found + __popc(mask & ((1u << lane) - 1));
-      if (take && at < kFewPicks) room[at] = key;
-      found += __popc(mask);
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, take);
+      if (mask == 0) return;
+      uint32_t at = found;
+      if constexpr (kWarps == 1) {
+        found += __popc(mask);
+      } else {
+        if (lane == 0) at = atomicAdd(&room.found, __popc(mask));  // any order: what is ranked is a set
+        at = __shfl_sync(0xFFFFFFFFu, at, 0);
+      }
+      at += __popc(mask & ((1u << lane) - 1));
+      if (take && at < kFewPicks) room.key[at] = key;
     });
-    __syncwarp();
+    row_sync<kWarps>();
+    if constexpr (kWarps > 1) found = room.found;
   };
   if (least) collect();
   if (found > kFewPicks) {
     uint64_t first = 0;
     each([&](uint64_t key) { first = max(first, key); });
-    __syncwarp();
-    room[lane] = first;
+    room.first[warp][lane] = first;
     __syncwarp();
     uint32_t rank = 0;
 #pragma unroll 8
-    for (uint32_t i = 0; i < 32; ++i) rank += room[i] > first || (room[i] == first && i < lane);
-    least = max(least, __shfl_sync(0xFFFFFFFFu, first, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1));
+    for (uint32_t i = 0; i < 32; ++i) {
+      const uint64_t other = room.first[warp][i];
+      rank += other > first || (other == first && i < lane);
+    }
+    uint64_t bound = __shfl_sync(0xFFFFFFFFu, first, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1);
+    if constexpr (kWarps > 1) {
+      if (lane == 0) room.least[warp] = bound;
+      __syncthreads();
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) bound = max(bound, room.least[w]);
+    }
+    least = max(least, bound);
     collect();
   }
   if (found <= kFewPicks) {
-    for (uint32_t i = lane; i < found; i += 32) {
-      const uint64_t key = room[i];
+    for (uint32_t i = t; i < found; i += 32 * kWarps) {
+      const uint64_t key = room.key[i];
       uint32_t rank = 0;
-      for (uint32_t j = 0; j < found; ++j) rank += room[j] > key;
+      for (uint32_t j = 0; j < found; ++j) rank += room.key[j] > key;
       if (rank < top) put(rank, key);
     }
-    __syncwarp();
+    row_sync<kWarps>();
     return;
   }
   uint64_t last = ~0ull;  // very many equal ones: one after the other
@@ -441,25 +472,34 @@ __device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, uint64_
     each([&](uint64_t key) {
       if (key < last) best = max(best, key);
     });
-    last = warp_max(best);
+    best = warp_max(best);
+    if constexpr (kWarps > 1) {
+      if (lane == 0) room.least[warp] = best;
+      __syncthreads();
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) best = max(best, room.least[w]);
+      __syncthreads();
+    }
+    last = best;
     if (last == 0) break;
-    if (lane == 0) put(j, last);
+    if (t == 0) put(j, last);
   }
-  __syncwarp();
+  row_sync<kWarps>();
 }
 
 constexpr uint32_t kJoinHeldMost = 96 * 1024;  // bytes of maxima in shared memory
+constexpr uint32_t kFewWarps = 8;              // of a row, where the rows are few
 
 // kWarps warps a row.  Many rows: one, and 16 rows a CTA, since a sector of the segments' numbers serves eight of them.
 template <uint32_t kSeg, uint32_t kWarps>
 __global__ void __launch_bounds__(kWarps == 1 ? 512 : 32 * kWarps) k_score_join(const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
   constexpr uint32_t kRows = kWarps == 1 ? 16 : 1;
   extern __shared__ float s_most[];  // [kRows][segs]
-  __shared__ uint64_t s_room[kRows][kFewPicks];
+  __shared__ KeyRoom<kWarps> s_room[kRows];
   __shared__ uint32_t s_seg[kRows][FT_LOGPROBS_MAX_TOP];
   __shared__ float s_part[3][kWarps];
   after_previous();
-  const uint32_t lane = threadIdx.x & 31, slot = kWarps == 1 ? threadIdx.x >> 5 : 0, m = blockIdx.x * kRows + slot;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = kWarps == 1 ? warp : 0, m = blockIdx.x * kRows + slot;
   const uint32_t n = a.tokens && !a.few ? *a.count : a.rows, t = kWarps == 1 ? lane : threadIdx.x;
   if (m >= n) return;
   const uint64_t row = a.row0 + (a.tokens && !a.few ? (uint32_t)a.row_of[m] : m);
@@ -474,9 +514,26 @@ __global__ void __launch_bounds__(kWarps == 1 ? 512 : 32 * kWarps) k_score_join(
   }
   const uint64_t seg_step = a.few ? 1 : a.rows, first = a.few ? (uint64_t)m * a.segs : m;
   float* held = s_most + (a.held ? slot * a.segs : 0);
-  float most = -INFINITY;
+  const auto most_of = [&](uint32_t s) { return a.held ? held[s] : a.most[first + s * seg_step]; };
+  // the first numbers of a thread are asked for at once
+  constexpr uint32_t kAhead = 4;
+  float ahead[3][kAhead], most = -INFINITY;
+#pragma unroll
+  for (uint32_t i = 0; i < kAhead; ++i) {
+    const uint32_t s = t + i * 32 * kWarps;
+    const uint64_t at = first + s * seg_step;
+    ahead[0][i] = s < a.segs ? a.most[at] : -INFINITY;
+    ahead[1][i] = s < a.segs ? a.sum[at] : 0.f;
+    ahead[2][i] = s < a.segs ? a.moment[at] : 0.f;
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kAhead; ++i) {
+    const uint32_t s = t + i * 32 * kWarps;
+    if (a.held && s < a.segs) held[s] = ahead[0][i];
+    most = fmaxf(most, ahead[0][i]);
+  }
 #pragma unroll 4
-  for (uint32_t s = t; s < a.segs; s += 32 * kWarps) {
+  for (uint32_t s = t + kAhead * 32 * kWarps; s < a.segs; s += 32 * kWarps) {
     const float x = a.most[first + s * seg_step];
     if (a.held) held[s] = x;
     most = fmaxf(most, x);
@@ -484,75 +541,87 @@ __global__ void __launch_bounds__(kWarps == 1 ? 512 : 32 * kWarps) k_score_join(
 #pragma unroll
   for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
   if constexpr (kWarps > 1) {
-    if (lane == 0) s_part[0][threadIdx.x >> 5] = most;
+    if (lane == 0) s_part[0][warp] = most;
     __syncthreads();
 #pragma unroll
     for (uint32_t w = 0; w < kWarps; ++w) most = fmaxf(most, s_part[0][w]);
   }
   const float about = most == -INFINITY ? 0.f : most, to_log2 = a.scale * kScoreLog2e;
   float sum = 0.f, moment = 0.f;
-#pragma unroll 4
-  for (uint32_t s = t; s < a.segs; s += 32 * kWarps) {
-    const uint64_t at = first + s * seg_step;
-    const float part = a.sum[at], part_moment = a.moment[at], x = a.held ? held[s] : a.most[at];
-    if (x == -INFINITY && part == 0.f) continue;  // nothing in it (a sum of NaN stays)
+  const auto add = [&](float x, float part, float part_moment) {
+    if (x == -INFINITY && part == 0.f) return;  // nothing in it (a sum of NaN stays)
     const float u = max_with_nan(((x == -INFINITY ? 0.f : x) - about) * to_log2, kLeastExponent), e = exp2f(u);
     sum = fmaf(part, e, sum);
     moment = fmaf(e, fmaf(part, u, part_moment), moment);
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < kAhead; ++i) add(ahead[0][i], ahead[1][i], ahead[2][i]);
+#pragma unroll 4
+  for (uint32_t s = t + kAhead * 32 * kWarps; s < a.segs; s += 32 * kWarps) {
+    const uint64_t at = first + s * seg_step;
+    add(most_of(s), a.sum[at], a.moment[at]);
   }
   sum = warp_sum(sum);
   moment = warp_sum(moment);
   if constexpr (kWarps > 1) {
-    if (lane == 0) { s_part[1][threadIdx.x >> 5] = sum; s_part[2][threadIdx.x >> 5] = moment; }
+    if (lane == 0) { s_part[1][warp] = sum; s_part[2][warp] = moment; }
     __syncthreads();
-    if (threadIdx.x >= 32) return;
     sum = moment = 0.f;
 #pragma unroll
     for (uint32_t w = 0; w < kWarps; ++w) { sum += s_part[1][w]; moment += s_part[2][w]; }
   }
   const float log_sum = logf(sum);
-  if (lane == 0) {
+  if (t == 0) {
     if (a.tokens) a.logprob[row] = (a.target[m] - about) * a.scale - log_sum;
     if (a.entropy) a.entropy[row] = log_sum - kScoreLn2 * moment / sum;
   }
   if (a.top == 0) return;
-  __syncwarp();
-  uint64_t* room = s_room[slot];
+  KeyRoom<kWarps>& room = s_room[slot];
   uint32_t* seg_of = s_seg[slot];
   const uint32_t segs = min(a.top, a.segs);
   uint64_t least = 0;
+  row_sync<kWarps>();
   if (a.segs > a.top) {
-    first_keys(a.top, 0, room,
+    first_keys<kWarps>(a.top, 0, room,
       [&](auto&& f) {
-        for (uint32_t s0 = 0; s0 < a.segs; s0 += 32) {
-          const uint32_t s = s0 + lane;
-          f(s < a.segs ? order_key(a.held ? held[s] : a.most[first + s * seg_step], s) : 0);
+#pragma unroll 4
+        for (uint32_t s0 = 0; s0 < a.segs; s0 += 32 * kWarps) {
+          const uint32_t s = s0 + t;
+          f(s < a.segs ? order_key(most_of(s), s) : 0);
         }
       },
       [&](uint32_t rank, uint64_t key) { seg_of[rank] = key_place(key); });
-  } else if (lane < a.segs) {
-    seg_of[lane] = lane;
-  }
-  __syncwarp();
-  if (a.segs > a.top) {  // no logit below the last segment's maximum is among the first
-    const uint32_t s = seg_of[a.top - 1];
-    least = order_key(a.held ? held[s] : a.most[first + s * seg_step], 0xFFFFFFFFu);
+    // no logit below the last segment's maximum is among the first
+    least = order_key(most_of(seg_of[a.top - 1]), 0xFFFFFFFFu);
+  } else {
+    if (t < a.segs) seg_of[t] = t;
+    row_sync<kWarps>();
   }
   const float* z = a.z + (uint64_t)m * a.ld_z;
-  for (uint32_t j = lane; j < a.top; j += 32) { a.top_ids[row * a.top + j] = -1; a.top_logprobs[row * a.top + j] = -INFINITY; }
-  __syncwarp();
-  first_keys(a.top, least, room,
+  if (a.top > a.vocab && t < a.top) { a.top_ids[row * a.top + t] = -1; a.top_logprobs[row * a.top + t] = -INFINITY; }
+  row_sync<kWarps>();
+  first_keys<kWarps>(a.top, least, room,
     [&](auto&& f) {
-      for (uint32_t j = 0; j < segs; ++j) {
-        const uint32_t c = seg_of[j] * kSeg + lane * (kSeg / 32);
-        if constexpr (kSeg == 128) {
-          const float4 q = *reinterpret_cast<const float4*>(z + c);
-          f(order_key(q.x, c));
-          f(order_key(q.y, c + 1));
-          f(order_key(q.z, c + 2));
-          f(order_key(q.w, c + 3));
-        } else {
-          f(order_key(z[c], c));
+      constexpr uint32_t kEach = kSeg / 32, kAtOnce = 4;  // logits of a lane in a segment; segments whose loads go out together
+      for (uint32_t j0 = kWarps == 1 ? 0 : warp; j0 < segs; j0 += kAtOnce * kWarps) {
+        float x[kAtOnce][kEach];
+        uint32_t c[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          const uint32_t j = j0 + i * kWarps;
+          c[i] = seg_of[j < segs ? j : j0] * kSeg + lane * kEach;
+          if constexpr (kEach == 4) {
+            const float4 q = *reinterpret_cast<const float4*>(z + c[i]);
+            x[i][0] = q.x; x[i][1] = q.y; x[i][2] = q.z; x[i][3] = q.w;
+          } else {
+            x[i][0] = z[c[i]];
+          }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          if (j0 + i * kWarps >= segs) break;
+#pragma unroll
+          for (uint32_t e = 0; e < kEach; ++e) f(order_key(x[i][e], c[i] + e));
         }
       }
     },
@@ -637,7 +706,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     for (auto k : {k_score_few<64, false>, k_score_few<64, true>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<64>));
     FT_CUDA(cudaFuncSetAttribute(k_score_join<kSegCols, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
-    FT_CUDA(cudaFuncSetAttribute(k_score_join<kFewCols, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
+    FT_CUDA(cudaFuncSetAttribute(k_score_join<kFewCols, kFewWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     p->score_attr_set = true;
   }
   if (a.few) {
@@ -645,7 +714,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const auto kernel = n == 32 ? (a.top ? k_score_few<32, true> : k_score_few<32, false>) : (a.top ? k_score_few<64, true> : k_score_few<64, false>);
     FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : kFewSmem<64>, st, map_x, map_w, p->view, a));
-    FT_CUDA(launch_chained(k_score_join<kFewCols, 8>, a.rows, 256, join_smem, st, p->view, a));
+    FT_CUDA(launch_chained(k_score_join<kFewCols, kFewWarps>, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
     p->gpu_launches += 2;
     return FT_OK;
   }
