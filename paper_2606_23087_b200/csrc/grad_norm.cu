@@ -17,7 +17,7 @@ constexpr uint32_t kGradVecs = 4;                                  // 16-byte ac
 constexpr uint32_t kGradChunk = kGradThreads * kGradVecs * 16;     // bytes
 constexpr uint32_t kGradPerLaunch = 320;                           // tensors a launch takes at most (kernel arguments hold 32 KiB)
 constexpr uint32_t kGradFew = 16;                                  // tensors of the launch with a small argument block
-constexpr uint32_t kGradCtasPerSm = 8;
+constexpr uint32_t kGradCtasPerSm = 6;
 constexpr uint32_t kGradLines = 2048;                              // of the workspace, at most
 
 struct GradTensorArg {

@@ -53,18 +53,33 @@ struct RotaryPiece {
     move(p, x);
     if (two) move(p + second, x + kE);
   }
+  // cs: the table's place of the piece's first pair (see rotary_place)
   template <bool kInterleaved>
-  __device__ __forceinline__ void turn(const float2* cs) {
+  __device__ __forceinline__ void turn(const float2* cs, uint32_t turned) {
+    float2 c[kE];
+    if constexpr (kVec) {
+#pragma unroll
+      for (int i = 0; i < kE; i += 2) *reinterpret_cast<float4*>(c + i) = *reinterpret_cast<const float4*>(cs + i * turned);
+    } else {
+      c[0] = cs[0];
+    }
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
       T &ta = kInterleaved ? x[2 * i] : x[i], &tb = kInterleaved ? x[2 * i + 1] : x[kE + i];
       const float a = widen1(ta), b = widen1(tb);
-      const float2 c = cs[i];
-      ta = narrow1<T>(fmaf(a, c.x, -(b * c.y)));
-      tb = narrow1<T>(fmaf(a, c.y, b * c.x));
+      ta = narrow1<T>(fmaf(a, c[i].x, -(b * c[i].y)));
+      tb = narrow1<T>(fmaf(a, c[i].y, b * c[i].x));
     }
   }
 };
+// Where the table holds pair p: two pairs of each piece side by side, then the next two of each, so that the pieces of a head, which
+// neighbouring lanes hold, read one range (a piece's pairs in a row were read at a quarter of the rate, and bound the kernel).
+template <int kE>
+__device__ __forceinline__ uint32_t rotary_place(uint32_t p, uint32_t turned) {
+  if constexpr (kE == 1) return p;
+  const uint32_t piece = p / kE, i = p % kE;
+  return (i / 2 * turned + piece) * 2 + i % 2;
+}
 
 // An element of the tables among the arguments, by an ordinary load: lanes that index constant memory each by themselves are served one
 // after the other.
@@ -74,7 +89,7 @@ __device__ __forceinline__ uint32_t load_argument(const uint8_t* p) { uint32_t v
 // CTA (row tile, heads): kRows rows, `slots` heads.  kE: pairs of a piece, 16 bytes of each element's row or a single one.
 template <typename T, int kE, bool kInterleaved, int kRows>
 __global__ void __launch_bounds__(kRotaryThreads) k_rotary(const __grid_constant__ RotaryArgs a) {
-  extern __shared__ float2 table[];  // [kRows][pairs]
+  extern __shared__ __align__(16) float2 table[];  // [kRows][pairs]
   const uint64_t row0 = (uint64_t)blockIdx.x * kRows;
   const uint32_t rows = (uint32_t)min((uint64_t)kRows, a.rows - row0);
   const uint32_t slot = threadIdx.x / a.units, unit = threadIdx.x - slot * a.units, head = blockIdx.y * a.slots + slot;
@@ -107,7 +122,7 @@ __global__ void __launch_bounds__(kRotaryThreads) k_rotary(const __grid_constant
     const int64_t turns = (int64_t)(load_argument(a.turns + p) * (uint64_t)(int64_t)position);  // of a turn, from -1/2 on
     float s, c;
     sincospif((float)turns * 0x1p-63f, &s, &c);
-    table[i] = make_float2(c, s);
+    table[r * a.pairs + rotary_place<kE>(p, a.turned)] = make_float2(c, s);
   }
   __syncthreads();
   if (!active) return;
@@ -115,7 +130,7 @@ __global__ void __launch_bounds__(kRotaryThreads) k_rotary(const __grid_constant
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     if (r >= rows) break;
-    if (turned) piece[r].template turn<kInterleaved>(table + r * a.pairs + unit * kE);
+    if (turned) piece[r].template turn<kInterleaved>(table + r * a.pairs + unit * (kE == 1 ? 1 : 2), a.turned);
     piece[r].store(dst + r * t.dst_row, second, two);
   }
 }
