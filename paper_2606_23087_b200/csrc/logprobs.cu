@@ -208,10 +208,13 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
 constexpr int kFewThreads = 256;
 constexpr uint32_t kFewTile = 128;                       // W's rows of a tile
 constexpr uint32_t kFewBox = kFewCols * kMmaK * 2;       // bytes of a box of W: a segment's rows, 64 columns of K
+constexpr uint32_t kFewSub = 2;                          // blocks of K of a stage: a row's 256 bytes are asked for together
 template <uint32_t kN>
-constexpr uint32_t kFewStage = kFewTile * kMmaK * 2 + kN * kMmaK * 2;
+constexpr uint32_t kFewBlock = kFewTile * kMmaK * 2 + kN * kMmaK * 2;  // bytes of a block of K: W's, then x's
 template <uint32_t kN>
-constexpr uint32_t kFewStages = kN == 32 ? 10 : 8;
+constexpr uint32_t kFewStage = kFewSub * kFewBlock<kN>;
+template <uint32_t kN>
+constexpr uint32_t kFewStages = (kN == 32 ? 10 : 8) / kFewSub;
 constexpr uint32_t kFewTurn = 32 * 33 * 4;               // bytes of a warp's 32 x 32 logits, turned over
 template <uint32_t kN>
 constexpr size_t kFewSmem = kFewStages<kN> * (size_t)kFewStage<kN> + 4 * kFewTurn + 1024 + 256;
@@ -273,12 +276,15 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
     uint32_t it = 0;
     for (uint32_t seg = seg0; seg < seg1 && !lost; seg += 4) {
       const uint32_t boxes = min(4u, seg1 - seg);
-      for (uint32_t k = 0; k < k_blocks; ++k, ++it) {
-        const uint32_t s = it % kStages, at = base + s * kStage;
+      for (uint32_t k = 0; k < k_blocks; k += kFewSub, ++it) {
+        const uint32_t s = it % kStages, at = base + s * kStage, subs = min(kFewSub, k_blocks - k);
         if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
-        mbar_expect_tx(&bar->full[s], boxes * kFewBox + kN * kMmaK * 2 + v.bulk_tx_slack);  // the slack: a test hook, 0
-        for (uint32_t b = 0; b < boxes; ++b) few_box(at + b * kFewBox, &map_w, (int32_t)(k * kMmaK), (int32_t)((seg + b) * kFewCols), &bar->full[s]);
-        few_box(at + kFewTile * kMmaK * 2, &map_x, (int32_t)(k * kMmaK), 0, &bar->full[s]);
+        mbar_expect_tx(&bar->full[s], subs * (boxes * kFewBox + kN * kMmaK * 2) + v.bulk_tx_slack);  // the slack: a test hook, 0
+        for (uint32_t b = 0; b < boxes; ++b)
+          for (uint32_t i = 0; i < subs; ++i)
+            few_box(at + i * kFewBlock<kN> + b * kFewBox, &map_w, (int32_t)((k + i) * kMmaK), (int32_t)((seg + b) * kFewCols), &bar->full[s]);
+        for (uint32_t i = 0; i < subs; ++i)
+          few_box(at + i * kFewBlock<kN> + kFewTile * kMmaK * 2, &map_x, (int32_t)((k + i) * kMmaK), 0, &bar->full[s]);
       }
     }
     // what still arrives in shared memory: the loads of the last stages, and the signals that their products are done
@@ -293,15 +299,17 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
       const uint32_t acc = tile & 1;
       if (!mbar_wait_bounded(&bar->acc_empty[acc], ((tile >> 1) & 1) ^ 1, limit_ns)) { lost = true; break; }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (uint32_t k = 0; k < k_blocks; ++k, ++it) {
-        const uint32_t s = it % kStages, sa = base + s * kStage, sb = sa + kFewTile * kMmaK * 2;
+      for (uint32_t k = 0; k < k_blocks; k += kFewSub, ++it) {
+        const uint32_t s = it % kStages;
         if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t part = k / each;
+        for (uint32_t i = 0; i < min(kFewSub, k_blocks - k); ++i) {
+          const uint32_t sa = base + s * kStage + i * kFewBlock<kN>, sb = sa + kFewTile * kMmaK * 2, part = (k + i) / each;
 #pragma unroll
-        for (uint32_t j = 0; j < kMmaK / 16; ++j)
-          few_product(tmem + acc * 256 + part * kN, mma_desc<false>(sa + j * kMmaStep<false>), mma_desc<false>(sb + j * kMmaStep<false>), kInstr,
-                      k > part * each || j > 0);
+          for (uint32_t j = 0; j < kMmaK / 16; ++j)
+            few_product(tmem + acc * 256 + part * kN, mma_desc<false>(sa + j * kMmaStep<false>), mma_desc<false>(sb + j * kMmaStep<false>), kInstr,
+                        k + i > part * each || j > 0);
+        }
         few_commit(&bar->empty[s]);
       }
       if (!lost) few_commit(&bar->acc_full[acc]);

@@ -217,10 +217,22 @@ __global__ void __launch_bounds__(kRmsWideThreads) k_rms_wide(RmsArgs a) {
 
 // ---- backward -----------------------------------------------------------------------------------------------------
 
+// Threads of a CTA, one CTA an SM.  Where the rows are in shared memory a thread reads them twice from there, for the row's sum and
+// for dx, and keeps only its sums over rows: 72 registers, 28 warps.  (With both operands kept in 128 registers 14 warps took 192 us for
+// 32768 rows x 3584 in bf16.)  Element by element they are kept.
+constexpr int kRmsGradThreads(bool vec, int elems) { return vec ? (elems > 16 ? 512 : 896) : (elems > 16 ? 256 : 512); }
+// Groups of kN threads: as many as that, and as leave room for two of their rows in shared memory.
+template <int kStreams, typename T, int V, bool kVec, int kN>
+constexpr int kRmsGradGroups = [] {
+  const int most = kRmsGradThreads(kVec, V * (kVec ? Pack<T>::kElems : 1)) / kN;
+  if (!kVec) return most;
+  const size_t row = 2ull * kStreams * V * kN * 16, room = kSmemMost - 1024 - (size_t)V * Pack<T>::kElems * kN * 4;
+  const int fit = (int)(room / row) < most ? (int)(room / row) : most;
+  return fit > 15 ? 15 : fit;  // a group has a named barrier, of which there are sixteen
+}();
 // Rows in shared memory or under way to it: as many as fit beside the weights.
 template <int kStreams, typename T, int V, int kN, int kThreads>
 constexpr int kRmsGradStages = stages_within(kSmemMost - 1024 - (size_t)V * Pack<T>::kElems * kN * 4, (size_t)kStreams * V * kThreads * 16);
-constexpr int kRmsGradGroups(int elems, int n) { return elems > 16 ? 256 / n : 512 / n; }
 
 // The CTA's threads form groups of kN; group i of the grid takes the rows i, i + groups, ...
 template <typename T, int V, bool kVec, int kN, int kGroups, bool kRes>
@@ -275,57 +287,88 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
   T* q = static_cast<T*>(a.dx) + first * a.lddx + t * E;
   const uint64_t q_step = step * a.lddx;
   uint32_t stage = 0, turn = 0;
+  // the sum over the group's threads
+  const auto group_sum = [&](float v) {
+    v = warp_sum(v);
+    if constexpr (nw > 1) {
+      if (lane == 0) red[turn][threadIdx.x >> 5] = v;
+      asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kN) : "memory");
+      const float* r1 = &red[turn][group * nw];
+      v = r1[0];
+#pragma unroll
+      for (int i = 1; i < nw; ++i) v += r1[i];
+      turn ^= 1;  // written again only behind the next row's barrier
+    }
+    return v;
+  };
   for (uint32_t r = 0; r < n_rows; ++r) {
-    F2 x[N], g[N], d[kRes ? N : 1];
     fetch_stats();
     if constexpr (kVec) fetch((stage + kStages - 1) % kStages);
     copy_async_commit();
     copy_async_wait<kVec ? kStages - 1 : 3>();
     __syncwarp();
     const float rstd = stats[r % 4][threadIdx.x >> 5];
-    in_s.take(stage, x);
-    in_g.take(stage, g);
-    if constexpr (kRes && !kVec) in_d.take(stage, d);
-    if constexpr (!kVec) fetch(0);
-    F2 s1[2] = {f2(0.f), f2(0.f)};
     const F2 by = f2(rstd);
+    F2 s1[2] = {f2(0.f), f2(0.f)};
+    if constexpr (kVec) {
+      const auto weights_of = [&](int k, F2 (&w)[E / 2]) {
 #pragma unroll
-    for (int i = 0; i < N; i += Q / 2) {
-      F2 w[Q / 2];
-      const float* p = weights + (i / (Q / 2) * kN + t) * Q;
-      if constexpr (kVec) {
-        Pack<float>::widen(*reinterpret_cast<const uint4*>(p), w);
-      } else {
-        const float2 v = *reinterpret_cast<const float2*>(p);
-        w[0] = f2(v.x, v.y);
+        for (int i = 0; i < E / 4; ++i)
+          Pack<float>::widen(*reinterpret_cast<const uint4*>(weights + ((k * E / 4 + i) * kN + t) * 4), w + 2 * i);
+      };
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        F2 x[E / 2], g[E / 2], w[E / 2];
+        in_s.take_chunk(stage, k, x);
+        in_g.take_chunk(stage, k, g);
+        weights_of(k, w);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {  // beyond the row dy and w are zero
+          const F2 xhat = x[i] * by;
+          dw[k * (E / 2) + i] = fma(g[i], xhat, dw[k * (E / 2) + i]);
+          s1[i & 1] = fma(g[i] * w[i], xhat, s1[i & 1]);
+        }
       }
+      const float c1 = group_sum(sum(s1[0] + s1[1])) * inv;
+      const F2 less = f2(-c1);
 #pragma unroll
-      for (int j = 0; j < Q / 2; ++j) {  // beyond the row dy and w are zero
-        x[i + j] = x[i + j] * by;
-        dw[i + j] = fma(g[i + j], x[i + j], dw[i + j]);
-        g[i + j] = g[i + j] * w[j];
-        s1[j & 1] = fma(g[i + j], x[i + j], s1[j & 1]);
+      for (int k = 0; k < V; ++k) {
+        F2 x[E / 2], g[E / 2], w[E / 2], d[E / 2];
+        in_s.take_chunk(stage, k, x);
+        in_g.take_chunk(stage, k, g);
+        if constexpr (kRes) in_d.take_chunk(stage, k, d);
+        weights_of(k, w);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const F2 v = fma(x[i] * by, less, g[i] * w[i]);
+          if constexpr (kRes) d[i] = fma(v, by, d[i]);
+          else d[i] = v * by;
+        }
+        if (in_s.has(k)) *reinterpret_cast<uint4*>(q + k * kN * E) = Pack<T>::narrow(d);
       }
-    }
-    float c1 = warp_sum(sum(s1[0] + s1[1]));
-    if constexpr (nw > 1) {
-      if (lane == 0) red[turn][threadIdx.x >> 5] = c1;
-      asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kN) : "memory");
-      const float* r1 = &red[turn][group * nw];
-      c1 = r1[0];
+    } else {
+      F2 x[N], g[N], d[kRes ? N : 1];
+      in_s.take(stage, x);
+      in_g.take(stage, g);
+      if constexpr (kRes) in_d.take(stage, d);
+      fetch(0);
 #pragma unroll
-      for (int i = 1; i < nw; ++i) c1 += r1[i];
-      turn ^= 1;  // written again only behind the next row's barrier
-    }
-    c1 *= inv;
-    if constexpr (kRes && kVec) in_d.take(stage, d);
+      for (int i = 0; i < N; ++i) {
+        const float2 v = *reinterpret_cast<const float2*>(weights + (i * kN + t) * Q);
+        x[i] = x[i] * by;
+        dw[i] = fma(g[i], x[i], dw[i]);
+        g[i] = g[i] * f2(v.x, v.y);
+        s1[i & 1] = fma(g[i], x[i], s1[i & 1]);
+      }
+      const float c1 = group_sum(sum(s1[0] + s1[1])) * inv;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const F2 v = fma(x[i], f2(-c1), g[i]);
-      if constexpr (kRes) x[i] = fma(v, by, d[i]);
-      else x[i] = v * by;
+      for (int i = 0; i < N; ++i) {
+        const F2 v = fma(x[i], f2(-c1), g[i]);
+        if constexpr (kRes) x[i] = fma(v, by, d[i]);
+        else x[i] = v * by;
+      }
+      in_s.store(q, x);
     }
-    in_s.store(q, x);
     q += q_step;
     stage = (stage + 1) % kStages;
   }
@@ -458,7 +501,7 @@ static cudaError_t rms_typed(const ft_pool* p, const RmsArgs& a, bool vec, cudaS
 
 template <typename T, bool kVec, int V, int kN, bool kRes>
 static cudaError_t rms_grad_rows(ft_pool* p, const RmsGradArgs& a, uint32_t* lines, cudaStream_t st) {
-  constexpr int E = kVec ? Pack<T>::kElems : 1, kGroups = kRmsGradGroups(V * E, kN), kStreams = kRes ? 3 : 2;
+  constexpr int E = kVec ? Pack<T>::kElems : 1, kStreams = kRes ? 3 : 2, kGroups = kRmsGradGroups<kStreams, T, V, kVec, kN>;
   constexpr size_t kRows = kVec ? (size_t)kStreams * kRmsGradStages<kStreams, T, V, kN, kN * kGroups> * V * kN * kGroups * 16 : 0, kSums = (kGroups - 1) * (size_t)V * E * kN * 4;
   constexpr size_t smem = (size_t)V * E * kN * 4 + (kRows > kSums ? kRows : kSums);
   static_assert(smem + 6 * (kN * kGroups / 32) * sizeof(float) <= kSmemMost, "every instance can be launched");

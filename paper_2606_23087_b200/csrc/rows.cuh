@@ -78,6 +78,9 @@ struct RowFeed {
       for (int k = 0; k < V; k += 2) f[k / 2] = f2(widen1(next[k]), widen1(next[k + 1]));
     }
   }
+  __device__ __forceinline__ void take_chunk(uint32_t stage, int k, F2 (&f)[kVec ? E / 2 : 1]) const {  // one of them, from shared memory
+    if constexpr (kVec) Pack<T>::widen(load_shared16(slot + (stage * V + k) * kThreads * 16), f);
+  }
   __device__ __forceinline__ void store(T* q, const F2 (&f)[V * E / 2]) const {  // q: the thread's first chunk of the output row
 #pragma unroll
     for (int k = 0; k < V; ++k) {
