@@ -240,8 +240,8 @@ __device__ __forceinline__ void few_product(uint32_t tmem, uint64_t da, uint64_t
 
 template <uint32_t kN, bool kKeep>
 __global__ void __launch_bounds__(kFewThreads, 1)
-k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
-            const __grid_constant__ ScorePiece a) {
+k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_tile,
+            const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
   extern __shared__ uint8_t smem_raw[];
   constexpr uint32_t kStages = kFewStages<kN>, kStage = kFewStage<kN>;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -280,9 +280,14 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
         const uint32_t s = it % kStages, at = base + s * kStage, subs = min(kFewSub, k_blocks - k);
         if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
         mbar_expect_tx(&bar->full[s], subs * (boxes * kFewBox + kN * kMmaK * 2) + v.bulk_tx_slack);  // the slack: a test hook, 0
-        for (uint32_t b = 0; b < boxes; ++b)
-          for (uint32_t i = 0; i < subs; ++i)
+        for (uint32_t i = 0; i < subs; ++i) {
+          if (boxes == 4) {  // one box: four of a quarter each take 6 % longer
+            few_box(at + i * kFewBlock<kN>, &map_tile, (int32_t)((k + i) * kMmaK), (int32_t)(seg * kFewCols), &bar->full[s]);
+            continue;
+          }
+          for (uint32_t b = 0; b < boxes; ++b)
             few_box(at + i * kFewBlock<kN> + b * kFewBox, &map_w, (int32_t)((k + i) * kMmaK), (int32_t)((seg + b) * kFewCols), &bar->full[s]);
+        }
         for (uint32_t i = 0; i < subs; ++i)
           few_box(at + i * kFewBlock<kN> + kFewTile * kMmaK * 2, &map_x, (int32_t)((k + i) * kMmaK), 0, &bar->full[s]);
       }
@@ -719,9 +724,10 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   }
   if (a.few) {
     const uint32_t n = a.rows <= 32 ? 32 : 64, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
-    if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    CUtensorMap map_tile;
+    if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, w, a.hidden, a.vocab, ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const auto kernel = n == 32 ? (a.top ? k_score_few<32, true> : k_score_few<32, false>) : (a.top ? k_score_few<64, true> : k_score_few<64, false>);
-    FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : kFewSmem<64>, st, map_x, map_w, p->view, a));
+    FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : kFewSmem<64>, st, map_x, map_w, map_tile, p->view, a));
     FT_CUDA(launch_chained(k_score_join<kFewCols, kFewWarps>, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
     p->gpu_launches += 2;
     return FT_OK;
