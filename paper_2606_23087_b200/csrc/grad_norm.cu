@@ -103,6 +103,7 @@ __device__ __forceinline__ double block_sum_double(double x) {  // for thread 0
 template <uint32_t kCap>
 __global__ void __launch_bounds__(kGradThreads, kGradCtasPerSm) k_grad_squares(const __grid_constant__ GradArgs<kCap> a) {
   let_next_start();
+  after_previous();
   double s = 0.0;
   // a contiguous share of the chunks
   const uint64_t c0 = a.chunks * blockIdx.x / gridDim.x, c1 = a.chunks * (blockIdx.x + 1) / gridDim.x;
@@ -153,8 +154,7 @@ static cudaError_t grad_squares(const ft_grad_tensor* t, uint32_t n, uint32_t gr
     d.bf16 = t[i].dtype == FT_BF16;
     at += (d.end + kGradChunk - 1) / kGradChunk;
   }
-  k_grad_squares<kCap><<<grid, kGradThreads, 0, st>>>(a);  // not chained: what came before may still be writing gradients
-  return cudaGetLastError();
+  return launch_chained(k_grad_squares<kCap>, dim3(grid), kGradThreads, 0, st, a);
 }
 
 static uint32_t grad_grid(const ft_pool* p) { return std::min<uint32_t>(kGradLines, kGradCtasPerSm * (uint32_t)p->sm_count); }

@@ -26,7 +26,7 @@ constexpr float kFp8Least = 0x1p-110f;  // the least magnitude that a group is s
 
 struct RmsArgs {
   uint64_t rows, ldx, ldr, lds, ldy, ldq, ldqs;
-  uint32_t cols, param_dtype;
+  uint32_t cols, param_dtype, rows_each;  // rows_each: of a CTA
   const void *x, *residual, *weight;
   void *sum, *y;
   uint8_t* q;
@@ -57,6 +57,27 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
   return r;
 }
 
+// E weights of consecutive columns from c on, 16 bytes at a time where they lie so; ones without weights or where the row has ended
+template <int E>
+__device__ __forceinline__ void weights_from(const void* weight, uint32_t dtype, uint32_t c, bool there, F2 (&w)[E / 2]) {
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) w[i] = f2(1.f);
+  if (!weight || !there) return;
+  if (dtype == FT_F32) {
+    const float* p = static_cast<const float*>(weight) + c;
+    if (aligned16(p)) {
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) Pack<float>::widen(*reinterpret_cast<const uint4*>(p + 4 * i), w + 2 * i);
+      return;
+    }
+  } else if (E == 8 && aligned16(static_cast<const __nv_bfloat16*>(weight) + c)) {
+    Pack<__nv_bfloat16>::widen(*reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(weight) + c), reinterpret_cast<F2*>(w));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) w[i] = f2(load_as(weight, dtype, c + 2 * i), load_as(weight, dtype, c + 2 * i + 1));
+}
+
 // ---- forward ------------------------------------------------------------------------------------------------------
 
 // CTAs of an SM: 896 threads of 72 registers, 512 where a thread holds 32 elements or goes element by element.
@@ -74,9 +95,12 @@ __global__ void __launch_bounds__(kN, (kRmsCtas<T, V, kVec, kN>)) k_rms(RmsArgs 
   constexpr int E = kVec ? Pack<T>::kElems : 1, N = V * E / 2, kStages = kRmsStages<kRes ? 2 : 1, T, V, kN>;  // N pairs
   using Feed = RowFeed<T, V, kVec, kN, kN, kStages>;
   Feed in, add;
-  const uint32_t n_rows = rows_from(a.rows, blockIdx.x, gridDim.x);
-  in.init(a.x, a.ldx, blockIdx.x, gridDim.x, n_rows, a.cols, threadIdx.x, ring + threadIdx.x);
-  if constexpr (kRes) add.init(a.residual, a.ldr, blockIdx.x, gridDim.x, n_rows, a.cols, threadIdx.x, ring + kStages * V * kN + threadIdx.x);
+  let_next_start();
+  after_previous();
+  const uint64_t row0 = (uint64_t)blockIdx.x * a.rows_each;
+  const uint32_t n_rows = (uint32_t)min((uint64_t)a.rows_each, a.rows - row0);
+  in.init(a.x, a.ldx, row0, 1, n_rows, a.cols, threadIdx.x, ring + threadIdx.x);
+  if constexpr (kRes) add.init(a.residual, a.ldr, row0, 1, n_rows, a.cols, threadIdx.x, ring + kStages * V * kN + threadIdx.x);
   const auto fetch = [&](uint32_t s) {
     in.fetch(s);
     if constexpr (kRes) add.fetch(s);
@@ -91,20 +115,18 @@ __global__ void __launch_bounds__(kN, (kRmsCtas<T, V, kVec, kN>)) k_rms(RmsArgs 
   if (kN > 32 && threadIdx.x < sizeof(red) / 4) (&red[0][0])[threadIdx.x] = 0.f;
   F2 w[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float wv[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t c = ((2 * i + j) / E * kN + threadIdx.x) * E + (2 * i + j) % E;
-      wv[j] = c < a.cols && a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f;
+  for (int k = 0; k < V * E; k += kVec ? E : 2) {
+    const uint32_t c = (k / E * kN + threadIdx.x) * E;
+    if constexpr (kVec) {
+      weights_from<E>(a.weight, a.param_dtype, c, in.has(k / E), *reinterpret_cast<F2(*)[E / 2]>(w + k / 2));
+    } else {
+      w[k / 2] = f2(in.has(k) && a.weight ? load_as(a.weight, a.param_dtype, c) : 1.f, in.has(k + 1) && a.weight ? load_as(a.weight, a.param_dtype, c + kN) : 1.f);
     }
-    w[i] = f2(wv[0], wv[1]);
   }
   if (kN > 32) __syncthreads();
   const float inv = 1.f / a.cols;
-  const uint64_t step = gridDim.x;
-  T* sum_out = a.sum ? static_cast<T*>(a.sum) + blockIdx.x * a.lds + threadIdx.x * E : nullptr;
-  T* y_out = a.y ? static_cast<T*>(a.y) + blockIdx.x * a.ldy + threadIdx.x * E : nullptr;
+  T* sum_out = a.sum ? static_cast<T*>(a.sum) + row0 * a.lds + threadIdx.x * E : nullptr;
+  T* y_out = a.y ? static_cast<T*>(a.y) + row0 * a.ldy + threadIdx.x * E : nullptr;
   uint32_t stage = 0;
   for (uint32_t r = 0; r < n_rows; ++r) {
     F2 x[N], ss[2] = {f2(0.f), f2(0.f)};
@@ -122,18 +144,18 @@ __global__ void __launch_bounds__(kN, (kRmsCtas<T, V, kVec, kN>)) k_rms(RmsArgs 
     if constexpr (!kVec) fetch(0);
     if (sum_out) {
       in.store(sum_out, x);
-      sum_out += step * a.lds;
+      sum_out += a.lds;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) ss[i & 1] = fma(x[i], x[i], ss[i & 1]);  // beyond the row x is zero
     const float rstd = rsqrtf(block_sum<kN>(sum(ss[0] + ss[1]), red[r & 1]) * inv + a.eps);
-    const uint64_t row = blockIdx.x + (uint64_t)r * step;
+    const uint64_t row = row0 + r;
     if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = x[i] * f2(rstd) * w[i];
     if (y_out) {
       in.store(y_out, x);
-      y_out += step * a.ldy;
+      y_out += a.ldy;
     }
     if constexpr (kVec) {
       if (a.q) {
@@ -242,6 +264,7 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
   __shared__ float red[2][kThreads / 32], stats[4][kThreads / 32];
   const uint32_t group = threadIdx.x / kN, t = threadIdx.x % kN;
   constexpr int Q = kVec ? 4 : 2;
+  after_previous();
   float* weights = reinterpret_cast<float*>(ring);  // [V E / Q][kN][Q]
   uint4* rows = ring + V * E * kN / 4;
   for (uint32_t i = threadIdx.x; i < V * E * kN; i += kThreads) {
@@ -470,11 +493,13 @@ static cudaError_t rms_rows(const ft_pool* p, const RmsArgs& a, cudaStream_t st)
     constexpr size_t smem = kVec ? (size_t)(kRes ? 2 : 1) * kRmsStages<kRes ? 2 : 1, T, V, kN> * V * kN * 16 : 0;
     if constexpr (smem + 2 * (kN / 32 + 3) / 4 * 16 > kSmemMost) return;  // rms_launch takes no such rows here
     else if ((e = allow_smem(kernel, smem)) != cudaSuccess) return;
-    int per_sm = 1;
-    if (a.rows > (uint64_t)p->sm_count) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kN, smem);
-    if (e != cudaSuccess) return;
-    kernel<<<(unsigned)std::min<uint64_t>(a.rows, (uint64_t)std::max(1, per_sm) * p->sm_count), kN, smem, st>>>(a);
-    e = cudaGetLastError();
+    // Few consecutive rows a CTA: what is read and written at a time then lies close together.  (Persistent CTAs that take every n-th
+    // row drift apart: 32768 rows x 3584 with a residual 164 us against 142, without one 88 against 73.  From 4 to 8 rows make little
+    // difference; with 2 the weights' loads show.)  A CTA each for rows that do not fill the device.
+    const uint64_t resident = (uint64_t)kRmsCtas<T, V, kVec, kN> * p->sm_count;
+    RmsArgs b = a;
+    b.rows_each = (uint32_t)std::max<uint64_t>(std::min<uint64_t>(a.rows / resident, 6), std::max<uint64_t>(1, a.rows >> 30));
+    e = launch_chained(kernel, dim3((unsigned)((a.rows + b.rows_each - 1) / b.rows_each)), kN, smem, st, b);
   });
   return e;
 }
@@ -509,8 +534,7 @@ static cudaError_t rms_grad_rows(ft_pool* p, const RmsGradArgs& a, uint32_t* lin
   const cudaError_t e = allow_smem(kernel, smem);
   if (e != cudaSuccess) return e;
   *lines = (uint32_t)std::min<uint64_t>((a.rows + kGroups - 1) / kGroups, (uint64_t)p->sm_count);
-  kernel<<<*lines, kN * kGroups, smem, st>>>(a);
-  return cudaGetLastError();
+  return launch_chained(kernel, dim3(*lines), kN * kGroups, smem, st, a);
 }
 
 // 16 elements a thread, which 256 threads make 4096; 32 up to 8192.

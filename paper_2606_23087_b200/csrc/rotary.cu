@@ -90,6 +90,8 @@ __device__ __forceinline__ uint32_t load_argument(const uint8_t* p) { uint32_t v
 template <typename T, int kE, bool kInterleaved, int kRows>
 __global__ void __launch_bounds__(kRotaryThreads) k_rotary(const __grid_constant__ RotaryArgs a) {
   extern __shared__ __align__(16) float2 table[];  // [kRows][pairs]
+  let_next_start();
+  after_previous();
   const uint64_t row0 = (uint64_t)blockIdx.x * kRows;
   const uint32_t rows = (uint32_t)min((uint64_t)kRows, a.rows - row0);
   const uint32_t slot = threadIdx.x / a.units, unit = threadIdx.x - slot * a.units, head = blockIdx.y * a.slots + slot;
@@ -146,10 +148,8 @@ static cudaError_t rotary_launch(const ft_pool* p, RotaryArgs& a, cudaStream_t s
   a.slots = std::max(1u, std::min(a.heads, kRotaryThreads / a.units));
   const uint32_t y = (a.heads + a.slots - 1) / a.slots;
   if ((a.rows + 3) / 4 * y < (uint64_t)p->sm_count)
-    k_rotary<T, kE, kInterleaved, 1><<<dim3((unsigned)a.rows, y), kRotaryThreads, a.pairs * sizeof(float2), st>>>(a);
-  else
-    k_rotary<T, kE, kInterleaved, 4><<<dim3((unsigned)((a.rows + 3) / 4), y), kRotaryThreads, 4 * a.pairs * sizeof(float2), st>>>(a);
-  return cudaGetLastError();
+    return launch_chained(k_rotary<T, kE, kInterleaved, 1>, dim3((unsigned)a.rows, y), kRotaryThreads, a.pairs * sizeof(float2), st, a);
+  return launch_chained(k_rotary<T, kE, kInterleaved, 4>, dim3((unsigned)((a.rows + 3) / 4), y), kRotaryThreads, 4 * a.pairs * sizeof(float2), st, a);
 }
 
 template <typename T>
