@@ -250,6 +250,8 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
   FewBarriers* bar = reinterpret_cast<FewBarriers*>(stages + kStages * kStage + 4 * kFewTurn);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   let_next_start();
+  if (threadIdx.x == 32)
+    for (const CUtensorMap* map : {&map_x, &map_w, &map_tile}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < kStages; ++s) { mbar_init(&bar->full[s], 1); mbar_init(&bar->empty[s], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&bar->acc_full[i], 1); mbar_init(&bar->acc_empty[i], 4); }
@@ -501,97 +503,18 @@ __device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, KeyRoom
   row_sync<kWarps>();
 }
 
-constexpr uint32_t kJoinHeldMost = 96 * 1024;  // bytes of maxima in shared memory
-constexpr uint32_t kFewWarps = 8;              // of a row, where the rows are few
-
-// kWarps warps a row.  Many rows: one, and 16 rows a CTA, since a sector of the segments' numbers serves eight of them.
-template <uint32_t kSeg, uint32_t kWarps>
-__global__ void __launch_bounds__(kWarps == 1 ? 512 : 32 * kWarps) k_score_join(const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
-  constexpr uint32_t kRows = kWarps == 1 ? 16 : 1;
-  extern __shared__ float s_most[];  // [kRows][segs]
-  __shared__ KeyRoom<kWarps> s_room[kRows];
-  __shared__ uint32_t s_seg[kRows][FT_LOGPROBS_MAX_TOP];
-  __shared__ float s_part[3][kWarps];
-  after_previous();
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = kWarps == 1 ? warp : 0, m = blockIdx.x * kRows + slot;
-  const uint32_t n = a.tokens && !a.few ? *a.count : a.rows, t = kWarps == 1 ? lane : threadIdx.x;
-  if (m >= n) return;
-  const uint64_t row = a.row0 + (a.tokens && !a.few ? (uint32_t)a.row_of[m] : m);
-  if (a.few && a.tokens && !has_label(a.tokens[row], a.vocab)) {
-    if (t == 0) {
-      a.logprob[row] = 0.f;
-      if (a.entropy) a.entropy[row] = 0.f;
-      if (a.tokens[row] != kNoLabel) note_error(v, a.call_seq, FT_ERR_BAD_TOKEN_ID, (uint32_t)row);
-    }
-    if (t < a.top) { a.top_ids[row * a.top + t] = -1; a.top_logprobs[row * a.top + t] = 0.f; }
-    return;
-  }
-  const uint64_t seg_step = a.few ? 1 : a.rows, first = a.few ? (uint64_t)m * a.segs : m;
-  float* held = s_most + (a.held ? slot * a.segs : 0);
-  const auto most_of = [&](uint32_t s) { return a.held ? held[s] : a.most[first + s * seg_step]; };
-  // the first numbers of a thread are asked for at once
-  constexpr uint32_t kAhead = 4;
-  float ahead[3][kAhead], most = -INFINITY;
-#pragma unroll
-  for (uint32_t i = 0; i < kAhead; ++i) {
-    const uint32_t s = t + i * 32 * kWarps;
-    const uint64_t at = first + s * seg_step;
-    ahead[0][i] = s < a.segs ? a.most[at] : -INFINITY;
-    ahead[1][i] = s < a.segs ? a.sum[at] : 0.f;
-    ahead[2][i] = s < a.segs ? a.moment[at] : 0.f;
-  }
-#pragma unroll
-  for (uint32_t i = 0; i < kAhead; ++i) {
-    const uint32_t s = t + i * 32 * kWarps;
-    if (a.held && s < a.segs) held[s] = ahead[0][i];
-    most = fmaxf(most, ahead[0][i]);
-  }
-#pragma unroll 4
-  for (uint32_t s = t + kAhead * 32 * kWarps; s < a.segs; s += 32 * kWarps) {
-    const float x = a.most[first + s * seg_step];
-    if (a.held) held[s] = x;
-    most = fmaxf(most, x);
-  }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-  if constexpr (kWarps > 1) {
-    if (lane == 0) s_part[0][warp] = most;
-    __syncthreads();
-#pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) most = fmaxf(most, s_part[0][w]);
-  }
-  const float about = most == -INFINITY ? 0.f : most, to_log2 = a.scale * kScoreLog2e;
-  float sum = 0.f, moment = 0.f;
-  const auto add = [&](float x, float part, float part_moment) {
-    if (x == -INFINITY && part == 0.f) return;  // nothing in it (a sum of NaN stays)
-    const float u = max_with_nan(((x == -INFINITY ? 0.f : x) - about) * to_log2, kLeastExponent), e = exp2f(u);
-    sum = fmaf(part, e, sum);
-    moment = fmaf(e, fmaf(part, u, part_moment), moment);
-  };
-#pragma unroll
-  for (uint32_t i = 0; i < kAhead; ++i) add(ahead[0][i], ahead[1][i], ahead[2][i]);
-#pragma unroll 4
-  for (uint32_t s = t + kAhead * 32 * kWarps; s < a.segs; s += 32 * kWarps) {
-    const uint64_t at = first + s * seg_step;
-    add(most_of(s), a.sum[at], a.moment[at]);
-  }
-  sum = warp_sum(sum);
-  moment = warp_sum(moment);
-  if constexpr (kWarps > 1) {
-    if (lane == 0) { s_part[1][warp] = sum; s_part[2][warp] = moment; }
-    __syncthreads();
-    sum = moment = 0.f;
-#pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) { sum += s_part[1][w]; moment += s_part[2][w]; }
-  }
+// A row's results from its joined numbers, by the warps of the row: the sum and moment about `about`, the largest logit (0 where that is -inf).
+// most_of(s): the maximum of segment s.
+template <uint32_t kSeg, uint32_t kWarps, class MostOf>
+__device__ __forceinline__ void row_results(const ScorePiece& a, uint64_t row, uint32_t m, float about, float sum, float moment, KeyRoom<kWarps>& room,
+                                            uint32_t* seg_of, MostOf&& most_of) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = kWarps == 1 ? lane : threadIdx.x;
   const float log_sum = logf(sum);
   if (t == 0) {
     if (a.tokens) a.logprob[row] = (a.target[m] - about) * a.scale - log_sum;
     if (a.entropy) a.entropy[row] = log_sum - kScoreLn2 * moment / sum;
   }
   if (a.top == 0) return;
-  KeyRoom<kWarps>& room = s_room[slot];
-  uint32_t* seg_of = s_seg[slot];
   const uint32_t segs = min(a.top, a.segs);
   uint64_t least = 0;
   row_sync<kWarps>();
@@ -644,6 +567,126 @@ __global__ void __launch_bounds__(kWarps == 1 ? 512 : 32 * kWarps) k_score_join(
       a.top_ids[row * a.top + rank] = (int32_t)key_place(key);
       a.top_logprobs[row * a.top + rank] = (key_value(key) - about) * a.scale - log_sum;
     });
+}
+
+// A segment's numbers, or those of several, taken into numbers about `about`.
+struct Joined {
+  float sum = 0.f, moment = 0.f;
+  __device__ __forceinline__ void add(float most, float part, float part_moment, float about, float to_log2) {
+    if (most == -INFINITY && part == 0.f) return;  // nothing in it (a sum of NaN stays)
+    const float u = max_with_nan(((most == -INFINITY ? 0.f : most) - about) * to_log2, kLeastExponent), e = exp2f(u);
+    sum = fmaf(part, e, sum);
+    moment = fmaf(e, fmaf(part, u, part_moment), moment);
+  }
+};
+__device__ __forceinline__ float finite_about(float most) { return most == -INFINITY ? 0.f : most; }
+
+constexpr uint32_t kJoinHeldMost = 132 * 1024;  // bytes of maxima in shared memory
+
+// kRows rows a CTA, and as many warps: as the segments' numbers lie, the threads go through them rows first, whole sectors at a time; a
+// warp then finishes a row, with the maxima in shared memory where they fit.  (A warp a row from the start read a sector for every
+// number: 61 us for 10813 rows x 256 segments.)
+template <uint32_t kRows>
+__global__ void __launch_bounds__(32 * kRows) k_score_join(const __grid_constant__ ScorePiece a) {
+  constexpr uint32_t kGroups = 32;
+  extern __shared__ float s_held[];  // [kRows][segs, made odd]
+  __shared__ float s_part[3][kGroups][kRows + 1];
+  __shared__ KeyRoom<1> s_room[kRows];
+  __shared__ uint32_t s_seg[kRows][FT_LOGPROBS_MAX_TOP];
+  after_previous();
+  const uint32_t n = a.tokens ? *a.count : a.rows, m0 = blockIdx.x * kRows;
+  if (m0 >= n) return;
+  const uint32_t r = threadIdx.x % kRows, g = threadIdx.x / kRows, held_ld = a.segs | 1;
+  const float to_log2 = a.scale * kScoreLog2e;
+  if (m0 + r < n) {
+    float most = -INFINITY;
+#pragma unroll 4
+    for (uint32_t s = g; s < a.segs; s += kGroups) {
+      const float x = a.most[(uint64_t)s * a.rows + m0 + r];
+      if (a.held) s_held[r * held_ld + s] = x;
+      most = fmaxf(most, x);
+    }
+    Joined mine;
+#pragma unroll 4
+    for (uint32_t s = g; s < a.segs; s += kGroups) {
+      const uint64_t at = (uint64_t)s * a.rows + m0 + r;
+      mine.add(a.held ? s_held[r * held_ld + s] : a.most[at], a.sum[at], a.moment[at], finite_about(most), to_log2);
+    }
+    s_part[0][g][r] = most;
+    s_part[1][g][r] = mine.sum;
+    s_part[2][g][r] = mine.moment;
+  }
+  __syncthreads();
+  const uint32_t lane = threadIdx.x & 31, q = threadIdx.x >> 5, m = m0 + q;
+  if (m >= n) return;
+  float most = s_part[0][lane][q];
+#pragma unroll
+  for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+  Joined all;
+  all.add(s_part[0][lane][q], s_part[1][lane][q], s_part[2][lane][q], finite_about(most), to_log2);
+  row_results<kSegCols, 1>(a, a.row0 + (a.tokens ? (uint32_t)a.row_of[m] : m), m, finite_about(most), warp_sum(all.sum), warp_sum(all.moment), s_room[q], s_seg[q],
+                           [&](uint32_t s) { return a.held ? s_held[q * held_ld + s] : a.most[(uint64_t)s * a.rows + m]; });
+}
+
+// Few rows: a CTA a row.
+constexpr uint32_t kFewWarps = 8;
+__global__ void __launch_bounds__(32 * kFewWarps) k_score_join_few(const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
+  extern __shared__ float s_held[];  // [segs]
+  __shared__ KeyRoom<kFewWarps> s_room;
+  __shared__ uint32_t s_seg[FT_LOGPROBS_MAX_TOP];
+  __shared__ float s_part[3][kFewWarps];
+  after_previous();
+  const uint32_t m = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const uint64_t row = a.row0 + m, first = (uint64_t)m * a.segs;
+  if (a.tokens && !has_label(a.tokens[row], a.vocab)) {
+    if (t == 0) {
+      a.logprob[row] = 0.f;
+      if (a.entropy) a.entropy[row] = 0.f;
+      if (a.tokens[row] != kNoLabel) note_error(v, a.call_seq, FT_ERR_BAD_TOKEN_ID, (uint32_t)row);
+    }
+    if (t < a.top) { a.top_ids[row * a.top + t] = -1; a.top_logprobs[row * a.top + t] = 0.f; }
+    return;
+  }
+  // a thread's first numbers are asked for at once
+  constexpr uint32_t kAhead = 4, kStep = 32 * kFewWarps;
+  float ahead[3][kAhead], most = -INFINITY;
+#pragma unroll
+  for (uint32_t i = 0; i < kAhead; ++i) {
+    const uint32_t s = t + i * kStep;
+    ahead[0][i] = s < a.segs ? a.most[first + s] : -INFINITY;
+    ahead[1][i] = s < a.segs ? a.sum[first + s] : 0.f;
+    ahead[2][i] = s < a.segs ? a.moment[first + s] : 0.f;
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kAhead; ++i) {
+    if (a.held && t + i * kStep < a.segs) s_held[t + i * kStep] = ahead[0][i];
+    most = fmaxf(most, ahead[0][i]);
+  }
+#pragma unroll 4
+  for (uint32_t s = t + kAhead * kStep; s < a.segs; s += kStep) {
+    const float x = a.most[first + s];
+    if (a.held) s_held[s] = x;
+    most = fmaxf(most, x);
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+  if (lane == 0) s_part[0][warp] = most;
+  __syncthreads();
+#pragma unroll
+  for (uint32_t w = 0; w < kFewWarps; ++w) most = fmaxf(most, s_part[0][w]);
+  const float about = finite_about(most), to_log2 = a.scale * kScoreLog2e;
+  Joined mine;
+#pragma unroll
+  for (uint32_t i = 0; i < kAhead; ++i) mine.add(ahead[0][i], ahead[1][i], ahead[2][i], about, to_log2);
+#pragma unroll 4
+  for (uint32_t s = t + kAhead * kStep; s < a.segs; s += kStep) mine.add(a.held ? s_held[s] : a.most[first + s], a.sum[first + s], a.moment[first + s], about, to_log2);
+  float sum = warp_sum(mine.sum), moment = warp_sum(mine.moment);
+  if (lane == 0) { s_part[1][warp] = sum; s_part[2][warp] = moment; }
+  __syncthreads();
+  sum = moment = 0.f;
+#pragma unroll
+  for (uint32_t w = 0; w < kFewWarps; ++w) { sum += s_part[1][w]; moment += s_part[2][w]; }
+  row_results<kFewCols, kFewWarps>(a, row, m, about, sum, moment, s_room, s_seg, [&](uint32_t s) { return a.held ? s_held[s] : a.most[first + s]; });
 }
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
@@ -705,9 +748,12 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   score_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, a.top);
   a.call_seq = status_seq(p);
   a.pairs = (uint32_t)p->sm_count / 2;
-  const uint32_t join_rows = a.few ? 1 : 16;
-  a.held = (uint64_t)join_rows * a.segs * sizeof(float) <= kJoinHeldMost;
-  const size_t join_smem = a.held ? (size_t)join_rows * a.segs * sizeof(float) : 0;
+  // the join's rows a CTA: 8 where 16 would leave SMs without work, or would not have their maxima in shared memory
+  const auto held_bytes = [&](uint64_t n) { return n * (a.segs | 1) * sizeof(float); };
+  const uint32_t join_rows = a.few ? 1 : piece >= 32u * (uint32_t)p->sm_count && held_bytes(16) <= kJoinHeldMost ? 16 : 8;
+  a.held = held_bytes(join_rows) <= kJoinHeldMost;
+  const size_t join_smem = a.held ? (size_t)held_bytes(join_rows) : 0;
+  const auto join = join_rows == 16 ? k_score_join<16> : k_score_join<8>;
   CUtensorMap map_x, map_w, map_z = {};
   if (mma_map(&map_w, w, a.hidden, a.vocab, ldw, a.few ? kFewCols : 64) != CUDA_SUCCESS ||
       (a.top && !a.few && mma_map(&map_z, a.z, a.ld_z, a.padded, a.ld_z, 32, true) != CUDA_SUCCESS))
@@ -719,8 +765,9 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<32>));
     for (auto k : {k_score_few<64, false>, k_score_few<64, true>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<64>));
-    FT_CUDA(cudaFuncSetAttribute(k_score_join<kSegCols, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
-    FT_CUDA(cudaFuncSetAttribute(k_score_join<kFewCols, kFewWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
+    for (auto k : {k_score_join<16>, k_score_join<8>})
+      FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
+    FT_CUDA(cudaFuncSetAttribute(k_score_join_few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     p->score_attr_set = true;
   }
   if (a.few) {
@@ -729,7 +776,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, w, a.hidden, a.vocab, ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const auto kernel = n == 32 ? (a.top ? k_score_few<32, true> : k_score_few<32, false>) : (a.top ? k_score_few<64, true> : k_score_few<64, false>);
     FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : kFewSmem<64>, st, map_x, map_w, map_tile, p->view, a));
-    FT_CUDA(launch_chained(k_score_join<kFewCols, kFewWarps>, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
+    FT_CUDA(launch_chained(k_score_join_few, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
     p->gpu_launches += 2;
     return FT_OK;
   }
@@ -745,7 +792,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     const bool high = a.rows > kMmaTile && a.hidden <= kScoreHigh * kMmaK;
     const auto kernel = a.top ? (high ? k_score<true, 2> : k_score<true, 1>) : (high ? k_score<false, 2> : k_score<false, 1>);
     FT_CUDA(launch_chained(kernel, 2 * a.pairs, kMmaThreads, kMmaSmem, st, map_x, map_w, map_z, p->view, a));
-    FT_CUDA(launch_chained(k_score_join<kSegCols, 1>, dim3((a.rows + join_rows - 1) / join_rows), 512, join_smem, st, p->view, a));
+    FT_CUDA(launch_chained(join, dim3((a.rows + join_rows - 1) / join_rows), 32 * join_rows, join_smem, st, a));
     p->gpu_launches += 2;
   }
   return FT_OK;
