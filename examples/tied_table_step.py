@@ -2,11 +2,18 @@
 
     pool_gather_padded -> pool_layer_norm -> pool_token_loss_grad -> pool_layer_norm_grad -> pool_embed_grad -> pool_adamw_step
 
+or, with norm="rms" and a limit to the gradients' norm,
+
+    pool_gather_padded -> pool_rms_norm -> pool_token_loss_grad -> pool_rms_norm_grad -> pool_embed_grad -> pool_grad_norm -> pool_adamw_step
+
+and pool_token_logprobs scores a microbatch against the table as it stands.
+
 The table is tied: it is the model's input (assembled rows at text positions) and its output (the vocabulary of the loss),
 so its fp32 gradient receives both.  What stands between the two in a model is left out here; a backbone's forward pass goes
 between the gather and the norm, its backward pass between the norm's gradient and the table's.  Torch supplies memory only.
 
     python examples/tied_table_step.py [--workload image_mix_7b] [--samples 16] [--hidden 512] [--steps 8] [--state-bits 8]
+                                       [--norm rms] [--max-norm 1.0]
 """
 import argparse
 import os
@@ -31,8 +38,9 @@ def check(rc, what):
 class TiedTable:
     """Pool, plan, table (fp32 master and the bf16 copy that the gather and the loss read), last norm and AdamW states."""
 
-    def __init__(self, w, state_bits=32, lr=2e-3, weight_decay=0.1):
+    def __init__(self, w, state_bits=32, lr=2e-3, weight_decay=0.1, norm="layer", max_norm=None):
         self.w, self.H, self.V, self.L = w, w.hidden, w.vocab, w.budget_L
+        self.rms, self.max_norm = norm == "rms", max_norm
         self.pool = fp.Pool(fp.PoolConfig(
             page_bytes=w.page_bytes, hbm_pages=w.hbm_pages, host_pages=w.host_pages, max_text_tokens=w.total_text_tokens_capacity,
             ring_seed=0, bind_seed=0, gva_hbm_start=0, gva_host_start=0, max_size=0, hidden=w.hidden, max_samples=w.n_samples,
@@ -57,7 +65,8 @@ class TiedTable:
         self.pos3 = new(3, L, dtype=torch.int32)
         self.ids, self.labels, self.mask = new(L, dtype=torch.int32), new(L, dtype=torch.int32), new(L, dtype=torch.uint8)
         self.mean, self.rstd, self.loss, self.lse = new(L), new(L), new(L), new(L)
-        self.norm_ws = new(max(1, self.pool.layer_norm_grad_workspace(L, H)), dtype=torch.uint8)
+        grad_workspace = self.pool.rms_norm_grad_workspace if self.rms else self.pool.layer_norm_grad_workspace
+        self.norm_ws = new(max(1, grad_workspace(L, H)), dtype=torch.uint8)
         self.loss_ws = new(self.pool.token_loss_workspace(L, H, V, True)[1], dtype=torch.uint8)
         # every label that counts has the same weight, whichever microbatch it is in
         n = 0
@@ -67,8 +76,10 @@ class TiedTable:
         self.n_labels = n
         self.grad_loss = new(1) + 1.0 / n
         self.states, tensors = [], []
-        for p, g, copy, decay in ((self.master, self.g_table, self.table, weight_decay), (self.gain, self.g_gain, None, 0.0),
-                                  (self.shift, self.g_shift, None, 0.0)):
+        learned = [(self.master, self.g_table, self.table, weight_decay), (self.gain, self.g_gain, None, 0.0)]
+        if not self.rms:
+            learned.append((self.shift, self.g_shift, None, 0.0))
+        for p, g, copy, decay in learned:
             k = p.numel()
             bits = state_bits if p is self.master else 32
             m, v = (new(k, dtype=torch.uint8 if bits == 8 else torch.float32) for _ in range(2))
@@ -80,6 +91,12 @@ class TiedTable:
                                           param_dtype=fp.FT_F32, grad_dtype=fp.FT_F32, state_bits=bits, reserved=0))
         self.tensors = (fp.AdamwTensor * len(tensors))(*tensors)
         self.adamw = fp.AdamwConfig(lr=lr, beta1=0.9, beta2=0.95, eps=1e-8, grad_scale=None, step=0)
+        if max_norm is not None:   # the factor goes from pool_grad_norm to pool_adamw_step on the device
+            self.grads = (fp.GradTensor * len(learned))(*[fp.GradTensor(grad=g.data_ptr(), n=g.numel(), dtype=fp.FT_F32)
+                                                          for _, g, _, _ in learned])
+            self.grad_norm, self.clip = new(1), new(1)
+            self.clip_ws = new(self.pool.grad_norm_workspace(), dtype=torch.uint8)
+            self.adamw.grad_scale = self.clip.data_ptr()
 
     def _stream(self):
         return torch.cuda.current_stream().cuda_stream
@@ -106,21 +123,38 @@ class TiedTable:
                                       self.pos3.data_ptr(), self.ids.data_ptr(), self.labels.data_ptr(), self.mask.data_ptr(),
                                       self._stream()), "pool_gather_padded")
 
+    def _norm(self):
+        p, s, L, H = self.pool, self._stream(), self.L, self.H
+        if self.rms:
+            check(p.rms_norm(L, H, self.embeds.data_ptr(), H, 0, 0, fp.FT_BF16, self.gain.data_ptr(), fp.FT_F32, 1e-5, 0, 0,
+                             self.hidden.data_ptr(), H, rstd_ptr=self.rstd.data_ptr(), stream=s), "pool_rms_norm")
+        else:
+            check(p.layer_norm(L, H, self.embeds.data_ptr(), H, fp.FT_BF16, self.gain.data_ptr(), self.shift.data_ptr(), fp.FT_F32, 1e-5,
+                               self.hidden.data_ptr(), H, self.mean.data_ptr(), self.rstd.data_ptr(), s), "pool_layer_norm")
+
+    def _norm_grad(self, more):
+        p, s, L, H = self.pool, self._stream(), self.L, self.H
+        if self.rms:
+            check(p.rms_norm_grad(L, H, self.d_hidden.data_ptr(), H, self.embeds.data_ptr(), H, 0, 0, fp.FT_BF16, self.gain.data_ptr(),
+                                  fp.FT_F32, self.rstd.data_ptr(), self.d_hidden.data_ptr(), H, self.g_gain.data_ptr(), more,
+                                  self.norm_ws.data_ptr(), self.norm_ws.numel(), s), "pool_rms_norm_grad")
+        else:
+            check(p.layer_norm_grad(L, H, self.d_hidden.data_ptr(), H, self.embeds.data_ptr(), H, fp.FT_BF16, self.gain.data_ptr(),
+                                    fp.FT_F32, self.mean.data_ptr(), self.rstd.data_ptr(), self.d_hidden.data_ptr(), H,
+                                    self.g_gain.data_ptr(), self.g_shift.data_ptr(), more, self.norm_ws.data_ptr(),
+                                    self.norm_ws.numel(), s), "pool_layer_norm_grad")
+
     def forward_backward(self, b):
         """Microbatch b: its losses into self.loss, its gradients on top of those of the microbatches before it."""
         p, s, L, H, V = self.pool, self._stream(), self.L, self.H, self.V
         more = b > 0
         self._gather(b)
-        check(p.layer_norm(L, H, self.embeds.data_ptr(), H, fp.FT_BF16, self.gain.data_ptr(), self.shift.data_ptr(), fp.FT_F32, 1e-5,
-                           self.hidden.data_ptr(), H, self.mean.data_ptr(), self.rstd.data_ptr(), s), "pool_layer_norm")
+        self._norm()
         check(p.token_loss_grad(L, H, V, self.hidden.data_ptr(), H, self.table.data_ptr(), H, self.labels.data_ptr(),
                                 self.grad_loss.data_ptr(), 0, self.loss.data_ptr(), self.lse.data_ptr(), self.d_hidden.data_ptr(), H,
                                 self.g_table.data_ptr(), fp.FT_F32, more, self.loss_ws.data_ptr(), self.loss_ws.numel(), s),
               "pool_token_loss_grad")
-        check(p.layer_norm_grad(L, H, self.d_hidden.data_ptr(), H, self.embeds.data_ptr(), H, fp.FT_BF16, self.gain.data_ptr(),
-                                fp.FT_F32, self.mean.data_ptr(), self.rstd.data_ptr(), self.d_hidden.data_ptr(), H,
-                                self.g_gain.data_ptr(), self.g_shift.data_ptr(), more, self.norm_ws.data_ptr(),
-                                self.norm_ws.numel(), s), "pool_layer_norm_grad")
+        self._norm_grad(more)
         check(p.embed_grad(self.plan, b, b + 1, True, self.d_hidden.data_ptr(), self.g_table.data_ptr(), V, s), "pool_embed_grad")
 
     def step(self):
@@ -129,9 +163,26 @@ class TiedTable:
         for b in range(self.n_mb):
             self.forward_backward(b)
             total += self.loss.sum()
+        if self.max_norm is not None:
+            check(self.pool.grad_norm(self.grads, self.max_norm, 0, 0, self.grad_norm.data_ptr(), self.clip.data_ptr(),
+                                      self.clip_ws.data_ptr(), self.clip_ws.numel(), self._stream()), "pool_grad_norm")
         self.adamw.step += 1
         check(self.pool.adamw_step(self.tensors, self.adamw, self._stream()), "pool_adamw_step")
         return total / self.n_labels
+
+    def score(self, b, top=4):
+        """Microbatch b against the table: per row the label's log probability (0 where there is no label), the entropy, and the `top`
+        likeliest tokens with their log probabilities."""
+        L, H, V = self.L, self.H, self.V
+        logprob, entropy, top_logprobs = (torch.empty(n, device="cuda") for n in (L, L, (L, top)))
+        ids = torch.empty(L, top, dtype=torch.int32, device="cuda")
+        ws = torch.empty(self.pool.token_logprobs_workspace(L, H, V, top)[1], dtype=torch.uint8, device="cuda")
+        self._gather(b)
+        self._norm()
+        check(self.pool.token_logprobs(L, H, V, self.hidden.data_ptr(), H, self.table.data_ptr(), H, self.labels.data_ptr(), 1.0,
+                                       logprob.data_ptr(), entropy.data_ptr(), top, ids.data_ptr(), top_logprobs.data_ptr(), ws.data_ptr(),
+                                       ws.numel(), self._stream()), "pool_token_logprobs")
+        return logprob, entropy, ids, top_logprobs
 
     def close(self):
         torch.cuda.synchronize()
@@ -139,9 +190,10 @@ class TiedTable:
         self.pool.destroy()
 
 
-def train(name="tiny", samples=None, hidden=None, steps=8, state_bits=32, page_bytes=None):
+def train(name="tiny", samples=None, hidden=None, steps=8, state_bits=32, page_bytes=None, norm="layer", max_norm=None):
     """Mean loss of each step."""
-    run = TiedTable(workloads.make_workload(name, n_samples=samples, hidden=hidden, page_bytes=page_bytes), state_bits)
+    run = TiedTable(workloads.make_workload(name, n_samples=samples, hidden=hidden, page_bytes=page_bytes), state_bits, norm=norm,
+                    max_norm=max_norm)
     losses = [run.step() for _ in range(steps)]
     losses = [float(x) for x in losses]
     code, detail = run.pool.status()
@@ -157,6 +209,8 @@ if __name__ == "__main__":
     ap.add_argument("--hidden", type=int)
     ap.add_argument("--steps", type=int, default=8)
     ap.add_argument("--state-bits", type=int, default=32, choices=(8, 32))
+    ap.add_argument("--norm", default="layer", choices=("layer", "rms"))
+    ap.add_argument("--max-norm", type=float)
     a = ap.parse_args()
-    for i, x in enumerate(train(a.workload, a.samples, a.hidden, a.steps, a.state_bits)):
+    for i, x in enumerate(train(a.workload, a.samples, a.hidden, a.steps, a.state_bits, norm=a.norm, max_norm=a.max_norm)):
         print(f"step {i + 1}: mean loss {x:.4f}")

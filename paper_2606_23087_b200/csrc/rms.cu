@@ -239,10 +239,11 @@ __global__ void __launch_bounds__(kRmsWideThreads) k_rms_wide(RmsArgs a) {
 
 // ---- backward -----------------------------------------------------------------------------------------------------
 
-// Threads of a CTA, one CTA an SM.  Where the rows are in shared memory a thread reads them twice from there, for the row's sum and
-// for dx, and keeps only its sums over rows: 72 registers, 28 warps.  (With both operands kept in 128 registers 14 warps took 192 us for
-// 32768 rows x 3584 in bf16.)  Element by element they are kept.
-constexpr int kRmsGradThreads(bool vec, int elems) { return vec ? (elems > 16 ? 512 : 896) : (elems > 16 ? 256 : 512); }
+// Threads of a CTA, one CTA an SM.  Where the rows are in shared memory a thread reads s twice from there, for the row's sum and for dx,
+// instead of keeping it, which leaves registers for 21 warps: 32768 rows x 3584 in bf16 with dsum 150 us (14 warps with both operands kept
+// 192, 28 warps with w dy read again as well 159).  Without dsum w dy is read again too (124 us, kept 131).  Element by element both
+// are kept.
+constexpr int kRmsGradThreads(bool vec, int elems) { return vec ? (elems > 16 ? 512 : 672) : (elems > 16 ? 256 : 512); }
 // Groups of kN threads: as many as that, and as leave room for two of their rows in shared memory.
 template <int kStreams, typename T, int V, bool kVec, int kN>
 constexpr int kRmsGradGroups = [] {
@@ -334,6 +335,7 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
     const F2 by = f2(rstd);
     F2 s1[2] = {f2(0.f), f2(0.f)};
     if constexpr (kVec) {
+      F2 a_kept[kRes ? N : 1];
       const auto weights_of = [&](int k, F2 (&w)[E / 2]) {
 #pragma unroll
         for (int i = 0; i < E / 4; ++i)
@@ -349,7 +351,9 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
         for (int i = 0; i < E / 2; ++i) {  // beyond the row dy and w are zero
           const F2 xhat = x[i] * by;
           dw[k * (E / 2) + i] = fma(g[i], xhat, dw[k * (E / 2) + i]);
-          s1[i & 1] = fma(g[i] * w[i], xhat, s1[i & 1]);
+          const F2 wg = g[i] * w[i];
+          if constexpr (kRes) a_kept[k * (E / 2) + i] = wg;
+          s1[i & 1] = fma(wg, xhat, s1[i & 1]);
         }
       }
       const float c1 = group_sum(sum(s1[0] + s1[1])) * inv;
@@ -358,14 +362,16 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
       for (int k = 0; k < V; ++k) {
         F2 x[E / 2], g[E / 2], w[E / 2], d[E / 2];
         in_s.take_chunk(stage, k, x);
-        in_g.take_chunk(stage, k, g);
-        if constexpr (kRes) in_d.take_chunk(stage, k, d);
-        weights_of(k, w);
+        if constexpr (kRes) {
+          in_d.take_chunk(stage, k, d);
+        } else {
+          in_g.take_chunk(stage, k, g);
+          weights_of(k, w);
+        }
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-          const F2 v = fma(x[i] * by, less, g[i] * w[i]);
-          if constexpr (kRes) d[i] = fma(v, by, d[i]);
-          else d[i] = v * by;
+          if constexpr (kRes) d[i] = fma(fma(x[i] * by, less, a_kept[k * (E / 2) + i]), by, d[i]);
+          else d[i] = fma(x[i] * by, less, g[i] * w[i]) * by;
         }
         if (in_s.has(k)) *reinterpret_cast<uint4*>(q + k * kN * E) = Pack<T>::narrow(d);
       }
