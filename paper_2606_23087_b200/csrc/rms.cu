@@ -276,15 +276,19 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
   const uint64_t step = (uint64_t)gridDim.x * kGroups, first = (uint64_t)blockIdx.x * kGroups + group;
   const uint32_t n_rows = rows_from(a.rows, first, step);
   using Feed = RowFeed<T, V, kVec, kN, kThreads, kStages>;
+  // Element by element a bf16 row of dsum is asked for where its turn begins: a row ahead it takes more registers than there are (32768 rows x
+  // 3583 337 us, so 268; 16384 fp32 rows 213, so 228).
+  constexpr bool kAheadD = kVec || sizeof(T) == 4;
   Feed in_s, in_g, in_d;
   in_s.init(a.s, a.lds, first, step, n_rows, a.cols, t, rows + threadIdx.x);
   in_g.init(a.dy, a.lddy, first, step, n_rows, a.cols, t, rows + kStages * V * kThreads + threadIdx.x);
-  if constexpr (kRes) in_d.init(a.dsum, a.lddsum, first, step, n_rows, a.cols, t, rows + 2 * kStages * V * kThreads + threadIdx.x);
+  if constexpr (kRes && kAheadD) in_d.init(a.dsum, a.lddsum, first, step, n_rows, a.cols, t, rows + 2 * kStages * V * kThreads + threadIdx.x);
   const auto fetch = [&](uint32_t s) {
     in_s.fetch(s);
     in_g.fetch(s);
-    if constexpr (kRes) in_d.fetch(s);
+    if constexpr (kRes && kAheadD) in_d.fetch(s);
   };
+  [[maybe_unused]] const T* d_row = static_cast<const T*>(a.dsum) + first * a.lddsum + t;  // dsum's current row, where it is not fetched ahead
   // a row's rstd comes three rows ahead as well, a copy a warp
   const uint32_t lane = threadIdx.x & 31, stat_at = shared_address(&stats[0][threadIdx.x >> 5]);
   const float* stat = a.rstd + first;
@@ -376,10 +380,17 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
         if (in_s.has(k)) *reinterpret_cast<uint4*>(q + k * kN * E) = Pack<T>::narrow(d);
       }
     } else {
-      F2 x[N], g[N], d[kRes ? N : 1];
+      F2 x[N], g[N], d_ahead[kRes && kAheadD ? N : 1];
+      [[maybe_unused]] T d[kRes && !kAheadD ? V : 1];
       in_s.take(stage, x);
       in_g.take(stage, g);
-      if constexpr (kRes) in_d.take(stage, d);
+      if constexpr (kRes && kAheadD) {
+        in_d.take(stage, d_ahead);
+      } else if constexpr (kRes) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) d[k] = in_s.has(k) ? d_row[k * kN] : narrow1<T>(0.f);
+        d_row += step * a.lddsum;
+      }
       fetch(0);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -393,7 +404,8 @@ __global__ void __launch_bounds__(kN * kGroups, 1) k_rms_grad(RmsGradArgs a) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const F2 v = fma(x[i], f2(-c1), g[i]);
-        if constexpr (kRes) x[i] = fma(v, by, d[i]);
+        if constexpr (kRes && kAheadD) x[i] = fma(v, by, d_ahead[i]);
+        else if constexpr (kRes) x[i] = fma(v, by, f2(widen1(d[2 * i]), widen1(d[2 * i + 1])));
         else x[i] = v * by;
       }
       in_s.store(q, x);
