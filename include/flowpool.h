@@ -583,7 +583,7 @@ int32_t pool_adamw_step(ft_pool* pool, const ft_adamw_tensor* tensors, uint32_t 
  *   angle_i = pos[axis_i][row] * freq_i;   (a, b) becomes (a cos - b sin, a sin + b cos) for the pair i of every head
  *   pos     device int32, row r of axis x at pos[x * pos_ld + r]; any value (the angle is taken modulo a turn in 64-bit
  *           fixed point: a far position's is off by 2^-33 of a turn at most)
- *   cfg     host.  freq: host [pairs], radians per position, at most 2^32; axis: host [pairs], 0..2, NULL = all 0 (sections in any
+ *   cfg     host.  freq: host [pairs], radians per position, from -8 to 8; axis: host [pairs], 0..2, NULL = all 0 (sections in any
  *           order are a table); the first 2 * pairs elements of a head are turned, element i with i + pairs (interleaved = 0) or
  *           2i with 2i + 1; the rest is copied.  inverse != 0 turns back: the backward pass of the same call
  *   tensors host [n_tensors]: element e of head h of row r lies at src[r * src_row + h * src_head + e] (strides in elements, so
@@ -591,7 +591,7 @@ int32_t pool_adamw_step(ft_pool* pool, const ft_adamw_tensor* tensors, uint32_t 
  *           written overlaps nothing else of the call
  * Products in fp32, rounded once.  Heads off 16-byte boundaries, and pairs that are no multiple of 8 (4 in fp32), go element by
  * element.
- * Errors: freq NULL, not finite or beyond 2^32, an axis above 2, pairs 0 or more than half of head_dim, a type, a NULL or misaligned
+ * Errors: freq NULL, not finite or beyond 8, an axis above 2, pairs 0 or more than half of head_dim, a type, a NULL or misaligned
  * operand, pos_ld < rows with several axes, heads or rows of dst that overlap INVALID_ARG; head_dim > 512, more than 8192 heads, rows >=
  * 2^31 CAPACITY.  rows = 0 does nothing.
  */

@@ -180,7 +180,7 @@ FT_EXPORT int32_t pool_rotary(ft_pool* p, uint64_t rows, const int32_t* pos, uin
   for (uint32_t i = 0; i < cfg->pairs; ++i) {
     const double f = cfg->freq[i];
     a.axis[i] = cfg->axis ? cfg->axis[i] : 0;
-    if (!(std::fabs(f) <= 4294967296.0) || a.axis[i] > 2) return FT_ERR_INVALID_ARG;
+    if (!(std::fabs(f) <= 8.0) || a.axis[i] > 2) return FT_ERR_INVALID_ARG;
     axes = std::max<uint32_t>(axes, a.axis[i]);
     long double t = f / 6.283185307179586476925286766559L;  // turns a position, of which whole ones count nothing
     t -= std::floor(t);
