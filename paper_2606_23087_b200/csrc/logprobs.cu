@@ -6,7 +6,9 @@
 //
 //   k_score_pick  takes the rows that count out of a piece of the rows: a dense copy of their x, their tokens and row numbers
 //   k_score       z by tiles; a row of a tile gives max, S and U of 128 columns (a segment), each about the segment's own maximum: every
-//                 term of U is negative, so nothing cancels in an entropy; the token's logit; and with alternatives z itself in fp32
+//                 term of U is negative, so nothing cancels in an entropy; the token's logit; and with alternatives z itself in fp32, where it
+//                 may be needed: a row's segments are dealt out to as many classes as there are alternatives, the largest logit seen so far
+//                 of each class is kept, and a segment whose maximum is below all of these holds none of the alternatives
 //   k_score_few   the same for up to 64 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
 //                 of x in its columns, so that no product is spent on rows that are not there; segments of 32 columns
 //   k_score_join  joins a row's segments.  Alternatives: the `top` segments with the largest maxima (equal ones: the first) hold the `top`
@@ -31,7 +33,7 @@ constexpr float kScoreLog2e = 1.4426950408889634f, kScoreLn2 = 0.693147180559945
 constexpr float kLeastExponent = -300.f;    // 2^-300 is zero; finite, so that its product with zero is one
 
 struct ScorePiece {
-  uint32_t rows, hidden, vocab, segs, padded, pairs, top, ld_z;
+  uint32_t rows, hidden, vocab, segs, padded, pairs, top, ld_z;  // padded: rows of xc
   uint32_t few;              // few rows: all of them are there, counted or not, and a row's segments lie side by side
   uint32_t held;             // the join keeps its rows' maxima in shared memory
   uint64_t row0, ldx;
@@ -47,13 +49,21 @@ struct ScorePiece {
   float* target;            // [count] the token's logit
   float *most, *sum, *moment;  // max, S, U of a row's segment: [segs][rows], few rows [rows][segs]
   __nv_bfloat16* xc;        // [padded][hidden]
-  float* z;                 // [padded][ld_z]
+  uint32_t classes;         // of a row's segments: `top`, rounded up to fours
+  uint32_t* seen;           // [rows][classes] the largest maximum so far of a class's segments, as ordered_bits
+  float* z;                 // [rows][ld_z]
 };
 
 __device__ __forceinline__ float max_with_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
+}
+
+// Whole numbers in the order of the values; a NaN counts as -inf, -0 as 0.  None of them is zero.
+__device__ __forceinline__ uint32_t ordered_bits(float z) {
+  const uint32_t b = __float_as_uint(fmaxf(z, -INFINITY) + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
 // A CTA takes kScorePickRows rows, a warp each; where they go it learns by counting the tokens before them itself, so nothing has to wait
@@ -91,6 +101,7 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
   }
   __syncthreads();
   const uint32_t vecs = a.hidden / 8, rows = min(kScorePickRows, a.rows - r0);
+  for (uint32_t i = threadIdx.x; i < rows * a.classes; i += blockDim.x) a.seen[(uint64_t)r0 * a.classes + i] = 0;
   for (uint32_t k = warp; k < rows; k += 8) {
     if (dest[k] < 0) continue;
     const uint4* src = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
@@ -98,6 +109,14 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
 #pragma unroll 8
     for (uint32_t c = lane; c < vecs; c += 32) dst[c] = src[c];
   }
+}
+
+// What k_score_pick clears, where every row counts
+__global__ void __launch_bounds__(256) k_score_clear(ScorePiece a) {
+  let_next_start();
+  after_previous();
+  const uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < (uint64_t)a.rows * a.classes) a.seen[i] = 0;
 }
 
 // max, S and U of a lane's segment, about its maximum
@@ -125,8 +144,8 @@ __device__ __forceinline__ SegStats segment_stats(Z&& z, float scale) {
 // z by tiles; a lane owns a row's segment
 template <bool kKeep, int kHigh>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
-k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_z,
-        const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
+k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ PoolView v,
+        const __grid_constant__ ScorePiece a) {
   let_next_start();
   after_previous();
   const uint32_t n = a.tokens ? *a.count : a.rows, n_tiles = (a.vocab + kMmaTile - 1) / kMmaTile, k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
@@ -136,6 +155,7 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
   bool lost;
   uint32_t z[kSegCols / 32][32];
   int32_t token = kNoLabel;
+  [[maybe_unused]] uint32_t bound = 0;  // no alternative of the lane's row lies in a segment whose maximum is below it
   mma_pair_tiles<false, false, kHigh>(map_x, map_w, (tiles + a.pairs - 1) / a.pairs * a.pairs * k_parts, v, &lost,
     [&](uint32_t item) {  // a pair takes the parts of a tile's K one after the other
       const uint32_t round = item / a.pairs, i = item % a.pairs + round / k_parts * a.pairs, part = round % k_parts;
@@ -150,6 +170,13 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
     [&](const MmaTile& t, uint32_t row) {
       const uint32_t m = t.m + row + (threadIdx.x & 31);
       token = a.tokens && m < n ? a.token[m] : kNoLabel;
+      if constexpr (kKeep) {  // (others raise it meanwhile: an older, lower one keeps more)
+        bound = 0xFFFFFFFFu;
+        for (uint32_t i = 0; m < n && i < a.classes; i += 4) {
+          const uint4 q = __ldcg(reinterpret_cast<const uint4*>(a.seen + (uint64_t)m * a.classes + i));
+          bound = min(bound, min(min(q.x, q.y), min(q.z, q.w)));
+        }
+      }
     },
     [&](const MmaTile& t, uint32_t, uint32_t tmem, uint32_t row, uint32_t col0, auto&& release) {
       const uint32_t c0 = t.n + col0;
@@ -182,18 +209,21 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
         for (uint32_t j = 0; j < kSegCols; ++j)
           if (j >= cols) z[j / 32][j % 32] = 0xFF800000u;
       }
-      if constexpr (kKeep) {
-#pragma unroll
-        for (uint32_t c = 0; c < kSegCols; c += 32)
-          MmaOut().put<false>(&map_z, (int32_t)(c0 + c), (int32_t)(t.m + row),
-                              [&](uint32_t j) { return make_uint4(z[c / 32][4 * j], z[c / 32][4 * j + 1], z[c / 32][4 * j + 2], z[c / 32][4 * j + 3]); });
-      }
       const SegStats g = segment_stats<kSegCols>([&](uint32_t j) { return __uint_as_float(z[j / 32][j % 32]); }, a.scale);
       if (m < n) {
         const uint64_t at = (uint64_t)(c0 / kSegCols) * a.rows + m;
         a.most[at] = g.most;
         a.sum[at] = g.sum;
         a.moment[at] = g.moment;
+        if constexpr (kKeep) {
+          const uint32_t most = ordered_bits(g.most), seg = c0 / kSegCols;
+          if (most >= bound) {
+            float* to = a.z + (uint64_t)m * a.ld_z + c0;
+#pragma unroll
+            for (uint32_t c = 0; c < kSegCols; c += 8) store32(to + c, &z[c / 32][c % 32]);
+            atomicMax(a.seen + (uint64_t)m * a.classes + seg % a.classes, most);  // any order: what is kept differs, not what is found
+          }
+        }
       }
     });
   give_up(v, a.call_seq, lost);
@@ -397,11 +427,8 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
 
 // ---- joining the segments of a row ----------------------------------------------------------------------------------
 
-// An order of (value, place): larger values first, equal ones by place.  A NaN counts as -inf, -0 as 0.  No key is zero.
-__device__ __forceinline__ uint64_t order_key(float z, uint32_t place) {
-  const uint32_t b = __float_as_uint(fmaxf(z, -INFINITY) + 0.f);
-  return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~place;
-}
+// An order of (value, place): larger values first, equal ones by place.  No key is zero.
+__device__ __forceinline__ uint64_t order_key(float z, uint32_t place) { return (uint64_t)ordered_bits(z) << 32 | (uint32_t)~place; }
 __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t b = (uint32_t)(key >> 32);
   return __uint_as_float(b & 0x80000000u ? b & 0x7FFFFFFFu : ~b);
@@ -713,7 +740,9 @@ static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_
   a->sum = reinterpret_cast<float*>(take(4ull * rows * a->segs));
   a->moment = reinterpret_cast<float*>(take(4ull * rows * a->segs));
   a->xc = reinterpret_cast<__nv_bfloat16*>(take(a->few ? 0 : 2ull * padded * hidden));
-  a->z = reinterpret_cast<float*>(take(top ? 4ull * padded * a->ld_z : 0));
+  a->classes = a->few ? 0 : (top + 3) / 4 * 4;
+  a->seen = reinterpret_cast<uint32_t*>(take(4ull * rows * a->classes));
+  a->z = reinterpret_cast<float*>(take(top ? 4ull * rows * a->ld_z : 0));
   return off;
 }
 
@@ -758,10 +787,8 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   a.held = held_bytes(join_rows) <= kJoinHeldMost;
   const size_t join_smem = a.held ? (size_t)held_bytes(join_rows) : 0;
   const auto join = join_rows == 16 ? k_score_join<16> : k_score_join<8>;
-  CUtensorMap map_x, map_w, map_z = {};
-  if (mma_map(&map_w, w, a.hidden, a.vocab, ldw, a.few ? kFewCols : 64) != CUDA_SUCCESS ||
-      (a.top && !a.few && mma_map(&map_z, a.z, a.ld_z, a.padded, a.ld_z, 32, true) != CUDA_SUCCESS))
-    return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+  CUtensorMap map_x, map_w;
+  if (mma_map(&map_w, w, a.hidden, a.vocab, ldw, a.few ? kFewCols : 64) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   if (!p->score_attr_set) {  // once per pool, hence once per device the pool lives on
     for (auto k : {k_score<false, 1>, k_score<false, 2>, k_score<true, 1>, k_score<true, 2>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
@@ -792,10 +819,15 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     if (a.tokens) {
       FT_CUDA(launch_chained(k_score_pick, dim3((a.rows + kScorePickRows - 1) / kScorePickRows), 256, 0, st, p->view, a));
       p->gpu_launches += 1;
+    } else if (a.top) {
+      FT_CUDA(launch_chained(k_score_clear, dim3((unsigned)(((uint64_t)a.rows * a.classes + 255) / 256)), 256, 0, st, a));
+      p->gpu_launches += 1;
     }
-    const bool high = a.rows > kMmaTile && a.hidden <= kScoreHigh * kMmaK;
+    // tiles of 512 rows, unless they would leave pairs without one
+    const uint64_t high_tiles = (uint64_t)((a.rows + 2 * kMmaTile - 1) / (2 * kMmaTile)) * ((a.vocab + kMmaTile - 1) / kMmaTile);
+    const bool high = a.rows > kMmaTile && a.hidden <= kScoreHigh * kMmaK && high_tiles > a.pairs;
     const auto kernel = a.top ? (high ? k_score<true, 2> : k_score<true, 1>) : (high ? k_score<false, 2> : k_score<false, 1>);
-    FT_CUDA(launch_chained(kernel, 2 * a.pairs, kMmaThreads, kMmaSmem, st, map_x, map_w, map_z, p->view, a));
+    FT_CUDA(launch_chained(kernel, 2 * a.pairs, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
     FT_CUDA(launch_chained(join, dim3((a.rows + join_rows - 1) / join_rows), 32 * join_rows, join_smem, st, a));
     p->gpu_launches += 2;
   }

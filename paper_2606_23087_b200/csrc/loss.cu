@@ -171,11 +171,6 @@ __global__ void __launch_bounds__(256) k_pick(PoolView v, LossPiece a) {
 
 // ---- the three products ---------------------------------------------------------------------------------------------
 
-// 32 bytes in one access: a whole sector a lane, where 16 bytes would write it in halves
-__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
 __device__ __forceinline__ void load32(const float* p, float (&v)[8]) {
   asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p) : "memory");

@@ -122,6 +122,12 @@ __device__ __forceinline__ uint32_t count_labels(const int32_t* labels, uint32_t
   return c;
 }
 
+// 32 bytes in one access: a whole sector a lane, where 16 bytes would write it in halves
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
 // 16 bytes at a shared-memory address (32 bits: a generic pointer kept in a structure is read as one, at twice the latency)
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16_async(uint32_t shared_dst, const void* gmem_src) {
