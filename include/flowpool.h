@@ -623,7 +623,7 @@ int32_t pool_rotary(ft_pool* pool, uint64_t rows, const int32_t* pos, uint64_t p
  *                         q = y / scale; all zero: scale 0; a value that is not finite: scale NaN.  They overlap nothing else
  *   rstd                  device fp32 [rows], what the backward pass reads; may be NULL
  * s is normalised as fp32 holds it, before it is rounded into `sum`.  Rows whose operands all start on 16-byte boundaries (q: 8, fp32
- * input 4) take wide accesses; others go element by element, those with q and rows beyond 16384 elements (fp32 with a residual 12288)
+ * input 4) take wide accesses; others go element by element (bf16 at 0.7 of the rate, fp32 at 0.9), those with q and rows beyond 16384 elements (fp32 with a residual 12288)
  * from cache in three passes.
  * Errors: cols 0, a type, eps negative or not finite, x NULL, none of sum, y and q, q without q_scale or the reverse, a misaligned
  * operand, a stride below what a row needs INVALID_ARG; cols > 2^30 CAPACITY.  rows = 0 does nothing.
@@ -639,7 +639,8 @@ int32_t pool_rms_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void* x
  *                                                          be dy, s or dsum, with that one's stride
  *   dweight = sum over rows of dy * xhat                   device fp32 [cols], may be NULL; accumulate != 0 adds to what it holds
  * Sums over rows are fp32, in an order fixed by the shapes and the device.  pool_rms_norm_grad_workspace gives the workspace's size.
- * rows = 0: dweight becomes zero unless accumulating.  Rows beyond 8192 elements (4096 off 16-byte boundaries) are read twice.
+ * rows = 0: dweight becomes zero unless accumulating.  Rows beyond 8192 elements (4096 off 16-byte boundaries) are read
+ * twice.  Rows off 16-byte boundaries go element by element, bf16 at half the rate and fp32 at two thirds.
  * Errors as pool_rms_norm; workspace NULL or misaligned INVALID_ARG, too small CAPACITY.
  */
 int32_t pool_rms_norm_grad_workspace(ft_pool* pool, uint64_t rows, uint32_t cols, uint64_t* bytes);
@@ -678,7 +679,7 @@ int32_t pool_grad_norm(ft_pool* pool, const ft_grad_tensor* tensors, uint32_t n_
  *   top_ids, top_logprobs   device int32 and fp32 [rows, top], the `top` largest logits' ids and log probabilities, largest first,
  *                           equal logits by ascending id; top = 0: neither
  *   tokens  device int32 [rows], -100: the row counts nothing (logprob, entropy and top_logprobs 0, top_ids -1), costs next to
- *           nothing and its x reaches no result.  NULL: every row counts and logprob must be NULL.  Asynchronous: any
+ *           nothing where there are more than 128 rows, and its x reaches no result.  NULL: every row counts and logprob must be NULL.  Asynchronous: any
  *           other token outside [0, vocab) BAD_TOKEN_ID (detail = row; the row is treated as -100)
  * Places beyond the vocabulary have id -1 and log probability -inf.  A logit that is NaN or +inf makes logprob, entropy and top_logprobs NaN;
  * as an alternative a NaN counts as -inf.

@@ -9,12 +9,14 @@
 //                 term of U is negative, so nothing cancels in an entropy; the token's logit; and with alternatives z itself in fp32, where it
 //                 may be needed: a row's segments are dealt out to as many classes as there are alternatives, the largest logit seen so far
 //                 of each class is kept, and a segment whose maximum is below all of these holds none of the alternatives
-//   k_score_few   the same for up to 64 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
+//   k_score_few   the same for up to 128 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
 //                 of x in its columns, so that no product is spent on rows that are not there; segments of 32 columns
 //   k_score_join  joins a row's segments.  Alternatives: the `top` segments with the largest maxima (equal ones: the first) hold the `top`
 //                 largest logits, so only those are read again
 //
-// Bound by the tensor cores, few rows by W.
+// Bound by the tensor cores, long calls by the card's power limit: 10813 rows that count of 16384 x 3584, vocabulary 32768, 8 alternatives 1.6 to
+// 1.9 ms (1.35 to 1.55 PFLOP/s; k_score alone 1.58 ms).  Few rows by W's bytes: 24 x 1024, 32768 23 us (18 of them k_score_few, whose first
+// and last 5 us read nothing), 24 x 4096, 131072 185 us (5.8 TB/s).
 #include <algorithm>
 #include <cmath>
 
@@ -24,7 +26,7 @@ namespace ft {
 
 constexpr uint32_t kSegCols = 128;     // columns of a segment: an epilogue warp's
 constexpr uint32_t kFewCols = 32;      // the same where the rows are few
-constexpr uint32_t kFewRows = 64;      // rows that count as few
+constexpr uint32_t kFewRows = 128;     // rows that count as few
 // The tensor cores truncate at every addition of 16 products, all one way: tiles of 256 rows are summed in parts of kScorePart blocks of K,
 // the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
 constexpr uint32_t kScorePart = 16, kScoreHigh = 66;
@@ -235,6 +237,9 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
 // memory, a row of x a column.  The products of up to kScorePart blocks of K go into columns of their own, as many as half of the tensor
 // memory holds; its other half takes the next tile meanwhile.
 //
+// 65 to 128 rows read x from L2 as often as W from memory, and still take 71 us for 100 x 4096, 32768, where tiles of 256 rows took 96.  Their
+// half of the tensor memory holds two parts of K: a logit over 4096 carries the truncation of 2048.
+//
 // Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 4..7 epilogue.  Waits are bounded as in mma_pair_tiles, and given up the same way.
 constexpr int kFewThreads = 256;
 constexpr uint32_t kFewTile = 128;                       // W's rows of a tile
@@ -245,7 +250,7 @@ constexpr uint32_t kFewBlock = kFewTile * kMmaK * 2 + kN * kMmaK * 2;  // bytes 
 template <uint32_t kN>
 constexpr uint32_t kFewStage = kFewSub * kFewBlock<kN>;
 template <uint32_t kN>
-constexpr uint32_t kFewStages = (kN == 32 ? 10 : 8) / kFewSub;
+constexpr uint32_t kFewStages = (kN == 32 ? 10 : kN == 64 ? 8 : 6) / kFewSub;
 constexpr uint32_t kFewTurn = 32 * 33 * 4;               // bytes of a warp's 32 x 32 logits, turned over
 template <uint32_t kN>
 constexpr size_t kFewSmem = kFewStages<kN> * (size_t)kFewStage<kN> + 4 * kFewTurn + 1024 + 256;
@@ -254,7 +259,7 @@ struct FewBarriers {
   uint64_t full[10], empty[10], acc_full[2], acc_empty[2], drain;
   uint32_t tmem, lost;
 };
-static_assert(sizeof(FewBarriers) <= 256 && kFewSmem<32> <= 227 * 1024 && kFewSmem<64> <= 227 * 1024, "kFewSmem");
+static_assert(sizeof(FewBarriers) <= 256 && kFewSmem<32> <= 227 * 1024 && kFewSmem<64> <= 227 * 1024 && kFewSmem<128> <= 227 * 1024, "kFewSmem");
 
 // `policy`: of the L2 cache.  W passes through it once: lines that leave first make way for themselves, not for what others have there
 // (24 rows x 4096, vocabulary 131072: 192 us without, 185 with).
@@ -796,17 +801,21 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<32>));
     for (auto k : {k_score_few<64, false>, k_score_few<64, true>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<64>));
+    for (auto k : {k_score_few<128, false>, k_score_few<128, true>})
+      FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<128>));
     for (auto k : {k_score_join<16>, k_score_join<8>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     FT_CUDA(cudaFuncSetAttribute(k_score_join_few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     p->score_attr_set = true;
   }
   if (a.few) {
-    const uint32_t n = a.rows <= 32 ? 32 : 64, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
+    const uint32_t n = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
     CUtensorMap map_tile;
     if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, w, a.hidden, a.vocab, ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
-    const auto kernel = n == 32 ? (a.top ? k_score_few<32, true> : k_score_few<32, false>) : (a.top ? k_score_few<64, true> : k_score_few<64, false>);
-    FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : kFewSmem<64>, st, map_x, map_w, map_tile, p->view, a));
+    const auto kernel = n == 32   ? (a.top ? k_score_few<32, true> : k_score_few<32, false>)
+                        : n == 64 ? (a.top ? k_score_few<64, true> : k_score_few<64, false>)
+                                  : (a.top ? k_score_few<128, true> : k_score_few<128, false>);
+    FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : n == 64 ? kFewSmem<64> : kFewSmem<128>, st, map_x, map_w, map_tile, p->view, a));
     FT_CUDA(launch_chained(k_score_join_few, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
     p->gpu_launches += 2;
     return FT_OK;

@@ -85,8 +85,8 @@ def test_logprobs_in_pieces_of_4_gib(pool):  # noqa: F811
 
 # ---- few rows ---------------------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("rows", [1, 16, 33, 64])
-def test_few_rows_that_do_not_count_reach_nothing(pool, rows):  # noqa: F811
+@pytest.mark.parametrize("rows", [1, 16, 33, 64, 65, 128, 129, 300])
+def test_rows_that_do_not_count_reach_nothing(pool, rows):  # noqa: F811
     x, w, tokens = score_inputs(rows, rows, 264, 3001, 1.0)
     x = x.clone()
     clean = run_scores(pool, x, w, tokens, 6)[1]
@@ -108,14 +108,14 @@ def test_few_rows_that_do_not_count_reach_nothing(pool, rows):  # noqa: F811
 @pytest.mark.parametrize("hidden", [8, 1024, 1088, 4104])
 def test_few_rows_at_the_ends_of_tiles_and_parts(pool, vocab, hidden):  # noqa: F811
     """Vocabularies that leave a CTA one segment, or none, and K in one part, a whole one and a little, and several."""
-    for rows, top in ((5, 8), (64, 0), (40, 32)):
+    for rows, top in ((5, 8), (64, 0), (40, 32), (128, 4)):
         x, w, tokens = score_inputs(rows + vocab, rows, hidden, vocab, 0.9, hidden + 8, hidden)
         rc, out = run_scores(pool, x, w, tokens, top)
         assert rc == 0
         check_scores(out, x, w, tokens, top, 1.0)
 
 
-@pytest.mark.parametrize("rows", [64, 65, 256, 257, 512, 513])
+@pytest.mark.parametrize("rows", [64, 65, 128, 129, 256, 257, 512, 513])
 def test_scores_do_not_depend_on_the_row_count_s_kernel(pool, rows):  # noqa: F811
     """The same rows alone, and among so many others that another kernel takes them: the same alternatives, numbers to their roundings."""
     x, w, tokens = score_inputs(3, 600, 512, 2500, 1.0)
