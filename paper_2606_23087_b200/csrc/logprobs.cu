@@ -453,12 +453,12 @@ __device__ __forceinline__ void row_sync() {  // of the warps that share a row
 
 // The `top` first of many keys, by the warps of a row: each(f) calls f(key) for every key of a thread, the lanes of a warp as often
 // (0: no key); put(rank, key) is called for each of the first.  `least`: a key that none of them is below, or 0.  Without one, or
-// where it leaves too many, it is the `top`-th largest of a warp's lanes' own first keys.  What it leaves, usually little more than
-// `top`, is ranked by counting.
-constexpr uint32_t kFewPicks = 64;  // keys that the room holds
+// where it leaves too many, it is the `top`-th largest of a warp's lanes' own first keys, or the smallest of what each warp's first keys
+// give for its share of `top`.  What it leaves (of 1024 segments some 20 for 8, 60 for 32) is ranked by counting.
+constexpr uint32_t kFewPicks = 128;  // keys that the room holds
 template <uint32_t kWarps>
 struct KeyRoom {
-  uint64_t key[kFewPicks], first[kWarps][32], least[kWarps];
+  uint64_t key[kFewPicks], first[kWarps][32], least[kWarps], share[kWarps];
   uint32_t found;
 };
 template <uint32_t kWarps, class Each, class Put>
@@ -500,10 +500,13 @@ __device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, KeyRoom
     }
     uint64_t bound = __shfl_sync(0xFFFFFFFFu, first, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1);
     if constexpr (kWarps > 1) {
-      if (lane == 0) room.least[warp] = bound;
+      const uint64_t share = __shfl_sync(0xFFFFFFFFu, first, __ffs(__ballot_sync(0xFFFFFFFFu, rank == (top + kWarps - 1) / kWarps - 1)) - 1);
+      if (lane == 0) { room.least[warp] = bound; room.share[warp] = share; }
       __syncthreads();
+      uint64_t all = ~0ull;
 #pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) bound = max(bound, room.least[w]);
+      for (uint32_t w = 0; w < kWarps; ++w) { bound = max(bound, room.least[w]); all = min(all, room.share[w]); }
+      bound = max(bound, all);
     }
     least = max(least, bound);
     collect();
