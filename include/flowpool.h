@@ -323,8 +323,9 @@ int32_t pool_free(ft_pool* pool, const uint32_t* sample_slot, uint32_t n, void* 
  * means that none can land later).  The bytes of that call are incomplete and the pool's state is no longer
  * trustworthy: after FT_ERR_TIMEOUT the only call a pool still supports is pool_destroy.  (Under the test hook
  * ft_tuning.bulk_timeout_test nothing was lost: the call's output is incomplete, the pool is intact.)
- * The library's only other device-side spins are those of pool_token_loss*: a CTA pair's warps wait on mbarriers for
- * operands and for one another, with that limit or a tile's own time if that is longer, and the same end (detail = CTA index).
+ * The library's only other device-side spins are those of pool_token_loss* and pool_token_logprobs: the warps of a CTA, or of a
+ * pair, wait on mbarriers for operands and for one another, with that limit or a tile's own time if that is longer, and the same
+ * end (detail = CTA index).
  */
 /* First asynchronous error since the last call of pool_status (smallest call, then smallest code, then smallest
  * detail), then cleared.  Synchronises the device.  Calls are numbered from the last read, on 28 bits: read the
@@ -623,8 +624,8 @@ int32_t pool_rotary(ft_pool* pool, uint64_t rows, const int32_t* pos, uint64_t p
  *                         q = y / scale; all zero: scale 0; a value that is not finite: scale NaN.  They overlap nothing else
  *   rstd                  device fp32 [rows], what the backward pass reads; may be NULL
  * s is normalised as fp32 holds it, before it is rounded into `sum`.  Rows whose operands all start on 16-byte boundaries (q: 8, fp32
- * input 4) take wide accesses; others go element by element (bf16 at 0.7 of the rate, fp32 at 0.9), those with q and rows beyond 16384 elements (fp32 with a residual 12288)
- * from cache in three passes.
+ * input 4) take wide accesses; others go element by element (bf16 at 0.7 of the rate, fp32 at 0.9), those with q and rows beyond 16384
+ * elements (fp32 with a residual 12288) from cache in three passes (at a quarter to a half).
  * Errors: cols 0, a type, eps negative or not finite, x NULL, none of sum, y and q, q without q_scale or the reverse, a misaligned
  * operand, a stride below what a row needs INVALID_ARG; cols > 2^30 CAPACITY.  rows = 0 does nothing.
  */
@@ -678,9 +679,9 @@ int32_t pool_grad_norm(ft_pool* pool, const ft_grad_tensor* tensors, uint32_t n_
  *   entropy[i] = - sum over v of p_v log p_v               device fp32 [rows], may be NULL
  *   top_ids, top_logprobs   device int32 and fp32 [rows, top], the `top` largest logits' ids and log probabilities, largest first,
  *                           equal logits by ascending id; top = 0: neither
- *   tokens  device int32 [rows], -100: the row counts nothing (logprob, entropy and top_logprobs 0, top_ids -1), costs next to
- *           nothing where there are more than 128 rows, and its x reaches no result.  NULL: every row counts and logprob must be NULL.  Asynchronous: any
- *           other token outside [0, vocab) BAD_TOKEN_ID (detail = row; the row is treated as -100)
+ *   tokens  device int32 [rows], -100: the row counts nothing (logprob, entropy and top_logprobs 0, top_ids -1), its x reaches no
+ *           result and beyond 128 rows it costs next to nothing.  NULL: every row counts and logprob must be NULL.  Asynchronous:
+ *           any other token outside [0, vocab) BAD_TOKEN_ID (detail = row; the row is treated as -100)
  * Places beyond the vocabulary have id -1 and log probability -inf.  A logit that is NaN or +inf makes logprob, entropy and top_logprobs NaN;
  * as an alternative a NaN counts as -inf.
  * The gradient of the log probability is pool_token_loss_grad's with -grad_loss.
@@ -758,7 +759,7 @@ int32_t pool_profile_read(ft_pool* pool, ft_kernel_time* out /* host [FT_K_COUNT
  *                        has queued in the same direction, and the application's behind them; the kernels share
  *                        the link but no queue.  Hence off by default
  *   bulk_wait_limit_us   bound, in microseconds, of every wait of the bulk-copy kernels for a staged load (default
- *                        2 000 000; 100..10 000 000), and of every wait inside pool_token_loss*, where it counts as 1 ms
+ *                        2 000 000; 100..10 000 000), and of every wait inside pool_token_loss* and pool_token_logprobs, where it counts as 1 ms
  *                        plus 4 us for each 64 of the dimension that a tile sums over (the products of a tile are waited
  *                        for as a whole) if it is set below that.  A load not seen within it is declared lost and the call
  *                        reports FT_ERR_TIMEOUT through the status word (see FT_ERR_TIMEOUT above)
@@ -768,7 +769,7 @@ int32_t pool_profile_read(ft_pool* pool, ft_kernel_time* out /* host [FT_K_COUNT
  *                        (bounded) for the loads it had issued, and returns; the call stores nothing from those
  *                        frames and reports FT_ERR_TIMEOUT.  Nothing faults and nothing spins beyond twice the
  *                        limit; accepted only with bulk_wait_limit_us set to at most 100 000.  This is the one knob
- *                        that changes results.  The loads of pool_token_loss* announce the 16 bytes too, and its
+ *                        that changes results.  The loads of pool_token_loss* and pool_token_logprobs announce the 16 bytes too, and their
  *                        kernels end the same way, the loads under way being waited for stage by stage
  */
 typedef struct {

