@@ -680,7 +680,7 @@ int32_t pool_grad_norm(ft_pool* pool, const ft_grad_tensor* tensors, uint32_t n_
  *   top_ids, top_logprobs   device int32 and fp32 [rows, top], the `top` largest logits' ids and log probabilities, largest first,
  *                           equal logits by ascending id; top = 0: neither
  *   tokens  device int32 [rows], -100: the row counts nothing (logprob, entropy and top_logprobs 0, top_ids -1), its x reaches no
- *           result and beyond 128 rows it costs next to nothing.  NULL: every row counts and logprob must be NULL.  Asynchronous:
+ *           result and beyond 256 rows it costs next to nothing.  NULL: every row counts and logprob must be NULL.  Asynchronous:
  *           any other token outside [0, vocab) BAD_TOKEN_ID (detail = row; the row is treated as -100)
  * Places beyond the vocabulary have id -1 and log probability -inf.  A logit that is NaN or +inf makes logprob, entropy and top_logprobs NaN;
  * as an alternative a NaN counts as -inf.

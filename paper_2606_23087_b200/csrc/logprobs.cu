@@ -9,7 +9,7 @@
 //                 term of U is negative, so nothing cancels in an entropy; the token's logit; and with alternatives z itself in fp32, where it
 //                 may be needed: a row's segments are dealt out to as many classes as there are alternatives, the largest logit seen so far
 //                 of each class is kept, and a segment whose maximum is below all of these holds none of the alternatives
-//   k_score_few   the same for up to 128 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
+//   k_score_few   the same for up to 256 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
 //                 of x in its columns, so that no product is spent on rows that are not there; segments of 32 columns
 //   k_score_join  joins a row's segments.  Alternatives: the `top` segments with the largest maxima (equal ones: the first) hold the `top`
 //                 largest logits, so only those are read again
@@ -26,7 +26,7 @@ namespace ft {
 
 constexpr uint32_t kSegCols = 128;     // columns of a segment: an epilogue warp's
 constexpr uint32_t kFewCols = 32;      // the same where the rows are few
-constexpr uint32_t kFewRows = 128;     // rows that count as few
+constexpr uint32_t kFewRows = 256;     // rows that count as few
 // The tensor cores truncate at every addition of 16 products, all one way: tiles of 256 rows are summed in parts of kScorePart blocks of K,
 // the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
 constexpr uint32_t kScorePart = 16, kScoreHigh = 66;
@@ -237,20 +237,23 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
 // memory, a row of x a column.  The products of up to kScorePart blocks of K go into columns of their own, as many as half of the tensor
 // memory holds; its other half takes the next tile meanwhile.
 //
-// 65 to 128 rows read x from L2 as often as W from memory, and still take 71 us for 100 x 4096, 32768, where tiles of 256 rows took 96.  Their
-// half of the tensor memory holds two parts of K: a logit over 4096 carries the truncation of 2048.
+// More than 64 rows read x from L2 as often as W from memory, or twice as often, and still take 64 us for 100 x 4096 and 71 for 200 x 3584, vocabulary
+// 32768, where CTA pairs with tiles of 256 rows took 96 and 91.  Their half of the tensor memory holds two parts of K, beyond 128 rows one: a
+// logit carries the truncation of half of K, or of all of it.
 //
 // Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 4..7 epilogue.  Waits are bounded as in mma_pair_tiles, and given up the same way.
 constexpr int kFewThreads = 256;
 constexpr uint32_t kFewTile = 128;                       // W's rows of a tile
 constexpr uint32_t kFewBox = kFewCols * kMmaK * 2;       // bytes of a box of W: a segment's rows, 64 columns of K
-constexpr uint32_t kFewSub = 2;                          // blocks of K of a stage: a row's 256 bytes are asked for together
+// Blocks of K of a stage.  Two: a row's 256 bytes are asked for together; one where x takes most of a stage.
+template <uint32_t kN>
+constexpr uint32_t kFewSub = kN > 128 ? 1 : 2;
 template <uint32_t kN>
 constexpr uint32_t kFewBlock = kFewTile * kMmaK * 2 + kN * kMmaK * 2;  // bytes of a block of K: W's, then x's
 template <uint32_t kN>
-constexpr uint32_t kFewStage = kFewSub * kFewBlock<kN>;
+constexpr uint32_t kFewStage = kFewSub<kN> * kFewBlock<kN>;
 template <uint32_t kN>
-constexpr uint32_t kFewStages = (kN == 32 ? 10 : kN == 64 ? 8 : 6) / kFewSub;
+constexpr uint32_t kFewStages = (kN == 32 ? 10 : kN == 64 ? 8 : kN == 128 ? 6 : 4) / kFewSub<kN>;
 constexpr uint32_t kFewTurn = 32 * 33 * 4;               // bytes of a warp's 32 x 32 logits, turned over
 template <uint32_t kN>
 constexpr size_t kFewSmem = kFewStages<kN> * (size_t)kFewStage<kN> + 4 * kFewTurn + 1024 + 256;
@@ -259,7 +262,7 @@ struct FewBarriers {
   uint64_t full[10], empty[10], acc_full[2], acc_empty[2], drain;
   uint32_t tmem, lost;
 };
-static_assert(sizeof(FewBarriers) <= 256 && kFewSmem<32> <= 227 * 1024 && kFewSmem<64> <= 227 * 1024 && kFewSmem<128> <= 227 * 1024, "kFewSmem");
+static_assert(sizeof(FewBarriers) <= 256 && kFewSmem<32> <= 227 * 1024 && kFewSmem<64> <= 227 * 1024 && kFewSmem<128> <= 227 * 1024 && kFewSmem<256> <= 227 * 1024, "kFewSmem");
 
 // `policy`: of the L2 cache.  W passes through it once: lines that leave first make way for themselves, not for what others have there
 // (24 rows x 4096, vocabulary 131072: 192 us without, 185 with).
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_tile,
             const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr uint32_t kStages = kFewStages<kN>, kStage = kFewStage<kN>;
+  constexpr uint32_t kStages = kFewStages<kN>, kStage = kFewStage<kN>, kSub = kFewSub<kN>;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* turned = reinterpret_cast<float*>(stages + kStages * kStage);
   FewBarriers* bar = reinterpret_cast<FewBarriers*>(stages + kStages * kStage + 4 * kFewTurn);
@@ -318,8 +321,8 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
     uint32_t it = 0;
     for (uint32_t seg = seg0; seg < seg1 && !lost; seg += 4) {
       const uint32_t boxes = min(4u, seg1 - seg);
-      for (uint32_t k = 0; k < k_blocks; k += kFewSub, ++it) {
-        const uint32_t s = it % kStages, at = base + s * kStage, subs = min(kFewSub, k_blocks - k);
+      for (uint32_t k = 0; k < k_blocks; k += kSub, ++it) {
+        const uint32_t s = it % kStages, at = base + s * kStage, subs = min(kSub, k_blocks - k);
         if (!mbar_wait_bounded(&bar->empty[s], ((it / kStages) & 1) ^ 1, limit_ns)) { lost = true; break; }
         mbar_expect_tx(&bar->full[s], subs * (boxes * kFewBox + kN * kMmaK * 2) + v.bulk_tx_slack);  // the slack: a test hook, 0
         for (uint32_t i = 0; i < subs; ++i) {
@@ -346,11 +349,11 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
       const uint32_t acc = tile & 1;
       if (!mbar_wait_bounded(&bar->acc_empty[acc], ((tile >> 1) & 1) ^ 1, limit_ns)) { lost = true; break; }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (uint32_t k = 0; k < k_blocks; k += kFewSub, ++it) {
+      for (uint32_t k = 0; k < k_blocks; k += kSub, ++it) {
         const uint32_t s = it % kStages;
         if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (uint32_t i = 0; i < min(kFewSub, k_blocks - k); ++i) {
+        for (uint32_t i = 0; i < min(kSub, k_blocks - k); ++i) {
           const uint32_t sa = base + s * kStage + i * kFewBlock<kN>, sb = sa + kFewTile * kMmaK * 2, part = (k + i) / each;
 #pragma unroll
           for (uint32_t j = 0; j < kMmaK / 16; ++j)
@@ -368,9 +371,6 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
   } else if (warp >= 4) {
     const uint32_t quarter = warp & 3;
     float* mine = turned + quarter * (kFewTurn / 4);
-    int32_t token[kN / 32];  // of the rows that the lane owns
-#pragma unroll
-    for (uint32_t g = 0; g < kN / 32; ++g) token[g] = a.tokens && g * 32 + lane < a.rows ? a.tokens[a.row0 + g * 32 + lane] : kNoLabel;
     const uint32_t used = (k_blocks + each - 1) / each;  // parts that hold something
     uint32_t tile = 0;
     for (uint32_t s0 = seg0; s0 < seg1 && !lost; s0 += 4, ++tile) {
@@ -378,46 +378,42 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
       lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], (tile >> 1) & 1, limit_ns));
       if (lost) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      uint32_t z[kN / 32][32];
-#pragma unroll
-      for (uint32_t g = 0; g < kN / 32; ++g) {
+      const uint32_t id = seg * kFewCols + lane;
+      // 32 rows of x at a time
+      for (uint32_t g = 0; g * 32 < a.rows && seg < seg1; ++g) {
+        uint32_t z[32];
         const uint32_t at = tmem + acc * 256 + g * 32 + (quarter << 21);
-        tmem_load32(at, z[g]);
+        tmem_load32(at, z);
         tmem_wait();
         for (uint32_t p = 1; p < used; ++p) {
           uint32_t more[32];
           tmem_load32(at + p * kN, more);
           tmem_wait();
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j) z[g][j] = __float_as_uint(__uint_as_float(z[g][j]) + __uint_as_float(more[j]));
+          for (uint32_t j = 0; j < 32; ++j) z[j] = __float_as_uint(__uint_as_float(z[j]) + __uint_as_float(more[j]));
         }
-      }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive_at(smem_u32(&bar->acc_empty[acc]));
-      if (seg >= seg1) continue;
-      const uint32_t id = seg * kFewCols + lane;
-#pragma unroll
-      for (uint32_t g = 0; g < kN / 32; ++g) {
-        if (g * 32 >= a.rows) break;
-        __syncwarp();
 #pragma unroll
         for (uint32_t j = 0; j < 32; ++j) {
-          const float x = id < a.vocab ? __uint_as_float(z[g][j]) : -INFINITY;
+          const float x = id < a.vocab ? __uint_as_float(z[j]) : -INFINITY;
           if (kKeep && g * 32 + j < a.rows) a.z[(uint64_t)(g * 32 + j) * a.ld_z + id] = x;
           mine[j * 33 + lane] = x;
         }
         __syncwarp();
         const uint32_t m = g * 32 + lane;
-        if (m >= a.rows) continue;
-        const uint32_t token_at = (uint32_t)token[g] - seg * kFewCols;
-        if (token_at < kFewCols) a.target[m] = mine[lane * 33 + token_at];
-        const SegStats t = segment_stats<kFewCols>([&](uint32_t j) { return mine[lane * 33 + j]; }, a.scale);
-        const uint64_t at = (uint64_t)m * a.segs + seg;
-        a.most[at] = t.most;
-        a.sum[at] = t.sum;
-        a.moment[at] = t.moment;
+        if (m < a.rows) {
+          const uint32_t token_at = (uint32_t)(a.tokens ? a.tokens[a.row0 + m] : kNoLabel) - seg * kFewCols;
+          if (token_at < kFewCols) a.target[m] = mine[lane * 33 + token_at];
+          const SegStats t = segment_stats<kFewCols>([&](uint32_t j) { return mine[lane * 33 + j]; }, a.scale);
+          const uint64_t to = (uint64_t)m * a.segs + seg;
+          a.most[to] = t.most;
+          a.sum[to] = t.sum;
+          a.moment[to] = t.moment;
+        }
+        __syncwarp();
       }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(smem_u32(&bar->acc_empty[acc]));
       __syncwarp();
     }
   }
@@ -730,10 +726,11 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_score_join_few(const __grid_
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
 
-static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, uint32_t top) {
+// Carves the workspace for pieces of `rows` rows; returns its bytes.  `few`: the call's rows are few, and one piece.
+static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, uint32_t top, bool few) {
   uint64_t off = 0;
   auto take = [&](uint64_t bytes) { const uint64_t o = off; off += align_up_sz(bytes, 256); return base + o; };
-  a->few = rows <= kFewRows;
+  a->few = few;
   const uint64_t padded = a->few ? rows : align_up_sz(rows, kMmaTile);
   const uint32_t cols = a->few ? kFewCols : kSegCols;
   a->rows = rows;
@@ -759,8 +756,9 @@ struct ScoreWork {
   uint64_t rows;
   uint64_t bytes(uint32_t piece) const {
     ScorePiece a;
-    return score_carve(&a, nullptr, piece, hidden, vocab, top);
+    return score_carve(&a, nullptr, piece, hidden, vocab, top, few());
   }
+  bool few() const { return rows <= kFewRows; }
   uint32_t least_rows() const { return (uint32_t)std::min<uint64_t>(rows, kMmaTile); }
   uint32_t best_rows() const {  // with alternatives, pieces whose logits take 4 GiB
     const uint64_t most = top ? std::max<uint64_t>(kMmaTile, (4ull << 30) / (4ull * vocab) / kMmaTile * kMmaTile) : kScoreRowsMost;
@@ -786,7 +784,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   if (!workspace || !aligned_to(workspace, 256)) return FT_ERR_INVALID_ARG;
   if (workspace_bytes < work.least()) return FT_ERR_CAPACITY;
   const uint32_t piece = work.piece_for(workspace_bytes);
-  score_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, a.top);
+  score_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, a.top, work.few());
   a.call_seq = status_seq(p);
   a.pairs = (uint32_t)p->sm_count / 2;
   // the join's rows a CTA: 8 where 16 would leave SMs without work, or would not have their maxima in shared memory
@@ -806,19 +804,23 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<64>));
     for (auto k : {k_score_few<128, false>, k_score_few<128, true>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<128>));
+    for (auto k : {k_score_few<256, false>, k_score_few<256, true>})
+      FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem<256>));
     for (auto k : {k_score_join<16>, k_score_join<8>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     FT_CUDA(cudaFuncSetAttribute(k_score_join_few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kJoinHeldMost));
     p->score_attr_set = true;
   }
   if (a.few) {
-    const uint32_t n = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
+    const uint32_t n = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : a.rows <= 128 ? 128 : 256, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
     CUtensorMap map_tile;
     if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, w, a.hidden, a.vocab, ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const auto kernel = n == 32   ? (a.top ? k_score_few<32, true> : k_score_few<32, false>)
                         : n == 64 ? (a.top ? k_score_few<64, true> : k_score_few<64, false>)
-                                  : (a.top ? k_score_few<128, true> : k_score_few<128, false>);
-    FT_CUDA(launch_chained(kernel, grid, kFewThreads, n == 32 ? kFewSmem<32> : n == 64 ? kFewSmem<64> : kFewSmem<128>, st, map_x, map_w, map_tile, p->view, a));
+                        : n == 128 ? (a.top ? k_score_few<128, true> : k_score_few<128, false>)
+                                   : (a.top ? k_score_few<256, true> : k_score_few<256, false>);
+    const size_t smem = n == 32 ? kFewSmem<32> : n == 64 ? kFewSmem<64> : n == 128 ? kFewSmem<128> : kFewSmem<256>;
+    FT_CUDA(launch_chained(kernel, grid, kFewThreads, smem, st, map_x, map_w, map_tile, p->view, a));
     FT_CUDA(launch_chained(k_score_join_few, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
     p->gpu_launches += 2;
     return FT_OK;

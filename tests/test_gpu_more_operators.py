@@ -774,7 +774,7 @@ def test_logprobs_refusals_and_empty_inputs(pool):
         pool.token_logprobs_workspace(rows, hidden, vocab, 33)
 
 
-@pytest.mark.parametrize("rows", [20, 100, 600])
+@pytest.mark.parametrize("rows", [20, 60, 100, 200, 600])
 def test_a_logprobs_wait_that_runs_out_reports_timeout_and_leaves_the_context_usable(rows):
     """Under the test hook every load announces 16 bytes more than it brings, so no stage is ever seen complete although all
     arrive: every warp of every pair waits a millisecond, gives up, waits once more for what it has under way, and returns."""

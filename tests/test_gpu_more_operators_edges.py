@@ -85,7 +85,7 @@ def test_logprobs_in_pieces_of_4_gib(pool):  # noqa: F811
 
 # ---- few rows ---------------------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("rows", [1, 16, 33, 64, 65, 128, 129, 300])
+@pytest.mark.parametrize("rows", [1, 16, 33, 64, 65, 128, 129, 256, 300])
 def test_rows_that_do_not_count_reach_nothing(pool, rows):  # noqa: F811
     x, w, tokens = score_inputs(rows, rows, 264, 3001, 1.0)
     x = x.clone()
@@ -108,11 +108,21 @@ def test_rows_that_do_not_count_reach_nothing(pool, rows):  # noqa: F811
 @pytest.mark.parametrize("hidden", [8, 1024, 1088, 4104])
 def test_few_rows_at_the_ends_of_tiles_and_parts(pool, vocab, hidden):  # noqa: F811
     """Vocabularies that leave a CTA one segment, or none, and K in one part, a whole one and a little, and several."""
-    for rows, top in ((5, 8), (64, 0), (40, 32), (128, 4)):
+    for rows, top in ((5, 8), (64, 0), (40, 32), (128, 4), (256, 1)):
         x, w, tokens = score_inputs(rows + vocab, rows, hidden, vocab, 0.9, hidden + 8, hidden)
         rc, out = run_scores(pool, x, w, tokens, top)
         assert rc == 0
         check_scores(out, x, w, tokens, top, 1.0)
+
+
+def test_pieces_of_as_many_rows_as_count_as_few(pool):  # noqa: F811
+    """The least workspace for 300 rows holds 256 at a time: a piece of that size is not a call of few rows."""
+    x, w, tokens = score_inputs(14, 300, 128, 900, 0.9)
+    first = run_scores(pool, x, w, tokens, 3)[1]
+    rc, out = run_scores(pool, x, w, tokens, 3, ws_bytes=lambda least, best: least, fill=255)
+    assert rc == 0
+    for k in out:
+        assert torch.equal(bits(out[k]), bits(first[k])), k
 
 
 @pytest.mark.parametrize("rows", [64, 65, 128, 129, 256, 257, 512, 513])
