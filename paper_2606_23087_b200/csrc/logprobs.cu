@@ -26,7 +26,7 @@ namespace ft {
 
 constexpr uint32_t kSegCols = 128;     // columns of a segment: an epilogue warp's
 constexpr uint32_t kFewCols = 32;      // the same where the rows are few
-constexpr uint32_t kFewRows = 256;     // rows that count as few
+constexpr uint32_t kFewRows = 256;     // rows that count as few, where K allows it (ScoreWork::few)
 // The tensor cores truncate at every addition of 16 products, all one way: tiles of 256 rows are summed in parts of kScorePart blocks of K,
 // the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
 constexpr uint32_t kScorePart = 16, kScoreHigh = 66;
@@ -726,6 +726,9 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_score_join_few(const __grid_
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
 
+// columns of tensor memory that so many rows take in k_score_few
+static uint32_t few_columns(uint32_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+
 // Carves the workspace for pieces of `rows` rows; returns its bytes.  `few`: the call's rows are few, and one piece.
 static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_t hidden, uint32_t vocab, uint32_t top, bool few) {
   uint64_t off = 0;
@@ -758,7 +761,8 @@ struct ScoreWork {
     ScorePiece a;
     return score_carve(&a, nullptr, piece, hidden, vocab, top, few());
   }
-  bool few() const { return rows <= kFewRows; }
+  // few rows, and no more of K in one piece than elsewhere
+  bool few() const { return rows <= kFewRows && (hidden + kMmaK - 1) / kMmaK <= kScoreHigh * (256 / few_columns((uint32_t)rows)); }
   uint32_t least_rows() const { return (uint32_t)std::min<uint64_t>(rows, kMmaTile); }
   uint32_t best_rows() const {  // with alternatives, pieces whose logits take 4 GiB
     const uint64_t most = top ? std::max<uint64_t>(kMmaTile, (4ull << 30) / (4ull * vocab) / kMmaTile * kMmaTile) : kScoreRowsMost;
@@ -812,7 +816,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     p->score_attr_set = true;
   }
   if (a.few) {
-    const uint32_t n = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : a.rows <= 128 ? 128 : 256, grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
+    const uint32_t n = few_columns(a.rows), grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
     CUtensorMap map_tile;
     if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, w, a.hidden, a.vocab, ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const auto kernel = n == 32   ? (a.top ? k_score_few<32, true> : k_score_few<32, false>)

@@ -105,7 +105,7 @@ def test_rows_that_do_not_count_reach_nothing(pool, rows):  # noqa: F811
 
 
 @pytest.mark.parametrize("vocab", [1, 31, 32, 33, 128, 129, 4736, 4737, 19000])
-@pytest.mark.parametrize("hidden", [8, 1024, 1088, 4104])
+@pytest.mark.parametrize("hidden", [8, 1024, 1088, 4104, 4232])
 def test_few_rows_at_the_ends_of_tiles_and_parts(pool, vocab, hidden):  # noqa: F811
     """Vocabularies that leave a CTA one segment, or none, and K in one part, a whole one and a little, and several."""
     for rows, top in ((5, 8), (64, 0), (40, 32), (128, 4), (256, 1)):
