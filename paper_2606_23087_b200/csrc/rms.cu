@@ -85,10 +85,10 @@ __device__ __forceinline__ void weights_from(const void* weight, uint32_t dtype,
 // CTAs of an SM: 896 threads of 72 registers, 512 where a thread holds 32 elements or goes element by element.
 template <typename T, int V, bool kVec, int kN>
 constexpr int kRmsCtas = kVec && V * Pack<T>::kElems <= 16 ? 896 / kN : 512 / kN;
-// Rows in shared memory or under way to it: as many as leave room for those CTAs, from two to four.
+// Rows in shared memory or under way to it: as many as leave room for those CTAs, from two to four; two where a call has few rows.
 constexpr int stages_within(size_t budget, size_t stage) { return budget / stage < 2 ? 2 : budget / stage > 4 ? 4 : (int)(budget / stage); }
 template <int kStreams, typename T, int V, int kN>
-constexpr int kRmsStages = stages_within(kSmemMost / kRmsCtas<T, V, true, kN> - 2048, (size_t)kStreams * V * kN * 16);
+constexpr int kRmsStages = V * Pack<T>::kElems <= 8 ? 2 : stages_within(kSmemMost / kRmsCtas<T, V, true, kN> - 2048, (size_t)kStreams * V * kN * 16);
 
 template <typename T, int V, bool kVec, int kN, bool kRes>
 __global__ void __launch_bounds__(kN, (kRmsCtas<T, V, kVec, kN>)) k_rms(RmsArgs a) {

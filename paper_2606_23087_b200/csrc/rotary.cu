@@ -183,9 +183,10 @@ FT_EXPORT int32_t pool_rotary(ft_pool* p, uint64_t rows, const int32_t* pos, uin
     a.axis[i] = cfg->axis ? cfg->axis[i] : 0;
     if (!(std::fabs(f) <= 8.0) || a.axis[i] > 2) return FT_ERR_INVALID_ARG;
     axes = std::max<uint32_t>(axes, a.axis[i]);
-    long double t = f / 6.283185307179586476925286766559L;  // turns a position, of which whole ones count nothing
-    t -= std::floor(t);
-    const uint64_t u = t < 1.0L ? (uint64_t)std::ldexp(t, 64) : 0;
+    long double t = f * 0.159154943091895335768883763372514362L;  // turns a position, of which whole ones count nothing
+    t -= (long double)(int64_t)t;
+    if (t < 0) t += 1;
+    const uint64_t u = t < 1.0L ? (uint64_t)(t * 0x1p64L) : 0;
     a.turns[i] = cfg->inverse ? 0 - u : u;
   }
   if (rows && (!pos || !aligned_to(pos, 4) || (axes && pos_ld < rows))) return FT_ERR_INVALID_ARG;
