@@ -242,10 +242,10 @@ __global__ void __launch_bounds__(kRmsWideThreads) k_rms_wide(RmsArgs a) {
 // ---- backward -----------------------------------------------------------------------------------------------------
 
 // Threads of a CTA, one CTA an SM.  Where the rows are in shared memory a thread reads s twice from there, for the row's sum and for dx,
-// instead of keeping it, which leaves registers for 21 warps: 32768 rows x 3584 in bf16 with dsum 150 us (14 warps with both operands kept
-// 192, 28 warps with w dy read again as well 159).  Without dsum w dy is read again too (124 us, kept 131).  Element by element both
-// are kept.
-constexpr int kRmsGradThreads(bool vec, int elems) { return vec ? (elems > 16 ? 512 : 672) : (elems > 16 ? 256 : 512); }
+// instead of keeping it, which leaves registers for more warps.  32768 rows x 3584 in bf16 with dsum: 32 warps of 8 elements a thread 142 us, 21
+// of 16 150, 14 of 16 with both operands kept 192; 16384 rows in fp32 143, 21 warps 190.  Without dsum w dy is read again too, and 21
+// warps of 16 elements do better: 124 us, 32 of 8 140.  Element by element both are kept.
+constexpr int kRmsGradThreads(bool vec, int elems) { return vec ? (elems > 16 ? 512 : elems > 8 ? 672 : 1024) : (elems > 16 ? 256 : 512); }
 // Groups of kN threads: as many as that, and as leave room for two of their rows in shared memory.
 template <int kStreams, typename T, int V, bool kVec, int kN>
 constexpr int kRmsGradGroups = [] {
@@ -557,18 +557,19 @@ static cudaError_t rms_grad_rows(ft_pool* p, const RmsGradArgs& a, uint32_t* lin
   return launch_chained(kernel, dim3(*lines), kN * kGroups, smem, st, a);
 }
 
-// 16 elements a thread, which 256 threads make 4096; 32 up to 8192.
+// 16 elements a thread, which 256 threads make 4096, with dsum 8 and 512 threads; 32 up to 8192.
 template <typename T, bool kVec, bool kRes>
 static cudaError_t rms_grad_launch(ft_pool* p, const RmsGradArgs& a, float* sums, uint32_t* lines, cudaStream_t st) {
   constexpr uint32_t E = kVec ? Pack<T>::kElems : 1;
-  constexpr int kFew = kChunks<T, kVec, 4>, kMany = kChunks<T, kVec, 16>, kLong = kChunks<T, true, 32>;
+  constexpr bool kEight = kVec && kRes;
+  constexpr int kFew = kChunks<T, kVec, 4>, kMany = kChunks<T, kVec, kEight ? 8 : 16>, kLong = kChunks<T, true, 32>, kMost = kEight ? 512 : 256;
   const uint32_t n = a.cols / E;
   if (n <= 32u * kFew) return rms_grad_rows<T, kVec, kFew, 32, kRes>(p, a, lines, st);
   cudaError_t e = cudaErrorInvalidConfiguration;
-  if (n <= kMany * 256u) {
+  if (n <= (uint32_t)(kMany * kMost)) {
     with_threads((n + kMany - 1) / kMany, [&](auto k) {
       constexpr int kN = decltype(k)::value;
-      if constexpr (kN <= 256) e = rms_grad_rows<T, kVec, kMany, kN, kRes>(p, a, lines, st);
+      if constexpr (kN <= kMost) e = rms_grad_rows<T, kVec, kMany, kN, kRes>(p, a, lines, st);
     });
   } else if (kVec && n <= kLong * 256u) {
     with_threads((n + kLong - 1) / kLong, [&](auto k) {
