@@ -5,7 +5,7 @@
 //   backward   xhat = s rstd,  a = w dy,  ds = rstd (a - xhat sum(a xhat) / c) + dsum,  dw = sum over rows of dy xhat
 //
 // Both are bound by HBM: each row is read and written once.  32768 rows x 3584 in bf16: with a residual 142 us (6.6 TB/s, the copy rate), without
-// one 73, with an 8-bit output 127; backward with dsum 150 us (6.2 TB/s, 6 us of it for joining the lines).  Rows off 16-byte boundaries go element by
+// one 73, with an 8-bit output 127; backward with dsum 154 us (6.1 TB/s, 6 us of it for joining the lines).  Rows off 16-byte boundaries go element by
 // element: 198 and 263 us.
 //
 //   k_rms           a few warps hold a row in registers, the rows that follow are on their way into shared memory
@@ -242,9 +242,8 @@ __global__ void __launch_bounds__(kRmsWideThreads) k_rms_wide(RmsArgs a) {
 // ---- backward -----------------------------------------------------------------------------------------------------
 
 // Threads of a CTA, one CTA an SM.  Where the rows are in shared memory a thread reads s twice from there, for the row's sum and for dx,
-// instead of keeping it, which leaves registers for more warps.  32768 rows x 3584 in bf16 with dsum: 32 warps of 8 elements a thread 142 us, 21
-// of 16 150, 14 of 16 with both operands kept 192; 16384 rows in fp32 143, 21 warps 190.  Without dsum w dy is read again too, and 21
-// warps of 16 elements do better: 124 us, 32 of 8 140.  Element by element both are kept.
+// instead of keeping it, which leaves registers for 21 warps of 16 elements a thread (with both operands kept 14: 32768 rows x 3584 in
+// bf16 with dsum 192 us, not 154) or 32 of 8.  Without dsum w dy is read again too.  Element by element both are kept.
 constexpr int kRmsGradThreads(bool vec, int elems) { return vec ? (elems > 16 ? 512 : elems > 8 ? 672 : 1024) : (elems > 16 ? 256 : 512); }
 // Groups of kN threads: as many as that, and as leave room for two of their rows in shared memory.
 template <int kStreams, typename T, int V, bool kVec, int kN>
@@ -557,20 +556,39 @@ static cudaError_t rms_grad_rows(ft_pool* p, const RmsGradArgs& a, uint32_t* lin
   return launch_chained(kernel, dim3(*lines), kN * kGroups, smem, st, a);
 }
 
-// 16 elements a thread, which 256 threads make 4096, with dsum 8 and 512 threads; 32 up to 8192.
+// Whether rows with dsum may go 8 elements a thread in groups of kN, and not 16.  More warps hide more, and twice as many threads reduce and issue:
+// 8 do better where 2, 4 or 8 groups make a CTA, and with two elements a word only where next to all of a group's threads have some.
+// us, 8 against 16 elements a thread, 0.7 GB in sustained passes: bf16 28672 x 4096 155 and 162, 30464 x 3840 157 and 160, 57344 x 2048 146 and
+// 161, 61440 x 1792 145 and 152, 65536 x 1024 89 and 93; but 32768 x 3584 (7/8 of the threads) 162 and 154, 36864 x 3200 173 and 158, 76000 x 1536
+// (5 groups) 192 and 152, 229376 x 512 (15) 194 and 173.  fp32 16384 x 3584 144 and 189, 18432 x 3200 144 and 190, 22528 x 2560 148 and 168,
+// 57344 x 1024 150 and 183; 114000 x 512 185 and 166.  Without dsum 16: 32768 x 3584 in bf16 124, 8 140.
+template <typename T, int kN>
+constexpr bool kRmsGradEight = [] {
+  const int groups = kRmsGradGroups<3, T, kChunks<T, true, 8>, true, kN>;
+  return groups == 2 || groups == 4 || groups == 8;
+}();
+
+// 16 elements a thread, which 256 threads make 4096, or 8 and 512 threads; 32 up to 8192.
 template <typename T, bool kVec, bool kRes>
 static cudaError_t rms_grad_launch(ft_pool* p, const RmsGradArgs& a, float* sums, uint32_t* lines, cudaStream_t st) {
   constexpr uint32_t E = kVec ? Pack<T>::kElems : 1;
-  constexpr bool kEight = kVec && kRes;
-  constexpr int kFew = kChunks<T, kVec, 4>, kMany = kChunks<T, kVec, kEight ? 8 : 16>, kLong = kChunks<T, true, 32>, kMost = kEight ? 512 : 256;
+  constexpr int kFew = kChunks<T, kVec, 4>, kEight = kChunks<T, true, 8>, kMany = kChunks<T, kVec, 16>, kLong = kChunks<T, true, 32>;
   const uint32_t n = a.cols / E;
   if (n <= 32u * kFew) return rms_grad_rows<T, kVec, kFew, 32, kRes>(p, a, lines, st);
   cudaError_t e = cudaErrorInvalidConfiguration;
-  if (n <= (uint32_t)(kMany * kMost)) {
-    with_threads((n + kMany - 1) / kMany, [&](auto k) {
-      constexpr int kN = decltype(k)::value;
-      if constexpr (kN <= kMost) e = rms_grad_rows<T, kVec, kMany, kN, kRes>(p, a, lines, st);
-    });
+  if (n <= kMany * 256u) {
+    bool eight = false;
+    if constexpr (kVec && kRes)
+      with_threads((n + kEight - 1) / kEight, [&](auto k) {
+        constexpr int kN = decltype(k)::value;
+        if constexpr (kRmsGradEight<T, kN>)
+          if ((eight = sizeof(T) == 4 || 16 * (n / kEight) >= 15u * kN)) e = rms_grad_rows<T, kVec, kEight, kN, kRes>(p, a, lines, st);
+      });
+    if (!eight)
+      with_threads((n + kMany - 1) / kMany, [&](auto k) {
+        constexpr int kN = decltype(k)::value;
+        if constexpr (kN <= 256) e = rms_grad_rows<T, kVec, kMany, kN, kRes>(p, a, lines, st);
+      });
   } else if (kVec && n <= kLong * 256u) {
     with_threads((n + kLong - 1) / kLong, [&](auto k) {
       constexpr int kN = decltype(k)::value;

@@ -334,7 +334,7 @@ def test_rms_norm_8_bits_of_extreme_rows(pool, dtype):
 
 @pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("shape", SHAPES + [(5000, 136), (2049, 77)])
+@pytest.mark.parametrize("shape", SHAPES + [(5000, 136), (2049, 77), (2600, 1000), (1400, 1784), (1400, 1592), (1300, 2040), (700, 2984), (660, 3848)])
 def test_rms_norm_grad_against_64_bits(pool, shape, dtype, residual):
     rows, cols = shape
     g = gen(rows * 31 + cols)
