@@ -4,15 +4,20 @@
 //   z = x W^T, u = (z - max) scale log2(e), S = sum(2^u), U = sum(u 2^u)
 //   logprob = (z_token - max) scale - ln S,  entropy = ln S - ln 2 U / S
 //
-//   k_score_pick  takes the rows that count out of a piece of the rows: a dense copy of their x, their tokens and row numbers
-//   k_score       z by tiles; a row of a tile gives max, S and U of 128 columns (a segment), each about the segment's own maximum: every
-//                 term of U is negative, so nothing cancels in an entropy; the token's logit; and with alternatives z itself in fp32, where it
+//   k_score_pick  takes the rows that count out of a piece of the rows: a dense copy of their x, their tokens, row numbers and tokens' logits
+//   k_score       z by tiles; a row of a tile gives max, S and U of 128 columns (a segment), the token's left out, each about the segment's own
+//                 maximum: every term of U is negative, so nothing cancels in an entropy; and with alternatives z itself in fp32, where it
 //                 may be needed: a row's segments are dealt out to as many classes as there are alternatives, the largest logit seen so far
 //                 of each class is kept, and a segment whose maximum is below all of these holds none of the alternatives
 //   k_score_few   the same for up to 256 rows, which are a matter of W's bytes: W's rows lie across the tensor memory's lanes and the rows
 //                 of x in its columns, so that no product is spent on rows that are not there; segments of 32 columns
 //   k_score_join  joins a row's segments.  Alternatives: the `top` segments with the largest maxima (equal ones: the first) hold the `top`
-//                 largest logits, so only those are read again
+//                 largest logits, so only those are read again.  The logits that a caller gets to see, the token's and the alternatives', it
+//                 takes once more as x . W[id] by fp32 FMAs, corrects the sums by them, and orders the list by them: the tensor cores
+//                 truncate at every addition, all one way, and in a logit that stands alone that does not average out (log probabilities of
+//                 likely tokens, about -1, K = 4104 in parts of 1024: off by 4.7e-6 of their size on average without this, 0.6e-6 with it;
+//                 in one piece 1.2e-5 and 1.5e-6.  Tokens at random, about -8: 1.2e-7 and 1.1e-7, 4.6e-7 and 3.8e-7)
+//   k_score_list  the same for long calls with alternatives, behind the join
 //
 // Bound by the tensor cores, long calls by the card's power limit: 10813 rows that count of 16384 x 3584, vocabulary 32768, 8 alternatives 1.6 to
 // 1.9 ms (1.35 to 1.55 PFLOP/s; k_score alone 1.58 ms).  Few rows by W's bytes: 24 x 1024, 32768 23 us (18 of them k_score_few, whose first
@@ -39,7 +44,8 @@ struct ScorePiece {
   uint32_t few;              // few rows: all of them are there, counted or not, and a row's segments lie side by side
   uint32_t held;             // the join keeps its rows' maxima in shared memory
   uint64_t row0, ldx;
-  const __nv_bfloat16* x;
+  uint64_t ldw;
+  const __nv_bfloat16 *x, *w;
   const int32_t* tokens;
   float scale;
   float *logprob, *entropy, *top_logprobs;
@@ -48,10 +54,12 @@ struct ScorePiece {
   // workspace
   uint32_t* count;          // rows of the piece that count
   int32_t *row_of, *token;  // [count] row in the piece, token
-  float* target;            // [count] the token's logit
+  float* target;            // [count] the token's logit, by FMAs
   float *most, *sum, *moment;  // max, S, U of a row's segment: [segs][rows], few rows [rows][segs]
   __nv_bfloat16* xc;        // [padded][hidden]
   uint32_t classes;         // of a row's segments: `top`, rounded up to fours
+  float4* joined;           // [count] a row's maximum, S and U
+  uint64_t* listed;         // [count][top] its alternatives but the token, as order_key of the logit that the sums give; 0: none
   uint32_t* seen;           // [rows][classes] the largest maximum so far of a class's segments, as ordered_bits
   float* z;                 // [rows][ld_z]
 };
@@ -67,6 +75,52 @@ __device__ __forceinline__ uint32_t ordered_bits(float z) {
   const uint32_t b = __float_as_uint(fmaxf(z, -INFINITY) + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+
+// A lane's share of x . w by fp32 FMAs: of every 32 pieces of 8 elements the one at its place.  The order depends on K alone, so that equal rows of W
+// give equal logits wherever they are taken.
+struct RowDot {
+  F2 acc[2] = {F2{0}, F2{0}};
+  __device__ __forceinline__ void add(uint4 x, uint4 w) {
+    F2 f[4], g[4];
+    Pack<__nv_bfloat16>::widen(x, f);
+    Pack<__nv_bfloat16>::widen(w, g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j & 1] = fma(f[j], g[j], acc[j & 1]);
+  }
+  __device__ __forceinline__ float total() const { return warp_sum(sum(acc[0] + acc[1])); }  // the whole warp
+};
+// x . w[i] by a warp, four pieces of each row a lane on their way at a time
+template <uint32_t kRowsOfW>
+__device__ __forceinline__ void row_dots(const __nv_bfloat16* x_row, const uint4* const (&w)[kRowsOfW], uint32_t hidden, float (&z)[kRowsOfW]) {
+  constexpr uint32_t kAhead = kRowsOfW == 1 ? 8 : 4;
+  const uint32_t vecs = hidden / 8;
+  const uint4* x = reinterpret_cast<const uint4*>(x_row);
+  RowDot dot[kRowsOfW];
+  for (uint32_t c0 = threadIdx.x & 31; c0 < vecs; c0 += 32 * kAhead) {
+    uint4 xv[kAhead], wv[kRowsOfW][kAhead];
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      const uint32_t c = c0 + 32 * i;
+      const bool there = c < vecs;
+      xv[i] = there ? x[c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (uint32_t r = 0; r < kRowsOfW; ++r) wv[r][i] = there ? w[r][c] : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (uint32_t r = 0; r < kRowsOfW; ++r) dot[r].add(xv[i], wv[r][i]);
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < kRowsOfW; ++r) z[r] = dot[r].total();
+}
+__device__ __forceinline__ float row_dot(const __nv_bfloat16* x_row, const uint4* w, uint32_t hidden) {
+  const uint4* const rows[1] = {w};
+  float z[1];
+  row_dots<1>(x_row, rows, hidden, z);
+  return z[0];
+}
+__device__ __forceinline__ const uint4* row_of_w(const ScorePiece& a, uint32_t id) { return reinterpret_cast<const uint4*>(a.w + id * a.ldw); }
 
 // A CTA takes kScorePickRows rows, a warp each; where they go it learns by counting the tokens before them itself, so nothing has to wait
 // for another CTA.  (32 rows a CTA: 42 us for 16384 rows x 3584 of which 66 % count, 31 with 8.)
@@ -107,9 +161,17 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
   for (uint32_t k = warp; k < rows; k += 8) {
     if (dest[k] < 0) continue;
     const uint4* src = reinterpret_cast<const uint4*>(a.x + (a.row0 + r0 + k) * a.ldx);
-    uint4* dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)dest[k] * a.hidden);
-#pragma unroll 8
-    for (uint32_t c = lane; c < vecs; c += 32) dst[c] = src[c];
+    const uint4* w = row_of_w(a, (uint32_t)tokens[r0 + k]);
+    uint4* __restrict__ dst = reinterpret_cast<uint4*>(a.xc + (uint64_t)dest[k] * a.hidden);
+    RowDot dot;
+#pragma unroll 4
+    for (uint32_t c = lane; c < vecs; c += 32) {
+      const uint4 x = src[c];
+      dot.add(x, w[c]);
+      dst[c] = x;
+    }
+    const float target = dot.total();
+    if (lane == 0) a.target[dest[k]] = target;
   }
 }
 
@@ -200,11 +262,10 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
       release();  // the products go on while the exponentials are taken
       if (kHigh == 1 && t.k1 < k_blocks) return;
       const uint32_t m = t.m + row + (threadIdx.x & 31), cols = min(kSegCols, a.vocab - c0), token_at = (uint32_t)token - c0;
-      if (token_at < kSegCols) {
-        uint32_t own = 0;
+      if (token_at < kSegCols) {  // the join adds it
 #pragma unroll
-        for (uint32_t j = 0; j < kSegCols; ++j) own = j == token_at ? z[j / 32][j % 32] : own;
-        a.target[m] = __uint_as_float(own);
+        for (uint32_t j = 0; j < kSegCols; ++j)
+          if (j == token_at) z[j / 32][j % 32] = 0xFF800000u;
       }
       if (cols < kSegCols) {  // beyond the vocabulary
 #pragma unroll
@@ -241,7 +302,7 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
 // 32768, where CTA pairs with tiles of 256 rows took 96 and 91.  Their half of the tensor memory holds two parts of K, beyond 128 rows one: a
 // logit carries the truncation of half of K, or of all of it.
 //
-// Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 4..7 epilogue.  Waits are bounded as in mma_pair_tiles, and given up the same way.
+// Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 3 the tokens' logits, 4..7 epilogue.  Waits are bounded as in mma_pair_tiles, and given up the same way.
 constexpr int kFewThreads = 256;
 constexpr uint32_t kFewTile = 128;                       // W's rows of a tile
 constexpr uint32_t kFewBox = kFewCols * kMmaK * 2;       // bytes of a box of W: a segment's rows, 64 columns of K
@@ -368,6 +429,13 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
       few_commit(&bar->drain);
       mbar_wait_bounded(&bar->drain, 0, limit_ns);
     }
+  } else if (warp == 3) {  // the tokens' logits
+    for (uint32_t m = blockIdx.x; a.tokens && m < a.rows; m += gridDim.x) {
+      const int32_t token = a.tokens[a.row0 + m];
+      if (!has_label(token, a.vocab)) continue;
+      const float target = row_dot(a.x + (a.row0 + m) * a.ldx, row_of_w(a, (uint32_t)token), a.hidden);
+      if (lane == 0) a.target[m] = target;
+    }
   } else if (warp >= 4) {
     const uint32_t quarter = warp & 3;
     float* mine = turned + quarter * (kFewTurn / 4);
@@ -402,7 +470,7 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
         const uint32_t m = g * 32 + lane;
         if (m < a.rows) {
           const uint32_t token_at = (uint32_t)(a.tokens ? a.tokens[a.row0 + m] : kNoLabel) - seg * kFewCols;
-          if (token_at < kFewCols) a.target[m] = mine[lane * 33 + token_at];
+          if (token_at < kFewCols) mine[lane * 33 + token_at] = -INFINITY;  // the join adds it
           const SegStats t = segment_stats<kFewCols>([&](uint32_t j) { return mine[lane * 33 + j]; }, a.scale);
           const uint64_t to = (uint64_t)m * a.segs + seg;
           a.most[to] = t.most;
@@ -538,72 +606,6 @@ __device__ __forceinline__ void first_keys(uint32_t top, uint64_t least, KeyRoom
   row_sync<kWarps>();
 }
 
-// A row's results from its joined numbers, by the warps of the row: the sum and moment about `about`, the largest logit (0 where that is -inf).
-// most_of(s): the maximum of segment s.
-template <uint32_t kSeg, uint32_t kWarps, class MostOf>
-__device__ __forceinline__ void row_results(const ScorePiece& a, uint64_t row, uint32_t m, float about, float sum, float moment, KeyRoom<kWarps>& room,
-                                            uint32_t* seg_of, MostOf&& most_of) {
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = kWarps == 1 ? lane : threadIdx.x;
-  const float log_sum = logf(sum);
-  if (t == 0) {
-    if (a.tokens) a.logprob[row] = (a.target[m] - about) * a.scale - log_sum;
-    if (a.entropy) a.entropy[row] = log_sum - kScoreLn2 * moment / sum;
-  }
-  if (a.top == 0) return;
-  const uint32_t segs = min(a.top, a.segs);
-  uint64_t least = 0;
-  row_sync<kWarps>();
-  if (a.segs > a.top) {
-    first_keys<kWarps>(a.top, 0, room,
-      [&](auto&& f) {
-#pragma unroll 4
-        for (uint32_t s0 = 0; s0 < a.segs; s0 += 32 * kWarps) {
-          const uint32_t s = s0 + t;
-          f(s < a.segs ? order_key(most_of(s), s) : 0);
-        }
-      },
-      [&](uint32_t rank, uint64_t key) { seg_of[rank] = key_place(key); });
-    // no logit below the last segment's maximum is among the first
-    least = order_key(most_of(seg_of[a.top - 1]), 0xFFFFFFFFu);
-  } else {
-    if (t < a.segs) seg_of[t] = t;
-    row_sync<kWarps>();
-  }
-  const float* z = a.z + (uint64_t)m * a.ld_z;
-  if (a.top > a.vocab && t < a.top) { a.top_ids[row * a.top + t] = -1; a.top_logprobs[row * a.top + t] = -INFINITY; }
-  row_sync<kWarps>();
-  first_keys<kWarps>(a.top, least, room,
-    [&](auto&& f) {
-      constexpr uint32_t kEach = kSeg / 32, kAtOnce = 4;  // logits of a lane in a segment; segments whose loads go out together
-      for (uint32_t j0 = kWarps == 1 ? 0 : warp; j0 < segs; j0 += kAtOnce * kWarps) {
-        float x[kAtOnce][kEach];
-        uint32_t c[kAtOnce];
-#pragma unroll
-        for (uint32_t i = 0; i < kAtOnce; ++i) {
-          const uint32_t j = j0 + i * kWarps;
-          c[i] = seg_of[j < segs ? j : j0] * kSeg + lane * kEach;
-          if constexpr (kEach == 4) {
-            const float4 q = *reinterpret_cast<const float4*>(z + c[i]);
-            x[i][0] = q.x; x[i][1] = q.y; x[i][2] = q.z; x[i][3] = q.w;
-          } else {
-            x[i][0] = z[c[i]];
-          }
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < kAtOnce; ++i) {
-          if (j0 + i * kWarps >= segs) break;
-#pragma unroll
-          for (uint32_t e = 0; e < kEach; ++e) f(order_key(x[i][e], c[i] + e));
-        }
-      }
-    },
-    [&](uint32_t rank, uint64_t key) {
-      if (key_place(key) >= a.vocab) return;
-      a.top_ids[row * a.top + rank] = (int32_t)key_place(key);
-      a.top_logprobs[row * a.top + rank] = (key_value(key) - about) * a.scale - log_sum;
-    });
-}
-
 // A segment's numbers, or those of several, taken into numbers about `about`.
 struct Joined {
   float sum = 0.f, moment = 0.f;
@@ -616,6 +618,122 @@ struct Joined {
 };
 __device__ __forceinline__ float finite_about(float most) { return most == -INFINITY ? 0.f : most; }
 
+// The room of a row, or of a warp's
+template <uint32_t kWarps>
+struct RowRoom {
+  KeyRoom<kWarps> keys;
+  uint32_t seg_of[FT_LOGPROBS_MAX_TOP];
+};
+
+// A row's alternatives but the token, into listed (zeros before), by the warps of the row.  most_of(s): the maximum of segment s.
+template <uint32_t kSeg, uint32_t kWarps, class MostOf>
+__device__ __forceinline__ void row_list(const ScorePiece& a, uint32_t m, int32_t token, uint64_t* listed, RowRoom<kWarps>& room, MostOf&& most_of) {
+  const uint32_t lane = threadIdx.x & 31, warp = kWarps == 1 ? 0 : threadIdx.x >> 5, t = kWarps == 1 ? lane : threadIdx.x;
+  const uint32_t segs = min(a.top, a.segs);
+  uint64_t least = 0;
+  row_sync<kWarps>();
+  if (t < a.top) listed[t] = 0;
+  if (a.segs > a.top) {
+    first_keys<kWarps>(a.top, 0, room.keys,
+      [&](auto&& f) {
+#pragma unroll 4
+        for (uint32_t s0 = 0; s0 < a.segs; s0 += 32 * kWarps) {
+          const uint32_t s = s0 + t;
+          f(s < a.segs ? order_key(most_of(s), s) : 0);
+        }
+      },
+      [&](uint32_t rank, uint64_t key) { room.seg_of[rank] = key_place(key); });
+    // no logit below the last segment's maximum is among the first
+    least = order_key(most_of(room.seg_of[a.top - 1]), 0xFFFFFFFFu);
+  } else {
+    if (t < a.segs) room.seg_of[t] = t;
+    row_sync<kWarps>();
+  }
+  const float* z = a.z + (uint64_t)m * a.ld_z;
+  first_keys<kWarps>(a.top, least, room.keys,
+    [&](auto&& f) {
+      constexpr uint32_t kEach = kSeg / 32, kAtOnce = 4;  // logits of a lane in a segment; segments whose loads go out together
+      for (uint32_t j0 = warp; j0 < segs; j0 += kAtOnce * kWarps) {
+        float v[kAtOnce][kEach];
+        uint32_t c[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          const uint32_t j = j0 + i * kWarps;
+          c[i] = room.seg_of[j < segs ? j : j0] * kSeg + lane * kEach;
+          if constexpr (kEach == 4) {
+            const float4 q = *reinterpret_cast<const float4*>(z + c[i]);
+            v[i][0] = q.x; v[i][1] = q.y; v[i][2] = q.z; v[i][3] = q.w;
+          } else {
+            v[i][0] = z[c[i]];
+          }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          if (j0 + i * kWarps >= segs) break;
+#pragma unroll
+          for (uint32_t e = 0; e < kEach; ++e) f(order_key((int32_t)(c[i] + e) == token ? -INFINITY : v[i][e], c[i] + e));
+        }
+      }
+    },
+    [&](uint32_t rank, uint64_t key) {
+      if (key_place(key) < a.vocab && (int32_t)key_place(key) != token) listed[rank] = key;
+    });
+}
+
+// A row's results, by a warp, from its joined numbers, which leave the token out: the largest logit, the sum and moment about it (about 0 where it is
+// -inf).  A lane has an alternative: its order_key by the sums (0: none), and its logit by FMAs.
+__device__ __forceinline__ void row_results(const ScorePiece& a, uint64_t row, int32_t token, float target, float most, float sum, float moment, uint64_t key,
+                                            float listed_logit) {
+  const uint32_t lane = threadIdx.x & 31;
+  const bool given = a.tokens != nullptr;
+  const float by_sums = key_value(key), logit = key ? listed_logit : -INFINITY;
+  float about = fmaxf(fmaxf(most, target), logit);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) about = fmaxf(about, __shfl_xor_sync(0xFFFFFFFFu, about, d));
+  about = finite_about(about);
+  const float to_log2 = a.scale * kScoreLog2e;
+  Joined others, all;
+  others.add(most, sum, moment, about, to_log2);
+  if (a.top) {
+    // The alternatives' terms by FMAs in the place of those that the sums hold.  A sum that is left far below those terms has lost its digits
+    // to them (logits so large that the sums' rounding is worth several powers of e): they are all that is known of it.
+    const auto power = [&](float z) { return max_with_nan((z - about) * to_log2, kLeastExponent); };
+    float term = 0.f, more = 0.f, more_moment = 0.f;
+    if (key && logit != -INFINITY) {
+      const float u = power(logit);
+      term = exp2f(u);
+      if (logit != by_sums) {
+        const float u0 = power(by_sums), e0 = exp2f(u0), d = (logit - by_sums) * a.scale;
+        more = fabsf(d) < 1.f ? e0 * expm1f(d) : term - e0;
+        more_moment = u * term - u0 * e0;
+      }
+    }
+    term = warp_sum(term);
+    others.sum += warp_sum(more);
+    others.moment += warp_sum(more_moment);
+    if (others.sum < 0.5f * term) others.sum = term;
+  }
+  all = others;
+  if (target != -INFINITY) all.add(target, given ? 1.f : 0.f, 0.f, about, to_log2);
+  // where the token is the likeliest, from what the others have: nothing is lost to the one
+  const float log_sum = given && target == about && all.sum < INFINITY ? log1pf(others.sum) : logf(all.sum);
+  const auto number = [&](float z) { return (z - about) * a.scale - log_sum; };
+  if (lane == 0) {
+    if (given) a.logprob[row] = number(target);
+    if (a.entropy) a.entropy[row] = log_sum - kScoreLn2 * all.moment / all.sum;
+  }
+  if (a.top == 0) return;
+  const uint64_t mine = key ? order_key(logit, key_place(key)) : 0, own = given ? order_key(target, (uint32_t)token) : 0;
+  uint32_t rank = own > mine;
+  for (uint32_t i = 0; i < a.top; ++i) rank += __shfl_sync(0xFFFFFFFFu, mine, i) > mine;
+  const uint32_t before = __popc(__ballot_sync(0xFFFFFFFFu, mine > own));
+  int32_t* ids = a.top_ids + row * a.top;
+  float* numbers = a.top_logprobs + row * a.top;
+  if (key && rank < a.top) { ids[rank] = (int32_t)key_place(key); numbers[rank] = number(logit); }
+  if (given && lane == 0 && before < a.top) { ids[before] = token; numbers[before] = number(target); }
+  if (lane >= a.vocab && lane < a.top) { ids[lane] = -1; numbers[lane] = -INFINITY; }
+}
+
 constexpr uint32_t kJoinHeldMost = 132 * 1024;  // bytes of maxima in shared memory
 
 // kRows rows a CTA, and as many warps: as the segments' numbers lie, the threads go through them rows first, whole sectors at a time; a
@@ -626,8 +744,7 @@ __global__ void __launch_bounds__(32 * kRows) k_score_join(const __grid_constant
   constexpr uint32_t kGroups = 32;
   extern __shared__ float s_held[];  // [kRows][segs, made odd]
   __shared__ float s_part[3][kGroups][kRows + 1];
-  __shared__ KeyRoom<1> s_room[kRows];
-  __shared__ uint32_t s_seg[kRows][FT_LOGPROBS_MAX_TOP];
+  __shared__ RowRoom<1> s_room[kRows];
   after_previous();
   const uint32_t n = a.tokens ? *a.count : a.rows, m0 = blockIdx.x * kRows;
   if (m0 >= n) return;
@@ -659,16 +776,59 @@ __global__ void __launch_bounds__(32 * kRows) k_score_join(const __grid_constant
   for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
   Joined all;
   all.add(s_part[0][lane][q], s_part[1][lane][q], s_part[2][lane][q], finite_about(most), to_log2);
-  row_results<kSegCols, 1>(a, a.row0 + (a.tokens ? (uint32_t)a.row_of[m] : m), m, finite_about(most), warp_sum(all.sum), warp_sum(all.moment), s_room[q], s_seg[q],
-                           [&](uint32_t s) { return a.held ? s_held[q * held_ld + s] : a.most[(uint64_t)s * a.rows + m]; });
+  const int32_t token = a.tokens ? a.token[m] : kNoLabel;
+  const float sum = warp_sum(all.sum), moment = warp_sum(all.moment);
+  if (a.top == 0) {
+    row_results(a, a.row0 + (a.tokens ? (uint32_t)a.row_of[m] : m), token, a.tokens ? a.target[m] : -INFINITY, most, sum, moment, 0, 0.f);
+    return;
+  }
+  if (lane == 0) a.joined[m] = make_float4(most, sum, moment, 0.f);
+  row_list<kSegCols, 1>(a, m, token, a.listed + (uint64_t)m * a.top, s_room[q],
+                        [&](uint32_t s) { return a.held ? s_held[q * held_ld + s] : a.most[(uint64_t)s * a.rows + m]; });
+}
+
+// The alternatives' logits by FMAs, two of them a warp at a time, and the results of the rows.  Bound by the rows of W that it gathers and, where K
+// is small, by its chain of latencies, which several rows a CTA share: with 1, 2, 4, 8 rows a CTA 4096 rows x 1024, 8 alternatives 29, 20, 17, 16 us (67 MB
+// of W's rows), 32 alternatives 49, 43, 41, 43 us (268 MB), 1599 x 4104, 20 alternatives 56, 54, 46, 69 us (262 MB).  One where four would leave SMs
+// with less than two CTAs.
+constexpr uint32_t kListWarps = 8, kListRows = 4;
+__global__ void __launch_bounds__(32 * kListWarps, 4) k_score_list(const __grid_constant__ ScorePiece a, uint32_t rows_each) {
+  __shared__ float s_logit[kListRows * FT_LOGPROBS_MAX_TOP];
+  let_next_start();
+  after_previous();
+  const uint32_t n = a.tokens ? *a.count : a.rows, m0 = blockIdx.x * rows_each, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (m0 >= n) return;
+  const uint32_t rows = min(rows_each, n - m0);
+  const auto x_of = [&](uint32_t m) { return a.tokens ? a.xc + (uint64_t)m * a.hidden : a.x + (a.row0 + m) * a.ldx; };
+  const uint32_t each = (a.top + 1) / 2;  // pairs of a row
+  for (uint32_t i = warp; i < rows * each; i += kListWarps) {
+    const uint32_t r = i / each, first = (i - r * each) * 2, second = min(first + 1, a.top - 1);
+    const uint64_t* listed = a.listed + (uint64_t)(m0 + r) * a.top;
+    const uint64_t k0 = listed[first], k1 = listed[second];
+    const uint4* const w[2] = {row_of_w(a, k0 ? key_place(k0) : 0), row_of_w(a, k1 ? key_place(k1) : 0)};
+    float z[2];
+    row_dots<2>(x_of(m0 + r), w, a.hidden, z);
+    if (lane == 0) {
+      s_logit[r * a.top + first] = z[0];
+      s_logit[r * a.top + second] = z[1];
+    }
+  }
+  __syncthreads();
+  if (warp >= rows) return;
+  const uint32_t m = m0 + warp;
+  const float4 j = a.joined[m];
+  const bool has = lane < a.top;
+  row_results(a, a.row0 + (a.tokens ? (uint32_t)a.row_of[m] : m), a.tokens ? a.token[m] : kNoLabel, a.tokens ? a.target[m] : -INFINITY, j.x, j.y, j.z,
+              has ? a.listed[(uint64_t)m * a.top + lane] : 0, has ? s_logit[warp * a.top + lane] : 0.f);
 }
 
 // Few rows: a CTA a row.
 constexpr uint32_t kFewWarps = 8;
-__global__ void __launch_bounds__(32 * kFewWarps) k_score_join_few(const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
+__global__ void __launch_bounds__(32 * kFewWarps, 2) k_score_join_few(const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
   extern __shared__ float s_held[];  // [segs]
-  __shared__ KeyRoom<kFewWarps> s_room;
-  __shared__ uint32_t s_seg[FT_LOGPROBS_MAX_TOP];
+  __shared__ RowRoom<kFewWarps> s_room;
+  __shared__ uint64_t s_listed[FT_LOGPROBS_MAX_TOP];
+  __shared__ float s_logit[FT_LOGPROBS_MAX_TOP];
   __shared__ float s_part[3][kFewWarps];
   after_previous();
   const uint32_t m = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -721,7 +881,20 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_score_join_few(const __grid_
   sum = moment = 0.f;
 #pragma unroll
   for (uint32_t w = 0; w < kFewWarps; ++w) { sum += s_part[1][w]; moment += s_part[2][w]; }
-  row_results<kFewCols, kFewWarps>(a, row, m, about, sum, moment, s_room, s_seg, [&](uint32_t s) { return a.held ? s_held[s] : a.most[first + s]; });
+  const int32_t token = a.tokens ? a.tokens[row] : kNoLabel;
+  if (a.top) {
+    row_list<kFewCols, kFewWarps>(a, m, token, s_listed, s_room, [&](uint32_t s) { return a.held ? s_held[s] : a.most[first + s]; });
+    for (uint32_t i = warp; i < a.top; i += kFewWarps) {
+      const uint64_t key = s_listed[i];
+      if (key == 0) continue;
+      const float z = row_dot(a.x + row * a.ldx, row_of_w(a, key_place(key)), a.hidden);
+      if (lane == 0) s_logit[i] = z;
+    }
+    __syncthreads();
+  }
+  if (warp) return;
+  const bool has = lane < a.top;
+  row_results(a, row, token, a.tokens ? a.target[m] : -INFINITY, most, sum, moment, has ? s_listed[lane] : 0, has ? s_logit[lane] : 0.f);
 }
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
@@ -749,6 +922,8 @@ static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_
   a->moment = reinterpret_cast<float*>(take(4ull * rows * a->segs));
   a->xc = reinterpret_cast<__nv_bfloat16*>(take(a->few ? 0 : 2ull * padded * hidden));
   a->classes = a->few ? 0 : (top + 3) / 4 * 4;
+  a->joined = reinterpret_cast<float4*>(take(a->few || top == 0 ? 0 : 16ull * rows));
+  a->listed = reinterpret_cast<uint64_t*>(take(a->few ? 0 : 8ull * rows * top));
   a->seen = reinterpret_cast<uint32_t*>(take(4ull * rows * a->classes));
   a->z = reinterpret_cast<float*>(take(top ? 4ull * rows * a->ld_z : 0));
   return off;
@@ -782,8 +957,7 @@ struct ScoreWork {
   }
 };
 
-static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, uint64_t ldw, uint64_t rows, void* workspace, uint64_t workspace_bytes,
-                              cudaStream_t st) {
+static int32_t token_logprobs(ft_pool* p, ScorePiece a, uint64_t rows, void* workspace, uint64_t workspace_bytes, cudaStream_t st) {
   const ScoreWork work{a.hidden, a.vocab, a.top, rows};
   if (!workspace || !aligned_to(workspace, 256)) return FT_ERR_INVALID_ARG;
   if (workspace_bytes < work.least()) return FT_ERR_CAPACITY;
@@ -798,7 +972,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   const size_t join_smem = a.held ? (size_t)held_bytes(join_rows) : 0;
   const auto join = join_rows == 16 ? k_score_join<16> : k_score_join<8>;
   CUtensorMap map_x, map_w;
-  if (mma_map(&map_w, w, a.hidden, a.vocab, ldw, a.few ? kFewCols : 64) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+  if (mma_map(&map_w, a.w, a.hidden, a.vocab, a.ldw, a.few ? kFewCols : 64) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   if (!p->score_attr_set) {  // once per pool, hence once per device the pool lives on
     for (auto k : {k_score<false, 1>, k_score<false, 2>, k_score<true, 1>, k_score<true, 2>})
       FT_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaSmem));
@@ -818,7 +992,7 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
   if (a.few) {
     const uint32_t n = few_columns(a.rows), grid = std::min<uint32_t>((uint32_t)p->sm_count, a.segs);
     CUtensorMap map_tile;
-    if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, w, a.hidden, a.vocab, ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    if (mma_map(&map_x, a.x, a.hidden, a.rows, a.ldx, n) != CUDA_SUCCESS || mma_map(&map_tile, a.w, a.hidden, a.vocab, a.ldw, kFewTile) != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const auto kernel = n == 32   ? (a.top ? k_score_few<32, true> : k_score_few<32, false>)
                         : n == 64 ? (a.top ? k_score_few<64, true> : k_score_few<64, false>)
                         : n == 128 ? (a.top ? k_score_few<128, true> : k_score_few<128, false>)
@@ -848,6 +1022,11 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, const __nv_bfloat16* w, 
     FT_CUDA(launch_chained(kernel, 2 * a.pairs, kMmaThreads, kMmaSmem, st, map_x, map_w, p->view, a));
     FT_CUDA(launch_chained(join, dim3((a.rows + join_rows - 1) / join_rows), 32 * join_rows, join_smem, st, a));
     p->gpu_launches += 2;
+    if (a.top) {
+      const uint32_t each = a.rows >= 2 * kListRows * (uint32_t)p->sm_count ? kListRows : 1;
+      FT_CUDA(launch_chained(k_score_list, dim3((a.rows + each - 1) / each), 32 * kListWarps, 0, st, a, each));
+      p->gpu_launches += 1;
+    }
   }
   return FT_OK;
 }
@@ -879,7 +1058,7 @@ FT_EXPORT int32_t pool_token_logprobs(ft_pool* p, uint64_t rows, uint32_t hidden
   if (top > FT_LOGPROBS_MAX_TOP) return FT_ERR_CAPACITY;
   if ((top && (!top_ids || !top_logprobs)) || !aligned_to(top_ids, 4) || !aligned_to(top_logprobs, 4)) return FT_ERR_INVALID_ARG;
   ScorePiece a = {};
-  a.hidden = hidden; a.vocab = vocab; a.ldx = ldx; a.x = static_cast<const __nv_bfloat16*>(x); a.tokens = tokens; a.scale = logit_scale;
+  a.hidden = hidden; a.vocab = vocab; a.ldx = ldx; a.x = static_cast<const __nv_bfloat16*>(x); a.ldw = ldw; a.w = static_cast<const __nv_bfloat16*>(w); a.tokens = tokens; a.scale = logit_scale;
   a.logprob = logprob; a.entropy = entropy; a.top = top; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
-  return token_logprobs(p, a, static_cast<const __nv_bfloat16*>(w), ldw, rows, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+  return token_logprobs(p, a, rows, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
