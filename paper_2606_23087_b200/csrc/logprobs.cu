@@ -31,9 +31,9 @@ namespace ft {
 
 constexpr uint32_t kSegCols = 128;     // columns of a segment: an epilogue warp's
 constexpr uint32_t kFewCols = 32;      // the same where the rows are few
-constexpr uint32_t kFewRows = 256;     // rows that count as few, where K allows it (ScoreWork::few)
-// The tensor cores truncate at every addition of 16 products, all one way: tiles of 256 rows are summed in parts of kScorePart blocks of K,
-// the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
+constexpr uint32_t kFewRows = 256;     // rows that count as few
+// The tensor cores truncate at every addition of 16 products, all one way: few rows and tiles of 256 rows are summed in parts of kScorePart blocks
+// of K, the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
 constexpr uint32_t kScorePart = 16, kScoreHigh = 66;
 constexpr uint32_t kScoreRowsMost = 65536;  // of a piece
 constexpr float kScoreLog2e = 1.4426950408889634f, kScoreLn2 = 0.6931471805599453f;
@@ -295,15 +295,18 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
 // ---- few rows -------------------------------------------------------------------------------------------------------
 
 // A CTA takes a contiguous run of W's rows, 128 of them (four segments) a tile: D = W x^T, a vocabulary entry a lane of the tensor
-// memory, a row of x a column.  The products of up to kScorePart blocks of K go into columns of their own, as many as half of the tensor
-// memory holds; its other half takes the next tile meanwhile.
+// memory, a row of x a column.  K goes in parts of up to kScorePart blocks, into the halves of the tensor memory in turn; the epilogue adds the
+// parts in its registers, so that a logit carries the truncation of 1024 of K whatever the rows and K.
 //
-// More than 64 rows read x from L2 as often as W from memory, or twice as often, and still take 64 us for 100 x 4096 and 71 for 200 x 3584, vocabulary
-// 32768, where CTA pairs with tiles of 256 rows took 96 and 91.  Their half of the tensor memory holds two parts of K, beyond 128 rows one: a
-// logit carries the truncation of half of K, or of all of it.
+// More than 64 rows read x from L2 as often as W from memory, or twice as often, and still take 70 us for 100 x 4096 and 77 for 200 x 3584, vocabulary
+// 32768, 8 alternatives (6 of them for the alternatives' logits by FMAs).
 //
-// Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 3 the tokens' logits, 4..7 epilogue.  Waits are bounded as in mma_pair_tiles, and given up the same way.
-constexpr int kFewThreads = 256;
+// Warps: 0 TMA, 1 matrix instructions, 2 tensor memory, 3 the tokens' logits, from 4 on the epilogue, a group of four warps for each 128 rows of x.
+// Waits are bounded as in mma_pair_tiles, and given up the same way.
+template <uint32_t kN>
+constexpr uint32_t kFewGroups = kN > 128 ? 2 : 1;
+template <uint32_t kN>
+constexpr int kFewThreads = 128 + 128 * kFewGroups<kN>;
 constexpr uint32_t kFewTile = 128;                       // W's rows of a tile
 constexpr uint32_t kFewBox = kFewCols * kMmaK * 2;       // bytes of a box of W: a segment's rows, 64 columns of K
 // Blocks of K of a stage.  Two: a row's 256 bytes are asked for together; one where x takes most of a stage.
@@ -317,7 +320,7 @@ template <uint32_t kN>
 constexpr uint32_t kFewStages = (kN == 32 ? 10 : kN == 64 ? 8 : kN == 128 ? 6 : 4) / kFewSub<kN>;
 constexpr uint32_t kFewTurn = 32 * 33 * 4;               // bytes of a warp's 32 x 32 logits, turned over
 template <uint32_t kN>
-constexpr size_t kFewSmem = kFewStages<kN> * (size_t)kFewStage<kN> + 4 * kFewTurn + 1024 + 256;
+constexpr size_t kFewSmem = kFewStages<kN> * (size_t)kFewStage<kN> + 4 * kFewGroups<kN> * kFewTurn + 1024 + 256;
 
 struct FewBarriers {
   uint64_t full[10], empty[10], acc_full[2], acc_empty[2], drain;
@@ -341,22 +344,31 @@ __device__ __forceinline__ void few_product(uint32_t tmem, uint64_t da, uint64_t
                ::"r"(tmem), "l"(da), "l"(db), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
 
+// 16 columns of the warp's 32 rows, as tmem_load32
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
+  __syncwarp();
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                 "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(addr) : "memory");
+}
+
 template <uint32_t kN, bool kKeep>
-__global__ void __launch_bounds__(kFewThreads, 1)
+__global__ void __launch_bounds__(kFewThreads<kN>, 1)
 k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_tile,
             const __grid_constant__ PoolView v, const __grid_constant__ ScorePiece a) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr uint32_t kStages = kFewStages<kN>, kStage = kFewStage<kN>, kSub = kFewSub<kN>;
+  constexpr uint32_t kStages = kFewStages<kN>, kStage = kFewStage<kN>, kSub = kFewSub<kN>, kGroups = kFewGroups<kN>;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* turned = reinterpret_cast<float*>(stages + kStages * kStage);
-  FewBarriers* bar = reinterpret_cast<FewBarriers*>(stages + kStages * kStage + 4 * kFewTurn);
+  FewBarriers* bar = reinterpret_cast<FewBarriers*>(stages + kStages * kStage + 4 * kGroups * kFewTurn);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   let_next_start();
   if (threadIdx.x == 32)
     for (const CUtensorMap* map : {&map_x, &map_w, &map_tile}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < kStages; ++s) { mbar_init(&bar->full[s], 1); mbar_init(&bar->empty[s], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&bar->acc_full[i], 1); mbar_init(&bar->acc_empty[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar->acc_full[i], 1); mbar_init(&bar->acc_empty[i], 4 * kGroups); }
     mbar_init(&bar->drain, 1);
     bar->lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -373,7 +385,7 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
   after_previous();
   const uint32_t tmem = bar->tmem, base = smem_u32(stages);
   const uint32_t k_blocks = (a.hidden + kMmaK - 1) / kMmaK;
-  const uint32_t parts = min((k_blocks + kScorePart - 1) / kScorePart, 256 / kN), each = (k_blocks + parts - 1) / parts;
+  const uint32_t parts = (k_blocks + kScorePart - 1) / kScorePart, each = ((k_blocks + parts - 1) / parts + 1) & ~1u;  // blocks of a part: whole stages
   const uint32_t seg0 = (uint32_t)((uint64_t)a.segs * blockIdx.x / gridDim.x), seg1 = (uint32_t)((uint64_t)a.segs * (blockIdx.x + 1) / gridDim.x);
   const uint64_t limit_ns = mma_wait_limit(v, k_blocks);
   bool lost = false;
@@ -405,25 +417,26 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
     for (uint32_t j = j0; j < it && !lost; ++j) lost = !mbar_wait_bounded(&bar->empty[j % kStages], (j / kStages) & 1, limit_ns);
   } else if (warp == 1 && lane == 0) {
     constexpr uint32_t kInstr = 1u << 4 | 1u << 7 | 1u << 10 | (kN >> 3) << 17 | (kFewTile >> 4) << 24;  // fp32 sums of bf16 x bf16
-    uint32_t it = 0, tile = 0;
-    for (uint32_t seg = seg0; seg < seg1 && !lost; seg += 4, ++tile) {
-      const uint32_t acc = tile & 1;
-      if (!mbar_wait_bounded(&bar->acc_empty[acc], ((tile >> 1) & 1) ^ 1, limit_ns)) { lost = true; break; }
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (uint32_t k = 0; k < k_blocks; k += kSub, ++it) {
-        const uint32_t s = it % kStages;
-        if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
+    uint32_t it = 0, n = 0;  // stages and parts so far
+    for (uint32_t seg = seg0; seg < seg1 && !lost; seg += 4) {
+      for (uint32_t k0 = 0; k0 < k_blocks && !lost; k0 += each, ++n) {
+        const uint32_t acc = n & 1, k1 = min(k0 + each, k_blocks);
+        if (!mbar_wait_bounded(&bar->acc_empty[acc], ((n >> 1) & 1) ^ 1, limit_ns)) { lost = true; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (uint32_t i = 0; i < min(kSub, k_blocks - k); ++i) {
-          const uint32_t sa = base + s * kStage + i * kFewBlock<kN>, sb = sa + kFewTile * kMmaK * 2, part = (k + i) / each;
+        for (uint32_t k = k0; k < k1; k += kSub, ++it) {
+          const uint32_t s = it % kStages;
+          if (!mbar_wait_bounded(&bar->full[s], (it / kStages) & 1, limit_ns)) { lost = true; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          for (uint32_t i = 0; i < min(kSub, k1 - k); ++i) {
+            const uint32_t sa = base + s * kStage + i * kFewBlock<kN>, sb = sa + kFewTile * kMmaK * 2;
 #pragma unroll
-          for (uint32_t j = 0; j < kMmaK / 16; ++j)
-            few_product(tmem + acc * 256 + part * kN, mma_desc<false>(sa + j * kMmaStep<false>), mma_desc<false>(sb + j * kMmaStep<false>), kInstr,
-                        k + i > part * each || j > 0);
+            for (uint32_t j = 0; j < kMmaK / 16; ++j)
+              few_product(tmem + acc * 256, mma_desc<false>(sa + j * kMmaStep<false>), mma_desc<false>(sb + j * kMmaStep<false>), kInstr, k + i > k0 || j > 0);
+          }
+          few_commit(&bar->empty[s]);
         }
-        few_commit(&bar->empty[s]);
+        if (!lost) few_commit(&bar->acc_full[acc]);
       }
-      if (!lost) few_commit(&bar->acc_full[acc]);
     }
     if (lost) {  // products under way still read shared memory and write tensor memory
       few_commit(&bar->drain);
@@ -437,37 +450,52 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
       if (lane == 0) a.target[m] = target;
     }
   } else if (warp >= 4) {
-    const uint32_t quarter = warp & 3;
-    float* mine = turned + quarter * (kFewTurn / 4);
-    const uint32_t used = (k_blocks + each - 1) / each;  // parts that hold something
-    uint32_t tile = 0;
-    for (uint32_t s0 = seg0; s0 < seg1 && !lost; s0 += 4, ++tile) {
-      const uint32_t acc = tile & 1, seg = s0 + quarter;
-      lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], (tile >> 1) & 1, limit_ns));
-      if (lost) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t id = seg * kFewCols + lane;
-      // 32 rows of x at a time
-      for (uint32_t g = 0; g * 32 < a.rows && seg < seg1; ++g) {
-        uint32_t z[32];
-        const uint32_t at = tmem + acc * 256 + g * 32 + (quarter << 21);
-        tmem_load32(at, z);
-        tmem_wait();
-        for (uint32_t p = 1; p < used; ++p) {
-          uint32_t more[32];
-          tmem_load32(at + p * kN, more);
-          tmem_wait();
+    constexpr uint32_t kRows = kN / kGroups;  // of x, a warp's columns
+    const uint32_t quarter = warp & 3, r0 = (warp - 4) / 4 * kRows;
+    float* mine = turned + (warp - 4) * (kFewTurn / 4);
+    uint32_t n = 0;
+    for (uint32_t s0 = seg0; s0 < seg1 && !lost; s0 += 4) {
+      const uint32_t seg = s0 + quarter, id = seg * kFewCols + lane;
+      uint32_t z[kRows / 32][32];
+      for (uint32_t k0 = 0; k0 < k_blocks; k0 += each, ++n) {
+        const uint32_t acc = n & 1, at = tmem + acc * 256 + r0 + (quarter << 21);
+        lost = !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bar->acc_full[acc], (n >> 1) & 1, limit_ns));
+        if (lost) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-          for (uint32_t j = 0; j < 32; ++j) z[j] = __float_as_uint(__uint_as_float(z[j]) + __uint_as_float(more[j]));
+        for (uint32_t g = 0; g < kRows / 32; ++g) {
+          if (r0 + 32 * g >= a.rows || seg >= seg1) continue;
+          if (k0 == 0) {
+            tmem_load32(at + 32 * g, z[g]);
+            continue;
+          }
+#pragma unroll
+          for (uint32_t h = 0; h < 32; h += 16) {
+            uint32_t more[16];
+            tmem_load16(at + 32 * g + h, more);
+            tmem_wait();
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) z[g][h + j] = __float_as_uint(__uint_as_float(z[g][h + j]) + __uint_as_float(more[j]));
+          }
         }
+        tmem_wait();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive_at(smem_u32(&bar->acc_empty[acc]));
+      }
+      if (lost) break;
+      // 32 rows of x at a time, those in front moved up behind them: unrolled, this much code takes 10 us to arrive where a call finds the caches cold
+#pragma unroll 1
+      for (uint32_t m0 = r0; m0 < min(r0 + kRows, a.rows) && seg < seg1; m0 += 32) {
+        const uint32_t m = m0 + lane;
+        __syncwarp();
 #pragma unroll
         for (uint32_t j = 0; j < 32; ++j) {
-          const float x = id < a.vocab ? __uint_as_float(z[j]) : -INFINITY;
-          if (kKeep && g * 32 + j < a.rows) a.z[(uint64_t)(g * 32 + j) * a.ld_z + id] = x;
+          const float x = id < a.vocab ? __uint_as_float(z[0][j]) : -INFINITY;
+          if (kKeep && m0 + j < a.rows) a.z[(uint64_t)(m0 + j) * a.ld_z + id] = x;
           mine[j * 33 + lane] = x;
         }
         __syncwarp();
-        const uint32_t m = g * 32 + lane;
         if (m < a.rows) {
           const uint32_t token_at = (uint32_t)(a.tokens ? a.tokens[a.row0 + m] : kNoLabel) - seg * kFewCols;
           if (token_at < kFewCols) mine[lane * 33 + token_at] = -INFINITY;  // the join adds it
@@ -477,12 +505,11 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
           a.sum[to] = t.sum;
           a.moment[to] = t.moment;
         }
-        __syncwarp();
+#pragma unroll
+        for (uint32_t g = 0; g + 1 < kRows / 32; ++g)
+#pragma unroll
+          for (uint32_t j = 0; j < 32; ++j) z[g][j] = z[g + 1][j];
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive_at(smem_u32(&bar->acc_empty[acc]));
-      __syncwarp();
     }
   }
   if (lost) bar->lost = 1;
@@ -936,8 +963,7 @@ struct ScoreWork {
     ScorePiece a;
     return score_carve(&a, nullptr, piece, hidden, vocab, top, few());
   }
-  // few rows, and no more of K in one piece than elsewhere
-  bool few() const { return rows <= kFewRows && (hidden + kMmaK - 1) / kMmaK <= kScoreHigh * (256 / few_columns((uint32_t)rows)); }
+  bool few() const { return rows <= kFewRows; }
   uint32_t least_rows() const { return (uint32_t)std::min<uint64_t>(rows, kMmaTile); }
   uint32_t best_rows() const {  // with alternatives, pieces whose logits take 4 GiB
     const uint64_t most = top ? std::max<uint64_t>(kMmaTile, (4ull << 30) / (4ull * vocab) / kMmaTile * kMmaTile) : kScoreRowsMost;
@@ -997,8 +1023,9 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, uint64_t rows, void* wor
                         : n == 64 ? (a.top ? k_score_few<64, true> : k_score_few<64, false>)
                         : n == 128 ? (a.top ? k_score_few<128, true> : k_score_few<128, false>)
                                    : (a.top ? k_score_few<256, true> : k_score_few<256, false>);
+    const int threads = n == 256 ? kFewThreads<256> : kFewThreads<128>;
     const size_t smem = n == 32 ? kFewSmem<32> : n == 64 ? kFewSmem<64> : n == 128 ? kFewSmem<128> : kFewSmem<256>;
-    FT_CUDA(launch_chained(kernel, grid, kFewThreads, smem, st, map_x, map_w, map_tile, p->view, a));
+    FT_CUDA(launch_chained(kernel, grid, threads, smem, st, map_x, map_w, map_tile, p->view, a));
     FT_CUDA(launch_chained(k_score_join_few, a.rows, 32 * kFewWarps, join_smem, st, p->view, a));
     p->gpu_launches += 2;
     return FT_OK;

@@ -64,6 +64,14 @@ def test_numbers_of_ordinary_values(pool, shape, likely):  # noqa: F811
 
 
 @pytest.mark.parametrize("likely", [False, True])
+@pytest.mark.parametrize("rows,hidden,vocab", [(100, 4096, 4001), (128, 4224, 4001), (129, 4096, 4001), (200, 4096, 4001), (256, 4224, 4001), (256, 12296, 1001), (40, 20488, 1001),
+                                               (5, 40008, 501)])
+def test_few_rows_are_summed_in_parts(pool, rows, hidden, vocab, likely):  # noqa: F811
+    """Up to 256 rows no more than 1024 of K in one piece, however many rows and however long K."""
+    check_precision(pool, rows, hidden, vocab, True, likely)
+
+
+@pytest.mark.parametrize("likely", [False, True])
 @pytest.mark.parametrize("rows,hidden,vocab", [(24, 4096, 5000), (200, 1032, 777), (1000, 1032, 20011)])
 def test_a_token_s_number_is_one_number(pool, rows, hidden, vocab, likely):  # noqa: F811
     """The same bits in both outputs where the token is listed, the list in the order of its numbers, and no token left out of it whose
