@@ -122,15 +122,17 @@ __device__ __forceinline__ float row_dot(const __nv_bfloat16* x_row, const uint4
 }
 __device__ __forceinline__ const uint4* row_of_w(const ScorePiece& a, uint32_t id) { return reinterpret_cast<const uint4*>(a.w + id * a.ldw); }
 
-// A CTA takes kScorePickRows rows, a warp each; where they go it learns by counting the tokens before them itself, so nothing has to wait
-// for another CTA.  (32 rows a CTA: 42 us for 16384 rows x 3584 of which 66 % count, 31 with 8.)
-constexpr uint32_t kScorePickRows = 8;
+// A CTA takes kRows rows (up to 32), its warps a row at a time; where they go it learns by counting the tokens before them itself, so nothing has to
+// wait for another CTA.  Those counts read the square of the rows, so long pieces take more rows a CTA: with 8, 16, 32 rows 8192 x 3584 (66 %
+// count) takes 24, 25, 40 us, 16384 x 3584 38, 33, 44, 65536 x 1024 (90 %) 76, 53, 50.
+constexpr uint32_t kScorePickRows = 8, kScorePickMany = 16, kScorePickManyFrom = 16384;
+template <uint32_t kRows>
 __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
   __shared__ uint32_t warp_count[8];
   __shared__ int32_t dest[32];
   let_next_start();
   after_previous();
-  const uint32_t r0 = blockIdx.x * kScorePickRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = r0 + lane;
+  const uint32_t r0 = blockIdx.x * kRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = r0 + lane;
   const int32_t* tokens = a.tokens + a.row0;
   const uint32_t mine = __reduce_add_sync(0xFFFFFFFFu, count_labels(tokens, r0, a.vocab));
   if (lane == 0) warp_count[warp] = mine;
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
   uint32_t before = 0;
 #pragma unroll
   for (int w = 0; w < 8; ++w) before += warp_count[w];
-  const int32_t t = lane < kScorePickRows && r < a.rows ? tokens[r] : kNoLabel;
+  const int32_t t = lane < kRows && r < a.rows ? tokens[r] : kNoLabel;
   const bool counts = has_label(t, a.vocab);
   const uint32_t mask = __ballot_sync(0xFFFFFFFFu, counts), pos = before + __popc(mask & ((1u << lane) - 1));
   if (warp == 0) {
@@ -146,7 +148,7 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
     if (counts) {
       a.row_of[pos] = (int32_t)r;
       a.token[pos] = t;
-    } else if (lane < kScorePickRows && r < a.rows) {
+    } else if (lane < kRows && r < a.rows) {
       const uint64_t row = a.row0 + r;
       a.logprob[row] = 0.f;
       if (a.entropy) a.entropy[row] = 0.f;
@@ -156,7 +158,7 @@ __global__ void __launch_bounds__(256) k_score_pick(PoolView v, ScorePiece a) {
     if (blockIdx.x == gridDim.x - 1 && lane == 0) *a.count = before + __popc(mask);
   }
   __syncthreads();
-  const uint32_t vecs = a.hidden / 8, rows = min(kScorePickRows, a.rows - r0);
+  const uint32_t vecs = a.hidden / 8, rows = min(kRows, a.rows - r0);
   for (uint32_t i = threadIdx.x; i < rows * a.classes; i += blockDim.x) a.seen[(uint64_t)r0 * a.classes + i] = 0;
   for (uint32_t k = warp; k < rows; k += 8) {
     if (dest[k] < 0) continue;
@@ -329,7 +331,8 @@ struct FewBarriers {
 static_assert(sizeof(FewBarriers) <= 256 && kFewSmem<32> <= 227 * 1024 && kFewSmem<64> <= 227 * 1024 && kFewSmem<128> <= 227 * 1024 && kFewSmem<256> <= 227 * 1024, "kFewSmem");
 
 // `policy`: of the L2 cache.  W passes through it once: lines that leave first make way for themselves, not for what others have there
-// (24 rows x 4096, vocabulary 131072: 192 us without, 185 with).
+// (24 rows x 4096, vocabulary 131072: 192 us without, 185 with).  The same for x, although every CTA reads it again: with
+// L2::evict_last it is as fast from 1 to 256 rows, with L2::evict_normal slower (200 x 3584 74 us, not 62).
 __device__ __forceinline__ uint64_t leave_first() { uint64_t p; asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p)); return p; }
 __device__ __forceinline__ void few_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* bar, uint64_t policy) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;"
@@ -1036,7 +1039,8 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, uint64_t rows, void* wor
     if ((a.tokens ? mma_map(&map_x, a.xc, a.hidden, a.padded, a.hidden) : mma_map(&map_x, a.x + r0 * a.ldx, a.hidden, a.rows, a.ldx)) != CUDA_SUCCESS)
       return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     if (a.tokens) {
-      FT_CUDA(launch_chained(k_score_pick, dim3((a.rows + kScorePickRows - 1) / kScorePickRows), 256, 0, st, p->view, a));
+      const uint32_t each = a.rows >= kScorePickManyFrom ? kScorePickMany : kScorePickRows;
+      FT_CUDA(launch_chained(each == kScorePickMany ? k_score_pick<kScorePickMany> : k_score_pick<kScorePickRows>, dim3((a.rows + each - 1) / each), 256, 0, st, p->view, a));
       p->gpu_launches += 1;
     } else if (a.top) {
       FT_CUDA(launch_chained(k_score_clear, dim3((unsigned)(((uint64_t)a.rows * a.classes + 255) / 256)), 256, 0, st, a));
