@@ -690,7 +690,8 @@ int32_t pool_grad_norm(ft_pool* pool, const ft_grad_tensor* tensors, uint32_t n_
  * parts of 1024 of hidden; up to four times that where it is summed in one piece of up to 4224: more than 256 rows in calls that fill the device.
  * The gradient of the log probability is pool_token_loss_grad's with -grad_loss.
  * x, w, hidden, ldx, ldw as in pool_token_loss.  pool_token_logprobs_workspace gives the smallest workspace and the one from which more
- * brings nothing; any size between the two works (alternatives keep a piece of the rows' logits in the workspace, up to 4 GiB).
+ * brings nothing; any size between the two works (alternatives keep a piece of the rows' logits in the workspace, up to 4 GiB), and a workspace
+ * that serves some rows serves fewer of them too, if not by the fastest way.  The size may change the last bits of a number.
  * Errors: as pool_token_loss; logit_scale not positive or not finite, logprob NULL with tokens or the reverse, top without top_ids and
  * top_logprobs INVALID_ARG; top > 32 CAPACITY.  rows = 0 does nothing.  Asynchronous: TIMEOUT, as pool_token_loss.
  */

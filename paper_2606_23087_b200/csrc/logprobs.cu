@@ -31,7 +31,7 @@ namespace ft {
 
 constexpr uint32_t kSegCols = 128;     // columns of a segment: an epilogue warp's
 constexpr uint32_t kFewCols = 32;      // the same where the rows are few
-constexpr uint32_t kFewRows = 256;     // rows that count as few
+constexpr uint32_t kFewRows = 256;     // rows that count as few, where the workspace has room (ScoreWork)
 // The tensor cores truncate at every addition of 16 products, all one way: few rows and tiles of 256 rows are summed in parts of kScorePart blocks
 // of K, the parts joined in registers.  Tiles of 512 rows have no registers for that: they are for rows beyond 256 and K up to kScoreHigh blocks.
 constexpr uint32_t kScorePart = 16, kScoreHigh = 66;
@@ -959,28 +959,34 @@ static uint64_t score_carve(ScorePiece* a, uint8_t* base, uint32_t rows, uint32_
   return off;
 }
 
+// Up to kFewRows rows go the way of few rows where its layout fits, and else by tiles: segments of 32 columns take more room than those of 128,
+// and a workspace that serves many rows has to serve the last, smaller call of a loop too.
 struct ScoreWork {
   uint32_t hidden, vocab, top;
   uint64_t rows;
-  uint64_t bytes(uint32_t piece) const {
+  uint64_t tile_bytes(uint32_t piece) const {
     ScorePiece a;
-    return score_carve(&a, nullptr, piece, hidden, vocab, top, few());
+    return score_carve(&a, nullptr, piece, hidden, vocab, top, false);
   }
-  bool few() const { return rows <= kFewRows; }
+  uint64_t few_bytes() const {
+    ScorePiece a;
+    return rows <= kFewRows ? score_carve(&a, nullptr, (uint32_t)rows, hidden, vocab, top, true) : ~0ull;
+  }
   uint32_t least_rows() const { return (uint32_t)std::min<uint64_t>(rows, kMmaTile); }
   uint32_t best_rows() const {  // with alternatives, pieces whose logits take 4 GiB
     const uint64_t most = top ? std::max<uint64_t>(kMmaTile, (4ull << 30) / (4ull * vocab) / kMmaTile * kMmaTile) : kScoreRowsMost;
     return (uint32_t)std::min<uint64_t>(rows, std::min<uint64_t>(most, kScoreRowsMost));
   }
-  uint64_t least() const { return bytes(least_rows()); }
-  uint64_t best() const { return bytes(best_rows()); }
-  // the largest piece that fits: all rows, or a multiple of 256
+  uint64_t least() const { return std::min(few_bytes(), tile_bytes(least_rows())); }
+  uint64_t best() const { return rows <= kFewRows ? few_bytes() : tile_bytes(best_rows()); }
+  bool few_in(uint64_t have) const { return few_bytes() <= have; }
+  // by tiles, the largest piece that fits: all rows, or a multiple of 256
   uint32_t piece_for(uint64_t have) const {
-    if (bytes(best_rows()) <= have) return best_rows();
+    if (tile_bytes(best_rows()) <= have) return best_rows();
     uint32_t lo = 1, hi = (best_rows() + kMmaTile - 1) / kMmaTile;  // in units of 256 rows
     while (hi - lo > 1) {
       const uint32_t mid = (lo + hi) / 2;
-      if (bytes(mid * kMmaTile) <= have) lo = mid; else hi = mid;
+      if (tile_bytes(mid * kMmaTile) <= have) lo = mid; else hi = mid;
     }
     return std::min(lo * kMmaTile, best_rows());
   }
@@ -990,8 +996,9 @@ static int32_t token_logprobs(ft_pool* p, ScorePiece a, uint64_t rows, void* wor
   const ScoreWork work{a.hidden, a.vocab, a.top, rows};
   if (!workspace || !aligned_to(workspace, 256)) return FT_ERR_INVALID_ARG;
   if (workspace_bytes < work.least()) return FT_ERR_CAPACITY;
-  const uint32_t piece = work.piece_for(workspace_bytes);
-  score_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, a.top, work.few());
+  const bool few = work.few_in(workspace_bytes);
+  const uint32_t piece = few ? (uint32_t)rows : work.piece_for(workspace_bytes);
+  score_carve(&a, static_cast<uint8_t*>(workspace), piece, a.hidden, a.vocab, a.top, few);
   a.call_seq = status_seq(p);
   a.pairs = (uint32_t)p->sm_count / 2;
   // the join's rows a CTA: 8 where 16 would leave SMs without work, or would not have their maxima in shared memory
