@@ -627,7 +627,8 @@ int32_t pool_rotary(ft_pool* pool, uint64_t rows, const int32_t* pos, uint64_t p
  * input 4) take wide accesses; others go element by element (bf16 at 0.7 of the rate, fp32 at 0.9), those with q and rows beyond 16384
  * elements (fp32 with a residual 12288) from cache in three passes (at a quarter to a half).
  * Errors: cols 0, a type, eps negative or not finite, x NULL, none of sum, y and q, q without q_scale or the reverse, a misaligned
- * operand, a stride below what a row needs INVALID_ARG; cols > 2^30 CAPACITY.  rows = 0 does nothing.
+ * operand, a stride below what a row needs, several rows of sum or y on x or the residual with another stride, sum on y INVALID_ARG; cols > 2^30
+ * CAPACITY.  rows = 0 does nothing.
  */
 int32_t pool_rms_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void* x, uint64_t ldx, const void* residual, uint64_t ldr,
                       uint32_t dtype, const void* weight, uint32_t param_dtype, float eps, void* sum, uint64_t lds, void* y,
@@ -642,7 +643,8 @@ int32_t pool_rms_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void* x
  * Sums over rows are fp32, in an order fixed by the shapes and the device.  pool_rms_norm_grad_workspace gives the workspace's size.
  * rows = 0: dweight becomes zero unless accumulating.  Rows beyond 8192 elements (4096 off 16-byte boundaries) are read
  * twice.  Rows off 16-byte boundaries go element by element, bf16 at half the rate and fp32 at two thirds.
- * Errors as pool_rms_norm; workspace NULL or misaligned INVALID_ARG, too small CAPACITY.
+ * Errors as pool_rms_norm, several rows of dx on dy, s or dsum with another stride included; workspace NULL or misaligned INVALID_ARG, too small
+ * CAPACITY.
  */
 int32_t pool_rms_norm_grad_workspace(ft_pool* pool, uint64_t rows, uint32_t cols, uint64_t* bytes);
 int32_t pool_rms_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const void* dy, uint64_t lddy, const void* s, uint64_t lds,

@@ -168,6 +168,10 @@ inline cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, uint32_t thre
 inline bool dtype_ok(uint32_t t) { return t == FT_BF16 || t == FT_F32; }
 inline uint32_t dtype_size(uint32_t t) { return t == FT_F32 ? 4u : 2u; }
 inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// A matrix written where one is read has that one's stride: with another, a row lands on rows that are still to be read.
+inline bool on_other_rows(uint64_t rows, const void* out, uint64_t ld_out, const void* in, uint64_t ld_in) {
+  return out && out == in && rows > 1 && ld_out != ld_in;
+}
 inline bool on_pool_device(const ft_pool* p) {
   int d = -1;
   return cudaGetDevice(&d) == cudaSuccess && d == p->device;

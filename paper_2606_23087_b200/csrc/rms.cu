@@ -636,6 +636,8 @@ FT_EXPORT int32_t pool_rms_norm(ft_pool* p, uint64_t rows, uint32_t cols, const 
   if (!x || (!y && !q && !sum) || bad(x, ldx, cols, es) || bad(residual, ldr, cols, es) || bad(sum, lds, cols, es) || bad(y, ldy, cols, es) ||
       bad(q, ldq, cols, 1) || !q != !q_scale || bad(q_scale, ldqs, (cols + kRmsGroup - 1) / kRmsGroup, 4) || !aligned_to(weight, ps) || !aligned_to(rstd, 4))
     return FT_ERR_INVALID_ARG;
+  const auto lands = [&](const void* out, uint64_t ld) { return on_other_rows(rows, out, ld, x, ldx) || on_other_rows(rows, out, ld, residual, ldr); };
+  if (lands(sum, lds) || lands(y, ldy) || (sum && sum == y)) return FT_ERR_INVALID_ARG;
   RmsArgs a;
   a.rows = rows; a.cols = cols; a.param_dtype = param_dtype; a.eps = eps;
   a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.weight = weight;
@@ -672,6 +674,7 @@ FT_EXPORT int32_t pool_rms_norm_grad(ft_pool* p, uint64_t rows, uint32_t cols, c
   const uint32_t es = dtype_size(dtype);
   if (!dy || !s || !rstd || !dx || lddy < cols || lds < cols || lddx < cols || (dsum && lddsum < cols)) return FT_ERR_INVALID_ARG;
   if (!aligned_to(dy, es) || !aligned_to(s, es) || !aligned_to(dsum, es) || !aligned_to(dx, es) || !aligned_to(weight, dtype_size(param_dtype))) return FT_ERR_INVALID_ARG;
+  if (on_other_rows(rows, dx, lddx, dy, lddy) || on_other_rows(rows, dx, lddx, s, lds) || on_other_rows(rows, dx, lddx, dsum, lddsum)) return FT_ERR_INVALID_ARG;
   if (!aligned_to(rstd, 4) || !workspace || !aligned_to(workspace, 256)) return FT_ERR_INVALID_ARG;
   if (workspace_bytes < rms_grad_ws(p, rows, cols)) return FT_ERR_CAPACITY;
   RmsGradArgs a;
