@@ -475,8 +475,8 @@ int32_t pool_embed_grad(ft_pool* pool, const ft_plan* plan, uint32_t mb_begin, u
  * A row's result depends on that row alone (a NaN stays in its row).  Rows whose operands all start on 16-byte boundaries
  * take wide accesses; any other width and stride works element by element (bf16 at 2/3 of the rate, fp32 at 9/10).  Rows
  * beyond 16384 elements are read three times, from cache, at a fifth to a fourth of the rate.
- * Errors: cols 0, a type, eps negative or not finite, a NULL or misaligned operand, a stride below cols INVALID_ARG;
- * cols > 2^30 CAPACITY.  rows = 0 does nothing.
+ * Errors: cols 0, a type, eps negative or not finite, a NULL or misaligned operand, a stride below cols, several rows of y on x with another
+ * stride INVALID_ARG; cols > 2^30 CAPACITY.  rows = 0 does nothing.
  */
 int32_t pool_layer_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void* x, uint64_t ldx, uint32_t dtype,
                         const void* weight, const void* bias, uint32_t param_dtype, float eps, void* y, uint64_t ldy,
@@ -491,7 +491,8 @@ int32_t pool_layer_norm(ft_pool* pool, uint64_t rows, uint32_t cols, const void*
  * mean and rstd as pool_layer_norm gave them.  Sums over rows are fp32, in an order fixed by the shapes and the device.
  * pool_layer_norm_grad_workspace gives the workspace's size.  rows = 0: dweight and dbias become zero unless accumulating.
  * Rows beyond 8192 elements (4096 where an operand is off 16 bytes) are read twice, a fourth to a third as fast.
- * Errors as pool_layer_norm; workspace NULL or misaligned INVALID_ARG, too small CAPACITY.
+ * Errors as pool_layer_norm, several rows of dx on dy or x with another stride included; workspace NULL or misaligned INVALID_ARG, too small
+ * CAPACITY.
  */
 int32_t pool_layer_norm_grad_workspace(ft_pool* pool, uint64_t rows, uint32_t cols, uint64_t* bytes);
 int32_t pool_layer_norm_grad(ft_pool* pool, uint64_t rows, uint32_t cols, const void* dy, uint64_t lddy, const void* x,

@@ -462,7 +462,7 @@ FT_EXPORT int32_t pool_layer_norm(ft_pool* p, uint64_t rows, uint32_t cols, cons
   if (cols > kNormColsLimit) return FT_ERR_CAPACITY;
   if (rows == 0) return FT_OK;
   const uint32_t es = dtype_size(dtype), ps = dtype_size(param_dtype);
-  if (!x || !y || ldx < cols || ldy < cols || !aligned_to(x, es) || !aligned_to(y, es)) return FT_ERR_INVALID_ARG;
+  if (!x || !y || ldx < cols || ldy < cols || !aligned_to(x, es) || !aligned_to(y, es) || on_other_rows(rows, y, ldy, x, ldx)) return FT_ERR_INVALID_ARG;
   if (!aligned_to(weight, ps) || !aligned_to(bias, ps) || !aligned_to(mean, 4) || !aligned_to(rstd, 4)) return FT_ERR_INVALID_ARG;
   NormArgs a;
   a.rows = rows; a.ldx = ldx; a.ldy = ldy; a.cols = cols; a.param_dtype = param_dtype;
@@ -501,6 +501,7 @@ FT_EXPORT int32_t pool_layer_norm_grad(ft_pool* p, uint64_t rows, uint32_t cols,
   const uint32_t es = dtype_size(dtype);
   if (!dy || !x || !mean || !rstd || !dx || lddy < cols || ldx < cols || lddx < cols) return FT_ERR_INVALID_ARG;
   if (!aligned_to(dy, es) || !aligned_to(x, es) || !aligned_to(dx, es) || !aligned_to(weight, dtype_size(param_dtype))) return FT_ERR_INVALID_ARG;
+  if (on_other_rows(rows, dx, lddx, dy, lddy) || on_other_rows(rows, dx, lddx, x, ldx)) return FT_ERR_INVALID_ARG;
   if (!aligned_to(mean, 4) || !aligned_to(rstd, 4) || !workspace || !aligned_to(workspace, 256)) return FT_ERR_INVALID_ARG;
   if (workspace_bytes < norm_grad_ws(p, rows, cols)) return FT_ERR_CAPACITY;
   NormGradArgs a;

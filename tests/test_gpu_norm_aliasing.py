@@ -66,3 +66,32 @@ def test_rms_norm_grad_on_its_inputs(pool, rows):  # noqa: F811
             ok = ld == 128 or rows == 1
             assert call(m, m[which], ld) == (0 if ok else INVALID), (which, ld)
             assert torch.equal(bits(m[which][:rows]), bits((exp if ok else values[which])[:rows]))
+
+
+@pytest.mark.parametrize("rows", [1, ROWS])
+def test_layer_norm_on_its_inputs(pool, rows):  # noqa: F811
+    g = gen(3)
+    w, mean, rstd = randn(g, COLS), randn(g, ROWS), torch.rand(ROWS, device="cuda", generator=g) + 0.5
+    n = pool.layer_norm_grad_workspace(ROWS, COLS)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    values = [matrix(g, 128) for _ in range(2)]
+
+    def norm(m, y, ld):
+        return pool.layer_norm(rows, COLS, m[0].data_ptr(), m[0].stride(0), fp.FT_F32, w.data_ptr(), 0, fp.FT_F32, EPS, y.data_ptr(), ld, stream=stream())
+
+    def grad(m, dx, ld):
+        return pool.layer_norm_grad(rows, COLS, m[1].data_ptr(), m[1].stride(0), m[0].data_ptr(), m[0].stride(0), fp.FT_F32, w.data_ptr(), fp.FT_F32, mean.data_ptr(),
+                                    rstd.data_ptr(), dx.data_ptr(), ld, 0, 0, False, ws.data_ptr(), n, stream())
+    for call, on in ((norm, (0,)), (grad, (0, 1))):
+        exp = torch.empty(ROWS, COLS, device="cuda")
+        assert call(values, exp, COLS) == 0
+        for which in on:
+            for ld in (COLS, 100, 128):
+                m = []
+                for v in values:
+                    b = torch.zeros(ROWS, 128, device="cuda")
+                    b[:, :COLS] = v
+                    m.append(b[:, :COLS])
+                ok = ld == 128 or rows == 1
+                assert call(m, m[which], ld) == (0 if ok else INVALID), (which, ld)
+                assert torch.equal(bits(m[which][:rows]), bits((exp if ok else values[which])[:rows]))
