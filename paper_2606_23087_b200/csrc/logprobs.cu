@@ -24,6 +24,7 @@
 // and last 5 us read nothing), 24 x 4096, 131072 185 us (5.8 TB/s).
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "mma_pair.cuh"
 
@@ -47,7 +48,7 @@ struct ScorePiece {
   uint64_t ldw;
   const __nv_bfloat16 *x, *w;
   const int32_t* tokens;
-  float scale;
+  float scale, to_log2;     // to_log2: scale log2(e), or fp32's largest number where that is beyond it
   float *logprob, *entropy, *top_logprobs;
   int32_t* top_ids;
   uint64_t call_seq;
@@ -190,12 +191,12 @@ struct SegStats {
   float most, sum, moment;
 };
 template <uint32_t kCols, class Z>
-__device__ __forceinline__ SegStats segment_stats(Z&& z, float scale) {
+__device__ __forceinline__ SegStats segment_stats(Z&& z, float to_log2) {
   float most = -INFINITY;
 #pragma unroll
   for (uint32_t j = 0; j < kCols; j += 2) most = fmaxf(most, fmaxf(z(j), z(j + 1)));
   F2 sums = f2(0.f), moments = f2(0.f);
-  const F2 less = f2(most == -INFINITY ? 0.f : -most), by = f2(scale * kScoreLog2e);
+  const F2 less = f2(most == -INFINITY ? 0.f : -most), by = f2(to_log2);
 #pragma unroll
   for (uint32_t j = 0; j < kCols; j += 2) {
     const float2 t = parts((f2(z(j), z(j + 1)) + less) * by);
@@ -274,7 +275,7 @@ k_score(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUten
         for (uint32_t j = 0; j < kSegCols; ++j)
           if (j >= cols) z[j / 32][j % 32] = 0xFF800000u;
       }
-      const SegStats g = segment_stats<kSegCols>([&](uint32_t j) { return __uint_as_float(z[j / 32][j % 32]); }, a.scale);
+      const SegStats g = segment_stats<kSegCols>([&](uint32_t j) { return __uint_as_float(z[j / 32][j % 32]); }, a.to_log2);
       if (m < n) {
         const uint64_t at = (uint64_t)(c0 / kSegCols) * a.rows + m;
         a.most[at] = g.most;
@@ -502,7 +503,7 @@ k_score_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ C
         if (m < a.rows) {
           const uint32_t token_at = (uint32_t)(a.tokens ? a.tokens[a.row0 + m] : kNoLabel) - seg * kFewCols;
           if (token_at < kFewCols) mine[lane * 33 + token_at] = -INFINITY;  // the join adds it
-          const SegStats t = segment_stats<kFewCols>([&](uint32_t j) { return mine[lane * 33 + j]; }, a.scale);
+          const SegStats t = segment_stats<kFewCols>([&](uint32_t j) { return mine[lane * 33 + j]; }, a.to_log2);
           const uint64_t to = (uint64_t)m * a.segs + seg;
           a.most[to] = t.most;
           a.sum[to] = t.sum;
@@ -721,7 +722,7 @@ __device__ __forceinline__ void row_results(const ScorePiece& a, uint64_t row, i
 #pragma unroll
   for (int d = 16; d; d >>= 1) about = fmaxf(about, __shfl_xor_sync(0xFFFFFFFFu, about, d));
   about = finite_about(about);
-  const float to_log2 = a.scale * kScoreLog2e;
+  const float to_log2 = a.to_log2;
   Joined others, all;
   others.add(most, sum, moment, about, to_log2);
   if (a.top) {
@@ -779,7 +780,7 @@ __global__ void __launch_bounds__(32 * kRows) k_score_join(const __grid_constant
   const uint32_t n = a.tokens ? *a.count : a.rows, m0 = blockIdx.x * kRows;
   if (m0 >= n) return;
   const uint32_t r = threadIdx.x % kRows, g = threadIdx.x / kRows, held_ld = a.segs | 1;
-  const float to_log2 = a.scale * kScoreLog2e;
+  const float to_log2 = a.to_log2;
   if (m0 + r < n) {
     float most = -INFINITY;
 #pragma unroll 4
@@ -899,7 +900,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) k_score_join_few(const __gr
   __syncthreads();
 #pragma unroll
   for (uint32_t w = 0; w < kFewWarps; ++w) most = fmaxf(most, s_part[0][w]);
-  const float about = finite_about(most), to_log2 = a.scale * kScoreLog2e;
+  const float about = finite_about(most), to_log2 = a.to_log2;
   Joined mine;
 #pragma unroll
   for (uint32_t i = 0; i < kAhead; ++i) mine.add(ahead[0][i], ahead[1][i], ahead[2][i], about, to_log2);
@@ -1097,6 +1098,7 @@ FT_EXPORT int32_t pool_token_logprobs(ft_pool* p, uint64_t rows, uint32_t hidden
   if ((top && (!top_ids || !top_logprobs)) || !aligned_to(top_ids, 4) || !aligned_to(top_logprobs, 4)) return FT_ERR_INVALID_ARG;
   ScorePiece a = {};
   a.hidden = hidden; a.vocab = vocab; a.ldx = ldx; a.x = static_cast<const __nv_bfloat16*>(x); a.ldw = ldw; a.w = static_cast<const __nv_bfloat16*>(w); a.tokens = tokens; a.scale = logit_scale;
+  a.to_log2 = std::min(logit_scale * kScoreLog2e, std::numeric_limits<float>::max());
   a.logprob = logprob; a.entropy = entropy; a.top = top; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
   return token_logprobs(p, a, rows, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
