@@ -718,31 +718,36 @@ __device__ __forceinline__ void row_results(const ScorePiece& a, uint64_t row, i
   const uint32_t lane = threadIdx.x & 31;
   const bool given = a.tokens != nullptr;
   const float by_sums = key_value(key), logit = key ? listed_logit : -INFINITY;
-  float about = fmaxf(fmaxf(most, target), logit);
+  const auto largest = [](float v) {
 #pragma unroll
-  for (int d = 16; d; d >>= 1) about = fmaxf(about, __shfl_xor_sync(0xFFFFFFFFu, about, d));
-  about = finite_about(about);
+    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+    return v;
+  };
   const float to_log2 = a.to_log2;
+  float about = finite_about(fmaxf(fmaxf(most, target), largest(logit)));
+  const auto power = [&](float z) { return max_with_nan((z - about) * to_log2, kLeastExponent); };
   Joined others, all;
   others.add(most, sum, moment, about, to_log2);
-  if (a.top) {
-    // The alternatives' terms by FMAs in the place of those that the sums hold.  A sum that is left far below those terms has lost its digits
-    // to them (logits so large that the sums' rounding is worth several powers of e): they are all that is known of it.
-    const auto power = [&](float z) { return max_with_nan((z - about) * to_log2, kLeastExponent); };
-    float term = 0.f, more = 0.f, more_moment = 0.f;
-    if (key && logit != -INFINITY) {
-      const float u = power(logit);
-      term = exp2f(u);
-      if (logit != by_sums) {
-        const float u0 = power(by_sums), e0 = exp2f(u0), d = (logit - by_sums) * a.scale;
-        more = fabsf(d) < 1.f ? e0 * expm1f(d) : term - e0;
-        more_moment = u * term - u0 * e0;
-      }
+  if (a.top) {  // the alternatives' terms by FMAs in the place of those that the sums hold
+    const bool there = key && logit != -INFINITY;
+    float more = 0.f, more_moment = 0.f;
+    bool apart = false;
+    if (there && logit != by_sums) {
+      const float u = power(logit), u0 = power(by_sums), e = exp2f(u), e0 = exp2f(u0), d = (logit - by_sums) * a.scale;
+      apart = fabsf(d) >= 1.f && fmaxf(e, e0) > 0x1p-12f;
+      more = fabsf(d) < 1.f ? e0 * expm1f(d) : e - e0;
+      more_moment = u * e - u0 * e0;
     }
-    term = warp_sum(term);
-    others.sum += warp_sum(more);
-    others.moment += warp_sum(more_moment);
-    if (others.sum < 0.5f * term) others.sum = term;
+    if (__any_sync(0xFFFFFFFFu, apart)) {
+      // A scale at which the sums' roundings are worth powers of e, in logits that count: beside terms by FMAs the sums mean nothing
+      about = finite_about(fmaxf(target, largest(logit)));
+      const float u = power(logit), e = there ? exp2f(u) : 0.f;
+      others.sum = warp_sum(e);
+      others.moment = warp_sum(there ? u * e : 0.f);
+    } else {
+      others.sum += warp_sum(more);
+      others.moment += warp_sum(more_moment);
+    }
   }
   all = others;
   if (target != -INFINITY) all.add(target, given ? 1.f : 0.f, 0.f, about, to_log2);
