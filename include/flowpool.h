@@ -584,7 +584,8 @@ int32_t pool_adamw_step(ft_pool* pool, const ft_adamw_tensor* tensors, uint32_t 
  * pool_gather_padded writes them (out_pos3) or a single one:
  *   angle_i = pos[axis_i][row] * freq_i;   (a, b) becomes (a cos - b sin, a sin + b cos) for the pair i of every head
  *   pos     device int32, row r of axis x at pos[x * pos_ld + r]; any value (the angle is taken modulo a turn in 64-bit
- *           fixed point: a far position's is off by 2^-33 of a turn at most)
+ *           fixed point: a far position's is off by less than 2^-31 of a turn; the fp32 value that the sine is taken of, near or
+ *           far, is rounded by up to 2^-26 of a turn)
  *   cfg     host.  freq: host [pairs], radians per position, from -8 to 8; axis: host [pairs], 0..2, NULL = all 0 (sections in any
  *           order are a table); the first 2 * pairs elements of a head are turned, element i with i + pairs (interleaved = 0) or
  *           2i with 2i + 1; the rest is copied.  inverse != 0 turns back: the backward pass of the same call

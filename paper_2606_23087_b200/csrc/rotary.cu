@@ -6,7 +6,9 @@
 //
 // Angles.  A position times a frequency loses what matters of a far position's angle in fp32 (at 10^5 some 2^-7 radians), so
 // the angle is taken in turns, as a 64-bit fraction: the host rounds freq / 2 pi modulo one turn to 64 bits, the product with
-// a 32-bit position wraps modulo one turn by itself, and is off by at most 2^-33 of a turn for any position.
+// a 32-bit position wraps modulo one turn by itself.  freq / 2 pi, below 1.28, is off by 1.64 x 2^-64 as an 80-bit product, by half of 2^-64
+// each where a turn is added and where it is rounded: the angle by less than 2^-31 of a turn for any position.  Its rounding to fp32, for the
+// sine, is up to 2^-26 of a turn.
 //
 // Bound by HBM: every element is read and written once.  32768 rows x 32 heads x 128 in bf16: 82 us (6.55 TB/s, the copy rate).  A CTA
 // works out the sines and cosines of its rows once into shared memory; a thread takes the same pairs of one head in each of its rows,
@@ -186,7 +188,9 @@ FT_EXPORT int32_t pool_rotary(ft_pool* p, uint64_t rows, const int32_t* pos, uin
     long double t = f * 0.159154943091895335768883763372514362L;  // turns a position, of which whole ones count nothing
     t -= (long double)(int64_t)t;
     if (t < 0) t += 1;
-    const uint64_t u = t < 1.0L ? (uint64_t)(t * 0x1p64L) : 0;
+    const long double units = t * 0x1p64L;
+    uint64_t u = units < 0x1p64L ? (uint64_t)units : 0;
+    if (units < 0x1p64L && units - (long double)u >= 0.5L) ++u;
     a.turns[i] = cfg->inverse ? 0 - u : u;
   }
   if (rows && (!pos || !aligned_to(pos, 4) || (axes && pos_ld < rows))) return FT_ERR_INVALID_ARG;
