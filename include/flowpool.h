@@ -692,7 +692,8 @@ int32_t pool_grad_norm(ft_pool* pool, const ft_grad_tensor* tensors, uint32_t n_
  * are listed, and the sum over the other tokens, come from the tensor cores' fp32 sums, which truncate at every addition.  What that leaves of
  * a log probability's error: about 1e-7 of it for tokens at random, 6e-7 for likely ones (log probabilities of -1), as long as a logit is summed in
  * parts of 1024 of hidden; up to four times that where it is summed in one piece of up to 4224: more than 256 rows in calls that fill the device.
- * The gradient of the log probability is pool_token_loss_grad's with -grad_loss.
+ * The gradient of the log probability is pool_token_loss_grad's with -grad_loss.  The loss has no logit_scale: at another one than 1 it takes
+ * scale * x for x, and its dx times scale is x's gradient (a power of two is exact in bf16; another scale rounds scale * x).
  * x, w, hidden, ldx, ldw as in pool_token_loss.  pool_token_logprobs_workspace gives the smallest workspace and the one from which more
  * brings nothing; any size between the two works (alternatives keep a piece of the rows' logits in the workspace, up to 4 GiB), and a workspace
  * that serves some rows serves fewer of them too, if not by the fastest way.  The size may change the last bits of a number.
