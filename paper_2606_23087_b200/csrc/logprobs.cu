@@ -65,12 +65,6 @@ struct ScorePiece {
   float* z;                 // [rows][ld_z]
 };
 
-__device__ __forceinline__ float max_with_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
 // Whole numbers in the order of the values; a NaN counts as -inf, -0 as 0.  None of them is zero.
 __device__ __forceinline__ uint32_t ordered_bits(float z) {
   const uint32_t b = __float_as_uint(fmaxf(z, -INFINITY) + 0.f);

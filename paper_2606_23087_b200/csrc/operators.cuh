@@ -95,6 +95,13 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
+// NaN wins, unlike in fmaxf
+__device__ __forceinline__ float max_with_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp; results below 2^-126 are zero
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

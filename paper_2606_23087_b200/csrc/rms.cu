@@ -52,13 +52,6 @@ __device__ __forceinline__ float2 rms_scale(float top) {
   top = fmaxf(top, kFp8Least);
   return make_float2(top / kFp8Most, kFp8Most / top);
 }
-// NaN wins, unlike in fmaxf
-__device__ __forceinline__ float max_or_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
 // E weights of consecutive columns from c on, 16 bytes at a time where they lie so; ones without weights or where the row has ended
 template <int E>
 __device__ __forceinline__ void weights_from(const void* weight, uint32_t dtype, uint32_t c, bool there, F2 (&w)[E / 2]) {
@@ -168,10 +161,10 @@ __global__ void __launch_bounds__(kN, (kRmsCtas<T, V, kVec, kN>)) k_rms(RmsArgs 
 #pragma unroll
           for (int i = 0; i < E / 2; ++i) {
             const float2 v = parts(x[k * (E / 2) + i]);
-            top = max_or_nan(top, max_or_nan(fabsf(v.x), fabsf(v.y)));
+            top = max_with_nan(top, max_with_nan(fabsf(v.x), fabsf(v.y)));
           }
 #pragma unroll
-          for (int d = kRmsGroup / E / 2; d; d >>= 1) top = max_or_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+          for (int d = kRmsGroup / E / 2; d; d >>= 1) top = max_with_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
           if (!in.has(k)) continue;
           const float2 scale = rms_scale(top);
           const uint32_t c = (k * kN + threadIdx.x) * E;
@@ -217,10 +210,10 @@ __global__ void __launch_bounds__(kRmsWideThreads) k_rms_wide(RmsArgs a) {
         for (int i = 0; i < 4; ++i) {
           const uint32_t c = c0 + 32 * i + (threadIdx.x & 31);
           y[i] = c < a.cols ? value(c) * rstd * weight(c) : 0.f;
-          top = max_or_nan(top, fabsf(y[i]));
+          top = max_with_nan(top, fabsf(y[i]));
         }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) top = max_or_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        for (int d = 16; d; d >>= 1) top = max_with_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
         const float2 scale = rms_scale(top);
         if ((threadIdx.x & 31) == 0) a.q_scale[row * a.ldqs + c0 / kRmsGroup] = scale.x;
 #pragma unroll
