@@ -19,9 +19,9 @@
 //                 in one piece 1.2e-5 and 1.5e-6.  Tokens at random, about -8: 1.2e-7 and 1.1e-7, 4.6e-7 and 3.8e-7)
 //   k_score_list  the same for long calls with alternatives, behind the join
 //
-// Bound by the tensor cores, long calls by the card's power limit: 10813 rows that count of 16384 x 3584, vocabulary 32768, 8 alternatives 1.6 to
-// 1.9 ms (1.35 to 1.55 PFLOP/s; k_score alone 1.58 ms).  Few rows by W's bytes: 24 x 1024, 32768 23 us (18 of them k_score_few, whose first
-// and last 5 us read nothing), 24 x 4096, 131072 185 us (5.8 TB/s).
+// Bound by the tensor cores, long calls by the card's power limit: 10813 rows that count of 16384 x 3584, vocabulary 32768, 8 alternatives 1.72 to
+// 1.76 ms (1.44 to 1.48 PFLOP/s; k_score alone 1.56 ms, k_score_list 91 us).  Few rows by W's bytes: 24 x 1024, 32768 24 us (18 of them
+// k_score_few, whose first and last 5 us read nothing, 10 alone the join), 24 x 4096, 131072 168 us (6.4 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <limits>
