@@ -20,7 +20,7 @@
 //   k_score_list  the same for long calls with alternatives, behind the join
 //
 // Bound by the tensor cores, long calls by the card's power limit: 10813 rows that count of 16384 x 3584, vocabulary 32768, 8 alternatives 1.72 to
-// 1.76 ms (1.44 to 1.48 PFLOP/s; k_score alone 1.56 ms, k_score_list 91 us).  Few rows by W's bytes: 24 x 1024, 32768 24 us (18 of them
+// 1.97 ms (1.29 to 1.48 PFLOP/s; k_score alone 1.56 ms, k_score_list 91 us).  Few rows by W's bytes: 24 x 1024, 32768 23 us (18 of them
 // k_score_few, whose first and last 5 us read nothing, 10 alone the join), 24 x 4096, 131072 168 us (6.4 TB/s).
 #include <algorithm>
 #include <cmath>
